@@ -18,8 +18,10 @@
  * pyramid blocks refreshed), the kept-count schedules (wf_default_schedule,
  * wf_level0_schedule, wf_schedule_from_proportions), other wavelet bases
  * with Eq. 11 taken literally (wf_wavelet_approx, wf_filter_wavelet), grouped
- * query heads (wf_filter, wf_sparse_attn, wf_step), and
- * wf_sparse_attn_noalloc for callers that cannot pass a workspace.
+ * query heads (wf_filter, wf_sparse_attn, wf_step),
+ * wf_sparse_attn_noalloc for callers that cannot pass a workspace, a cache in
+ * 8-bit or 4-bit codes (wf_cache_quantize, wf_cache_dequantize), and the
+ * attention of several sequences over one cached prompt (wf_prefix_attn).
  *
  * Conventions shared by every entry point
  * - A tensor is described by wf_tensor: [batch, heads, seq, head_dim] with
@@ -65,7 +67,9 @@ typedef enum {
   WF_ERR_SCHEDULE = -9     /* kept counts infeasible for the shape */
 } wf_status;
 
-typedef enum { WF_F32 = 0, WF_BF16 = 1 } wf_dtype;
+/* WF_MXFP8 and WF_MXFP4 are the forms of a quantised cache (wf_cache_quantize);
+ * the calls that take them say so, every other call refuses them. */
+typedef enum { WF_F32 = 0, WF_BF16 = 1, WF_MXFP8 = 2, WF_MXFP4 = 3 } wf_dtype;
 
 typedef struct {
   int32_t batch;    /* B */
@@ -363,6 +367,86 @@ wf_status wf_step_wavelet(const void* Q, const wf_tensor* q, const void* top, co
                           const wf_tensor* kv, const void* Kg, const void* Vg, const wf_tensor* g, int levels,
                           const int32_t* keep, int wavelet, int32_t* idx, int32_t* level_sets, void* O,
                           const wf_tensor* o, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * 5. A quantised cache.  Blocks of 32 consecutive channels of a row share one
+ * power of two s = 2^e; an element x is kept as the code of x / s in
+ *   WF_MXFP8: E4M3 (1 sign, 4 exponent, 3 mantissa bits; largest value 448),
+ *   WF_MXFP4: E2M1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives),
+ * rounded to nearest, ties to the even code.  e is the least integer in
+ * [-127, 127] with max |x| <= 448 s (6 s), so nothing saturates, and x / s is
+ * exact: code and scale are defined to the bit.  A block that holds a NaN or an
+ * infinity has no such scale: it is kept as a NaN scale and reads back as NaN
+ * in all 32 channels; the blocks around it are not touched.
+ *
+ * Layout: a code tensor is described by a wf_tensor of dtype WF_MXFP8 or
+ * WF_MXFP4 whose head_dim and strides count elements, one code a byte
+ * (WF_MXFP8) or two a byte, channel 2 i in the low half (WF_MXFP4).  Its scales
+ * are bytes e + 127 (255: NaN), contiguous [B][H][rows][head_dim / 32], 4-byte
+ * aligned.  K and V have code and scale tensors of the same shape and strides.
+ * Codes and scales of rows never written may hold anything that reads back.
+ *
+ * wf_scales_bytes: size of the scales of kv (0 if kv is not a valid quantised
+ * cache).
+ *
+ * wf_cache_quantize: the count = nt->seq rows Knew (and Vnew), WF_F32 or
+ * WF_BF16, into the caches at token positions [pos, pos + count), quantised
+ * as they are written; no other row is touched.  count may be 0 (then Knew and Vnew may be NULL).  Vnew, Vc and Vs
+ * are all NULL for keys alone.  The new rows must not overlap the caches.
+ *
+ * wf_cache_dequantize: m = out->seq rows read back into Kout (and Vout), WF_F32
+ * or WF_BF16 (code times scale, rounded once): with idx == NULL the rows
+ * [pos, pos + m); else row idx[u][i] of unit u = b H + h (device, int32
+ * [B*H][m], out-of-range entries clamped to [0, n)), and pos must be 0.  m may
+ * be 0.
+ *
+ * scales_bytes: the size of each scale tensor.  Errors: WF_ERR_INVALID_ARG for
+ * a missing pointer, V given in part, or a window outside [0, n);
+ * WF_ERR_WORKSPACE for scales that are too small; shape, dtype and alignment
+ * errors as elsewhere.  Nothing is enqueued on an error.
+ * ------------------------------------------------------------------------- */
+size_t wf_scales_bytes(const wf_tensor* kv);
+wf_status wf_cache_quantize(const void* Knew, const void* Vnew, const wf_tensor* nt, void* Kc, void* Ks, void* Vc,
+                            void* Vs, const wf_tensor* kv, size_t scales_bytes, int64_t pos, void* stream);
+wf_status wf_cache_dequantize(const void* Kc, const void* Ks, const void* Vc, const void* Vs, const wf_tensor* kv,
+                              size_t scales_bytes, const int32_t* idx, int64_t pos, void* Kout, void* Vout,
+                              const wf_tensor* out, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * 6. Attention of B sequences over P cached prompts, each prompt's rows read
+ * once for all of its sequences (Eq. 3's cached attention for several answers
+ * to one prompt; P = B gives every sequence a prompt of its own).
+ *
+ * Q: [B,Hq,q,d] WF_F32 or WF_BF16, any q >= 1 (q = 1: one token a sequence).
+ * K, V: the prompts [P,H,n,d] (kv), in Q's dtype, or quantised with their
+ * scales Ks, Vs (else NULL).  P divides B: sequence b reads prompt
+ * b / (B / P).  Hq = G H as in wf_filter: query head hq reads key head hq / G.
+ * The prompt rows of unit u = p H + h that are attended:
+ *   idx == NULL: rows [0, k), 0 <= k <= n;
+ *   idx (device, int32 [P*H][k]): the k rows idx[u][..], 0 <= k <= n, in any
+ *     order, out-of-range entries clamped to [0, n);
+ *   prefix_len (device, int32 [P], may be NULL): only the first
+ *     min(k, max(0, prefix_len[p])) of them.
+ * Kg, Vg: each sequence's own rows [B,H,n_g,d] (descriptor g, Q's dtype; NULL
+ * when n_g = 0), of which the first min(n_g, max(0, gen_len[b])) count
+ * (gen_len: device, int32 [B], NULL: all).  Rows past a length are never read.
+ *   O = softmax(scale Q [K_p; Kg_b]^T) [V_p; Vg_b]
+ * with fp32 logits, softmax and accumulation, scale = 1/sqrt(d) when the
+ * argument is 0, no mask beyond the lengths; O (o: shape and dtype of Q) is
+ * written rounded to that dtype.  A query row with no row to attend to, or
+ * whose logits are all -inf, gets O = 0.  A NaN or an infinity reaches the query
+ * rows that attend to its row only.
+ * bf16 queries run on the tensor cores, fp32 queries in fp32 arithmetic.  The
+ * same inputs give the same bits.
+ * ws: device scratch of at least wf_prefix_attn_workspace_bytes() bytes,
+ * 256-byte aligned; its first 4 bytes are wf_filter's status word (zero it
+ * once, read it with wf_workspace_status).
+ * ------------------------------------------------------------------------- */
+size_t wf_prefix_attn_workspace_bytes(const wf_tensor* q, const wf_tensor* kv, int k, int n_g);
+wf_status wf_prefix_attn(const void* Q, const wf_tensor* q, const void* K, const void* V, const wf_tensor* kv,
+                         const void* Ks, const void* Vs, const int32_t* idx, int k, const int32_t* prefix_len,
+                         const void* Kg, const void* Vg, const wf_tensor* g, const int32_t* gen_len, void* O,
+                         const wf_tensor* o, float scale, void* ws, size_t ws_bytes, void* stream);
 
 /* Device status of the last wf_step calls that used workspace ws: waits for
  * `stream`, returns WF_ERR_TIMEOUT (and clears the word) if a bounded device

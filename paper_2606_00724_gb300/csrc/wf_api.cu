@@ -9,6 +9,7 @@
 #include <utility>
 
 #include "wf_internal.cuh"
+#include "wf_prefix.cuh"
 #include "wf_testing.h"
 
 #define WF_API extern "C" __attribute__((visibility("default")))
@@ -30,6 +31,22 @@ wf_status check_desc(const wf_tensor* t, bool allow_empty) {
   if (t->stride_b < 0 || t->stride_h < 0 || t->stride_s < 0) return WF_ERR_SHAPE;
   const int64_t es = elem_size(t->dtype);
   if ((t->stride_b * es) % 16 || (t->stride_h * es) % 16 || (t->stride_s * es) % 16) return WF_ERR_ALIGN;
+  if (t->seq > 1 && t->stride_s < t->head_dim) return WF_ERR_SHAPE;
+  return WF_OK;
+}
+
+bool quantised(const wf_tensor* t) { return t->dtype == WF_MXFP8 || t->dtype == WF_MXFP4; }
+
+// The same of a quantised cache's codes (strides in elements, rows and strides
+// of whole 16 bytes).
+wf_status check_codes(const wf_tensor* t) {
+  if (!t) return WF_ERR_INVALID_ARG;
+  if (!quantised(t)) return WF_ERR_DTYPE;
+  if (t->batch < 1 || t->heads < 1 || t->seq < 1) return WF_ERR_SHAPE;
+  if (t->head_dim != 64 && t->head_dim != 128) return WF_ERR_SHAPE;
+  if (t->stride_b < 0 || t->stride_h < 0 || t->stride_s < 0) return WF_ERR_SHAPE;
+  const int64_t unit = t->dtype == WF_MXFP4 ? 32 : 16;  // elements of 16 bytes
+  if (t->stride_b % unit || t->stride_h % unit || t->stride_s % unit) return WF_ERR_ALIGN;
   if (t->seq > 1 && t->stride_s < t->head_dim) return WF_ERR_SHAPE;
   return WF_OK;
 }
@@ -468,6 +485,130 @@ WF_API wf_status wf_step_wavelet(const void* Q, const wf_tensor* q, const void* 
   const float sc = 1.0f / sqrtf((float)q->head_dim);
   e = wf::launch_attn(ap, Q, *q, K, V, *kv, idx, Kg, Vg, n_g > 0 ? g : nullptr, O, *o, sc, scratch, status, s);
   return cuda_status(e);
+}
+
+// ---------------------------------------------------------------------------
+// The quantised cache.
+// ---------------------------------------------------------------------------
+namespace {
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// The row counts that the kernels' 32-bit row numbers take.
+bool too_many_rows(int64_t units, int64_t rows) { return units * rows >= (int64_t)1 << 30; }
+
+// Descriptors and sizes of a call that moves rows (f) into or out of a cache.
+wf_status check_mx_args(const wf_tensor* f, const wf_tensor* kv, size_t scales_bytes) {
+  wf_status st;
+  if ((st = check_codes(kv)) != WF_OK) return st;
+  if ((st = check_desc(f, true)) != WF_OK) return st;
+  if (!same_units(f, kv)) return WF_ERR_SHAPE;
+  if (too_many_rows((int64_t)kv->batch * kv->heads, f->seq)) return WF_ERR_UNSUPPORTED;
+  return scales_bytes < wf_scales_bytes(kv) ? WF_ERR_WORKSPACE : WF_OK;
+}
+
+}  // namespace
+
+WF_API size_t wf_scales_bytes(const wf_tensor* kv) {
+  if (check_codes(kv) != WF_OK) return 0;
+  return (size_t)kv->batch * kv->heads * kv->seq * (kv->head_dim / 32);
+}
+
+WF_API wf_status wf_cache_quantize(const void* Knew, const void* Vnew, const wf_tensor* nt, void* Kc, void* Ks,
+                                   void* Vc, void* Vs, const wf_tensor* kv, size_t scales_bytes, int64_t pos,
+                                   void* stream) {
+  const wf_status st = check_mx_args(nt, kv, scales_bytes);
+  if (st != WF_OK) return st;
+  if (pos < 0 || pos > kv->seq || nt->seq > kv->seq - pos) return WF_ERR_INVALID_ARG;
+  if (nt->seq == 0) return WF_OK;  // a tensor without rows may have no address
+  if (!Knew || !Kc || !Ks) return WF_ERR_INVALID_ARG;
+  if ((Vnew != nullptr) != (Vc != nullptr) || (Vnew != nullptr) != (Vs != nullptr)) return WF_ERR_INVALID_ARG;
+  if (!aligned16(Knew) || !aligned16(Vnew) || !aligned16(Kc) || !aligned16(Vc) || !aligned4(Ks) || !aligned4(Vs))
+    return WF_ERR_ALIGN;
+  return cuda_status(wf::launch_quantize(Knew, Vnew, *nt, Kc, Ks, Vc, Vs, *kv, pos, static_cast<cudaStream_t>(stream)));
+}
+
+WF_API wf_status wf_cache_dequantize(const void* Kc, const void* Ks, const void* Vc, const void* Vs,
+                                     const wf_tensor* kv, size_t scales_bytes, const int32_t* idx, int64_t pos,
+                                     void* Kout, void* Vout, const wf_tensor* out, void* stream) {
+  const wf_status st = check_mx_args(out, kv, scales_bytes);
+  if (st != WF_OK) return st;
+  if (idx ? pos != 0 : (pos < 0 || pos > kv->seq || out->seq > kv->seq - pos)) return WF_ERR_INVALID_ARG;
+  if (out->seq == 0) return WF_OK;
+  if (!Kc || !Ks || !Kout) return WF_ERR_INVALID_ARG;
+  if ((Vout != nullptr) != (Vc != nullptr) || (Vout != nullptr) != (Vs != nullptr)) return WF_ERR_INVALID_ARG;
+  if (!aligned16(Kout) || !aligned16(Vout) || !aligned16(Kc) || !aligned16(Vc) || !aligned4(Ks) || !aligned4(Vs) ||
+      !aligned4(idx))
+    return WF_ERR_ALIGN;
+  return cuda_status(
+      wf::launch_dequantize(Kc, Ks, Vc, Vs, *kv, idx, pos, Kout, Vout, *out, static_cast<cudaStream_t>(stream)));
+}
+
+// ---------------------------------------------------------------------------
+// Attention over shared prompts.
+// ---------------------------------------------------------------------------
+namespace {
+
+wf_status check_prefix_args(const wf_tensor* q, const wf_tensor* kv, int k, int n_g) {
+  wf_status st;
+  if ((st = check_desc(q, false)) != WF_OK) return st;
+  if (!kv) return WF_ERR_INVALID_ARG;
+  if ((st = quantised(kv) ? check_codes(kv) : check_desc(kv, false)) != WF_OK) return st;
+  if (!quantised(kv) && kv->dtype != q->dtype) return WF_ERR_DTYPE;
+  if (kv->head_dim != q->head_dim || q->heads % kv->heads || q->batch % kv->batch) return WF_ERR_SHAPE;
+  if (k < 0 || k > kv->seq || n_g < 0) return WF_ERR_INVALID_ARG;
+  if (too_many_rows((int64_t)q->batch * q->heads, q->seq)) return WF_ERR_UNSUPPORTED;
+  return WF_OK;
+}
+
+}  // namespace
+
+WF_API size_t wf_prefix_attn_workspace_bytes(const wf_tensor* q, const wf_tensor* kv, int k, int n_g) {
+  if (check_prefix_args(q, kv, k, n_g) != WF_OK) return 0;
+  return wf::plan_prefix(*q, *kv, k, n_g).total;
+}
+
+WF_API wf_status wf_prefix_attn(const void* Q, const wf_tensor* q, const void* K, const void* V, const wf_tensor* kv,
+                                const void* Ks, const void* Vs, const int32_t* idx, int k, const int32_t* prefix_len,
+                                const void* Kg, const void* Vg, const wf_tensor* g, const int32_t* gen_len, void* O,
+                                const wf_tensor* o, float scale, void* ws, size_t ws_bytes, void* stream) {
+  const int n_g = g ? g->seq : 0;
+  wf_status st = check_prefix_args(q, kv, k, n_g);
+  if (st != WF_OK) return st;
+  if ((st = check_desc(o, false)) != WF_OK) return st;
+  if (!same_units(q, o) || o->seq != q->seq) return WF_ERR_SHAPE;
+  if (o->dtype != q->dtype) return WF_ERR_DTYPE;
+  if (g) {
+    if ((st = check_desc(g, true)) != WF_OK) return st;
+    if (g->batch != q->batch || g->heads != kv->heads || g->head_dim != q->head_dim) return WF_ERR_SHAPE;
+    if (g->dtype != q->dtype) return WF_ERR_DTYPE;
+  }
+  if (!Q || !K || !V || !O || !ws) return WF_ERR_INVALID_ARG;
+  if (quantised(kv) ? (!Ks || !Vs) : (Ks || Vs)) return WF_ERR_INVALID_ARG;
+  if (n_g > 0 && (!Kg || !Vg)) return WF_ERR_INVALID_ARG;
+  if (!(scale >= 0.f) || isinf(scale)) return WF_ERR_INVALID_ARG;
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned4(Ks) || !aligned4(Vs))
+    return WF_ERR_ALIGN;
+  if (n_g > 0 && (!aligned16(Kg) || !aligned16(Vg))) return WF_ERR_ALIGN;
+  if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0 || !aligned4(idx) || !aligned4(prefix_len) || !aligned4(gen_len))
+    return WF_ERR_ALIGN;
+  wf::PrefixPlan p = wf::plan_prefix(*q, *kv, k, n_g);
+  if (ws_bytes < p.total) return WF_ERR_WORKSPACE;
+  wf::PrefixArgs& a = p.a;
+  const int64_t code = kv->dtype == WF_MXFP4 ? 2 : 1;  // elements a byte of the codes' strides
+  a.Q = Q; a.qsb = q->stride_b; a.qsh = q->stride_h; a.qss = q->stride_s;
+  a.K = K; a.V = V;
+  a.ksb = kv->stride_b / code; a.ksh = kv->stride_h / code; a.kss = kv->stride_s / code;
+  a.Ks = static_cast<const uint8_t*>(Ks); a.Vs = static_cast<const uint8_t*>(Vs);
+  a.Kg = Kg; a.Vg = Vg;
+  if (n_g > 0) { a.gsb = g->stride_b; a.gsh = g->stride_h; a.gss = g->stride_s; }
+  a.O = O; a.osb = o->stride_b; a.osh = o->stride_h; a.oss = o->stride_s;
+  a.idx = idx; a.plen = prefix_len; a.glen = gen_len;
+  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + p.off_ml);
+  a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + p.off_o);
+  a.sl2 = 1.4426950408889634f * (scale == 0.f ? 1.0f / sqrtf((float)q->head_dim) : scale);
+  a.status = static_cast<int*>(ws);
+  return cuda_status(wf::launch_prefix(p, static_cast<cudaStream_t>(stream)));
 }
 
 WF_API wf_status wf_workspace_status(void* ws, void* stream) {

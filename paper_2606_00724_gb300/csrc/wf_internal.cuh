@@ -70,6 +70,13 @@ cudaError_t launch_dwt(const void* K, const wf_tensor& kv, int levels, void* coe
 cudaError_t launch_cache_update(const void* Kn, const void* Vn, const wf_tensor& nt, void* K, void* V,
                                 const wf_tensor& kv, int64_t pos, int levels, void* coeffs, cudaStream_t s);
 
+// The quantised cache: see wf_cache_quantize, wf_cache_dequantize (Vn, Vo null: keys alone).
+cudaError_t launch_quantize(const void* Kn, const void* Vn, const wf_tensor& nt, void* Kc, void* Ks, void* Vc,
+                            void* Vs, const wf_tensor& kv, int64_t pos, cudaStream_t s);
+cudaError_t launch_dequantize(const void* Kc, const void* Ks, const void* Vc, const void* Vs, const wf_tensor& kv,
+                              const int32_t* idx, int64_t pos, void* Ko, void* Vo, const wf_tensor& out,
+                              cudaStream_t s);
+
 // Filter workspace plan for one call.  A unit is one (batch, KV head); its
 // query block is the qs rows of each of its G query heads, q = G qs rows.
 struct FilterPlan {

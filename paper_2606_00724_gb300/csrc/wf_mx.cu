@@ -1,0 +1,207 @@
+// A cache in 8-bit or 4-bit codes: rows quantised as they are written
+// (wf_cache_quantize) and read back (wf_cache_dequantize).
+//
+// Both move bytes and hardly compute, so they are bound by memory: a thread
+// takes 16 bytes of the floating-point side (8 bf16 or 4 fp32 channels), so
+// that a warp reads or writes 512 consecutive bytes there and the matching 128
+// to 256 bytes of codes, and UN rows, all of them loaded before the first is
+// used.  The 4 or 8 lanes that share a block find its largest magnitude with
+// shuffles, as integers: the bits of |x| are ordered as the values are, with
+// infinities and NaN above them.
+#include "wf_mx.cuh"
+#include "wf_sm100.cuh"
+
+namespace wf {
+namespace {
+
+constexpr int NTH = 256;
+
+struct MxArgs {
+  const void* src[2];    // K and V: fp32 / bf16 rows (quantise) or codes (read back)
+  void* dst[2];          // codes or rows
+  uint8_t* scales[2];
+  int64_t fsb, fsh, fss; // strides of the fp32 / bf16 rows, in elements
+  int64_t csb, csh, css; // strides of the codes, in bytes
+  const int32_t* idx;    // [unit][rows] rows to read back, or null: pos + row
+  int64_t pos;
+  uint32_t rows, total;  // rows a unit, of all units
+  int H, n;
+};
+
+template <int BYTES> struct Word;
+template <> struct Word<8> { typedef uint2 type; };
+template <> struct Word<4> { typedef uint32_t type; };
+template <> struct Word<2> { typedef uint16_t type; };
+
+__device__ __forceinline__ uint32_t half_word(const uint2& w, int i) { return ((i < 2 ? w.x : w.y) >> (16 * (i & 1))) & 0xffffu; }
+__device__ __forceinline__ uint32_t half_word(uint32_t w, int i) { return (w >> (16 * i)) & 0xffffu; }
+
+// Codes of the N channels of one thread, two at a time: a code pair is 16 bits
+// (E4M3) or 8 (E2M1).
+template <bool FP4, int N>
+__device__ __forceinline__ typename Word<FP4 ? N / 2 : N>::type pack_codes(const float* y) {
+  constexpr int BITS = FP4 ? 8 : 16;
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) w[i * BITS / 32] |= mx_encode2<FP4>(y[2 * i], y[2 * i + 1]) << (i * BITS % 32);
+  if constexpr (!FP4 && N == 8) return make_uint2(w[0], w[1]);
+  else return (typename Word<FP4 ? N / 2 : N>::type)w[0];
+}
+template <bool FP4, int N>
+__device__ __forceinline__ void unpack_codes(const typename Word<FP4 ? N / 2 : N>::type& c, float* y) {
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    uint32_t pair;
+    if constexpr (FP4) pair = ((uint32_t)c >> (8 * i)) & 0xffu;
+    else pair = half_word(c, i);
+    const float2 v = mx_decode2<FP4>(pair);
+    y[2 * i] = v.x;
+    y[2 * i + 1] = v.y;
+  }
+}
+
+template <typename T, bool FP4, int D, int UN>
+__global__ void __launch_bounds__(NTH) quantize_kernel(const __grid_constant__ MxArgs a) {
+  constexpr int N = Vec<T>::N;          // channels a thread
+  constexpr int TPR = D / N;            // threads a row
+  constexpr int TPB = kMxBlock / N;     // threads a block
+  constexpr int RPC = NTH / TPR;        // rows a pass of the CTA
+  typedef typename Word<FP4 ? N / 2 : N>::type W;
+  const int t = threadIdx.x % TPR, y = blockIdx.y;
+  const uint32_t r0 = blockIdx.x * (RPC * UN) + threadIdx.x / TPR;
+  sm100::grid_dep_wait();
+  uint4 v[UN];
+#pragma unroll
+  for (int i = 0; i < UN; ++i) {
+    const uint32_t r = min(r0 + RPC * i, a.total - 1);
+    const uint32_t u = r / a.rows;
+    const int64_t o = (int64_t)(u / a.H) * a.fsb + (int64_t)(u % a.H) * a.fsh + (int64_t)(r - u * a.rows) * a.fss;
+    v[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.src[y]) + o) + t);
+  }
+  sm100::grid_dep_launch();
+#pragma unroll
+  for (int i = 0; i < UN; ++i) {
+    const uint32_t r = r0 + RPC * i;
+    float x[N];
+    widen_vec(static_cast<const T*>(nullptr), v[i], x);
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+#pragma unroll
+    for (int s = 1; s < TPB; s *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
+    const uint32_t byte = mx_scale_byte<FP4>(top);
+    const float inv = byte == 255 ? 0.f : mx_inv_scale(byte);
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = byte == 255 ? 0.f : x[e] * inv;
+    if (r < a.total) {
+      const uint32_t u = r / a.rows;
+      const int64_t row = a.pos + (r - u * a.rows);
+      char* c = static_cast<char*>(a.dst[y]) + (int64_t)(u / a.H) * a.csb + (int64_t)(u % a.H) * a.csh + row * a.css;
+      reinterpret_cast<W*>(c)[t] = pack_codes<FP4, N>(x);
+      if (t % TPB == 0) a.scales[y][((int64_t)u * a.n + row) * (D / kMxBlock) + t / TPB] = (uint8_t)byte;
+    }
+  }
+}
+
+template <typename T, bool FP4, int D, int UN>
+__global__ void __launch_bounds__(NTH) dequantize_kernel(const __grid_constant__ MxArgs a) {
+  constexpr int N = Vec<T>::N, TPR = D / N, TPB = kMxBlock / N, RPC = NTH / TPR;
+  typedef typename Word<FP4 ? N / 2 : N>::type W;
+  const int t = threadIdx.x % TPR, y = blockIdx.y;
+  const uint32_t r0 = blockIdx.x * (RPC * UN) + threadIdx.x / TPR;
+  sm100::grid_dep_wait();
+  W c[UN];
+  uint32_t byte[UN];
+  int64_t row[UN];
+#pragma unroll
+  for (int i = 0; i < UN; ++i) {
+    const uint32_t r = min(r0 + RPC * i, a.total - 1);
+    row[i] = a.pos + r % a.rows;
+    if (a.idx) row[i] = min(max(__ldg(a.idx + r), 0), a.n - 1);
+  }
+#pragma unroll
+  for (int i = 0; i < UN; ++i) {
+    const uint32_t u = min(r0 + RPC * i, a.total - 1) / a.rows;
+    const char* p = static_cast<const char*>(a.src[y]) + (int64_t)(u / a.H) * a.csb + (int64_t)(u % a.H) * a.csh +
+                    row[i] * a.css;
+    c[i] = __ldg(reinterpret_cast<const W*>(p) + t);
+    byte[i] = __ldg(a.scales[y] + ((int64_t)u * a.n + row[i]) * (D / kMxBlock) + t / TPB);
+  }
+  sm100::grid_dep_launch();
+#pragma unroll
+  for (int i = 0; i < UN; ++i) {
+    const uint32_t r = r0 + RPC * i;
+    if (r >= a.total) break;
+    float x[N];
+    unpack_codes<FP4, N>(c[i], x);
+    const float s = mx_scale(byte[i]);
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] *= s;
+    const uint32_t u = r / a.rows;
+    const int64_t o = (int64_t)(u / a.H) * a.fsb + (int64_t)(u % a.H) * a.fsh + (int64_t)(r - u * a.rows) * a.fss;
+    st_vec(static_cast<T*>(a.dst[y]) + o + t * N, x);
+  }
+}
+
+template <typename T, bool FP4, int D, bool BACK>
+cudaError_t launch_un(const MxArgs& a, int tensors, cudaStream_t s) {
+  constexpr int RPC = NTH / (D / Vec<T>::N);
+  // Four rows a thread from a few waves of CTAs on: fewer CTAs and more loads in
+  // flight a thread; below that, as many threads as possible.
+  const bool many = (int64_t)a.total * tensors > 8ll * RPC * 8 * sm_count();
+  const int un = many ? 4 : 1;
+  const dim3 grid((a.total + RPC * un - 1) / (RPC * un), (unsigned)tensors);
+  Launch l(grid, NTH, 0, s);
+  if (BACK) return many ? l(dequantize_kernel<T, FP4, D, 4>, a) : l(dequantize_kernel<T, FP4, D, 1>, a);
+  return many ? l(quantize_kernel<T, FP4, D, 4>, a) : l(quantize_kernel<T, FP4, D, 1>, a);
+}
+
+template <bool BACK>
+cudaError_t launch(const MxArgs& a, int dtype, int fmt, int d, int tensors, cudaStream_t s) {
+  if (a.total == 0) return cudaSuccess;
+  const bool fp4 = fmt == WF_MXFP4, wide = d == 128;
+#define WF_MX(T)                                                                                       \
+  (fp4 ? (wide ? launch_un<T, true, 128, BACK>(a, tensors, s) : launch_un<T, true, 64, BACK>(a, tensors, s)) \
+       : (wide ? launch_un<T, false, 128, BACK>(a, tensors, s) : launch_un<T, false, 64, BACK>(a, tensors, s)))
+  return dtype == WF_BF16 ? WF_MX(bf16) : WF_MX(float);
+#undef WF_MX
+}
+
+MxArgs mx_args(const wf_tensor& f, const wf_tensor& kv) {
+  MxArgs a = {};
+  const int half = kv.dtype == WF_MXFP4 ? 2 : 1;  // strides of whole 16 bytes, so the division is exact
+  a.fsb = f.stride_b; a.fsh = f.stride_h; a.fss = f.stride_s;
+  a.csb = kv.stride_b / half; a.csh = kv.stride_h / half; a.css = kv.stride_s / half;
+  a.rows = (uint32_t)f.seq;
+  a.total = (uint32_t)((int64_t)kv.batch * kv.heads * f.seq);
+  a.H = kv.heads;
+  a.n = kv.seq;
+  return a;
+}
+
+}  // namespace
+
+cudaError_t launch_quantize(const void* Kn, const void* Vn, const wf_tensor& nt, void* Kc, void* Ks, void* Vc,
+                            void* Vs, const wf_tensor& kv, int64_t pos, cudaStream_t s) {
+  MxArgs a = mx_args(nt, kv);
+  a.src[0] = Kn; a.src[1] = Vn;
+  a.dst[0] = Kc; a.dst[1] = Vc;
+  a.scales[0] = static_cast<uint8_t*>(Ks); a.scales[1] = static_cast<uint8_t*>(Vs);
+  a.pos = pos;
+  return launch<false>(a, nt.dtype, kv.dtype, kv.head_dim, Vn ? 2 : 1, s);
+}
+
+cudaError_t launch_dequantize(const void* Kc, const void* Ks, const void* Vc, const void* Vs, const wf_tensor& kv,
+                              const int32_t* idx, int64_t pos, void* Ko, void* Vo, const wf_tensor& out,
+                              cudaStream_t s) {
+  MxArgs a = mx_args(out, kv);
+  a.src[0] = Kc; a.src[1] = Vc;
+  a.dst[0] = Ko; a.dst[1] = Vo;
+  a.scales[0] = static_cast<uint8_t*>(const_cast<void*>(Ks));
+  a.scales[1] = static_cast<uint8_t*>(const_cast<void*>(Vs));
+  a.idx = idx;
+  a.pos = pos;
+  return launch<true>(a, out.dtype, kv.dtype, kv.head_dim, Vo ? 2 : 1, s);
+}
+
+}  // namespace wf

@@ -1,0 +1,76 @@
+// Attention over shared prompts (wf_prefix_attn): what its kernels share.
+#pragma once
+
+#include "wf_internal.cuh"
+
+namespace wf {
+
+// One call.  A prompt unit is one (prompt, key head): its R = each G q query
+// rows are those of all its sequences, row r belonging to sequence
+// r / (G q) of the prompt, head (r / q) % G of the group and row r % q of the
+// block.  An own unit is one (sequence, key head) with its G q rows.  A part is
+// what one CTA finds for its rows over a range of their keys: the row's maximum
+// m (log2 units) and sum l of 2^(s - m), and the unnormalised O; parts [0, S)
+// are ranges of the prompt, the rest of the own rows.
+struct PrefixArgs {
+  const void* Q;
+  int64_t qsb, qsh, qss;
+  const void* K;
+  const void* V;
+  const uint8_t* Ks;
+  const uint8_t* Vs;
+  int64_t ksb, ksh, kss;  // elements (fp32, bf16) or bytes (codes)
+  const void* Kg;
+  const void* Vg;
+  int64_t gsb, gsh, gss;
+  void* O;
+  int64_t osb, osh, oss;
+  const int32_t* idx;
+  const int32_t* plen;
+  const int32_t* glen;
+  int B, P, H, G, q, d, n, k, ng;
+  int each;       // sequences a prompt
+  int R, Ro;      // query rows of a prompt unit, of an own unit
+  int S, So;      // parts of the prompt, of the own rows
+  int mt, mto;    // row tiles of a prompt unit, of an own unit
+  int64_t rows;   // B Hq q
+  float* part_o;  // [parts][rows][d], rows in [B, Hq, q] order
+  float2* part_ml;
+  float sl2;      // scale log2(e)
+  int* status;
+};
+
+// The workspace of a call: the status word, then the parts.
+struct PrefixPlan {
+  PrefixArgs a;  // shapes and splits; pointers are filled in by the call
+  int dtype, fmt;
+  int parts;     // 1: the kernel writes O itself
+  size_t off_ml, off_o, total;
+};
+PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g);
+cudaError_t launch_prefix(const PrefixPlan& p, cudaStream_t s);
+
+// Sequence, query head and block row of row r of unit u.
+struct RowAt {
+  int b, hq, i;
+};
+__device__ __forceinline__ RowAt prompt_row(const PrefixArgs& a, int u, int r) {
+  const int s = r / a.Ro, w = r - s * a.Ro, g = w / a.q;
+  return {(u / a.H) * a.each + s, (u % a.H) * a.G + g, w - g * a.q};
+}
+__device__ __forceinline__ RowAt own_row(const PrefixArgs& a, int u, int r) {
+  const int g = r / a.q;
+  return {u / a.H, (u % a.H) * a.G + g, r - g * a.q};
+}
+__device__ __forceinline__ int64_t flat_row(const PrefixArgs& a, const RowAt& r) {
+  return ((int64_t)r.b * (a.H * a.G) + r.hq) * a.q + r.i;
+}
+// Rows that count of prompt p, of sequence b.
+__device__ __forceinline__ int prompt_count(const PrefixArgs& a, int p) {
+  return a.plen ? min(a.k, max(0, __ldg(a.plen + p))) : a.k;
+}
+__device__ __forceinline__ int own_count(const PrefixArgs& a, int b) {
+  return a.glen ? min(a.ng, max(0, __ldg(a.glen + b))) : a.ng;
+}
+
+}  // namespace wf

@@ -24,7 +24,7 @@ import torch
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libwf.so")
 
-WF_F32, WF_BF16 = 0, 1
+WF_F32, WF_BF16, WF_MXFP8, WF_MXFP4 = 0, 1, 2, 3
 _DTYPES = {torch.float32: WF_F32, torch.bfloat16: WF_BF16}
 
 
@@ -66,6 +66,12 @@ SIGNATURES = {
     "wf_step": (_I, [_P, _T, _P, _P, _T, _P, _P, _T, _P, _SZ, _I, _I, _P, _P, _P, _P, _T, _P, _SZ, _P]),
     "wf_step_wavelet_workspace_bytes": (_SZ, [_T, _T, _I, _P, _I, _I]),
     "wf_step_wavelet": (_I, [_P, _T, _P, _P, _P, _T, _P, _P, _T, _I, _P, _I, _P, _P, _P, _T, _P, _SZ, _P]),
+    "wf_scales_bytes": (_SZ, [_T]),
+    "wf_cache_quantize": (_I, [_P, _P, _T, _P, _P, _P, _P, _T, _SZ, _I64, _P]),
+    "wf_cache_dequantize": (_I, [_P, _P, _P, _P, _T, _SZ, _P, _I64, _P, _P, _T, _P]),
+    "wf_prefix_attn_workspace_bytes": (_SZ, [_T, _T, _I, _I]),
+    "wf_prefix_attn": (_I, [_P, _T, _P, _P, _T, _P, _P, _P, _I, _P, _P, _P, _T, _P, _P, _T, ctypes.c_float, _P, _SZ,
+                            _P]),
     "wf_workspace_status": (_I, [_P, _P]),
     # include/wf_testing.h (test-only)
     "wf_testing_set_wait_failure": (_I, [_I, ctypes.c_longlong]),
@@ -111,8 +117,55 @@ def desc(t: torch.Tensor) -> wf_tensor:
     return wf_tensor(B, H, S, D, sb, sh, ss, code)
 
 
+def code_desc(codes: torch.Tensor, fmt: int) -> wf_tensor:
+    """wf_tensor for the codes of a quantised cache: [B, H, rows, d] bytes
+    (WF_MXFP8) or [B, H, rows, d / 2] (WF_MXFP4), last axis contiguous."""
+    if codes.dim() != 4 or codes.element_size() != 1:
+        raise ValueError("expected a [B, H, rows, bytes] tensor of 8-bit codes")
+    if fmt not in (WF_MXFP8, WF_MXFP4):
+        raise ValueError(f"unknown format {fmt}")
+    per = 2 if fmt == WF_MXFP4 else 1
+    sb, sh, ss, sd = codes.stride()
+    B, H, S, W = codes.shape
+    if W > 1 and sd != 1:
+        raise ValueError("head_dim axis must be contiguous")
+    return wf_tensor(B, H, S, W * per, sb * per, sh * per, ss * per, fmt)
+
+
+def _scales(K_scales, V_scales):
+    """Size of the smaller scale tensor (contiguous bytes; 0 if there is none)."""
+    size = 0
+    for s in (K_scales, V_scales):
+        if s is not None:
+            if s.element_size() != 1 or not s.is_contiguous():
+                raise ValueError("scales must be contiguous bytes")
+            size = min(size, s.nbytes) if size else s.nbytes
+    return size
+
+
+def _on_gpu(*tensors):
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise ValueError("expected tensors on the GPU")
+
+
+def _pair(K, V, what: str):
+    """V, where it is given, lies as K does."""
+    if K is not None and V is not None and not (_same_layout(V, K) and V.dtype == K.dtype):
+        raise ValueError(f"{what} must share dtype, shape and strides")
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+def _ints(t):
+    """Address of a contiguous int32 tensor, or None."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or not t.is_contiguous():
+        raise ValueError("indices and lengths must be contiguous int32 tensors")
+    return t.data_ptr()
 
 
 def _same_layout(a, b) -> bool:
@@ -301,6 +354,67 @@ def wf_step_wavelet(Q, top, K, V, Kg, Vg, levels: int, keep, wavelet: int, idx, 
                                  _ptr(Kg), _ptr(Vg), dg, levels,
                                  _keep_arr(keep), wavelet, _ptr(idx), _ptr(level_sets), _ptr(O), do,
                                  _ptr(ws), ws.nbytes, _stream(stream)), "wf_step_wavelet")
+
+
+def wf_scales_bytes(codes: torch.Tensor, fmt: int) -> int:
+    return int(lib().wf_scales_bytes(code_desc(codes, fmt)))
+
+
+def wf_cache_quantize(Knew, Vnew, Kc, Ks, Vc, Vs, fmt: int, pos: int, stream=None) -> None:
+    """Quantise Knew (and Vnew) into the caches' codes and scales at
+    [pos, pos + count) (see the C header; Vnew, Vc, Vs all None: keys alone)."""
+    _on_gpu(Knew, Vnew, Kc, Ks, Vc, Vs)
+    _pair(Knew, Vnew, "Knew and Vnew")
+    _pair(Kc, Vc, "Kc and Vc")
+    _check(lib().wf_cache_quantize(_ptr(Knew), _ptr(Vnew), desc(Knew), _ptr(Kc), _ptr(Ks), _ptr(Vc), _ptr(Vs),
+                                   code_desc(Kc, fmt), _scales(Ks, Vs), pos, _stream(stream)), "wf_cache_quantize")
+
+
+def wf_cache_dequantize(Kc, Ks, Vc, Vs, fmt: int, Kout, Vout, pos: int = 0, idx=None, stream=None) -> None:
+    """Rows [pos, pos + m), or the rows idx ([B*H][m] int32), of the caches
+    into Kout (and Vout) ([B, H, m, d]) (see the C header)."""
+    _on_gpu(Kc, Ks, Vc, Vs, Kout, Vout, idx)
+    _pair(Kout, Vout, "Kout and Vout")
+    _pair(Kc, Vc, "Kc and Vc")
+    if idx is not None and tuple(idx.shape) != (Kout.shape[0] * Kout.shape[1], Kout.shape[2]):
+        raise ValueError("idx must be [B*H, m]")
+    _check(lib().wf_cache_dequantize(_ptr(Kc), _ptr(Ks), _ptr(Vc), _ptr(Vs), code_desc(Kc, fmt), _scales(Ks, Vs),
+                                     _ints(idx), pos, _ptr(Kout), _ptr(Vout), desc(Kout), _stream(stream)),
+           "wf_cache_dequantize")
+
+
+def _prefix_desc(K, fmt):
+    return desc(K) if fmt is None else code_desc(K, fmt)
+
+
+def wf_prefix_attn_workspace_bytes(Q: torch.Tensor, K: torch.Tensor, k: int, n_g: int, fmt=None) -> int:
+    return int(lib().wf_prefix_attn_workspace_bytes(desc(Q), _prefix_desc(K, fmt), k, n_g))
+
+
+def wf_prefix_attn(Q, K, V, k: int, Kg, Vg, O, ws, idx=None, prefix_len=None, gen_len=None, Ks=None, Vs=None,
+                   fmt=None, scale: float = 0.0, stream=None) -> None:
+    """Attention of Q [B, Hq, q, d] over P cached prompts K, V [P, H, n, d], the
+    first k rows or the rows idx [P*H, k] of each, and each sequence's own rows
+    Kg, Vg [B, H, n_g, d] (see the C header).  fmt (WF_MXFP8, WF_MXFP4): K and V
+    are codes, with scales Ks and Vs."""
+    dq, dk, do = desc(Q), _prefix_desc(K, fmt), desc(O)
+    dg = desc(Kg) if Kg is not None else None
+    _on_gpu(Q, K, V, Kg, Vg, O, ws, idx, prefix_len, gen_len, Ks, Vs)
+    _pair(K, V, "K and V")
+    _pair(Kg, Vg, "Kg and Vg")
+    if fmt is not None:
+        need = K.shape[0] * K.shape[1] * K.shape[2] * (Q.shape[3] // 32)
+        if Ks is None or Vs is None or _scales(Ks, Vs) < need:
+            raise ValueError("a quantised prompt needs the scales of its K and V")
+    if idx is not None and tuple(idx.shape) != (K.shape[0] * K.shape[1], k):
+        raise ValueError("idx must be [P*H, k]")
+    if prefix_len is not None and prefix_len.numel() != K.shape[0]:
+        raise ValueError("prefix_len must have an entry a prompt")
+    if gen_len is not None and gen_len.numel() != Q.shape[0]:
+        raise ValueError("gen_len must have an entry a sequence")
+    _check(lib().wf_prefix_attn(_ptr(Q), dq, _ptr(K), _ptr(V), dk, _ptr(Ks), _ptr(Vs), _ints(idx), k,
+                                _ints(prefix_len), _ptr(Kg), _ptr(Vg), dg, _ints(gen_len), _ptr(O), do, float(scale),
+                                _ptr(ws), ws.nbytes, _stream(stream)), "wf_prefix_attn")
 
 
 def wf_workspace_status(ws: torch.Tensor, stream=None):
