@@ -608,6 +608,9 @@ WF_API wf_status wf_prefix_attn(const void* Q, const wf_tensor* q, const void* K
   a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + p.off_o);
   a.sl2 = 1.4426950408889634f * (scale == 0.f ? 1.0f / sqrtf((float)q->head_dim) : scale);
   a.status = static_cast<int*>(ws);
+  const wf::WaitControls wc = wf::wait_controls();
+  a.wait_limit = wc.limit;
+  a.stall = wc.stall;
   return cuda_status(wf::launch_prefix(p, static_cast<cudaStream_t>(stream)));
 }
 

@@ -1,5 +1,5 @@
 // Attention of several sequences over one cached prompt (wf_prefix_attn), in
-// fp32 arithmetic, and the joining of parts.
+// fp32 arithmetic for fp32 queries, and the joining of parts.
 //
 // Every query row of a prompt's key head, whatever its sequence, meets the same
 // keys, so the rows of all of them are stacked and the prompt is read once a
@@ -257,30 +257,29 @@ __global__ void __launch_bounds__(NTH) join_kernel(const __grid_constant__ Prefi
   for (int e = 0; e < 4; ++e) from_f32(op[e], l == 0.f ? 0.f : o[e] * inv);
 }
 
-template <typename T, int CACHE, int D>
+template <int CACHE, int D>
 cudaError_t launch_simt(const PrefixArgs& a, cudaStream_t s) {
   const int64_t items = (int64_t)a.P * a.H * a.mt * a.S + (int64_t)a.B * a.H * a.mto * a.So;
+  if (!items) return cudaSuccess;
   const bool few = (a.R > a.Ro ? a.R : a.Ro) <= 16;
-  const auto k = few ? simt_kernel<T, CACHE, D, 16> : simt_kernel<T, CACHE, D, 64>;
+  const auto k = few ? simt_kernel<float, CACHE, D, 16> : simt_kernel<float, CACHE, D, 64>;
   const size_t smem = few ? simt_smem<D, 16>() : simt_smem<D, 64>();
-  if (items) {
-    cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(k), smem);
-    if (e != cudaSuccess) return e;
-    if ((e = Launch(dim3((unsigned)items), NTH, smem, s)(k, a)) != cudaSuccess) return e;
-  }
-  if (a.S + a.So == 1) return cudaSuccess;
-  const int per = NTH / (D / 4);
-  return Launch(dim3((unsigned)((a.rows + per - 1) / per)), NTH, 0, s)(join_kernel<T, D>, a);
+  const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(k), smem);
+  return e != cudaSuccess ? e : Launch(dim3((unsigned)items), NTH, smem, s)(k, a);
 }
 
-template <typename T>
-cudaError_t launch_type(const PrefixPlan& p, cudaStream_t s) {
+cudaError_t launch_parts(const PrefixPlan& p, cudaStream_t s) {
   const bool wide = p.a.d == 128;
-  if (p.fmt == WF_MXFP8)
-    return wide ? launch_simt<T, kFp8, 128>(p.a, s) : launch_simt<T, kFp8, 64>(p.a, s);
-  if (p.fmt == WF_MXFP4)
-    return wide ? launch_simt<T, kFp4, 128>(p.a, s) : launch_simt<T, kFp4, 64>(p.a, s);
-  return wide ? launch_simt<T, kPlain, 128>(p.a, s) : launch_simt<T, kPlain, 64>(p.a, s);
+  if (p.dtype == WF_BF16) return launch_prefix_tc(p, s);
+  if (p.fmt == WF_MXFP8) return wide ? launch_simt<kFp8, 128>(p.a, s) : launch_simt<kFp8, 64>(p.a, s);
+  if (p.fmt == WF_MXFP4) return wide ? launch_simt<kFp4, 128>(p.a, s) : launch_simt<kFp4, 64>(p.a, s);
+  return wide ? launch_simt<kPlain, 128>(p.a, s) : launch_simt<kPlain, 64>(p.a, s);
+}
+
+template <typename T, int D>
+cudaError_t launch_join(const PrefixArgs& a, cudaStream_t s) {
+  const int per = NTH / (D / 4);
+  return Launch(dim3((unsigned)((a.rows + per - 1) / per)), NTH, 0, s)(join_kernel<T, D>, a);
 }
 
 }  // namespace
@@ -296,15 +295,16 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   a.rows = (int64_t)a.B * q.heads * a.q;
   p.dtype = q.dtype;
   p.fmt = kv.dtype;
-  const int tr = (a.R > a.Ro ? a.R : a.Ro) <= 16 ? 16 : 64;
+  const bool tc = p.dtype == WF_BF16;
+  const int tr = tc ? kPrefixTcRows : (a.R > a.Ro ? a.R : a.Ro) <= 16 ? 16 : 64;
   a.mt = (a.R + tr - 1) / tr;
   a.mto = (a.Ro + tr - 1) / tr;
-  // Splits: two CTAs an SM, as many parts as fill them once, of at least four
-  // tiles each.
-  const int slots = 304;
+  // Splits: as many parts as fill the SMs once (one CTA an SM, two of the fp32
+  // kernel), of at least two tiles of 128 keys each.
+  const int slots = tc ? 152 : 304;
   auto split = [&](int64_t units, int keys) {
     if (!keys) return 0;
-    const int64_t most = std::max(1, (keys + 4 * TK - 1) / (4 * TK));
+    const int64_t most = std::max(1, (keys + 255) / 256);
     return (int)std::min(most, std::max<int64_t>(1, slots / units));
   };
   a.S = split((int64_t)a.P * a.H * a.mt, k);
@@ -318,7 +318,10 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
 }
 
 cudaError_t launch_prefix(const PrefixPlan& p, cudaStream_t s) {
-  return p.dtype == WF_BF16 ? launch_type<bf16>(p, s) : launch_type<float>(p, s);
+  const cudaError_t e = launch_parts(p, s);
+  if (e != cudaSuccess || p.parts == 1) return e;
+  if (p.dtype == WF_BF16) return p.a.d == 128 ? launch_join<bf16, 128>(p.a, s) : launch_join<bf16, 64>(p.a, s);
+  return p.a.d == 128 ? launch_join<float, 128>(p.a, s) : launch_join<float, 64>(p.a, s);
 }
 
 }  // namespace wf

@@ -38,7 +38,11 @@ struct PrefixArgs {
   float2* part_ml;
   float sl2;      // scale log2(e)
   int* status;
+  long long wait_limit;  // bound of the tensor-core kernel's waits (cycles)
+  int stall;             // test-only: its first wait is on a barrier that nothing completes
 };
+
+constexpr int kPrefixTcRows = 256;  // query rows a CTA of the tensor-core kernel
 
 // The workspace of a call: the status word, then the parts.
 struct PrefixPlan {
@@ -49,6 +53,7 @@ struct PrefixPlan {
 };
 PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g);
 cudaError_t launch_prefix(const PrefixPlan& p, cudaStream_t s);
+cudaError_t launch_prefix_tc(const PrefixPlan& p, cudaStream_t s);  // the parts (or O) of bf16 queries
 
 // Sequence, query head and block row of row r of unit u.
 struct RowAt {

@@ -1,0 +1,570 @@
+// Attention over shared prompts for bf16 queries on the tensor cores.
+//
+// A CTA takes up to 256 stacked query rows of a unit and a range of its keys,
+// in tiles of 128 keys that arrive in a ring of shared-memory stages:
+//   S = Q K^T  (128 rows x 128 keys, TMEM)
+//   P = 2^(s - m), bf16, written over S in TMEM
+//   O += P V   (A operand from TMEM, V the MN-major B operand)
+// The query rows lie on the TMEM lanes, so a thread owns a row: its maximum and
+// sum are serial and no exchange between lanes is needed.  m is raised lazily,
+// when a tile's maximum exceeds it by more than 2^8, so P stays below 2^8 and O
+// is rescaled only then.
+//
+// Two warpgroups form P in turn, each with an S and an O of its own in TMEM.
+// With more than 128 rows (`wide`) they own a row tile each and meet the same
+// key tiles; with at most 128 they share the row tile and take every other key
+// tile, so that one works while the other's products run, and their O are put
+// together at the end.  The producers' copies and the MMA thread's products
+// run ahead of both: the key tile of the next step is multiplied as soon as P
+// of this one is consumed.
+//
+// bf16 prompt rows are copied by cp.async into the 128-byte-swizzled stages,
+// gathered through idx where there is one.  Codes are copied raw into a ring of
+// the thread's own, then widened to bf16 (exact: at most 4 digits and a power of
+// two) into the stage.  Rows past a count are zero-filled and never read.
+//
+// P is rounded to bf16 as the operand of the product; sums, maxima and O stay in
+// fp32.  Every wait is bounded: one that gives up sets the status word and the
+// abort word, every role leaves its loops, work in flight is drained and the
+// tensor memory freed.
+#include <float.h>
+
+#include "wf_mx.cuh"
+#include "wf_prefix.cuh"
+#include "wf_sm100.cuh"
+
+namespace wf {
+namespace {
+
+using namespace sm100;
+
+constexpr int TM = kPrefixTcRows / 2;  // rows of a row tile, keys of a key tile
+constexpr int HALF = TM * 128;         // 64 channels of a tile of bf16 rows
+constexpr float kLazy = 8.f;
+
+template <int D, int FMT>
+struct Cfg {
+  static constexpr bool CODES = FMT != WF_BF16;
+  static constexpr int NPT = CODES ? 256 : 128;          // producer threads
+  static constexpr int NTH = 256 + NPT + 32;             // softmax warps, producers, MMA warp
+  static constexpr int TILE = TM * D * 2;                // a stage
+  static constexpr int ROWB = FMT == WF_MXFP4 ? D / 2 : D;  // bytes of a row of codes
+  static constexpr int CPT = CODES ? TM * ROWB / 16 / NPT : 0;  // 16-byte chunks of codes a thread and tile
+  static constexpr int DEPTH = FMT == WF_MXFP8 ? 3 : 4;  // tiles of codes in flight
+  static constexpr int RAW = CODES ? DEPTH * NPT * CPT * 20 : 0;  // chunks and their scale words
+  static constexpr int STAGES = (232448 - 2048 - 2 * TILE - RAW) / TILE > 8 ? 8 : (232448 - 2048 - 2 * TILE - RAW) / TILE;
+  static constexpr size_t SMEM = 1024 + 2 * TILE + RAW + (size_t)STAGES * TILE + 512;
+};
+
+struct Bars {
+  unsigned long long full[8], empty[8], qfull, sfull[2], pready[2], odone[2], stall, drain;
+  uint32_t tmem, abort;
+};
+
+__device__ __forceinline__ uint32_t bar(const unsigned long long& b) { return smem_u32(&b); }
+
+// A wait that gives up, or follows one that did, returns false.
+__device__ __forceinline__ bool wait(uint32_t b, uint32_t parity, Bars& s, const PrefixArgs& a) {
+  if (mbar_wait_bounded(b, parity, a.wait_limit, smem_u32(&s.abort))) return true;
+  if (!abort_set(smem_u32(&s.abort))) {
+    atomicExch(&s.abort, 1u);
+    atomicExch(a.status, 1);
+  }
+  return false;
+}
+
+// The same for a whole warp: every lane gets one answer.
+__device__ __forceinline__ bool warp_wait(uint32_t b, uint32_t parity, Bars& s, const PrefixArgs& a) {
+  return __all_sync(0xffffffffu, wait(b, parity, s, a));
+}
+
+// D[tmem] (+)= A[tmem] B[smem]: A's rows on the lanes, two bf16 a column.
+__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                            uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+// What a CTA works on.
+struct Item {
+  bool own, wide;
+  int u, part, r0, nr;  // unit, part, first row, rows
+  int k0, k1, T;        // keys [k0, k1), tiles
+};
+
+__device__ __forceinline__ Item item_of(const PrefixArgs& a) {
+  Item w;
+  const int prompts = a.P * a.H * a.mt * a.S;
+  int it = blockIdx.x;
+  w.own = it >= prompts;
+  if (w.own) it -= prompts;
+  const int mt = w.own ? a.mto : a.mt, S = w.own ? a.So : a.S;
+  const int tile = it % mt, sp = (it / mt) % S;
+  w.u = it / mt / S;
+  w.part = w.own ? a.S + sp : sp;
+  w.r0 = tile * kPrefixTcRows;
+  w.nr = min(kPrefixTcRows, (w.own ? a.Ro : a.R) - w.r0);
+  w.wide = w.nr > TM;
+  const int count = w.own ? own_count(a, w.u / a.H) : prompt_count(a, w.u / a.H);
+  const int tiles = (count + TM - 1) / TM, per = (tiles + S - 1) / S;
+  w.k0 = min(count, sp * per * TM);
+  w.k1 = min(count, (sp + 1) * per * TM);
+  w.T = (w.k1 - w.k0 + TM - 1) / TM;
+  return w;
+}
+
+// Key tiles meet the MMA thread in the order K_0 .. K_(A-1), then V_j, K_(j+A)
+// for j = 0 .., A = 1 (wide) or 2.  f(tile, is V) for each in that order.
+template <typename F>
+__device__ __forceinline__ void in_order(int T, int A, F f) {
+  for (int t = 0; t < min(A, T); ++t) f(t, false);
+  for (int j = 0; j < T; ++j) {
+    f(j, true);
+    if (j + A < T) f(j + A, false);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Producers.
+// ---------------------------------------------------------------------------
+// Byte offset of 16-byte chunk ch of row r in a swizzled tile.
+__device__ __forceinline__ uint32_t swizzled(int r, int ch) {
+  return (uint32_t)((ch >> 3) * HALF + r * 128 + (((ch ^ r) & 7) << 4));
+}
+
+// One tile of bf16 rows, NPT threads: chunk tid % CH of rows tid / CH + RS i.
+// With idx, lane ch of the CH lanes that share a row looks up rows
+// tid / CH + RS (ch + CH k) and the lanes pass them on.
+template <int D, int NPT>
+__device__ __forceinline__ void copy_tile(uint32_t st, const bf16* base, int64_t stride, const int32_t* idx, int n, int t0,
+                                          int k1, int tid) {
+  constexpr int CH = D / 8, RS = NPT / CH, NI = TM / RS;
+  const int ch = tid % CH, rr = tid / CH;
+  const bf16* src = base + ch * 8;
+  if (idx) {
+    constexpr int NL = (NI + CH - 1) / CH;
+    int row[NL];
+#pragma unroll
+    for (int k = 0; k < NL; ++k) {
+      const int j = t0 + rr + RS * (ch + CH * k);
+      row[k] = ch + CH * k < NI && j < k1 ? min(max(__ldg(idx + j), 0), n - 1) : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int r = rr + RS * i;
+      const int at = __shfl_sync(0xffffffffu, row[i / CH], i % CH, CH);
+      const bool ok = t0 + r < k1;
+      cp_async16_zfill(st + swizzled(r, ch), src + (ok ? (int64_t)at * stride : 0), ok);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int r = rr + RS * i;
+      const bool ok = t0 + r < k1;
+      cp_async16_zfill(st + swizzled(r, ch), src + (ok ? (int64_t)(t0 + r) * stride : 0), ok);
+    }
+  }
+}
+
+template <int D, int FMT>
+__device__ void produce(const PrefixArgs& a, const Item& w, uint32_t sq, uint32_t ring, uint32_t raw, Bars& s, int tid) {
+  typedef Cfg<D, FMT> C;
+  constexpr int CH = D / 8, NPT = C::NPT;
+  // The query rows, K-major; rows past the last are zero.
+  const int rows = w.wide ? 2 * TM : TM;
+  for (int e = tid; e < rows * CH; e += NPT) {
+    const int r = e / CH, ch = e % CH;
+    const bool ok = r < w.nr;
+    const RowAt at = w.own ? own_row(a, w.u, w.r0 + (ok ? r : 0)) : prompt_row(a, w.u, w.r0 + (ok ? r : 0));
+    const bf16* q = static_cast<const bf16*>(a.Q) + at.b * a.qsb + at.hq * a.qsh + at.i * a.qss + ch * 8;
+    cp_async16_zfill(sq + (r / TM) * C::TILE + swizzled(r % TM, ch), q, ok);
+  }
+  cp_async_arrive_noinc(bar(s.qfull));
+  const int64_t b = w.u / a.H, h = w.u % a.H;
+  const int A = w.wide ? 1 : 2;
+  if (!C::CODES || w.own) {
+    const int64_t sb = w.own ? a.gsb : a.ksb, sh = w.own ? a.gsh : a.ksh, ss = w.own ? a.gss : a.kss;
+    const bf16* K = static_cast<const bf16*>(w.own ? a.Kg : a.K) + b * sb + h * sh;
+    const bf16* V = static_cast<const bf16*>(w.own ? a.Vg : a.V) + b * sb + h * sh;
+    const int32_t* idx = a.idx && !w.own ? a.idx + (int64_t)w.u * a.k : nullptr;
+    int pos = 0;
+    bool ok = true;
+    in_order(w.T, A, [&](int t, bool v) {
+      const int st = pos % C::STAGES, n = pos / C::STAGES;
+      ++pos;
+      if (ok && n > 0) ok = warp_wait(bar(s.empty[st]), (n - 1) & 1, s, a);
+      if (ok) copy_tile<D, NPT>(ring + st * C::TILE, v ? V : K, ss, idx, a.n, w.k0 + t * TM, w.k1, tid);
+      cp_async_arrive_noinc(bar(s.full[st]));
+    });
+    cp_async_wait_all();
+    return;
+  }
+  if constexpr (C::CODES) {
+    // Codes: chunk c = tid + NPT i of a tile is 16 bytes of row c / (ROWB / 16).
+    // The thread copies its chunks and the scale words of their rows into its
+    // own slots DEPTH - 1 tiles ahead and widens them itself, so its own
+    // cp.async groups are all it waits for.
+    constexpr int CR = C::ROWB / 16, CPT = C::CPT, EL = FMT == WF_MXFP4 ? 32 : 16;  // elements a chunk
+    constexpr int SR = D / kMxBlock;  // scale bytes a row: 4 or 2
+    const int32_t* idx = a.idx ? a.idx + (int64_t)w.u * a.k : nullptr;
+    const int64_t srow = (int64_t)w.u * a.n;
+    const int64_t sbytes = (int64_t)a.P * a.H * a.n * SR;
+    const uint32_t chunks = raw + (uint32_t)tid * 16, words = raw + C::DEPTH * NPT * CPT * 16 + (uint32_t)tid * 4;
+    const int total = 2 * w.T;
+    // Tile and kind of position p: the order of in_order.
+    auto at = [&](int p, int& t, bool& v) {
+      const int lead = min(A, w.T);
+      if (p < lead) { t = p; v = false; return; }
+      p -= lead;
+      const int pairs = w.T - lead;  // V_j, K_(j+A)
+      if (p < 2 * pairs) { t = p / 2 + ((p & 1) ? A : 0); v = !(p & 1); return; }
+      t = pairs + (p - 2 * pairs); v = true;
+    };
+    // Bit pattern of which half of the scale word a row's bytes are (2 bytes a row).
+    auto issue = [&](int p) {
+      if (p < total) {
+        int t; bool v;
+        at(p, t, v);
+        const uint8_t* base = static_cast<const uint8_t*>(v ? a.V : a.K) + b * a.ksb + h * a.ksh;
+        const uint8_t* sc = v ? a.Vs : a.Ks;
+        const int slot = p % C::DEPTH;
+#pragma unroll
+        for (int i = 0; i < CPT; ++i) {
+          const int c = tid + NPT * i, r = c / CR, x = c % CR, j = w.k0 + t * TM + r;
+          const bool ok = j < w.k1;
+          const int row = !ok ? 0 : idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j;
+          cp_async16_zfill(chunks + (uint32_t)(slot * CPT + i) * (NPT * 16), base + (int64_t)row * a.kss + x * 16, ok);
+          const int64_t so = ((srow + row) * SR) & ~(int64_t)3;
+          cp_async4(words + (uint32_t)(slot * CPT + i) * (NPT * 4), sc + so, (int)min((int64_t)4, sbytes - so));
+        }
+      }
+      cp_async_commit();
+    };
+    for (int p = 0; p < C::DEPTH - 1; ++p) issue(p);
+    for (int p = 0; p < total; ++p) {
+      const int st = p % C::STAGES, n = p / C::STAGES, slot = p % C::DEPTH;
+      issue(p + C::DEPTH - 1);
+      cp_async_wait<C::DEPTH - 1>();
+      if (n > 0 && !warp_wait(bar(s.empty[st]), (n - 1) & 1, s, a)) break;
+      int t; bool v;
+      at(p, t, v);
+#pragma unroll
+      for (int i = 0; i < CPT; ++i) {
+        const int c = tid + NPT * i, r = c / CR, x = c % CR, j = w.k0 + t * TM + r;
+        const uint4 code = lds_v4(chunks + (uint32_t)(slot * CPT + i) * (NPT * 16));
+        uint32_t word = lds_u32(words + (uint32_t)(slot * CPT + i) * (NPT * 4));
+        if (SR == 2) {
+          const int row = j >= w.k1 ? 0 : idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j;
+          word >>= ((srow + row) & 1) * 16;
+        }
+        const float f = j < w.k1 ? mx_scale((word >> (x * EL / kMxBlock * 8)) & 0xffu) : 0.f;
+        const uint32_t cw[4] = {code.x, code.y, code.z, code.w};
+        constexpr int OUT = EL / 8;  // bf16 chunks
+#pragma unroll
+        for (int o = 0; o < OUT; ++o) {
+          uint32_t y[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 z = FMT == WF_MXFP4 ? mx_decode2<true>((cw[o] >> (8 * e)) & 0xffu)
+                                             : mx_decode2<false>((cw[2 * o + e / 2] >> (16 * (e & 1))) & 0xffffu);
+            y[e] = pack_bf16(z.x * f, z.y * f);
+          }
+          sts_v4(ring + st * C::TILE + swizzled(r, x * OUT + o), make_uint4(y[0], y[1], y[2], y[3]));
+        }
+      }
+      fence_proxy_async();
+      mbar_arrive(bar(s.full[st]));
+    }
+    cp_async_wait_all();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// MMA thread.
+// ---------------------------------------------------------------------------
+template <int D, int FMT>
+__device__ void multiply(const PrefixArgs& a, const Item& w, uint32_t sq, uint32_t ring, Bars& s) {
+  typedef Cfg<D, FMT> C;
+  const uint32_t tm = s.tmem;
+  const uint32_t qk = idesc_bf16(TM, TM, 0, 0), pv = idesc_bf16(TM, D, 0, 1);
+  const int A = w.wide ? 1 : 2;
+  bool ok = wait(bar(a.stall ? s.stall : s.qfull), 0, s, a);
+  fence_proxy_async();
+  int pos = 0;
+  auto arrived = [&](int p) {
+    if (ok) ok = wait(bar(s.full[p % C::STAGES]), (p / C::STAGES) & 1, s, a);
+    fence_proxy_async();
+    tc_fence_after();
+  };
+  auto scores = [&](int g, int p) {
+    const uint32_t q = sq + (w.wide ? g : 0) * C::TILE, st = ring + (p % C::STAGES) * C::TILE;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk)
+      mma_bf16(tm + TM * g, smem_desc_sw128(q + (kk / 4) * HALF + (kk % 4) * 32, 16, 1024),
+               smem_desc_sw128(st + (kk / 4) * HALF + (kk % 4) * 32, 16, 1024), qk, kk != 0);
+    mma_commit(bar(s.sfull[g]));
+  };
+  for (int t = 0; t < min(A, w.T) && ok; ++t, ++pos) {
+    arrived(pos);
+    if (!ok) break;
+    if (w.wide) { scores(0, pos); scores(1, pos); }
+    else scores(t & 1, pos);
+    mma_commit(bar(s.empty[pos % C::STAGES]));
+  }
+  for (int j = 0; j < w.T && ok; ++j) {
+    const bool more = j + A < w.T;
+    arrived(pos);
+#pragma unroll 1
+    for (int g = w.wide ? 0 : j & 1; g <= (w.wide ? 1 : j & 1) && ok; ++g) {
+      const int i = w.wide ? j : j >> 1;  // the warpgroup's step
+      ok = wait(bar(s.pready[g]), i & 1, s, a);
+      tc_fence_after();
+      if (!ok) break;
+      const uint32_t st = ring + (pos % C::STAGES) * C::TILE;
+#pragma unroll
+      for (int kq = 0; kq < TM / 16; ++kq)
+        mma_bf16_ts(tm + 2 * TM + D * g, tm + TM * g + 8 * kq, smem_desc_sw128(st + kq * 2048, HALF, 1024), pv,
+                    i > 0 || kq > 0);
+      if (j + (w.wide ? 1 : 2) >= w.T) mma_commit(bar(s.odone[g]));
+      if (more) {
+        if (!(w.wide && g)) arrived(pos + 1);
+        if (ok) scores(g, pos + 1);
+      }
+    }
+    if (!ok) break;
+    mma_commit(bar(s.empty[pos % C::STAGES]));
+    if (more) mma_commit(bar(s.empty[(pos + 1) % C::STAGES]));
+    pos += more ? 2 : 1;
+  }
+  if (!ok) {  // products issued so far end before the tensor memory is freed
+    mma_commit(bar(s.drain));
+    (void)mbar_wait_bounded(bar(s.drain), 0, kDefaultWaitLimit);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Softmax warpgroups.
+// ---------------------------------------------------------------------------
+template <int D, int FMT>
+__device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* ring, Bars& s, int g, int r) {
+  const uint32_t lanes = (uint32_t)(r & ~31) << 16;  // the warp's quarter of the TMEM lanes
+  const uint32_t tm = s.tmem, sc = tm + TM * g + lanes, oc = tm + 2 * TM + D * g + lanes;
+  const int rt = w.wide ? g * TM : 0;                // first row of the warpgroup's tile
+  const bool active = rt + (r & ~31) < w.nr;         // the warp has a row
+  const int step = w.wide ? 1 : 2, first = w.wide ? 0 : g;
+  float m = -FLT_MAX, l = 0.f;  // finite, so that logits of -inf add 0 and not 2^(-inf + inf)
+  bool ok = true;
+  if (active) {
+    int i = 0;
+#pragma unroll 1
+    for (int t = first; t < w.T; t += step, ++i) {
+      if (!(ok = warp_wait(bar(s.sfull[g]), i & 1, s, a))) break;
+      tc_fence_after();
+      const int nk = w.k1 - (w.k0 + t * TM);  // keys of the tile
+      float top = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < TM / 32; ++c) {
+        float v[32];
+        tmem_ld32(sc + 32 * c, v);
+        if (nk < TM) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = 32 * c + e < nk ? v[e] : -INFINITY;
+        }
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) top = fmax3(top, v[e], v[e + 1]);
+      }
+      const float mt = top * a.sl2;
+      float f = 1.f;
+      if (mt > m + kLazy) {
+        f = ex2(m - mt);  // 0 on the first tile
+        m = mt;
+        l *= f;
+      }
+      // The products into O are done: this S was issued behind them.
+      if (i > 0 && __any_sync(0xffffffffu, f != 1.f)) {
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          float o[32];
+          tmem_ld32(oc + 32 * c, o);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] *= f;
+          tmem_st32(oc + 32 * c, reinterpret_cast<const uint32_t*>(o));
+        }
+      }
+      float sum[2] = {0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < TM / 32; ++c) {
+        float v[32];
+        uint32_t p[16];
+        tmem_ld32(sc + 32 * c, v);
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+          float p0 = ex2(fmaf(v[e], a.sl2, -m)), p1 = ex2(fmaf(v[e + 1], a.sl2, -m));
+          if (nk < TM) {
+            p0 = 32 * c + e < nk ? p0 : 0.f;
+            p1 = 32 * c + e + 1 < nk ? p1 : 0.f;
+          }
+          sum[0] += p0;
+          sum[1] += p1;
+          p[e / 2] = pack_bf16(p0, p1);
+        }
+        tmem_st16(sc + 16 * c, p);
+      }
+      l += sum[0] + sum[1];
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if ((r & 31) == 0) mbar_arrive(bar(s.pready[g]));
+    }
+  }
+  // The last products: of both warpgroups, whose stages are the exchange below.
+  if (ok && w.T > 0 && (w.wide || w.T > 1 || g == 0)) ok = warp_wait(bar(s.odone[g]), 0, s, a);
+  if (ok && !w.wide && (g == 0 ? w.T > 1 : w.T > 0)) ok = warp_wait(bar(s.odone[g ^ 1]), 0, s, a);
+  tc_fence_after();
+  const bool have = w.T > first;  // this warpgroup had a tile
+  const int row = rt + r;
+  float* ex = reinterpret_cast<float*>(ring);  // [128][D + 4]: O of the second warpgroup, m and l
+  if (!w.wide && w.T > 1) {
+    if (g == 1 && active) {
+#pragma unroll 1
+      for (int c = 0; c < D / 32; ++c) {
+        float o[32];
+        tmem_ld32(oc + 32 * c, o);
+#pragma unroll
+        for (int e = 0; e < 32; e += 4)
+          *reinterpret_cast<float4*>(ex + r * (D + 4) + 32 * c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+      }
+      ex[r * (D + 4) + D] = m;
+      ex[r * (D + 4) + D + 1] = l;
+    }
+    named_sync(1, 256);
+  }
+  if (!w.wide && g == 1) return;
+  if (!active || abort_set(smem_u32(&s.abort))) return;
+  float f0 = 1.f, f1 = 0.f;
+  if (!w.wide && w.T > 1) {
+    const float m1 = ex[r * (D + 4) + D], l1 = ex[r * (D + 4) + D + 1];
+    const float M = fmaxf(m, m1);
+    f0 = ex2(m - M);
+    f1 = ex2(m1 - M);
+    m = M;
+    l = l * f0 + l1 * f1;
+  }
+  const RowAt at = row < w.nr ? (w.own ? own_row(a, w.u, w.r0 + row) : prompt_row(a, w.u, w.r0 + row)) : RowAt{0, 0, 0};
+  const bool whole = a.S + a.So == 1;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int64_t flat = (int64_t)w.part * a.rows + flat_row(a, at);
+  bf16* op = static_cast<bf16*>(a.O) + at.b * a.osb + at.hq * a.osh + at.i * a.oss;
+#pragma unroll 1
+  for (int c = 0; c < D / 32; ++c) {
+    float o[32];
+    if (have) tmem_ld32(oc + 32 * c, o);
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+      if (!have || l == 0.f) o[e] = 0.f;
+      else if (!w.wide && w.T > 1) o[e] = o[e] * f0 + f1 * ex[r * (D + 4) + 32 * c + e];
+    }
+    if (row >= w.nr) continue;
+    if (whole) {
+#pragma unroll
+      for (int e = 0; e < 32; e += 8) {
+        float y[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) y[k] = o[e + k] * inv;
+        st_vec(op + 32 * c + e, y);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 32; e += 4) st_vec(a.part_o + flat * D + 32 * c + e, o + e);
+    }
+  }
+  if (!whole && row < w.nr) a.part_ml[flat] = make_float2(m, l);
+}
+
+template <int D, int FMT>
+__global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_constant__ PrefixArgs a) {
+  typedef Cfg<D, FMT> C;
+  extern __shared__ uint8_t raw_smem[];
+  uint8_t* sm = raw_smem + ((1024u - (smem_u32(raw_smem) & 1023u)) & 1023u);
+  uint8_t* ring = sm + 2 * C::TILE;
+  uint8_t* raw = ring + C::STAGES * C::TILE;
+  Bars& s = *reinterpret_cast<Bars*>(raw + C::RAW);
+  const int tid = threadIdx.x, warp = tid >> 5;
+  constexpr int MMA_WARP = C::NTH / 32 - 1;
+  grid_dep_wait();
+  const Item w = item_of(a);
+  if (warp == MMA_WARP) {
+    tmem_alloc(smem_u32(&s.tmem), 512);
+    tmem_relinquish();
+  }
+  if (tid == 0) {
+    for (int i = 0; i < C::STAGES; ++i) {
+      mbar_init(bar(s.full[i]), C::NPT);
+      mbar_init(bar(s.empty[i]), 1);
+    }
+    mbar_init(bar(s.qfull), C::NPT);
+    for (int g = 0; g < 2; ++g) {
+      const int rows = w.wide ? w.nr - g * TM : w.nr;
+      mbar_init(bar(s.sfull[g]), 1);
+      mbar_init(bar(s.pready[g]), (min(rows, TM) + 31) / 32);
+      mbar_init(bar(s.odone[g]), 1);
+    }
+    mbar_init(bar(s.stall), 1);
+    mbar_init(bar(s.drain), 1);
+    s.abort = 0;
+    fence_mbar_init();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  grid_dep_launch();  // after the barrier that publishes the tensor memory (see Launch)
+  if (warp < 8) {
+    soften<D, FMT>(a, w, ring, s, warp >> 2, tid & 127);
+  } else if (warp < MMA_WARP) {
+    produce<D, FMT>(a, w, smem_u32(sm), smem_u32(ring), smem_u32(raw), s, tid - 256);
+  } else if ((tid & 31) == 0) {
+    multiply<D, FMT>(a, w, smem_u32(sm), smem_u32(ring), s);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == MMA_WARP) {
+    tc_fence_after();
+    tmem_dealloc(s.tmem, 512);
+  }
+}
+
+template <int D, int FMT>
+cudaError_t launch(const PrefixArgs& a, cudaStream_t s) {
+  typedef Cfg<D, FMT> C;
+  const int64_t items = (int64_t)a.P * a.H * a.mt * a.S + (int64_t)a.B * a.H * a.mto * a.So;
+  if (!items) return cudaSuccess;
+  const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(tc_kernel<D, FMT>), C::SMEM);
+  if (e != cudaSuccess) return e;
+  return Launch(dim3((unsigned)items), C::NTH, C::SMEM, s)(tc_kernel<D, FMT>, a);
+}
+
+}  // namespace
+
+cudaError_t launch_prefix_tc(const PrefixPlan& p, cudaStream_t s) {
+  const bool wide = p.a.d == 128;
+  if (p.fmt == WF_MXFP8) return wide ? launch<128, WF_MXFP8>(p.a, s) : launch<64, WF_MXFP8>(p.a, s);
+  if (p.fmt == WF_MXFP4) return wide ? launch<128, WF_MXFP4>(p.a, s) : launch<64, WF_MXFP4>(p.a, s);
+  return wide ? launch<128, WF_BF16>(p.a, s) : launch<64, WF_BF16>(p.a, s);
+}
+
+}  // namespace wf

@@ -252,3 +252,20 @@ def test_captured_in_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(O, want)
+
+
+@pytest.mark.parametrize("cache", [None, "mxfp8"])
+@pytest.mark.parametrize("B", [2, 12])
+def test_a_wait_that_gives_up_is_reported(B, cache):
+    # The first wait of every CTA is on a barrier that nothing completes: the call ends, the status word is set, and
+    # the next call works.
+    c = Case(B, 1, 2, 1, 32, 128, 700, 20, "bf16", cache, seed=14)
+    want = c.run()
+    wf.wf_testing_set_wait_failure(True, 20000)
+    try:
+        with pytest.raises(wf.WfError) as e:
+            c.run()
+        assert e.value.status == -7
+    finally:
+        wf.wf_testing_set_wait_failure(False, 0)
+    assert torch.equal(c.run(), want)
