@@ -201,7 +201,6 @@ __global__ void __launch_bounds__(NTH, 2) simt_kernel(const __grid_constant__ Pr
     }
   }
   grid_dep_launch();
-  const int parts = a.S + a.So;
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
 #pragma unroll
@@ -209,7 +208,7 @@ __global__ void __launch_bounds__(NTH, 2) simt_kernel(const __grid_constant__ Pr
     const int r = ty * RT + i;
     if (r >= nr) continue;
     const RowAt w = own ? own_row(a, u, r0 + r) : prompt_row(a, u, r0 + r);
-    if (parts == 1) {
+    if (a.whole) {
       const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
       T* op = static_cast<T*>(a.O) + w.b * a.osb + w.hq * a.osh + w.i * a.oss;
 #pragma unroll
@@ -308,10 +307,12 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
     return (int)std::min(most, std::max<int64_t>(1, slots / units));
   };
   a.S = split((int64_t)a.P * a.H * a.mt, k);
-  a.So = split((int64_t)a.B * a.H * a.mto, n_g);
+  p.fold = tc && n_g > 0 && n_g <= kPrefixFold;
+  a.So = p.fold ? 0 : split((int64_t)a.B * a.H * a.mto, n_g);
   p.parts = a.S + a.So;
+  a.whole = p.parts == 1 && !p.fold;
   p.off_ml = 256;
-  const int kept = p.parts == 1 ? 0 : p.parts;
+  const int kept = a.whole ? 0 : p.parts;
   p.off_o = align_up(p.off_ml + sizeof(float2) * (size_t)a.rows * kept, 256);
   p.total = p.off_o + sizeof(float) * (size_t)a.rows * a.d * kept;
   return p;
@@ -319,7 +320,8 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
 
 cudaError_t launch_prefix(const PrefixPlan& p, cudaStream_t s) {
   const cudaError_t e = launch_parts(p, s);
-  if (e != cudaSuccess || p.parts == 1) return e;
+  if (e != cudaSuccess || p.a.whole) return e;
+  if (p.fold) return launch_prefix_own(p, s);
   if (p.dtype == WF_BF16) return p.a.d == 128 ? launch_join<bf16, 128>(p.a, s) : launch_join<bf16, 64>(p.a, s);
   return p.a.d == 128 ? launch_join<float, 128>(p.a, s) : launch_join<float, 64>(p.a, s);
 }

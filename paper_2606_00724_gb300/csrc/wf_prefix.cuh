@@ -33,6 +33,7 @@ struct PrefixArgs {
   int R, Ro;      // query rows of a prompt unit, of an own unit
   int S, So;      // parts of the prompt, of the own rows
   int mt, mto;    // row tiles of a prompt unit, of an own unit
+  int whole;      // a part is the whole softmax: O goes out as it is
   int64_t rows;   // B Hq q
   float* part_o;  // [parts][rows][d], rows in [B, Hq, q] order
   float2* part_ml;
@@ -42,6 +43,9 @@ struct PrefixArgs {
   int stall;             // test-only: its first wait is on a barrier that nothing completes
 };
 
+// Own rows up to which they are attended where the parts are joined, a CTA a
+// block of query rows; more are ranges of their own for the prompt's kernel.
+constexpr int kPrefixFold = 512;
 constexpr int kPrefixTcRows = 256;  // query rows a CTA of the tensor-core kernel
 
 // The workspace of a call: the status word, then the parts.
@@ -49,10 +53,12 @@ struct PrefixPlan {
   PrefixArgs a;  // shapes and splits; pointers are filled in by the call
   int dtype, fmt;
   int parts;     // 1: the kernel writes O itself
+  bool fold;     // the own rows are attended where the parts are joined (So = 0)
   size_t off_ml, off_o, total;
 };
 PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g);
 cudaError_t launch_prefix(const PrefixPlan& p, cudaStream_t s);
+cudaError_t launch_prefix_own(const PrefixPlan& p, cudaStream_t s);  // own rows and the joining of parts, bf16
 cudaError_t launch_prefix_tc(const PrefixPlan& p, cudaStream_t s);  // the parts (or O) of bf16 queries
 
 // Sequence, query head and block row of row r of unit u.

@@ -466,7 +466,7 @@ __device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* ring, Bars& 
     l = l * f0 + l1 * f1;
   }
   const RowAt at = row < w.nr ? (w.own ? own_row(a, w.u, w.r0 + row) : prompt_row(a, w.u, w.r0 + row)) : RowAt{0, 0, 0};
-  const bool whole = a.S + a.So == 1;
+  const bool whole = a.whole;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int64_t flat = (int64_t)w.part * a.rows + flat_row(a, at);
   bf16* op = static_cast<bf16*>(a.O) + at.b * a.osb + at.hq * a.osh + at.i * a.oss;

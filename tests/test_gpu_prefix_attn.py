@@ -107,6 +107,8 @@ SHAPES = [  # B, P, H, G, q, n, ng
     (1, 1, 1, 1, 300, 200, 300),  # a long block of one sequence
     (40, 1, 3, 1, 1, 127, 128),
     (2, 1, 40, 1, 4, 64, 3),
+    (3, 1, 2, 1, 1, 90, 1300),    # long generations
+    (2, 1, 2, 2, 20, 260, 700),
 ]
 
 
