@@ -384,7 +384,8 @@ wf_status wf_step_wavelet(const void* Q, const wf_tensor* q, const void* top, co
  * (WF_MXFP8) or two a byte, channel 2 i in the low half (WF_MXFP4).  Its scales
  * are bytes e + 127 (255: NaN), contiguous [B][H][rows][head_dim / 32], 4-byte
  * aligned.  K and V have code and scale tensors of the same shape and strides.
- * Codes and scales of rows never written may hold anything that reads back.
+ * The E4M3 codes 0x7f and 0xff (that format's NaN) are never written; a caller
+ * who makes codes of its own must not use them.
  *
  * wf_scales_bytes: size of the scales of kv (0 if kv is not a valid quantised
  * cache).

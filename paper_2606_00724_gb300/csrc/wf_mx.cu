@@ -8,6 +8,8 @@
 // used.  The 4 or 8 lanes that share a block find its largest magnitude with
 // shuffles, as integers: the bits of |x| are ordered as the values are, with
 // infinities and NaN above them.
+#include <algorithm>
+
 #include "wf_mx.cuh"
 #include "wf_sm100.cuh"
 
@@ -24,9 +26,33 @@ struct MxArgs {
   int64_t csb, csh, css; // strides of the codes, in bytes
   const int32_t* idx;    // [unit][rows] rows to read back, or null: pos + row
   int64_t pos;
-  uint32_t rows, total;  // rows a unit, of all units
-  int H, n;
+  uint32_t total;        // rows of all units
+  FastDiv rows, heads;   // rows a unit; heads
+  int n;
 };
+
+// Unit, batch entry and head, and row within the unit of row r of all units.
+struct At {
+  uint32_t u, b, h, i;
+};
+__device__ __forceinline__ At row_at(const MxArgs& a, uint32_t r) {
+  At w;
+  w.u = fastdiv(r, a.rows);
+  w.i = r - w.u * a.rows.d;
+  w.b = fastdiv(w.u, a.heads);
+  w.h = w.u - w.b * a.heads.d;
+  return w;
+}
+
+// Bits of the largest magnitude of a thread's channels, as an fp32 number (a NaN
+// wins over every number).
+__device__ __forceinline__ uint32_t top_bits(const float*, const uint4& v) {
+  return max(max(v.x & 0x7fffffffu, v.y & 0x7fffffffu), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu));
+}
+__device__ __forceinline__ uint32_t top_bits(const bf16*, const uint4& v) {
+  const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+  return max(m & 0xffff0000u, m << 16);
+}
 
 template <int BYTES> struct Word;
 template <> struct Word<8> { typedef uint2 type; };
@@ -73,9 +99,8 @@ __global__ void __launch_bounds__(NTH) quantize_kernel(const __grid_constant__ M
   uint4 v[UN];
 #pragma unroll
   for (int i = 0; i < UN; ++i) {
-    const uint32_t r = min(r0 + RPC * i, a.total - 1);
-    const uint32_t u = r / a.rows;
-    const int64_t o = (int64_t)(u / a.H) * a.fsb + (int64_t)(u % a.H) * a.fsh + (int64_t)(r - u * a.rows) * a.fss;
+    const At w = row_at(a, min(r0 + RPC * i, a.total - 1));
+    const int64_t o = w.b * a.fsb + w.h * a.fsh + w.i * a.fss;
     v[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.src[y]) + o) + t);
   }
   sm100::grid_dep_launch();
@@ -84,9 +109,7 @@ __global__ void __launch_bounds__(NTH) quantize_kernel(const __grid_constant__ M
     const uint32_t r = r0 + RPC * i;
     float x[N];
     widen_vec(static_cast<const T*>(nullptr), v[i], x);
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < N; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+    uint32_t top = top_bits(static_cast<const T*>(nullptr), v[i]);
 #pragma unroll
     for (int s = 1; s < TPB; s *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
     const uint32_t byte = mx_scale_byte<FP4>(top);
@@ -94,11 +117,11 @@ __global__ void __launch_bounds__(NTH) quantize_kernel(const __grid_constant__ M
 #pragma unroll
     for (int e = 0; e < N; ++e) x[e] = byte == 255 ? 0.f : x[e] * inv;
     if (r < a.total) {
-      const uint32_t u = r / a.rows;
-      const int64_t row = a.pos + (r - u * a.rows);
-      char* c = static_cast<char*>(a.dst[y]) + (int64_t)(u / a.H) * a.csb + (int64_t)(u % a.H) * a.csh + row * a.css;
+      const At w = row_at(a, r);
+      const int64_t row = a.pos + w.i;
+      char* c = static_cast<char*>(a.dst[y]) + w.b * a.csb + w.h * a.csh + row * a.css;
       reinterpret_cast<W*>(c)[t] = pack_codes<FP4, N>(x);
-      if (t % TPB == 0) a.scales[y][((int64_t)u * a.n + row) * (D / kMxBlock) + t / TPB] = (uint8_t)byte;
+      if (t % TPB == 0) a.scales[y][((int64_t)w.u * a.n + row) * (D / kMxBlock) + t / TPB] = (uint8_t)byte;
     }
   }
 }
@@ -116,16 +139,15 @@ __global__ void __launch_bounds__(NTH) dequantize_kernel(const __grid_constant__
 #pragma unroll
   for (int i = 0; i < UN; ++i) {
     const uint32_t r = min(r0 + RPC * i, a.total - 1);
-    row[i] = a.pos + r % a.rows;
+    row[i] = a.pos + row_at(a, r).i;
     if (a.idx) row[i] = min(max(__ldg(a.idx + r), 0), a.n - 1);
   }
 #pragma unroll
   for (int i = 0; i < UN; ++i) {
-    const uint32_t u = min(r0 + RPC * i, a.total - 1) / a.rows;
-    const char* p = static_cast<const char*>(a.src[y]) + (int64_t)(u / a.H) * a.csb + (int64_t)(u % a.H) * a.csh +
-                    row[i] * a.css;
+    const At w = row_at(a, min(r0 + RPC * i, a.total - 1));
+    const char* p = static_cast<const char*>(a.src[y]) + w.b * a.csb + w.h * a.csh + row[i] * a.css;
     c[i] = __ldg(reinterpret_cast<const W*>(p) + t);
-    byte[i] = __ldg(a.scales[y] + ((int64_t)u * a.n + row[i]) * (D / kMxBlock) + t / TPB);
+    byte[i] = __ldg(a.scales[y] + ((int64_t)w.u * a.n + row[i]) * (D / kMxBlock) + t / TPB);
   }
   sm100::grid_dep_launch();
 #pragma unroll
@@ -137,8 +159,8 @@ __global__ void __launch_bounds__(NTH) dequantize_kernel(const __grid_constant__
     const float s = mx_scale(byte[i]);
 #pragma unroll
     for (int e = 0; e < N; ++e) x[e] *= s;
-    const uint32_t u = r / a.rows;
-    const int64_t o = (int64_t)(u / a.H) * a.fsb + (int64_t)(u % a.H) * a.fsh + (int64_t)(r - u * a.rows) * a.fss;
+    const At w = row_at(a, r);
+    const int64_t o = w.b * a.fsb + w.h * a.fsh + w.i * a.fss;
     st_vec(static_cast<T*>(a.dst[y]) + o + t * N, x);
   }
 }
@@ -172,9 +194,9 @@ MxArgs mx_args(const wf_tensor& f, const wf_tensor& kv) {
   const int half = kv.dtype == WF_MXFP4 ? 2 : 1;  // strides of whole 16 bytes, so the division is exact
   a.fsb = f.stride_b; a.fsh = f.stride_h; a.fss = f.stride_s;
   a.csb = kv.stride_b / half; a.csh = kv.stride_h / half; a.css = kv.stride_s / half;
-  a.rows = (uint32_t)f.seq;
   a.total = (uint32_t)((int64_t)kv.batch * kv.heads * f.seq);
-  a.H = kv.heads;
+  a.rows = make_fastdiv((uint32_t)std::max(1, f.seq));
+  a.heads = make_fastdiv((uint32_t)kv.heads);
   a.n = kv.seq;
   return a;
 }

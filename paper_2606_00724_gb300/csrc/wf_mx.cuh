@@ -44,4 +44,36 @@ __device__ __forceinline__ float2 mx_decode2(uint32_t c) {
   return __half22float2(__half2(h));
 }
 
+// Codes widened to pairs of bf16, exactly.  A code's exponent and mantissa bits
+// placed in those of a bf16 number, whose bias is larger by 120 (E4M3) or 126
+// (E2M1), stand for code x 2^-120 (2^-126), subnormal codes for subnormal
+// numbers, so one product with 2^(120 + e) is the value.  That factor is a
+// number for scale bytes up to kMxOne; for larger ones the rest of the scale is
+// a second product.
+template <bool FP4> constexpr uint32_t kMxOne = FP4 ? 128 : 134;
+template <bool FP4>
+__device__ __forceinline__ uint32_t mx_factor(uint32_t byte) {
+  return ((min(byte, kMxOne<FP4>) + (FP4 ? 126u : 120u)) << 7) * 0x10001u;
+}
+template <bool FP4>
+__device__ __forceinline__ uint32_t mx_second_factor(uint32_t byte) {
+  return byte == 255 ? 0x7fff7fffu : ((max(byte, kMxOne<FP4>) - kMxOne<FP4> + 127u) << 7) * 0x10001u;
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// Pair i (channels 2 i, 2 i + 1) of a word of codes, before the factor: 2 pairs
+// of E4M3 or 4 of E2M1.
+template <bool FP4>
+__device__ __forceinline__ uint32_t mx_pair(uint32_t w, int i) {
+  if (FP4) {
+    const uint32_t b = __byte_perm(w, 0, 0x4440 + i);
+    return ((b * 0x00040040u) & 0x01c001c0u) | ((b * 0x01001000u) & 0x80008000u);
+  }
+  const uint32_t b = __byte_perm(w, 0, i ? 0x4342 : 0x4140);
+  return ((b * 16u) & 0x07f007f0u) | ((b * 256u) & 0x80008000u);
+}
+
 }  // namespace wf

@@ -30,10 +30,6 @@ enum Cache { kPlain, kFp8, kFp4 };
 
 // 4 consecutive channels (4 c ..) of a row, in fp32.
 __device__ __forceinline__ float4 row4(const float* p, int c) { return __ldg(reinterpret_cast<const float4*>(p) + c); }
-__device__ __forceinline__ float4 row4(const bf16* p, int c) {
-  const uint2 w = __ldg(reinterpret_cast<const uint2*>(p) + c);
-  return make_float4(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y));
-}
 template <bool FP4>
 __device__ __forceinline__ float4 code4(const uint8_t* p, const uint8_t* scales, int c) {
   const uint32_t w = FP4 ? __ldg(reinterpret_cast<const uint16_t*>(p) + c) : __ldg(reinterpret_cast<const uint32_t*>(p) + c);

@@ -33,6 +33,7 @@ struct PrefixArgs {
   int R, Ro;      // query rows of a prompt unit, of an own unit
   int S, So;      // parts of the prompt, of the own rows
   int mt, mto;    // row tiles of a prompt unit, of an own unit
+  int ob;         // query rows a CTA where the own rows are folded in
   int whole;      // a part is the whole softmax: O goes out as it is
   int64_t rows;   // B Hq q
   float* part_o;  // [parts][rows][d], rows in [B, Hq, q] order

@@ -48,11 +48,12 @@ __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b
 template <int D>
 __device__ __forceinline__ uint32_t at(int r, int ch) { return (uint32_t)(r * (2 * D) + ((ch ^ (r & 7)) << 4)); }
 
+// Query rows, then two stages of a K and a V tile; the warps' O and the parts'
+// weights take the stages' place.
 template <int D, int WR>
-constexpr size_t own_smem() {
-  // Query rows, then two stages of a K and a V tile; the warps' O, m and l take
-  // the stages' place.
-  const size_t q = 16 * WR * D * 2, stages = 4 * KT * D * 2, o = (4 / WR) * 16 * WR * (D + 4) * 4;
+size_t own_smem(int rows, int S) {
+  const size_t q = 16 * WR * D * 2, stages = 4 * KT * D * 2;
+  const size_t o = (4 / WR) * 16 * WR * (D + 4) * sizeof(float) + (size_t)rows * (S + 4 / WR) * sizeof(float2);
   return q + (stages > o ? stages : o);
 }
 
@@ -61,13 +62,12 @@ template <int D, int WR>
 __global__ void __launch_bounds__(NTH) own_join_kernel(const __grid_constant__ PrefixArgs a) {
   constexpr int WK = 4 / WR, RB = 16 * WR, CH = D / 8, KW = KT / WK, TILE = KT * D * 2, PO = D + 4;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ float2 sml[4 * 16];  // m and l of every warp's rows
-  __shared__ float sM[RB], sinv[RB];
   uint8_t* sq = smem;
   uint8_t* st = smem + RB * D * 2;
-  float* so = reinterpret_cast<float*>(st);  // [WK][RB][PO]
+  float* so = reinterpret_cast<float*>(st);                      // [WK][RB][PO]
+  float2* sml = reinterpret_cast<float2*>(so + WK * RB * PO);    // [a.ob][WK + S]: m and l, then the weight
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rw = warp % WR, kw = warp / WR;
-  const int nb = (a.Ro + RB - 1) / RB, u = blockIdx.x / nb, r0 = (blockIdx.x % nb) * RB, nr = min(RB, a.Ro - r0);
+  const int nb = (a.Ro + a.ob - 1) / a.ob, u = blockIdx.x / nb, r0 = (blockIdx.x % nb) * a.ob, nr = min(a.ob, a.Ro - r0);
   const int b = u / a.H, h = u % a.H;
   grid_dep_wait();
   const int nk = own_count(a, b);
@@ -179,64 +179,89 @@ __global__ void __launch_bounds__(NTH) own_join_kernel(const __grid_constant__ P
     float* row = so + (kw * RB + r) * PO + 2 * (lane & 3);
 #pragma unroll
     for (int c = 0; c < D / 8; ++c) *reinterpret_cast<float2*>(row + 8 * c) = make_float2(o[c][2 * i], o[c][2 * i + 1]);
-    if ((lane & 3) == 0) sml[kw * RB + r] = make_float2(m[i], l[i]);
+    if ((lane & 3) == 0 && r < nr) sml[r * (WK + a.S) + kw] = make_float2(m[i], l[i]);
+  }
+  const int NP = WK + a.S;
+  for (int e = tid; e < nr * a.S; e += NTH) {
+    const int r = e / a.S, j = e - r * a.S;
+    sml[r * NP + WK + j] = a.part_ml[j * a.rows + flat_row(a, own_row(a, u, r0 + r))];
   }
   __syncthreads();
-  // M and 1 / l of every row over the warps' and the prompt's parts, 8 threads
-  // a row (RB = 16), 4 or 2.
-  constexpr int TPR = NTH / RB;
-  {
-    const int r = tid / TPR, c = tid % TPR;
-    const bool ok = r < nr;
-    const int64_t flat = flat_row(a, own_row(a, u, r0 + (ok ? r : 0)));
+  // Weights 2^(m - M) / sum of 2^(m - M) l of a row's parts, a warp a row; a part
+  // without a key (l = 0) has weight 0.
+  for (int r = warp; r < nr; r += 4) {
+    float2* ml = sml + r * NP;
     float M = -FLT_MAX, L = 0.f;
-    auto take = [&](float2 ml) {
-      if (ml.y == 0.f) return;
-      const float mn = fmaxf(M, ml.x);
-      L = L * ex2(M - mn) + ml.y * ex2(ml.x - mn);
-      M = mn;
-    };
-    for (int j = c; j < WK; j += TPR) take(sml[j * RB + r]);
-    for (int j = c; j < a.S; j += TPR) take(a.part_ml[j * a.rows + flat]);
+    for (int j = lane; j < NP; j += 32)
+      if (ml[j].y != 0.f) M = fmaxf(M, ml[j].x);
 #pragma unroll
-    for (int x = 1; x < TPR; x *= 2) {
-      const float m1 = __shfl_xor_sync(0xffffffffu, M, x), l1 = __shfl_xor_sync(0xffffffffu, L, x);
-      const float mn = fmaxf(M, m1);
-      L = L * ex2(M - mn) + l1 * ex2(m1 - mn);
-      M = mn;
-    }
-    if (c == 0) {
-      sM[r] = M;
-      sinv[r] = L == 0.f ? 0.f : 1.f / L;
-    }
+    for (int x = 1; x < 32; x *= 2) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, x));
+    for (int j = lane; j < NP; j += 32)
+      if (ml[j].y != 0.f) L += ex2(ml[j].x - M) * ml[j].y;
+#pragma unroll
+    for (int x = 1; x < 32; x *= 2) L += __shfl_xor_sync(0xffffffffu, L, x);
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    for (int j = lane; j < NP; j += 32) ml[j].x = ml[j].y == 0.f ? 0.f : ex2(ml[j].x - M) * inv;
   }
   __syncthreads();
-  for (int e = tid; e < nr * (D / 4); e += NTH) {
-    const int r = e / (D / 4), c = e % (D / 4);
-    const RowAt w = own_row(a, u, r0 + r);
-    const int64_t flat = flat_row(a, w);
-    const float M = sM[r], inv = sinv[r];
-    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-    auto add = [&](float2 ml, const float4& v) {
-      const float f = ml.y == 0.f ? 0.f : ex2(ml.x - M) * inv;
-      y.x = fmaf(f, v.x, y.x); y.y = fmaf(f, v.y, y.y); y.z = fmaf(f, v.z, y.z); y.w = fmaf(f, v.w, y.w);
+  // O: EB groups of 4 channels a thread, so that the loads of several parts and
+  // groups are in flight together.
+  constexpr int EB = 4;
+  const int items = nr * (D / 4);
+  for (int e0 = tid; e0 < items; e0 += EB * NTH) {
+    float4 y[EB];
+    const float* po[EB];
+    int r[EB];
+#pragma unroll
+    for (int x = 0; x < EB; ++x) {
+      const int e = min(e0 + x * NTH, items - 1), c = e % (D / 4);
+      r[x] = e / (D / 4);
+      po[x] = a.part_o + flat_row(a, own_row(a, u, r0 + r[x])) * D + 4 * c;
+      y[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    auto add = [&](int x, float f, const float4& v) {
+      y[x].x = fmaf(f, v.x, y[x].x); y[x].y = fmaf(f, v.y, y[x].y);
+      y[x].z = fmaf(f, v.z, y[x].z); y[x].w = fmaf(f, v.w, y[x].w);
     };
-    for (int j = 0; j < WK; ++j)
-      add(sml[j * RB + r], *reinterpret_cast<const float4*>(so + (j * RB + r) * PO + 4 * c));
-#pragma unroll 4
-    for (int j = 0; j < a.S; ++j)
-      add(a.part_ml[j * a.rows + flat], *reinterpret_cast<const float4*>(a.part_o + (j * a.rows + flat) * D + 4 * c));
-    *reinterpret_cast<uint2*>(static_cast<bf16*>(a.O) + w.b * a.osb + w.hq * a.osh + w.i * a.oss + 4 * c) =
-        make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+    for (int j = 0; j < a.S; j += 4) {
+      float4 v[4][EB];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int x = 0; x < EB; ++x)
+          v[k][x] = j + k < a.S && e0 + x * NTH < items ? *reinterpret_cast<const float4*>(po[x] + (j + k) * a.rows * D)
+                                                        : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int x = 0; x < EB; ++x) add(x, j + k < a.S ? sml[r[x] * NP + WK + j + k].x : 0.f, v[k][x]);
+    }
+#pragma unroll
+    for (int x = 0; x < EB; ++x) {
+      const int e = e0 + x * NTH;
+      if (e >= items) break;
+      const int c = e % (D / 4);
+#pragma unroll
+      for (int j = 0; j < WK; ++j)
+        add(x, sml[r[x] * NP + j].x, *reinterpret_cast<const float4*>(so + (j * RB + r[x]) * PO + 4 * c));
+      const RowAt w = own_row(a, u, r0 + r[x]);
+      *reinterpret_cast<uint2*>(static_cast<bf16*>(a.O) + w.b * a.osb + w.hq * a.osh + w.i * a.oss + 4 * c) =
+          make_uint2(pack_bf16(y[x].x, y[x].y), pack_bf16(y[x].z, y[x].w));
+    }
   }
 }
 
 template <int D, int WR>
-cudaError_t launch(const PrefixArgs& a, cudaStream_t s) {
-  const size_t smem = own_smem<D, WR>();
+cudaError_t launch(PrefixArgs a, cudaStream_t s) {
+  // Query rows a CTA: all that its warps hold, fewer (down to 4) where that
+  // leaves SMs without a CTA and the parts' bytes to the others.
+  a.ob = 16 * WR;
+  const int64_t units = (int64_t)a.B * a.H;
+  while (a.ob > 4 && units * ((a.Ro + a.ob - 1) / a.ob) < 2 * sm_count()) a.ob /= 2;
+  const size_t smem = own_smem<D, WR>(a.ob, a.S);
   const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(own_join_kernel<D, WR>), smem);
   if (e != cudaSuccess) return e;
-  const int64_t blocks = (int64_t)a.B * a.H * ((a.Ro + 16 * WR - 1) / (16 * WR));
+  const int64_t blocks = units * ((a.Ro + a.ob - 1) / a.ob);
   return Launch(dim3((unsigned)blocks), NTH, smem, s)(own_join_kernel<D, WR>, a);
 }
 

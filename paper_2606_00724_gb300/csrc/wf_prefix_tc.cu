@@ -215,80 +215,92 @@ __device__ void produce(const PrefixArgs& a, const Item& w, uint32_t sq, uint32_
     return;
   }
   if constexpr (C::CODES) {
-    // Codes: chunk c = tid + NPT i of a tile is 16 bytes of row c / (ROWB / 16).
-    // The thread copies its chunks and the scale words of their rows into its
-    // own slots DEPTH - 1 tiles ahead and widens them itself, so its own
-    // cp.async groups are all it waits for.
-    constexpr int CR = C::ROWB / 16, CPT = C::CPT, EL = FMT == WF_MXFP4 ? 32 : 16;  // elements a chunk
-    constexpr int SR = D / kMxBlock;  // scale bytes a row: 4 or 2
+    // The thread copies its chunks of 16 bytes and the scale words of their rows
+    // into slots of its own DEPTH - 1 tiles ahead and widens them itself, so its
+    // own cp.async groups are all it waits for.
+    constexpr bool FP4 = FMT == WF_MXFP4;
+    constexpr int CR = C::ROWB / 16, CPT = C::CPT, RS = NPT / CR;
+    constexpr int EL = FP4 ? 32 : 16, OUT = EL / 8;  // channels a chunk, bf16 chunks they make
+    constexpr int SR = D / kMxBlock;                 // scale bytes a row: 4 or 2
+    const int x = tid % CR, rr = tid / CR;           // chunk x of rows rr + RS i
     const int32_t* idx = a.idx ? a.idx + (int64_t)w.u * a.k : nullptr;
-    const int64_t srow = (int64_t)w.u * a.n;
-    const int64_t sbytes = (int64_t)a.P * a.H * a.n * SR;
+    const int64_t srow = (int64_t)w.u * a.n, sbytes = (int64_t)a.P * a.H * a.n * SR;
+    const uint8_t* kbase = static_cast<const uint8_t*>(a.K) + b * a.ksb + h * a.ksh + x * 16;
+    const uint8_t* vbase = static_cast<const uint8_t*>(a.V) + b * a.ksb + h * a.ksh + x * 16;
     const uint32_t chunks = raw + (uint32_t)tid * 16, words = raw + C::DEPTH * NPT * CPT * 16 + (uint32_t)tid * 4;
-    const int total = 2 * w.T;
+    const int total = 2 * w.T, lead = min(A, w.T), pairs = w.T - lead;
     // Tile and kind of position p: the order of in_order.
-    auto at = [&](int p, int& t, bool& v) {
-      const int lead = min(A, w.T);
-      if (p < lead) { t = p; v = false; return; }
-      p -= lead;
-      const int pairs = w.T - lead;  // V_j, K_(j+A)
-      if (p < 2 * pairs) { t = p / 2 + ((p & 1) ? A : 0); v = !(p & 1); return; }
-      t = pairs + (p - 2 * pairs); v = true;
+    auto place = [&](int p, int& t, bool& v) {
+      const int o = p - lead;
+      v = o >= 0 && (o >= 2 * pairs || !(o & 1));
+      t = o < 0 ? p : o >= 2 * pairs ? o - pairs : o / 2 + ((o & 1) ? A : 0);
     };
-    // Bit pattern of which half of the scale word a row's bytes are (2 bytes a row).
-    auto issue = [&](int p) {
+    auto row_of = [&](int j) { return j >= w.k1 ? 0 : idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j; };
+    auto issue = [&](int p, int slot) {
       if (p < total) {
         int t; bool v;
-        at(p, t, v);
-        const uint8_t* base = static_cast<const uint8_t*>(v ? a.V : a.K) + b * a.ksb + h * a.ksh;
+        place(p, t, v);
+        const uint8_t* base = v ? vbase : kbase;
         const uint8_t* sc = v ? a.Vs : a.Ks;
-        const int slot = p % C::DEPTH;
+        const int j0 = w.k0 + t * TM + rr;
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
-          const int c = tid + NPT * i, r = c / CR, x = c % CR, j = w.k0 + t * TM + r;
-          const bool ok = j < w.k1;
-          const int row = !ok ? 0 : idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j;
-          cp_async16_zfill(chunks + (uint32_t)(slot * CPT + i) * (NPT * 16), base + (int64_t)row * a.kss + x * 16, ok);
+          const int row = row_of(j0 + RS * i);
+          cp_async16_zfill(chunks + (uint32_t)(slot * CPT + i) * (NPT * 16), base + row * a.kss, j0 + RS * i < w.k1);
+          // The row's scale word: 4 bytes, or those of a pair of rows (of which
+          // the last may have no second).
           const int64_t so = ((srow + row) * SR) & ~(int64_t)3;
-          cp_async4(words + (uint32_t)(slot * CPT + i) * (NPT * 4), sc + so, (int)min((int64_t)4, sbytes - so));
+          cp_async4(words + (uint32_t)(slot * CPT + i) * (NPT * 4), sc + so,
+                    SR == 4 || so + 4 <= sbytes ? 4 : (int)(sbytes - so));
         }
       }
       cp_async_commit();
     };
-    for (int p = 0; p < C::DEPTH - 1; ++p) issue(p);
+    for (int p = 0; p < C::DEPTH - 1; ++p) issue(p, p);
+    int slot = 0, st = 0, n = 0;
+#pragma unroll 1
     for (int p = 0; p < total; ++p) {
-      const int st = p % C::STAGES, n = p / C::STAGES, slot = p % C::DEPTH;
-      issue(p + C::DEPTH - 1);
+      issue(p + C::DEPTH - 1, slot ? slot - 1 : C::DEPTH - 1);
       cp_async_wait<C::DEPTH - 1>();
-      if (n > 0 && !warp_wait(bar(s.empty[st]), (n - 1) & 1, s, a)) break;
-      int t; bool v;
-      at(p, t, v);
+      uint4 code[CPT];
+      uint32_t byte[CPT];
 #pragma unroll
       for (int i = 0; i < CPT; ++i) {
-        const int c = tid + NPT * i, r = c / CR, x = c % CR, j = w.k0 + t * TM + r;
-        const uint4 code = lds_v4(chunks + (uint32_t)(slot * CPT + i) * (NPT * 16));
-        uint32_t word = lds_u32(words + (uint32_t)(slot * CPT + i) * (NPT * 4));
-        if (SR == 2) {
-          const int row = j >= w.k1 ? 0 : idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j;
-          word >>= ((srow + row) & 1) * 16;
-        }
-        const float f = j < w.k1 ? mx_scale((word >> (x * EL / kMxBlock * 8)) & 0xffu) : 0.f;
-        const uint32_t cw[4] = {code.x, code.y, code.z, code.w};
-        constexpr int OUT = EL / 8;  // bf16 chunks
+        code[i] = lds_v4(chunks + (uint32_t)(slot * CPT + i) * (NPT * 16));
+        byte[i] = lds_u32(words + (uint32_t)(slot * CPT + i) * (NPT * 4));
+      }
 #pragma unroll
-        for (int o = 0; o < OUT; ++o) {
-          uint32_t y[4];
+      for (int i = 0; i < CPT; ++i) {
+        int t; bool v;
+        place(p, t, v);
+        const int j = w.k0 + t * TM + rr + RS * i;
+        int sh = x * EL / kMxBlock * 8;
+        if (SR == 2) sh += (int)((srow + row_of(j)) & 1) * 16;
+        byte[i] = j < w.k1 ? (byte[i] >> sh) & 0xffu : 0u;  // rows past the last are zeros whatever their scale
+      }
+      if (n > 0 && !warp_wait(bar(s.empty[st]), (n - 1) & 1, s, a)) break;
+      const uint32_t dst = ring + st * C::TILE;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 z = FMT == WF_MXFP4 ? mx_decode2<true>((cw[o] >> (8 * e)) & 0xffu)
-                                             : mx_decode2<false>((cw[2 * o + e / 2] >> (16 * (e & 1))) & 0xffffu);
-            y[e] = pack_bf16(z.x * f, z.y * f);
-          }
-          sts_v4(ring + st * C::TILE + swizzled(r, x * OUT + o), make_uint4(y[0], y[1], y[2], y[3]));
+      for (int i = 0; i < CPT; ++i) {
+        const uint32_t cw[4] = {code[i].x, code[i].y, code[i].z, code[i].w};
+        const uint32_t f = mx_factor<FP4>(byte[i]);
+        uint32_t y[OUT * 4];
+#pragma unroll
+        for (int e = 0; e < OUT * 4; ++e)
+          y[e] = mul_bf16x2(FP4 ? mx_pair<true>(cw[e / 4], e % 4) : mx_pair<false>(cw[e / 2], e % 2), f);
+        if (__any_sync(0xffffffffu, byte[i] > kMxOne<FP4>)) {
+          const uint32_t f2 = mx_second_factor<FP4>(byte[i]);
+#pragma unroll
+          for (int e = 0; e < OUT * 4; ++e) y[e] = mul_bf16x2(y[e], f2);
         }
+#pragma unroll
+        for (int o = 0; o < OUT; ++o)
+          sts_v4(dst + swizzled(rr + RS * i, x * OUT + o), make_uint4(y[4 * o], y[4 * o + 1], y[4 * o + 2], y[4 * o + 3]));
       }
       fence_proxy_async();
       mbar_arrive(bar(s.full[st]));
+      slot = slot + 1 == C::DEPTH ? 0 : slot + 1;
+      if (++st == C::STAGES) { st = 0; ++n; }
     }
     cp_async_wait_all();
   }

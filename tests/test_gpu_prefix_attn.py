@@ -271,3 +271,28 @@ def test_a_wait_that_gives_up_is_reported(B, cache):
     finally:
         wf.wf_testing_set_wait_failure(False, 0)
     assert torch.equal(c.run(), want)
+
+
+@pytest.mark.parametrize("fmt", ["mxfp8", "mxfp4"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_every_code_and_scale_is_read_exactly(dtype, fmt):
+    # One prompt row a unit: the weight is 1, so O is the value row, to the bit.  Unit h holds every code, the scale
+    # bytes go through 0 (2^-127) to 254; bf16 rounds what lies below its smallest normal number to nearest even.
+    d, H = 128, 255
+    codes = np.concatenate([np.arange(127), [0], np.arange(128, 255), [0]]).astype(np.uint8)
+    V = np.zeros((1, H, 1, d if fmt == "mxfp8" else d // 2), np.uint8)
+    for h in range(H):
+        V[0, h, 0] = np.roll(codes, 37 * h)[:d] if fmt == "mxfp8" else (np.arange(d // 2) * 7 + h) % 256
+    S = np.repeat(np.arange(H, dtype=np.uint8)[None, :, None, None], 4, axis=3)
+    want = torch.from_numpy(mx.values(V, S, fmt))[:, :, 0]
+    K = np.zeros_like(V)
+    one = np.full_like(S, 127)
+    Q = torch.ones(1, H, 1, d, dtype=DT[dtype], device="cuda")
+    K, V, one, S = (torch.from_numpy(x).cuda() for x in (K, V, one, S))
+    O = torch.empty_like(Q)
+    ws = torch.zeros(wf.wf_prefix_attn_workspace_bytes(Q, K, 1, 0, fmt=FMT[fmt]), dtype=torch.uint8, device="cuda")
+    wf.wf_prefix_attn(Q, K, V, 1, None, None, O, ws, Ks=one, Vs=S, fmt=FMT[fmt])
+    normal = (want == 0) | ((want.abs() >= 2.0 ** -126) & (want.abs() <= torch.finfo(DT[dtype]).max))
+    got = O.double().cpu()[:, :, 0]
+    assert torch.equal(got[normal], want[normal])
+    assert normal.double().mean() > 0.9
