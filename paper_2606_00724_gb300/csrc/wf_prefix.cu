@@ -287,6 +287,8 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   a.each = a.B / a.P;
   a.Ro = a.G * a.q;
   a.R = a.each * a.Ro;
+  a.by_q = make_fastdiv((uint32_t)a.q);
+  a.by_Ro = make_fastdiv((uint32_t)a.Ro);
   a.rows = (int64_t)a.B * q.heads * a.q;
   p.dtype = q.dtype;
   p.fmt = kv.dtype;

@@ -31,6 +31,7 @@ struct PrefixArgs {
   int B, P, H, G, q, d, n, k, ng;
   int each;       // sequences a prompt
   int R, Ro;      // query rows of a prompt unit, of an own unit
+  FastDiv by_q, by_Ro;
   int S, So;      // parts of the prompt, of the own rows
   int mt, mto;    // row tiles of a prompt unit, of an own unit
   int ob;         // query rows a CTA where the own rows are folded in
@@ -67,11 +68,11 @@ struct RowAt {
   int b, hq, i;
 };
 __device__ __forceinline__ RowAt prompt_row(const PrefixArgs& a, int u, int r) {
-  const int s = r / a.Ro, w = r - s * a.Ro, g = w / a.q;
+  const int s = fastdiv(r, a.by_Ro), w = r - s * a.Ro, g = fastdiv(w, a.by_q);
   return {(u / a.H) * a.each + s, (u % a.H) * a.G + g, w - g * a.q};
 }
 __device__ __forceinline__ RowAt own_row(const PrefixArgs& a, int u, int r) {
-  const int g = r / a.q;
+  const int g = fastdiv(r, a.by_q);
   return {u / a.H, (u % a.H) * a.G + g, r - g * a.q};
 }
 __device__ __forceinline__ int64_t flat_row(const PrefixArgs& a, const RowAt& r) {

@@ -41,6 +41,7 @@ using namespace sm100;
 constexpr int TM = kPrefixTcRows / 2;  // rows of a row tile, keys of a key tile
 constexpr int HALF = TM * 128;         // 64 channels of a tile of bf16 rows
 constexpr float kLazy = 8.f;
+constexpr int kPCol = TM / 2;            // P's columns among S's
 
 template <int D, int FMT>
 struct Cfg {
@@ -48,6 +49,7 @@ struct Cfg {
   static constexpr int NPT = CODES ? 256 : 128;          // producer threads
   static constexpr int NTH = 256 + NPT + 32;             // softmax warps, producers, MMA warp
   static constexpr int TILE = TM * D * 2;                // a stage
+  static constexpr int CW = CODES ? 16 : 32;             // columns of S in flight (17 warps leave 96 registers, 13 leave 128)
   static constexpr int ROWB = FMT == WF_MXFP4 ? D / 2 : D;  // bytes of a row of codes
   static constexpr int CPT = CODES ? TM * ROWB / 16 / NPT : 0;  // 16-byte chunks of codes a thread and tile
   static constexpr int DEPTH = FMT == WF_MXFP8 ? 3 : 4;  // tiles of codes in flight
@@ -171,6 +173,12 @@ __device__ __forceinline__ void copy_tile(uint32_t st, const bf16* base, int64_t
       const bool ok = t0 + r < k1;
       cp_async16_zfill(st + swizzled(r, ch), src + (ok ? (int64_t)at * stride : 0), ok);
     }
+  } else if (t0 + TM <= k1) {
+    const bf16* p = src + (t0 + rr) * stride;
+    const uint32_t dst = st + swizzled(rr, ch);
+    static_assert(RS % 8 == 0, "a thread's rows share their swizzle");
+#pragma unroll
+    for (int i = 0; i < NI; ++i, p += RS * stride) cp_async16(dst + RS * i * 128, p);
   } else {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
@@ -350,7 +358,7 @@ __device__ void multiply(const PrefixArgs& a, const Item& w, uint32_t sq, uint32
       const uint32_t st = ring + (pos % C::STAGES) * C::TILE;
 #pragma unroll
       for (int kq = 0; kq < TM / 16; ++kq)
-        mma_bf16_ts(tm + 2 * TM + D * g, tm + TM * g + 8 * kq, smem_desc_sw128(st + kq * 2048, HALF, 1024), pv,
+        mma_bf16_ts(tm + 2 * TM + D * g, tm + TM * g + kPCol + 8 * kq, smem_desc_sw128(st + kq * 2048, HALF, 1024), pv,
                     i > 0 || kq > 0);
       if (j + (w.wide ? 1 : 2) >= w.T) mma_commit(bar(s.odone[g]));
       if (more) {
@@ -372,8 +380,110 @@ __device__ void multiply(const PrefixArgs& a, const Item& w, uint32_t sq, uint32
 // ---------------------------------------------------------------------------
 // Softmax warpgroups.
 // ---------------------------------------------------------------------------
+// CW columns of a thread's TMEM lane; valid behind got().
+template <int CW>
+__device__ __forceinline__ void get(uint32_t taddr, uint32_t* v) {
+  if constexpr (CW == 32) {
+    tmem_ld32_issue(taddr, v);
+  } else {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr)
+        : "memory");
+  }
+}
+// The registers pass through the wait, so no use of them moves before it.
+template <int CW>
+__device__ __forceinline__ void got(uint32_t* v) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                 "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
+  if constexpr (CW == 32)
+    asm volatile("" : "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]),
+                 "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])::"memory");
+}
+template <int N>
+__device__ __forceinline__ void put(uint32_t taddr, const uint32_t* p) {
+  if constexpr (N == 16) tmem_st16(taddr, p);
+  else
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(p[0]),
+                 "r"(p[1]), "r"(p[2]), "r"(p[3]), "r"(p[4]), "r"(p[5]), "r"(p[6]), "r"(p[7])
+                 : "memory");
+}
+
+// P of one tile from S, in two passes of chunks of CW columns, the next chunk
+// on its way while one is worked on: the row's maximum, first to last; then P,
+// last to first, starting on the two chunks still in registers.  P goes to the
+// upper half of S's columns, always onto columns already read.
+template <int D, int CW, bool MASK>
+__device__ __forceinline__ void soften_tile(const PrefixArgs& a, uint32_t sc, uint32_t oc, bool have_o, int nk, float& m,
+                                            float& l) {
+  constexpr int NC = TM / CW;
+  uint32_t v[2][CW];
+  auto mask = [&](int c) {
+    if (MASK) {
+#pragma unroll
+      for (int e = 0; e < CW; ++e) v[c & 1][e] = CW * c + e < nk ? v[c & 1][e] : __float_as_uint(-INFINITY);
+    }
+  };
+  float top = -INFINITY;
+  get<CW>(sc, v[0]);
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    got<CW>(v[c & 1]);
+    if (c + 1 < NC) get<CW>(sc + CW * (c + 1), v[(c + 1) & 1]);
+    mask(c);
+#pragma unroll
+    for (int e = 0; e < CW; e += 2) top = fmax3(top, __uint_as_float(v[c & 1][e]), __uint_as_float(v[c & 1][e + 1]));
+  }
+  const float mt = top * a.sl2;
+  float f = 1.f;
+  if (mt > m + kLazy) {
+    f = ex2(m - mt);  // 0 on the first tile
+    m = mt;
+    l *= f;
+  }
+  // The products into O are done: this S was issued behind them.
+  if (have_o && __any_sync(0xffffffffu, f != 1.f)) {
+#pragma unroll 1
+    for (int c = 0; c < D / 16; ++c) {
+      uint32_t o[16];
+      get<16>(oc + 16 * c, o);
+      got<16>(o);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+      tmem_st16(oc + 16 * c, o);
+    }
+  }
+  const f32x2 sl = pk2(a.sl2, a.sl2), nm = pk2(-m, -m);
+  f32x2 sum = pk2(0.f, 0.f);
+#pragma unroll
+  for (int c = NC - 1; c >= 0; --c) {
+    if (c < NC - 2) {
+      got<CW>(v[c & 1]);
+      mask(c);
+    }
+    uint32_t p[CW / 2];
+#pragma unroll
+    for (int e = 0; e < CW; e += 2) {
+      const float2 x = up2(fma2(pk2(__uint_as_float(v[c & 1][e]), __uint_as_float(v[c & 1][e + 1])), sl, nm));
+      const float p0 = ex2(x.x), p1 = ex2(x.y);
+      sum = add2(sum, pk2(p0, p1));
+      p[e / 2] = pack_bf16(p0, p1);
+    }
+    if (c >= 2) get<CW>(sc + CW * (c - 2), v[c & 1]);
+    put<CW / 2>(sc + kPCol + CW / 2 * c, p);
+  }
+  const float2 x = up2(sum);
+  l += x.x + x.y;
+}
+
 template <int D, int FMT>
 __device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* ring, Bars& s, int g, int r) {
+  typedef Cfg<D, FMT> C;
   const uint32_t lanes = (uint32_t)(r & ~31) << 16;  // the warp's quarter of the TMEM lanes
   const uint32_t tm = s.tmem, sc = tm + TM * g + lanes, oc = tm + 2 * TM + D * g + lanes;
   const int rt = w.wide ? g * TM : 0;                // first row of the warpgroup's tile
@@ -388,56 +498,8 @@ __device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* ring, Bars& 
       if (!(ok = warp_wait(bar(s.sfull[g]), i & 1, s, a))) break;
       tc_fence_after();
       const int nk = w.k1 - (w.k0 + t * TM);  // keys of the tile
-      float top = -INFINITY;
-#pragma unroll
-      for (int c = 0; c < TM / 32; ++c) {
-        float v[32];
-        tmem_ld32(sc + 32 * c, v);
-        if (nk < TM) {
-#pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = 32 * c + e < nk ? v[e] : -INFINITY;
-        }
-#pragma unroll
-        for (int e = 0; e < 32; e += 2) top = fmax3(top, v[e], v[e + 1]);
-      }
-      const float mt = top * a.sl2;
-      float f = 1.f;
-      if (mt > m + kLazy) {
-        f = ex2(m - mt);  // 0 on the first tile
-        m = mt;
-        l *= f;
-      }
-      // The products into O are done: this S was issued behind them.
-      if (i > 0 && __any_sync(0xffffffffu, f != 1.f)) {
-#pragma unroll 1
-        for (int c = 0; c < D / 32; ++c) {
-          float o[32];
-          tmem_ld32(oc + 32 * c, o);
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] *= f;
-          tmem_st32(oc + 32 * c, reinterpret_cast<const uint32_t*>(o));
-        }
-      }
-      float sum[2] = {0.f, 0.f};
-#pragma unroll
-      for (int c = 0; c < TM / 32; ++c) {
-        float v[32];
-        uint32_t p[16];
-        tmem_ld32(sc + 32 * c, v);
-#pragma unroll
-        for (int e = 0; e < 32; e += 2) {
-          float p0 = ex2(fmaf(v[e], a.sl2, -m)), p1 = ex2(fmaf(v[e + 1], a.sl2, -m));
-          if (nk < TM) {
-            p0 = 32 * c + e < nk ? p0 : 0.f;
-            p1 = 32 * c + e + 1 < nk ? p1 : 0.f;
-          }
-          sum[0] += p0;
-          sum[1] += p1;
-          p[e / 2] = pack_bf16(p0, p1);
-        }
-        tmem_st16(sc + 16 * c, p);
-      }
-      l += sum[0] + sum[1];
+      if (nk >= TM) soften_tile<D, C::CW, false>(a, sc, oc, i > 0, TM, m, l);
+      else soften_tile<D, C::CW, true>(a, sc, oc, i > 0, nk, m, l);
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
