@@ -315,64 +315,98 @@ __device__ void produce(const PrefixArgs& a, const Item& w, uint32_t sq, uint32_
 }
 
 // ---------------------------------------------------------------------------
-// MMA thread.
+// MMA warp.  All 32 lanes walk the loop, so that addresses and descriptors are
+// uniform over the warp, as the instruction takes them; one lane issues.
 // ---------------------------------------------------------------------------
+__device__ __forceinline__ bool elect() {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r));
+  return r != 0;
+}
+
 template <int D, int FMT>
 __device__ void multiply(const PrefixArgs& a, const Item& w, uint32_t sq, uint32_t ring, Bars& s) {
   typedef Cfg<D, FMT> C;
-  const uint32_t tm = s.tmem;
-  const uint32_t qk = idesc_bf16(TM, TM, 0, 0), pv = idesc_bf16(TM, D, 0, 1);
+  const uint32_t tm = __shfl_sync(0xffffffffu, s.tmem, 0);
+  constexpr uint32_t qk = idesc_bf16(TM, TM, 0, 0), pv = idesc_bf16(TM, D, 0, 1);
   const int A = w.wide ? 1 : 2;
-  bool ok = wait(bar(a.stall ? s.stall : s.qfull), 0, s, a);
+  const uint64_t q0 = smem_desc_sw128(sq, 16, 1024), k0 = smem_desc_sw128(ring, 16, 1024),
+                 v0 = smem_desc_sw128(ring, HALF, 1024);
+  bool ok = warp_wait(bar(a.stall ? s.stall : s.qfull), 0, s, a);
   fence_proxy_async();
-  int pos = 0;
-  auto arrived = [&](int p) {
-    if (ok) ok = wait(bar(s.full[p % C::STAGES]), (p / C::STAGES) & 1, s, a);
+  int st = 0, ph = 0;  // ring stage and the parity of its phase
+  auto arrived = [&](int stage, int parity) {
+    if (ok) ok = warp_wait(bar(s.full[stage]), parity, s, a);
     fence_proxy_async();
     tc_fence_after();
   };
-  auto scores = [&](int g, int p) {
-    const uint32_t q = sq + (w.wide ? g : 0) * C::TILE, st = ring + (p % C::STAGES) * C::TILE;
+  auto scores = [&](int g, int stage) {
+    if (elect()) {
+      const uint64_t q = q0 + (w.wide ? g : 0) * (C::TILE >> 4), k = k0 + stage * (C::TILE >> 4);
 #pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk)
-      mma_bf16(tm + TM * g, smem_desc_sw128(q + (kk / 4) * HALF + (kk % 4) * 32, 16, 1024),
-               smem_desc_sw128(st + (kk / 4) * HALF + (kk % 4) * 32, 16, 1024), qk, kk != 0);
-    mma_commit(bar(s.sfull[g]));
+      for (int kk = 0; kk < D / 16; ++kk) {
+        constexpr int H4 = HALF >> 4;
+        mma_bf16(tm + TM * g, q + (kk / 4) * H4 + (kk % 4) * 2, k + (kk / 4) * H4 + (kk % 4) * 2, qk, kk != 0);
+      }
+      mma_commit(bar(s.sfull[g]));
+    }
+    __syncwarp();
   };
-  for (int t = 0; t < min(A, w.T) && ok; ++t, ++pos) {
-    arrived(pos);
+  auto release = [&](int stage) {
+    if (elect()) mma_commit(bar(s.empty[stage]));
+    __syncwarp();
+  };
+  auto next = [&](int& stage, int& parity) {
+    if (++stage == C::STAGES) { stage = 0; parity ^= 1; }
+  };
+  for (int t = 0; t < min(A, w.T) && ok; ++t) {
+    arrived(st, ph);
     if (!ok) break;
-    if (w.wide) { scores(0, pos); scores(1, pos); }
-    else scores(t & 1, pos);
-    mma_commit(bar(s.empty[pos % C::STAGES]));
+    if (w.wide) { scores(0, st); scores(1, st); }
+    else scores(t & 1, st);
+    release(st);
+    next(st, ph);
   }
+#pragma unroll 1
   for (int j = 0; j < w.T && ok; ++j) {
     const bool more = j + A < w.T;
-    arrived(pos);
+    const int sv = st;
+    arrived(sv, ph);
+    next(st, ph);
+    const int sk = st;  // of the next key tile
 #pragma unroll 1
     for (int g = w.wide ? 0 : j & 1; g <= (w.wide ? 1 : j & 1) && ok; ++g) {
       const int i = w.wide ? j : j >> 1;  // the warpgroup's step
-      ok = wait(bar(s.pready[g]), i & 1, s, a);
+      ok = warp_wait(bar(s.pready[g]), i & 1, s, a);
       tc_fence_after();
       if (!ok) break;
-      const uint32_t st = ring + (pos % C::STAGES) * C::TILE;
+      if (elect()) {
+        const uint64_t v = v0 + sv * (C::TILE >> 4);
 #pragma unroll
-      for (int kq = 0; kq < TM / 16; ++kq)
-        mma_bf16_ts(tm + 2 * TM + D * g, tm + TM * g + kPCol + 8 * kq, smem_desc_sw128(st + kq * 2048, HALF, 1024), pv,
-                    i > 0 || kq > 0);
-      if (j + (w.wide ? 1 : 2) >= w.T) mma_commit(bar(s.odone[g]));
+        for (int kq = 0; kq < TM / 16; ++kq)
+          mma_bf16_ts(tm + 2 * TM + D * g, tm + TM * g + kPCol + 8 * kq, v + kq * (2048 >> 4), pv, i > 0 || kq > 0);
+        if (j + A >= w.T) mma_commit(bar(s.odone[g]));
+      }
+      __syncwarp();
       if (more) {
-        if (!(w.wide && g)) arrived(pos + 1);
-        if (ok) scores(g, pos + 1);
+        if (!(w.wide && g)) arrived(sk, ph);
+        if (ok) scores(g, sk);
       }
     }
     if (!ok) break;
-    mma_commit(bar(s.empty[pos % C::STAGES]));
-    if (more) mma_commit(bar(s.empty[(pos + 1) % C::STAGES]));
-    pos += more ? 2 : 1;
+    release(sv);
+    if (more) {
+      release(sk);
+      next(st, ph);
+    }
   }
   if (!ok) {  // products issued so far end before the tensor memory is freed
-    mma_commit(bar(s.drain));
+    if (elect()) mma_commit(bar(s.drain));
+    __syncwarp();
     (void)mbar_wait_bounded(bar(s.drain), 0, kDefaultWaitLimit);
   }
 }
@@ -611,7 +645,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
     soften<D, FMT>(a, w, ring, s, warp >> 2, tid & 127);
   } else if (warp < MMA_WARP) {
     produce<D, FMT>(a, w, smem_u32(sm), smem_u32(ring), smem_u32(raw), s, tid - 256);
-  } else if ((tid & 31) == 0) {
+  } else {
     multiply<D, FMT>(a, w, smem_u32(sm), smem_u32(ring), s);
   }
   tc_fence_before();
