@@ -47,9 +47,9 @@ template <int D, int FMT>
 struct Cfg {
   static constexpr bool CODES = FMT != WF_BF16;
   static constexpr int NPT = CODES ? 256 : 128;          // producer threads
-  static constexpr int NTH = 256 + NPT + 32;             // softmax warps, producers, MMA warp
+  static constexpr int NTH = 256 + NPT + 64;             // softmax warps, producers, MMA warps
   static constexpr int TILE = TM * D * 2;                // a stage
-  static constexpr int CW = CODES ? 16 : 32;             // columns of S in flight (17 warps leave 96 registers, 13 leave 128)
+  static constexpr int CW = 16;                          // columns of S in flight
   static constexpr int ROWB = FMT == WF_MXFP4 ? D / 2 : D;  // bytes of a row of codes
   static constexpr int CPT = CODES ? TM * ROWB / 16 / NPT : 0;  // 16-byte chunks of codes a thread and tile
   static constexpr int DEPTH = FMT == WF_MXFP8 ? 3 : 4;  // tiles of codes in flight
@@ -59,7 +59,7 @@ struct Cfg {
 };
 
 struct Bars {
-  unsigned long long full[8], empty[8], qfull, sfull[2], pready[2], odone[2], stall, drain;
+  unsigned long long full[8], empty[8], qfull, sfull[2], pready[2], odone[2], turn[2], drain[2], stall;
   uint32_t tmem, abort;
 };
 
@@ -131,7 +131,9 @@ __device__ __forceinline__ Item item_of(const PrefixArgs& a) {
 }
 
 // Key tiles meet the MMA thread in the order K_0 .. K_(A-1), then V_j, K_(j+A)
-// for j = 0 .., A = 1 (wide) or 2.  f(tile, is V) for each in that order.
+// for j = 0 .., A = 1 (wide) or 2, and the last V_j.  f(tile, is V) for each in
+// that order.  So with L = min(A, T), K_t has ring position t (t < L) or
+// L + 2 (t - A) + 1, and V_j position L + 2 j (j < T - L) or T + j.
 template <typename F>
 __device__ __forceinline__ void in_order(int T, int A, F f) {
   for (int t = 0; t < min(A, T); ++t) f(t, false);
@@ -315,8 +317,13 @@ __device__ void produce(const PrefixArgs& a, const Item& w, uint32_t sq, uint32_
 }
 
 // ---------------------------------------------------------------------------
-// MMA warp.  All 32 lanes walk the loop, so that addresses and descriptors are
-// uniform over the warp, as the instruction takes them; one lane issues.
+// MMA warps, one a warpgroup: the tensor unit queues about four products (256
+// cycles), less than the waits of a step take, so one warp waits for its operands
+// while the other's products run.  The steps (PV, then the next QK) go out in
+// turn: unordered, the warpgroups fell into step, both waiting for products
+// and then both forming P (4030 cycles a tile instead of 2900).  All 32 lanes
+// walk the loop, so that addresses and descriptors are uniform over the warp, as
+// the instruction takes them; one lane issues.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ bool elect() {
   uint32_t r;
@@ -329,85 +336,65 @@ __device__ __forceinline__ bool elect() {
 }
 
 template <int D, int FMT>
-__device__ void multiply(const PrefixArgs& a, const Item& w, uint32_t sq, uint32_t ring, Bars& s) {
+__device__ void multiply(const PrefixArgs& a, const Item& w, uint32_t sq, uint32_t ring, Bars& s, int g) {
   typedef Cfg<D, FMT> C;
   const uint32_t tm = __shfl_sync(0xffffffffu, s.tmem, 0);
   constexpr uint32_t qk = idesc_bf16(TM, TM, 0, 0), pv = idesc_bf16(TM, D, 0, 1);
-  const int A = w.wide ? 1 : 2;
-  const uint64_t q0 = smem_desc_sw128(sq, 16, 1024), k0 = smem_desc_sw128(ring, 16, 1024),
+  constexpr int T4 = C::TILE >> 4, H4 = HALF >> 4;  // in units of a descriptor's address
+  const uint64_t q = smem_desc_sw128(sq, 16, 1024) + (w.wide ? g : 0) * T4, k0 = smem_desc_sw128(ring, 16, 1024),
                  v0 = smem_desc_sw128(ring, HALF, 1024);
+  const int A = w.wide ? 1 : 2, first = w.wide ? 0 : g;
   bool ok = warp_wait(bar(a.stall ? s.stall : s.qfull), 0, s, a);
-  fence_proxy_async();
-  int st = 0, ph = 0;  // ring stage and the parity of its phase
-  auto arrived = [&](int stage, int parity) {
-    if (ok) ok = warp_wait(bar(s.full[stage]), parity, s, a);
+  // Ring position of key tile t and of value tile t: see in_order.
+  const int lead = min(A, w.T);
+  auto arrived = [&](int pos) {
+    if (ok) ok = warp_wait(bar(s.full[pos % C::STAGES]), (pos / C::STAGES) & 1, s, a);
     fence_proxy_async();
     tc_fence_after();
   };
-  auto scores = [&](int g, int stage) {
+  auto scores = [&](int stage) {
     if (elect()) {
-      const uint64_t q = q0 + (w.wide ? g : 0) * (C::TILE >> 4), k = k0 + stage * (C::TILE >> 4);
+      const uint64_t k = k0 + stage * T4;
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) {
-        constexpr int H4 = HALF >> 4;
+      for (int kk = 0; kk < D / 16; ++kk)
         mma_bf16(tm + TM * g, q + (kk / 4) * H4 + (kk % 4) * 2, k + (kk / 4) * H4 + (kk % 4) * 2, qk, kk != 0);
-      }
       mma_commit(bar(s.sfull[g]));
+      mma_commit(bar(s.empty[stage]));
     }
     __syncwarp();
   };
-  auto release = [&](int stage) {
-    if (elect()) mma_commit(bar(s.empty[stage]));
-    __syncwarp();
-  };
-  auto next = [&](int& stage, int& parity) {
-    if (++stage == C::STAGES) { stage = 0; parity ^= 1; }
-  };
-  for (int t = 0; t < min(A, w.T) && ok; ++t) {
-    arrived(st, ph);
-    if (!ok) break;
-    if (w.wide) { scores(0, st); scores(1, st); }
-    else scores(t & 1, st);
-    release(st);
-    next(st, ph);
+  if (first < w.T) {
+    arrived(first);
+    if (ok) scores(first % C::STAGES);
   }
 #pragma unroll 1
-  for (int j = 0; j < w.T && ok; ++j) {
+  for (int j = first, i = 0; j < w.T && ok; j += A, ++i) {
     const bool more = j + A < w.T;
-    const int sv = st;
-    arrived(sv, ph);
-    next(st, ph);
-    const int sk = st;  // of the next key tile
-#pragma unroll 1
-    for (int g = w.wide ? 0 : j & 1; g <= (w.wide ? 1 : j & 1) && ok; ++g) {
-      const int i = w.wide ? j : j >> 1;  // the warpgroup's step
-      ok = warp_wait(bar(s.pready[g]), i & 1, s, a);
-      tc_fence_after();
-      if (!ok) break;
-      if (elect()) {
-        const uint64_t v = v0 + sv * (C::TILE >> 4);
-#pragma unroll
-        for (int kq = 0; kq < TM / 16; ++kq)
-          mma_bf16_ts(tm + 2 * TM + D * g, tm + TM * g + kPCol + 8 * kq, v + kq * (2048 >> 4), pv, i > 0 || kq > 0);
-        if (j + A >= w.T) mma_commit(bar(s.odone[g]));
-      }
-      __syncwarp();
-      if (more) {
-        if (!(w.wide && g)) arrived(sk, ph);
-        if (ok) scores(g, sk);
-      }
-    }
+    const int pv_pos = j < w.T - lead ? lead + 2 * j : w.T + j, pk_pos = pv_pos + 1;
+    arrived(pv_pos);
+    if (more) arrived(pk_pos);
+    if (ok) ok = warp_wait(bar(s.pready[g]), i & 1, s, a);
+    if (ok && (g || i > 0)) ok = warp_wait(bar(s.turn[g]), (g ? i : i - 1) & 1, s, a);
+    tc_fence_after();
     if (!ok) break;
-    release(sv);
-    if (more) {
-      release(sk);
-      next(st, ph);
+    const int sv = pv_pos % C::STAGES;
+    if (elect()) {
+      const uint64_t v = v0 + sv * T4;
+#pragma unroll
+      for (int kq = 0; kq < TM / 16; ++kq)
+        mma_bf16_ts(tm + 2 * TM + D * g, tm + TM * g + kPCol + 8 * kq, v + kq * (2048 >> 4), pv, i > 0 || kq > 0);
+      mma_commit(bar(s.empty[sv]));
+      if (!more) mma_commit(bar(s.odone[g]));
     }
+    __syncwarp();
+    if (more) scores(pk_pos % C::STAGES);
+    if (elect()) mbar_arrive(bar(s.turn[g ^ 1]));
+    __syncwarp();
   }
   if (!ok) {  // products issued so far end before the tensor memory is freed
-    if (elect()) mma_commit(bar(s.drain));
+    if (elect()) mma_commit(bar(s.drain[g]));
     __syncwarp();
-    (void)mbar_wait_bounded(bar(s.drain), 0, kDefaultWaitLimit);
+    (void)mbar_wait_bounded(bar(s.drain[g]), 0, kDefaultWaitLimit);
   }
 }
 
@@ -613,7 +600,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   uint8_t* raw = ring + C::STAGES * C::TILE;
   Bars& s = *reinterpret_cast<Bars*>(raw + C::RAW);
   const int tid = threadIdx.x, warp = tid >> 5;
-  constexpr int MMA_WARP = C::NTH / 32 - 1;
+  constexpr int MMA_WARP = C::NTH / 32 - 2;
   grid_dep_wait();
   const Item w = item_of(a);
   if (warp == MMA_WARP) {
@@ -623,7 +610,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   if (tid == 0) {
     for (int i = 0; i < C::STAGES; ++i) {
       mbar_init(bar(s.full[i]), C::NPT);
-      mbar_init(bar(s.empty[i]), 1);
+      mbar_init(bar(s.empty[i]), w.wide ? 2 : 1);  // a commit of every MMA warp that reads the stage
     }
     mbar_init(bar(s.qfull), C::NPT);
     for (int g = 0; g < 2; ++g) {
@@ -631,9 +618,10 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
       mbar_init(bar(s.sfull[g]), 1);
       mbar_init(bar(s.pready[g]), (min(rows, TM) + 31) / 32);
       mbar_init(bar(s.odone[g]), 1);
+      mbar_init(bar(s.drain[g]), 1);
+      mbar_init(bar(s.turn[g]), 1);
     }
     mbar_init(bar(s.stall), 1);
-    mbar_init(bar(s.drain), 1);
     s.abort = 0;
     fence_mbar_init();
   }
@@ -646,7 +634,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   } else if (warp < MMA_WARP) {
     produce<D, FMT>(a, w, smem_u32(sm), smem_u32(ring), smem_u32(raw), s, tid - 256);
   } else {
-    multiply<D, FMT>(a, w, smem_u32(sm), smem_u32(ring), s);
+    multiply<D, FMT>(a, w, smem_u32(sm), smem_u32(ring), s, warp - MMA_WARP);
   }
   tc_fence_before();
   __syncthreads();
