@@ -47,9 +47,10 @@ template <int D, int FMT>
 struct Cfg {
   static constexpr bool CODES = FMT != WF_BF16;
   static constexpr int NPT = CODES ? 256 : 128;          // producer threads
-  static constexpr int NTH = 256 + NPT + 64;             // softmax warps, producers, MMA warps
+  // Softmax warps, producers, two MMA warps (and two idle ones, to make whole
+  // warpgroups, where registers move between them).
+  static constexpr int NTH = 256 + NPT + (CODES ? 128 : 64);
   static constexpr int TILE = TM * D * 2;                // a stage
-  static constexpr int CW = 16;                          // columns of S in flight
   static constexpr int ROWB = FMT == WF_MXFP4 ? D / 2 : D;  // bytes of a row of codes
   static constexpr int CPT = CODES ? TM * ROWB / 16 / NPT : 0;  // 16-byte chunks of codes a thread and tile
   static constexpr int DEPTH = FMT == WF_MXFP8 ? 3 : 4;  // tiles of codes in flight
@@ -401,105 +402,85 @@ __device__ void multiply(const PrefixArgs& a, const Item& w, uint32_t sq, uint32
 // ---------------------------------------------------------------------------
 // Softmax warpgroups.
 // ---------------------------------------------------------------------------
-// CW columns of a thread's TMEM lane; valid behind got().
-template <int CW>
+// 16 columns of a thread's TMEM lane; valid behind got(), through which the
+// registers pass, so that no use of them moves before the wait.
 __device__ __forceinline__ void get(uint32_t taddr, uint32_t* v) {
-  if constexpr (CW == 32) {
-    tmem_ld32_issue(taddr, v);
-  } else {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
-          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-        : "r"(taddr)
-        : "memory");
-  }
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr)
+      : "memory");
 }
-// The registers pass through the wait, so no use of them moves before it.
-template <int CW>
 __device__ __forceinline__ void got(uint32_t* v) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
                : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
                  "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
-  if constexpr (CW == 32)
-    asm volatile("" : "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]),
-                 "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])::"memory");
-}
-template <int N>
-__device__ __forceinline__ void put(uint32_t taddr, const uint32_t* p) {
-  if constexpr (N == 16) tmem_st16(taddr, p);
-  else
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(p[0]),
-                 "r"(p[1]), "r"(p[2]), "r"(p[3]), "r"(p[4]), "r"(p[5]), "r"(p[6]), "r"(p[7])
-                 : "memory");
 }
 
-// P of one tile from S, in two passes of chunks of CW columns, the next chunk
-// on its way while one is worked on: the row's maximum, first to last; then P,
-// last to first, starting on the two chunks still in registers.  P goes to the
-// upper half of S's columns, always onto columns already read.
-template <int D, int CW, bool MASK>
+// P of one tile from S: one pass over chunks of CW columns, the next chunk on its
+// way while one is worked on, with the maximum of the tiles before as m.  P
+// stays in registers until the tile's own maximum is known; where that is more
+// than 2^kLazy above m (the first tile, seldom later) m is raised, O and l are
+// rescaled and the pass runs again, S being still there.  P goes to the upper
+// half of S's columns.
+constexpr int CW = 16;
+template <int D, bool MASK>
 __device__ __forceinline__ void soften_tile(const PrefixArgs& a, uint32_t sc, uint32_t oc, bool have_o, int nk, float& m,
                                             float& l) {
   constexpr int NC = TM / CW;
-  uint32_t v[2][CW];
-  auto mask = [&](int c) {
-    if (MASK) {
-#pragma unroll
-      for (int e = 0; e < CW; ++e) v[c & 1][e] = CW * c + e < nk ? v[c & 1][e] : __float_as_uint(-INFINITY);
-    }
-  };
-  float top = -INFINITY;
-  get<CW>(sc, v[0]);
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    got<CW>(v[c & 1]);
-    if (c + 1 < NC) get<CW>(sc + CW * (c + 1), v[(c + 1) & 1]);
-    mask(c);
-#pragma unroll
-    for (int e = 0; e < CW; e += 2) top = fmax3(top, __uint_as_float(v[c & 1][e]), __uint_as_float(v[c & 1][e + 1]));
-  }
-  const float mt = top * a.sl2;
-  float f = 1.f;
-  if (mt > m + kLazy) {
-    f = ex2(m - mt);  // 0 on the first tile
-    m = mt;
-    l *= f;
-  }
-  // The products into O are done: this S was issued behind them.
-  if (have_o && __any_sync(0xffffffffu, f != 1.f)) {
+  const f32x2 sl = pk2(a.sl2, a.sl2);
+  uint32_t p[TM / 2];
+  f32x2 sum[2];
 #pragma unroll 1
-    for (int c = 0; c < D / 16; ++c) {
-      uint32_t o[16];
-      get<16>(oc + 16 * c, o);
-      got<16>(o);
+  for (;;) {
+    const f32x2 nm = pk2(-m, -m);
+    uint32_t v[2][CW];
+    float top = -INFINITY;
+    sum[0] = sum[1] = pk2(0.f, 0.f);
+    get(sc, v[0]);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-      tmem_st16(oc + 16 * c, o);
+    for (int c = 0; c < NC; ++c) {
+      uint32_t* x = v[c & 1];
+      got(x);
+      if (c + 1 < NC) get(sc + CW * (c + 1), v[(c + 1) & 1]);
+      if (MASK) {
+#pragma unroll
+        for (int e = 0; e < CW; ++e) x[e] = CW * c + e < nk ? x[e] : __float_as_uint(-INFINITY);
+      }
+#pragma unroll
+      for (int e = 0; e < CW; e += 2) {
+        const float s0 = __uint_as_float(x[e]), s1 = __uint_as_float(x[e + 1]);
+        top = fmax3(top, s0, s1);
+        const float2 z = up2(fma2(pk2(s0, s1), sl, nm));
+        const float p0 = ex2(z.x), p1 = ex2(z.y);
+        sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], pk2(p0, p1));
+        p[(CW * c + e) / 2] = pack_bf16(p0, p1);
+      }
+    }
+    const float mt = top * a.sl2;
+    const bool raise = mt > m + kLazy;
+    if (!__any_sync(0xffffffffu, raise)) break;
+    const float f = raise ? ex2(m - mt) : 1.f;  // 0 on the first tile
+    m = raise ? mt : m;
+    l *= f;
+    if (have_o) {  // the products into O are done: this S was issued behind them
+#pragma unroll 1
+      for (int c = 0; c < D / CW; ++c) {
+        uint32_t o[CW];
+        get(oc + CW * c, o);
+        got(o);
+#pragma unroll
+        for (int e = 0; e < CW; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+        tmem_st16(oc + CW * c, o);
+      }
     }
   }
-  const f32x2 sl = pk2(a.sl2, a.sl2), nm = pk2(-m, -m);
-  f32x2 sum = pk2(0.f, 0.f);
 #pragma unroll
-  for (int c = NC - 1; c >= 0; --c) {
-    if (c < NC - 2) {
-      got<CW>(v[c & 1]);
-      mask(c);
-    }
-    uint32_t p[CW / 2];
-#pragma unroll
-    for (int e = 0; e < CW; e += 2) {
-      const float2 x = up2(fma2(pk2(__uint_as_float(v[c & 1][e]), __uint_as_float(v[c & 1][e + 1])), sl, nm));
-      const float p0 = ex2(x.x), p1 = ex2(x.y);
-      sum = add2(sum, pk2(p0, p1));
-      p[e / 2] = pack_bf16(p0, p1);
-    }
-    if (c >= 2) get<CW>(sc + CW * (c - 2), v[c & 1]);
-    put<CW / 2>(sc + kPCol + CW / 2 * c, p);
-  }
-  const float2 x = up2(sum);
-  l += x.x + x.y;
+  for (int c = 0; c < TM / 32; ++c) tmem_st16(sc + kPCol + 16 * c, p + 16 * c);
+  const float2 z = up2(add2(sum[0], sum[1]));
+  l += z.x + z.y;
 }
 
 template <int D, int FMT>
@@ -519,8 +500,8 @@ __device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* ring, Bars& 
       if (!(ok = warp_wait(bar(s.sfull[g]), i & 1, s, a))) break;
       tc_fence_after();
       const int nk = w.k1 - (w.k0 + t * TM);  // keys of the tile
-      if (nk >= TM) soften_tile<D, C::CW, false>(a, sc, oc, i > 0, TM, m, l);
-      else soften_tile<D, C::CW, true>(a, sc, oc, i > 0, nk, m, l);
+      if (nk >= TM) soften_tile<D, false>(a, sc, oc, i > 0, TM, m, l);
+      else soften_tile<D, true>(a, sc, oc, i > 0, nk, m, l);
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
@@ -600,7 +581,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   uint8_t* raw = ring + C::STAGES * C::TILE;
   Bars& s = *reinterpret_cast<Bars*>(raw + C::RAW);
   const int tid = threadIdx.x, warp = tid >> 5;
-  constexpr int MMA_WARP = C::NTH / 32 - 2;
+  constexpr int MMA_WARP = 8 + C::NPT / 32;
   grid_dep_wait();
   const Item w = item_of(a);
   if (warp == MMA_WARP) {
@@ -629,12 +610,17 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   __syncthreads();
   tc_fence_after();
   grid_dep_launch();  // after the barrier that publishes the tensor memory (see Launch)
+  // Registers of the 20 warps with codes: 96 each at launch, 5 warps a quarter of
+  // the SM; 2 x 128 + 2 x 80 + 64 = 5 x 96.
   if (warp < 8) {
+    if (C::CODES) asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
     soften<D, FMT>(a, w, ring, s, warp >> 2, tid & 127);
   } else if (warp < MMA_WARP) {
+    if (C::CODES) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     produce<D, FMT>(a, w, smem_u32(sm), smem_u32(ring), smem_u32(raw), s, tid - 256);
   } else {
-    multiply<D, FMT>(a, w, smem_u32(sm), smem_u32(ring), s, warp - MMA_WARP);
+    if (C::CODES) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp < MMA_WARP + 2) multiply<D, FMT>(a, w, smem_u32(sm), smem_u32(ring), s, warp - MMA_WARP);
   }
   tc_fence_before();
   __syncthreads();
