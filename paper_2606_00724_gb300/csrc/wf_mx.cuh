@@ -64,16 +64,26 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-// Pair i (channels 2 i, 2 i + 1) of a word of codes, before the factor: 2 pairs
-// of E4M3 or 4 of E2M1.
+// A word of codes before the factor: 4 E4M3 codes to 2 pairs, 8 E2M1 codes to 4.
+// The bytes of the results are formed for all codes of the word at once (the
+// upper one: sign and upper exponent bits, the lower one: the rest) and then
+// put in their places.
 template <bool FP4>
-__device__ __forceinline__ uint32_t mx_pair(uint32_t w, int i) {
+__device__ __forceinline__ void mx_pairs(uint32_t w, uint32_t* y) {
   if (FP4) {
-    const uint32_t b = __byte_perm(w, 0, 0x4440 + i);
-    return ((b * 0x00040040u) & 0x01c001c0u) | ((b * 0x01001000u) & 0x80008000u);
+    const uint32_t he = ((w << 4) & 0x80808080u) | ((w >> 2) & 0x01010101u), le = (w << 6) & 0xc0c0c0c0u;
+    const uint32_t ho = (w & 0x80808080u) | ((w >> 6) & 0x01010101u), lo = (w << 2) & 0xc0c0c0c0u;
+    const uint32_t e0 = __byte_perm(le, he, 0x5140), e1 = __byte_perm(le, he, 0x7362);  // channels 0, 2 and 4, 6
+    const uint32_t o0 = __byte_perm(lo, ho, 0x5140), o1 = __byte_perm(lo, ho, 0x7362);  // 1, 3 and 5, 7
+    y[0] = __byte_perm(e0, o0, 0x5410);
+    y[1] = __byte_perm(e0, o0, 0x7632);
+    y[2] = __byte_perm(e1, o1, 0x5410);
+    y[3] = __byte_perm(e1, o1, 0x7632);
+  } else {
+    const uint32_t h = (w & 0x80808080u) | ((w >> 4) & 0x07070707u), l = (w << 4) & 0xf0f0f0f0u;
+    y[0] = __byte_perm(l, h, 0x5140);
+    y[1] = __byte_perm(l, h, 0x7362);
   }
-  const uint32_t b = __byte_perm(w, 0, i ? 0x4342 : 0x4140);
-  return ((b * 16u) & 0x07f007f0u) | ((b * 256u) & 0x80008000u);
 }
 
 }  // namespace wf

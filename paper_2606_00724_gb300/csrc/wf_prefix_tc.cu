@@ -19,9 +19,10 @@
 // of this one is consumed.
 //
 // bf16 prompt rows are copied by cp.async into the 128-byte-swizzled stages,
-// gathered through idx where there is one.  Codes are copied raw into a ring of
-// the thread's own, then widened to bf16 (exact: at most 4 digits and a power of
-// two) into the stage.  Rows past a count are zero-filled and never read.
+// gathered through idx where there is one.  Codes are copied as they are by two
+// loader warps into a ring of their own, and the producers widen them to bf16
+// (exact: at most 4 digits and a power of two) into the stage.  Rows past a
+// count are zero-filled and never read.
 //
 // P is rounded to bf16 as the operand of the product; sums, maxima and O stay in
 // fp32.  Every wait is bounded: one that gives up sets the status word and the
@@ -47,20 +48,28 @@ template <int D, int FMT>
 struct Cfg {
   static constexpr bool CODES = FMT != WF_BF16;
   static constexpr int NPT = CODES ? 256 : 128;          // producer threads
-  // Softmax warps, producers, two MMA warps (and two idle ones, to make whole
-  // warpgroups, where registers move between them).
+  // Softmax warps, producers, two MMA warps and, with codes, two loader warps.
   static constexpr int NTH = 256 + NPT + (CODES ? 128 : 64);
   static constexpr int TILE = TM * D * 2;                // a stage
   static constexpr int ROWB = FMT == WF_MXFP4 ? D / 2 : D;  // bytes of a row of codes
-  static constexpr int CPT = CODES ? TM * ROWB / 16 / NPT : 0;  // 16-byte chunks of codes a thread and tile
   static constexpr int DEPTH = FMT == WF_MXFP8 ? 3 : 4;  // tiles of codes in flight
-  static constexpr int RAW = CODES ? DEPTH * NPT * CPT * 20 : 0;  // chunks and their scale words
+  // A tile's chunks of codes go to the widening threads so that the 8 lanes of a
+  // shared-memory phase hold the PX chunks of one 64-channel half for 8 / PX
+  // consecutive rows: the stores into the swizzled stage then take 8 different
+  // banks of 16 bytes, and the loads do as well with chunk x of row r at chunk
+  // place(x, r) of the slot's row.
+  static constexpr int CR = ROWB / 16, PX = D == 128 ? CR / 2 : CR;
+  __device__ static int place(int x, int r) { return D == 128 ? x ^ (r * ROWB / 128 % 2 * PX) : x; }
+  static constexpr int SLOT = TM * ROWB + TM * 4;        // a tile of codes and its scales
+  static constexpr int RAW = CODES ? DEPTH * SLOT : 0;
+  // Stages beside two tiles of query rows; with one tile its place is a stage more.
   static constexpr int STAGES = (232448 - 2048 - 2 * TILE - RAW) / TILE > 8 ? 8 : (232448 - 2048 - 2 * TILE - RAW) / TILE;
   static constexpr size_t SMEM = 1024 + 2 * TILE + RAW + (size_t)STAGES * TILE + 512;
 };
 
+constexpr int kMaxStages = 9;
 struct Bars {
-  unsigned long long full[8], empty[8], qfull, sfull[2], pready[2], odone[2], turn[2], drain[2], stall;
+  unsigned long long full[kMaxStages], empty[kMaxStages], raw_full[4], raw_empty[4], qfull, sfull[2], pready[2], odone[2], turn[2], drain[2], stall;
   uint32_t tmem, abort;
 };
 
@@ -99,6 +108,11 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+__device__ __forceinline__ uint32_t lds_u8(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, int bytes) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
@@ -131,7 +145,16 @@ __device__ __forceinline__ Item item_of(const PrefixArgs& a) {
   return w;
 }
 
-// Key tiles meet the MMA thread in the order K_0 .. K_(A-1), then V_j, K_(j+A)
+// The ring of stages: position p of the order below is in stage p % n.
+struct Ring {
+  uint32_t base;
+  int n;
+  uint32_t inv;  // 2^32 / n rounded up: exact quotients below 2^28
+  __device__ __forceinline__ int turn(int p) const { return (int)__umulhi((uint32_t)p, inv); }
+  __device__ __forceinline__ int stage(int p) const { return p - turn(p) * n; }
+};
+
+// Key tiles meet the MMA warps in the order K_0 .. K_(A-1), then V_j, K_(j+A)
 // for j = 0 .., A = 1 (wide) or 2, and the last V_j.  f(tile, is V) for each in
 // that order.  So with L = min(A, T), K_t has ring position t (t < L) or
 // L + 2 (t - A) + 1, and V_j position L + 2 j (j < T - L) or T + j.
@@ -193,7 +216,7 @@ __device__ __forceinline__ void copy_tile(uint32_t st, const bf16* base, int64_t
 }
 
 template <int D, int FMT>
-__device__ void produce(const PrefixArgs& a, const Item& w, uint32_t sq, uint32_t ring, uint32_t raw, Bars& s, int tid) {
+__device__ void produce(const PrefixArgs& a, const Item& w, uint32_t sq, const Ring& ring, uint32_t raw, Bars& s, int tid) {
   typedef Cfg<D, FMT> C;
   constexpr int CH = D / 8, NPT = C::NPT;
   // The query rows, K-major; rows past the last are zero.
@@ -216,90 +239,58 @@ __device__ void produce(const PrefixArgs& a, const Item& w, uint32_t sq, uint32_
     int pos = 0;
     bool ok = true;
     in_order(w.T, A, [&](int t, bool v) {
-      const int st = pos % C::STAGES, n = pos / C::STAGES;
+      const int st = ring.stage(pos), n = ring.turn(pos);
       ++pos;
       if (ok && n > 0) ok = warp_wait(bar(s.empty[st]), (n - 1) & 1, s, a);
-      if (ok) copy_tile<D, NPT>(ring + st * C::TILE, v ? V : K, ss, idx, a.n, w.k0 + t * TM, w.k1, tid);
+      if (ok) copy_tile<D, NPT>(ring.base + st * C::TILE, v ? V : K, ss, idx, a.n, w.k0 + t * TM, w.k1, tid);
       cp_async_arrive_noinc(bar(s.full[st]));
     });
     cp_async_wait_all();
     return;
   }
   if constexpr (C::CODES) {
-    // The thread copies its chunks of 16 bytes and the scale words of their rows
-    // into slots of its own DEPTH - 1 tiles ahead and widens them itself, so its
-    // own cp.async groups are all it waits for.
+    // Widen the tiles that the loader warps bring.  Two groups of four warps take
+    // every other tile, so that one's waits run under the other's work: with all
+    // eight on each tile a third of the time went by in waits.  Thread tid of a
+    // group takes chunk x of rows rr + RS i.
     constexpr bool FP4 = FMT == WF_MXFP4;
-    constexpr int CR = C::ROWB / 16, CPT = C::CPT, RS = NPT / CR;
+    constexpr int CR = C::CR, PX = C::PX, NG = NPT / 2, CPT = TM * CR / NG, RS = NG / CR;
     constexpr int EL = FP4 ? 32 : 16, OUT = EL / 8;  // channels a chunk, bf16 chunks they make
-    constexpr int SR = D / kMxBlock;                 // scale bytes a row: 4 or 2
-    const int x = tid % CR, rr = tid / CR;           // chunk x of rows rr + RS i
-    const int32_t* idx = a.idx ? a.idx + (int64_t)w.u * a.k : nullptr;
-    const int64_t srow = (int64_t)w.u * a.n, sbytes = (int64_t)a.P * a.H * a.n * SR;
-    const uint8_t* kbase = static_cast<const uint8_t*>(a.K) + b * a.ksb + h * a.ksh + x * 16;
-    const uint8_t* vbase = static_cast<const uint8_t*>(a.V) + b * a.ksb + h * a.ksh + x * 16;
-    const uint32_t chunks = raw + (uint32_t)tid * 16, words = raw + C::DEPTH * NPT * CPT * 16 + (uint32_t)tid * 4;
-    const int total = 2 * w.T, lead = min(A, w.T), pairs = w.T - lead;
-    // Tile and kind of position p: the order of in_order.
-    auto place = [&](int p, int& t, bool& v) {
-      const int o = p - lead;
-      v = o >= 0 && (o >= 2 * pairs || !(o & 1));
-      t = o < 0 ? p : o >= 2 * pairs ? o - pairs : o / 2 + ((o & 1) ? A : 0);
-    };
-    auto row_of = [&](int j) { return j >= w.k1 ? 0 : idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j; };
-    auto issue = [&](int p, int slot) {
-      if (p < total) {
-        int t; bool v;
-        place(p, t, v);
-        const uint8_t* base = v ? vbase : kbase;
-        const uint8_t* sc = v ? a.Vs : a.Ks;
-        const int j0 = w.k0 + t * TM + rr;
-#pragma unroll
-        for (int i = 0; i < CPT; ++i) {
-          const int row = row_of(j0 + RS * i);
-          cp_async16_zfill(chunks + (uint32_t)(slot * CPT + i) * (NPT * 16), base + row * a.kss, j0 + RS * i < w.k1);
-          // The row's scale word: 4 bytes, or those of a pair of rows (of which
-          // the last may have no second).
-          const int64_t so = ((srow + row) * SR) & ~(int64_t)3;
-          cp_async4(words + (uint32_t)(slot * CPT + i) * (NPT * 4), sc + so,
-                    SR == 4 || so + 4 <= sbytes ? 4 : (int)(sbytes - so));
-        }
-      }
-      cp_async_commit();
-    };
-    for (int p = 0; p < C::DEPTH - 1; ++p) issue(p, p);
-    int slot = 0, st = 0, n = 0;
+    static_assert(RS % 8 == 0, "a thread's rows share their swizzle and place");
+    const int group = tid / NG, gt = tid % NG;
+    const int x = gt % PX + PX * (gt / 8 % (CR / PX)), rr = gt / PX % (8 / PX) + 8 / PX * (gt / (8 * CR / PX));
+    const uint32_t chunk = (uint32_t)(rr * CR + C::place(x, rr)) * 16;
+    const uint32_t scale = TM * C::ROWB + rr * 4 + x * EL / kMxBlock;
 #pragma unroll 1
-    for (int p = 0; p < total; ++p) {
-      issue(p + C::DEPTH - 1, slot ? slot - 1 : C::DEPTH - 1);
-      cp_async_wait<C::DEPTH - 1>();
+    for (int p = group; p < 2 * w.T; p += 2) {
+      const int slot = p % C::DEPTH, st = ring.stage(p), n = ring.turn(p);
+      if (!warp_wait(bar(s.raw_full[slot]), p / C::DEPTH & 1, s, a)) break;
+      // The tile's codes go to registers and the slot back to the loaders at once,
+      // so that a copy's latency covers one tile's widening and not two.
+      const uint32_t src = raw + slot * C::SLOT, dst = ring.base + st * C::TILE;
       uint4 code[CPT];
       uint32_t byte[CPT];
+      bool large = false;  // a scale that takes a second factor
 #pragma unroll
       for (int i = 0; i < CPT; ++i) {
-        code[i] = lds_v4(chunks + (uint32_t)(slot * CPT + i) * (NPT * 16));
-        byte[i] = lds_u32(words + (uint32_t)(slot * CPT + i) * (NPT * 4));
+        code[i] = lds_v4(src + chunk + NG * 16 * i);
+        byte[i] = lds_u8(src + scale + RS * 4 * i);
       }
 #pragma unroll
-      for (int i = 0; i < CPT; ++i) {
-        int t; bool v;
-        place(p, t, v);
-        const int j = w.k0 + t * TM + rr + RS * i;
-        int sh = x * EL / kMxBlock * 8;
-        if (SR == 2) sh += (int)((srow + row_of(j)) & 1) * 16;
-        byte[i] = j < w.k1 ? (byte[i] >> sh) & 0xffu : 0u;  // rows past the last are zeros whatever their scale
-      }
+      for (int i = 0; i < CPT; ++i) large |= byte[i] > kMxOne<FP4>;
+      large = __any_sync(0xffffffffu, large);
+      if ((gt & 31) == 0) mbar_arrive(bar(s.raw_empty[slot]));
       if (n > 0 && !warp_wait(bar(s.empty[st]), (n - 1) & 1, s, a)) break;
-      const uint32_t dst = ring + st * C::TILE;
 #pragma unroll
       for (int i = 0; i < CPT; ++i) {
         const uint32_t cw[4] = {code[i].x, code[i].y, code[i].z, code[i].w};
         const uint32_t f = mx_factor<FP4>(byte[i]);
         uint32_t y[OUT * 4];
 #pragma unroll
-        for (int e = 0; e < OUT * 4; ++e)
-          y[e] = mul_bf16x2(FP4 ? mx_pair<true>(cw[e / 4], e % 4) : mx_pair<false>(cw[e / 2], e % 2), f);
-        if (__any_sync(0xffffffffu, byte[i] > kMxOne<FP4>)) {
+        for (int e = 0; e < 4; ++e) mx_pairs<FP4>(cw[e], y + e * OUT);
+#pragma unroll
+        for (int e = 0; e < OUT * 4; ++e) y[e] = mul_bf16x2(y[e], f);
+        if (large) {
           const uint32_t f2 = mx_second_factor<FP4>(byte[i]);
 #pragma unroll
           for (int e = 0; e < OUT * 4; ++e) y[e] = mul_bf16x2(y[e], f2);
@@ -309,12 +300,83 @@ __device__ void produce(const PrefixArgs& a, const Item& w, uint32_t sq, uint32_
           sts_v4(dst + swizzled(rr + RS * i, x * OUT + o), make_uint4(y[4 * o], y[4 * o + 1], y[4 * o + 2], y[4 * o + 3]));
       }
       fence_proxy_async();
-      mbar_arrive(bar(s.full[st]));
-      slot = slot + 1 == C::DEPTH ? 0 : slot + 1;
-      if (++st == C::STAGES) { st = 0; ++n; }
+      __syncwarp();
+      if ((gt & 31) == 0) mbar_arrive(bar(s.full[st]));
     }
-    cp_async_wait_all();
   }
+}
+
+// The loader warps of a prompt in codes: tiles of codes and their scales, as
+// they are, into DEPTH slots.  A warp brings half of a tile's rows: lane l looks
+// up two of them (rows q = l, l + 32 of the warp's 64) one tile ahead, copies
+// their scales, and the lanes pass the rows on for the chunks.  A row's scale
+// bytes have 4 bytes of a slot; where they are 2, they are stored by the thread,
+// since the smallest copy is 4 bytes on 4.
+template <int D, int FMT>
+__device__ void load_codes(const PrefixArgs& a, const Item& w, uint32_t raw, Bars& s, int warp, int lane) {
+  typedef Cfg<D, FMT> C;
+  constexpr int CR = C::CR, RP = 32 / CR, NI = 64 / RP, SR = D / kMxBlock;  // rows a pass of the warp, passes
+  const int64_t b = w.u / a.H, h = w.u % a.H;
+  const int x = lane % CR;
+  const int32_t* idx = a.idx ? a.idx + (int64_t)w.u * a.k : nullptr;
+  const uint8_t* kbase = static_cast<const uint8_t*>(a.K) + b * a.ksb + h * a.ksh + x * 16;
+  const uint8_t* vbase = static_cast<const uint8_t*>(a.V) + b * a.ksb + h * a.ksh + x * 16;
+  const int64_t srow = (int64_t)w.u * a.n * SR;
+  // Row q of the warp's half is row 64 warp + q of the tile; -1 past the last.
+  auto look_up = [&](int t, int* row) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int j = w.k0 + t * TM + 64 * warp + lane + 32 * k;
+      row[k] = j >= w.k1 ? -1 : idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j;
+    }
+  };
+  int slot = 0, n = 0;
+  bool ok = true;
+  const uint32_t first = (uint32_t)((64 * warp + lane / CR) * CR) * 16;  // this lane's first row in a slot
+  auto bring = [&](int t, const int* row, bool v) {
+    if (ok && n > 0) ok = warp_wait(bar(s.raw_empty[slot]), (n - 1) & 1, s, a);
+    if (ok) {
+      const uint32_t dst = raw + slot * C::SLOT;
+      const uint8_t* base = v ? vbase : kbase;
+      const uint8_t* sc = (v ? a.Vs : a.Ks) + srow;
+      const bool full = w.k0 + (t + 1) * TM <= w.k1;
+      if (!idx && full) {
+        const uint8_t* p = base + (w.k0 + t * TM + 64 * warp + lane / CR) * a.kss;
+#pragma unroll
+        for (int i = 0; i < NI; ++i, p += RP * a.kss)
+          cp_async16(dst + first + RP * CR * 16 * i + C::place(x, lane / CR + RP * i) * 16, p);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          const int at = __shfl_sync(0xffffffffu, row[RP * i / 32], (RP * i + lane / CR) % 32);
+          cp_async16_zfill(dst + first + RP * CR * 16 * i + C::place(x, lane / CR + RP * i) * 16,
+                           base + max(at, 0) * a.kss, at >= 0);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t at = dst + TM * C::ROWB + (uint32_t)(64 * warp + lane + 32 * k) * 4;
+        const uint8_t* p = sc + (int64_t)max(row[k], 0) * SR;
+        if (SR == 4) cp_async4(at, p, row[k] < 0 ? 0 : 4);  // rows past the last: scale 2^-127 of zeros
+        else sts_u32(at, row[k] < 0 ? 0u : __ldg(reinterpret_cast<const uint16_t*>(p)));
+      }
+    }
+    if (SR == 2) mbar_arrive(bar(s.raw_full[slot]));  // releases the plain stores
+    cp_async_arrive_noinc(bar(s.raw_full[slot]));
+    if (++slot == C::DEPTH) { slot = 0; ++n; }
+  };
+  int row[2], ahead[2], tile = -1;
+  bool kind = false;
+  in_order(w.T, w.wide ? 1 : 2, [&](int t, bool v) {
+    look_up(t, ahead);
+    if (tile >= 0) bring(tile, row, kind);
+    row[0] = ahead[0];
+    row[1] = ahead[1];
+    kind = v;
+    tile = t;
+  });
+  if (tile >= 0) bring(tile, row, kind);
+  cp_async_wait_all();
 }
 
 // ---------------------------------------------------------------------------
@@ -337,19 +399,19 @@ __device__ __forceinline__ bool elect() {
 }
 
 template <int D, int FMT>
-__device__ void multiply(const PrefixArgs& a, const Item& w, uint32_t sq, uint32_t ring, Bars& s, int g) {
+__device__ void multiply(const PrefixArgs& a, const Item& w, uint32_t sq, const Ring& ring, Bars& s, int g) {
   typedef Cfg<D, FMT> C;
   const uint32_t tm = __shfl_sync(0xffffffffu, s.tmem, 0);
   constexpr uint32_t qk = idesc_bf16(TM, TM, 0, 0), pv = idesc_bf16(TM, D, 0, 1);
   constexpr int T4 = C::TILE >> 4, H4 = HALF >> 4;  // in units of a descriptor's address
-  const uint64_t q = smem_desc_sw128(sq, 16, 1024) + (w.wide ? g : 0) * T4, k0 = smem_desc_sw128(ring, 16, 1024),
-                 v0 = smem_desc_sw128(ring, HALF, 1024);
+  const uint64_t q = smem_desc_sw128(sq, 16, 1024) + (w.wide ? g : 0) * T4, k0 = smem_desc_sw128(ring.base, 16, 1024),
+                 v0 = smem_desc_sw128(ring.base, HALF, 1024);
   const int A = w.wide ? 1 : 2, first = w.wide ? 0 : g;
   bool ok = warp_wait(bar(a.stall ? s.stall : s.qfull), 0, s, a);
   // Ring position of key tile t and of value tile t: see in_order.
   const int lead = min(A, w.T);
   auto arrived = [&](int pos) {
-    if (ok) ok = warp_wait(bar(s.full[pos % C::STAGES]), (pos / C::STAGES) & 1, s, a);
+    if (ok) ok = warp_wait(bar(s.full[ring.stage(pos)]), ring.turn(pos) & 1, s, a);
     fence_proxy_async();
     tc_fence_after();
   };
@@ -366,19 +428,19 @@ __device__ void multiply(const PrefixArgs& a, const Item& w, uint32_t sq, uint32
   };
   if (first < w.T) {
     arrived(first);
-    if (ok) scores(first % C::STAGES);
+    if (ok) scores(first);
   }
 #pragma unroll 1
   for (int j = first, i = 0; j < w.T && ok; j += A, ++i) {
     const bool more = j + A < w.T;
     const int pv_pos = j < w.T - lead ? lead + 2 * j : w.T + j, pk_pos = pv_pos + 1;
     arrived(pv_pos);
-    if (more) arrived(pk_pos);
+    if (more && w.wide) arrived(pk_pos);
     if (ok) ok = warp_wait(bar(s.pready[g]), i & 1, s, a);
     if (ok && (g || i > 0)) ok = warp_wait(bar(s.turn[g]), (g ? i : i - 1) & 1, s, a);
     tc_fence_after();
     if (!ok) break;
-    const int sv = pv_pos % C::STAGES;
+    const int sv = ring.stage(pv_pos);
     if (elect()) {
       const uint64_t v = v0 + sv * T4;
 #pragma unroll
@@ -388,7 +450,11 @@ __device__ void multiply(const PrefixArgs& a, const Item& w, uint32_t sq, uint32
       if (!more) mma_commit(bar(s.odone[g]));
     }
     __syncwarp();
-    if (more) scores(pk_pos % C::STAGES);
+    // With one row tile the products are short and the rows' arrival is what
+    // bounds the loop: the value tile's stage goes back before the wait for the
+    // next key tile.
+    if (more && !w.wide) arrived(pk_pos);
+    if (more && ok) scores(ring.stage(pk_pos));
     if (elect()) mbar_arrive(bar(s.turn[g ^ 1]));
     __syncwarp();
   }
@@ -577,21 +643,27 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   typedef Cfg<D, FMT> C;
   extern __shared__ uint8_t raw_smem[];
   uint8_t* sm = raw_smem + ((1024u - (smem_u32(raw_smem) & 1023u)) & 1023u);
-  uint8_t* ring = sm + 2 * C::TILE;
-  uint8_t* raw = ring + C::STAGES * C::TILE;
+  uint8_t* raw = sm + (2 + C::STAGES) * C::TILE;
   Bars& s = *reinterpret_cast<Bars*>(raw + C::RAW);
   const int tid = threadIdx.x, warp = tid >> 5;
   constexpr int MMA_WARP = 8 + C::NPT / 32;
   grid_dep_wait();
   const Item w = item_of(a);
+  uint8_t* stages = sm + (w.wide ? 2 : 1) * C::TILE;
+  const int ns = C::STAGES + (w.wide ? 0 : 1);
+  const Ring ring = {smem_u32(stages), ns, 0xffffffffu / ns + 1};
   if (warp == MMA_WARP) {
     tmem_alloc(smem_u32(&s.tmem), 512);
     tmem_relinquish();
   }
   if (tid == 0) {
-    for (int i = 0; i < C::STAGES; ++i) {
-      mbar_init(bar(s.full[i]), C::NPT);
+    for (int i = 0; i < ns; ++i) {
+      mbar_init(bar(s.full[i]), C::CODES && !w.own ? C::NPT / 64 : C::NPT);
       mbar_init(bar(s.empty[i]), w.wide ? 2 : 1);  // a commit of every MMA warp that reads the stage
+    }
+    for (int i = 0; i < C::DEPTH && C::CODES; ++i) {
+      mbar_init(bar(s.raw_full[i]), D == 128 ? 64 : 128);
+      mbar_init(bar(s.raw_empty[i]), C::NPT / 64);
     }
     mbar_init(bar(s.qfull), C::NPT);
     for (int g = 0; g < 2; ++g) {
@@ -614,13 +686,14 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   // the SM; 2 x 128 + 2 x 80 + 64 = 5 x 96.
   if (warp < 8) {
     if (C::CODES) asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
-    soften<D, FMT>(a, w, ring, s, warp >> 2, tid & 127);
+    soften<D, FMT>(a, w, stages, s, warp >> 2, tid & 127);
   } else if (warp < MMA_WARP) {
     if (C::CODES) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    produce<D, FMT>(a, w, smem_u32(sm), smem_u32(ring), smem_u32(raw), s, tid - 256);
+    produce<D, FMT>(a, w, smem_u32(sm), ring, smem_u32(raw), s, tid - 256);
   } else {
     if (C::CODES) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    if (warp < MMA_WARP + 2) multiply<D, FMT>(a, w, smem_u32(sm), smem_u32(ring), s, warp - MMA_WARP);
+    if (warp < MMA_WARP + 2) multiply<D, FMT>(a, w, smem_u32(sm), ring, s, warp - MMA_WARP);
+    else if (!w.own) load_codes<D, FMT>(a, w, smem_u32(raw), s, warp - MMA_WARP - 2, tid & 31);
   }
   tc_fence_before();
   __syncthreads();
