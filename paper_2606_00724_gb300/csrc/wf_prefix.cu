@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(NTH, 2) simt_kernel(const __grid_constant__ Pr
     const int r = e / (D / 4), c = e % (D / 4);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (r < nr) {
-      const RowAt w = own ? own_row(a, u, r0 + r) : prompt_row(a, u, r0 + r);
+      const RowAt w = own ? own_row(a, u / a.H, u % a.H, r0 + r) : prompt_row(a, u / a.H, u % a.H, r0 + r);
       v = row4(static_cast<const T*>(a.Q) + w.b * a.qsb + w.hq * a.qsh + w.i * a.qss, c);
     }
     *reinterpret_cast<float4*>(sq + r * PITCH + 4 * c) = v;
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(NTH, 2) simt_kernel(const __grid_constant__ Pr
     for (int w = 1; w < 16; w *= 2) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
     const int r = ty * RT + i;
     if (r >= nr) continue;
-    const RowAt w = own ? own_row(a, u, r0 + r) : prompt_row(a, u, r0 + r);
+    const RowAt w = own ? own_row(a, u / a.H, u % a.H, r0 + r) : prompt_row(a, u / a.H, u % a.H, r0 + r);
     if (a.whole) {
       const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
       T* op = static_cast<T*>(a.O) + w.b * a.osb + w.hq * a.osh + w.i * a.oss;
@@ -308,6 +308,11 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   p.fold = tc && n_g > 0 && n_g <= kPrefixFold;
   a.So = p.fold ? 0 : split((int64_t)a.B * a.H * a.mto, n_g);
   p.parts = a.S + a.So;
+  a.by_H = make_fastdiv(a.H);
+  a.by_S = make_fastdiv(std::max(1, a.S));
+  a.by_So = make_fastdiv(std::max(1, a.So));
+  a.by_mt = make_fastdiv(a.mt);
+  a.by_mto = make_fastdiv(a.mto);
   a.whole = p.parts == 1 && !p.fold;
   p.off_ml = 256;
   const int kept = a.whole ? 0 : p.parts;

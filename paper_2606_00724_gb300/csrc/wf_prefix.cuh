@@ -31,7 +31,7 @@ struct PrefixArgs {
   int B, P, H, G, q, d, n, k, ng;
   int each;       // sequences a prompt
   int R, Ro;      // query rows of a prompt unit, of an own unit
-  FastDiv by_q, by_Ro;
+  FastDiv by_q, by_Ro, by_H, by_S, by_So, by_mt, by_mto;
   int S, So;      // parts of the prompt, of the own rows
   int mt, mto;    // row tiles of a prompt unit, of an own unit
   int ob;         // query rows a CTA where the own rows are folded in
@@ -63,17 +63,18 @@ cudaError_t launch_prefix(const PrefixPlan& p, cudaStream_t s);
 cudaError_t launch_prefix_own(const PrefixPlan& p, cudaStream_t s);  // own rows and the joining of parts, bf16
 cudaError_t launch_prefix_tc(const PrefixPlan& p, cudaStream_t s);  // the parts (or O) of bf16 queries
 
-// Sequence, query head and block row of row r of unit u.
+// Sequence, query head and block row of row r of the unit of prompt p (or of
+// sequence b) and key head h.
 struct RowAt {
   int b, hq, i;
 };
-__device__ __forceinline__ RowAt prompt_row(const PrefixArgs& a, int u, int r) {
+__device__ __forceinline__ RowAt prompt_row(const PrefixArgs& a, int p, int h, int r) {
   const int s = fastdiv(r, a.by_Ro), w = r - s * a.Ro, g = fastdiv(w, a.by_q);
-  return {(u / a.H) * a.each + s, (u % a.H) * a.G + g, w - g * a.q};
+  return {p * a.each + s, h * a.G + g, w - g * a.q};
 }
-__device__ __forceinline__ RowAt own_row(const PrefixArgs& a, int u, int r) {
+__device__ __forceinline__ RowAt own_row(const PrefixArgs& a, int b, int h, int r) {
   const int g = fastdiv(r, a.by_q);
-  return {u / a.H, (u % a.H) * a.G + g, r - g * a.q};
+  return {b, h * a.G + g, r - g * a.q};
 }
 __device__ __forceinline__ int64_t flat_row(const PrefixArgs& a, const RowAt& r) {
   return ((int64_t)r.b * (a.H * a.G) + r.hq) * a.q + r.i;

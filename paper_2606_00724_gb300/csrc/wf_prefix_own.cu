@@ -23,6 +23,9 @@ using namespace sm100;
 constexpr int NTH = 128;
 constexpr int KT = 64;  // keys a tile
 
+__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void ldsm4(uint32_t* r, uint32_t a) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
@@ -48,13 +51,13 @@ __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b
 template <int D>
 __device__ __forceinline__ uint32_t at(int r, int ch) { return (uint32_t)(r * (2 * D) + ((ch ^ (r & 7)) << 4)); }
 
-// Query rows, then two stages of a K and a V tile; the warps' O and the parts'
-// weights take the stages' place.
+// Query rows; one or two stages of a K and a V tile, whose place the warps' O
+// take; the parts' m and l, then their weights.
 template <int D, int WR>
-size_t own_smem(int rows, int S) {
-  const size_t q = 16 * WR * D * 2, stages = 4 * KT * D * 2;
-  const size_t o = (4 / WR) * 16 * WR * (D + 4) * sizeof(float) + (size_t)rows * (S + 4 / WR) * sizeof(float2);
-  return q + (stages > o ? stages : o);
+size_t own_smem(int rows, int S, int ng) {
+  const size_t q = 16 * WR * D * 2, stages = (ng > KT ? 4 : 2) * KT * D * 2;
+  const size_t o = (4 / WR) * 16 * WR * (D + 4) * sizeof(float);
+  return q + (stages > o ? stages : o) + (size_t)rows * (S + 4 / WR) * sizeof(float2);
 }
 
 // WR warps along the rows, 4 / WR along the keys.
@@ -65,12 +68,20 @@ __global__ void __launch_bounds__(NTH) own_join_kernel(const __grid_constant__ P
   uint8_t* sq = smem;
   uint8_t* st = smem + RB * D * 2;
   float* so = reinterpret_cast<float*>(st);                      // [WK][RB][PO]
-  float2* sml = reinterpret_cast<float2*>(so + WK * RB * PO);    // [a.ob][WK + S]: m and l, then the weight
+  const size_t room = max((size_t)(a.ng > KT ? 4 : 2) * TILE, WK * RB * PO * sizeof(float));
+  float2* sml = reinterpret_cast<float2*>(st + room);            // [a.ob][WK + S]: m and l, then the weight
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rw = warp % WR, kw = warp / WR;
   const int nb = (a.Ro + a.ob - 1) / a.ob, u = blockIdx.x / nb, r0 = (blockIdx.x % nb) * a.ob, nr = min(a.ob, a.Ro - r0);
   const int b = u / a.H, h = u % a.H;
+  const int NP = WK + a.S;
   grid_dep_wait();
   const int nk = own_count(a, b);
+  // The parts' m and l and the query rows are on their way first: neither waits
+  // for the length.
+  for (int e = tid; e < nr * a.S; e += NTH) {
+    const int r = e / a.S, j = e - r * a.S;
+    cp_async8(smem_u32(sml + r * NP + WK + j), a.part_ml + j * a.rows + flat_row(a, own_row(a, b, h, r0 + r)));
+  }
   const bf16* K = static_cast<const bf16*>(a.Kg) + b * a.gsb + h * a.gsh;
   const bf16* V = static_cast<const bf16*>(a.Vg) + b * a.gsb + h * a.gsh;
 
@@ -87,10 +98,10 @@ __global__ void __launch_bounds__(NTH) own_join_kernel(const __grid_constant__ P
     }
     cp_async_commit();
   };
-  if (nk > 0) {
+  if (a.ng > 0) {
     for (int e = tid; e < RB * CH; e += NTH) {
       const int r = e / CH, ch = e % CH;
-      const RowAt w = own_row(a, u, r0 + min(r, nr - 1));
+      const RowAt w = own_row(a, b, h, r0 + min(r, nr - 1));
       cp_async16_zfill(smem_u32(sq) + at<D>(r, ch),
                        static_cast<const bf16*>(a.Q) + w.b * a.qsb + w.hq * a.qsh + w.i * a.qss + ch * 8, r < nr);
     }
@@ -181,11 +192,6 @@ __global__ void __launch_bounds__(NTH) own_join_kernel(const __grid_constant__ P
     for (int c = 0; c < D / 8; ++c) *reinterpret_cast<float2*>(row + 8 * c) = make_float2(o[c][2 * i], o[c][2 * i + 1]);
     if ((lane & 3) == 0 && r < nr) sml[r * (WK + a.S) + kw] = make_float2(m[i], l[i]);
   }
-  const int NP = WK + a.S;
-  for (int e = tid; e < nr * a.S; e += NTH) {
-    const int r = e / a.S, j = e - r * a.S;
-    sml[r * NP + WK + j] = a.part_ml[j * a.rows + flat_row(a, own_row(a, u, r0 + r))];
-  }
   __syncthreads();
   // Weights 2^(m - M) / sum of 2^(m - M) l of a row's parts, a warp a row; a part
   // without a key (l = 0) has weight 0.
@@ -216,7 +222,7 @@ __global__ void __launch_bounds__(NTH) own_join_kernel(const __grid_constant__ P
     for (int x = 0; x < EB; ++x) {
       const int e = min(e0 + x * NTH, items - 1), c = e % (D / 4);
       r[x] = e / (D / 4);
-      po[x] = a.part_o + flat_row(a, own_row(a, u, r0 + r[x])) * D + 4 * c;
+      po[x] = a.part_o + flat_row(a, own_row(a, b, h, r0 + r[x])) * D + 4 * c;
       y[x] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
     auto add = [&](int x, float f, const float4& v) {
@@ -244,7 +250,7 @@ __global__ void __launch_bounds__(NTH) own_join_kernel(const __grid_constant__ P
 #pragma unroll
       for (int j = 0; j < WK; ++j)
         add(x, sml[r[x] * NP + j].x, *reinterpret_cast<const float4*>(so + (j * RB + r[x]) * PO + 4 * c));
-      const RowAt w = own_row(a, u, r0 + r[x]);
+      const RowAt w = own_row(a, b, h, r0 + r[x]);
       *reinterpret_cast<uint2*>(static_cast<bf16*>(a.O) + w.b * a.osb + w.hq * a.osh + w.i * a.oss + 4 * c) =
           make_uint2(pack_bf16(y[x].x, y[x].y), pack_bf16(y[x].z, y[x].w));
     }
@@ -258,7 +264,7 @@ cudaError_t launch(PrefixArgs a, cudaStream_t s) {
   a.ob = 16 * WR;
   const int64_t units = (int64_t)a.B * a.H;
   while (a.ob > 4 && units * ((a.Ro + a.ob - 1) / a.ob) < 2 * sm_count()) a.ob /= 2;
-  const size_t smem = own_smem<D, WR>(a.ob, a.S);
+  const size_t smem = own_smem<D, WR>(a.ob, a.S, a.ng);
   const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(own_join_kernel<D, WR>), smem);
   if (e != cudaSuccess) return e;
   const int64_t blocks = units * ((a.Ro + a.ob - 1) / a.ob);

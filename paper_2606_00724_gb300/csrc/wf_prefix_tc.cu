@@ -44,6 +44,13 @@ constexpr int HALF = TM * 128;         // 64 channels of a tile of bf16 rows
 constexpr float kLazy = 8.f;
 constexpr int kPCol = TM / 2;            // P's columns among S's
 
+constexpr int kMaxStages = 9;
+struct Bars {
+  unsigned long long full[kMaxStages], empty[kMaxStages], raw_full[4], raw_empty[4], qfull, sfull[2], pready[2], odone[2], turn[2], drain[2], stall;
+  uint32_t tmem, abort;
+  int64_t row[kPrefixTcRows];  // a row's offset in Q while the rows are read, then in the output
+};
+
 template <int D, int FMT>
 struct Cfg {
   static constexpr bool CODES = FMT != WF_BF16;
@@ -62,15 +69,10 @@ struct Cfg {
   __device__ static int place(int x, int r) { return D == 128 ? x ^ (r * ROWB / 128 % 2 * PX) : x; }
   static constexpr int SLOT = TM * ROWB + TM * 4;        // a tile of codes and its scales
   static constexpr int RAW = CODES ? DEPTH * SLOT : 0;
+  static constexpr int ROOM = 232448 - (int)sizeof(Bars) - 2 * TILE - RAW;
   // Stages beside two tiles of query rows; with one tile its place is a stage more.
-  static constexpr int STAGES = (232448 - 2048 - 2 * TILE - RAW) / TILE > 8 ? 8 : (232448 - 2048 - 2 * TILE - RAW) / TILE;
-  static constexpr size_t SMEM = 1024 + 2 * TILE + RAW + (size_t)STAGES * TILE + 512;
-};
-
-constexpr int kMaxStages = 9;
-struct Bars {
-  unsigned long long full[kMaxStages], empty[kMaxStages], raw_full[4], raw_empty[4], qfull, sfull[2], pready[2], odone[2], turn[2], drain[2], stall;
-  uint32_t tmem, abort;
+  static constexpr int STAGES = ROOM / TILE > kMaxStages - 1 ? kMaxStages - 1 : ROOM / TILE;
+  static constexpr size_t SMEM = 2 * TILE + RAW + (size_t)STAGES * TILE + sizeof(Bars);
 };
 
 __device__ __forceinline__ uint32_t bar(const unsigned long long& b) { return smem_u32(&b); }
@@ -117,10 +119,11 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, int byt
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
-// What a CTA works on.
+// What a CTA works on: from the launch alone, and its keys from the lengths.
 struct Item {
   bool own, wide;
-  int u, part, r0, nr;  // unit, part, first row, rows
+  int u, b, h;          // unit: prompt or sequence, key head
+  int part, r0, nr;     // part, first row, rows
   int k0, k1, T;        // keys [k0, k1), tiles
 };
 
@@ -130,19 +133,25 @@ __device__ __forceinline__ Item item_of(const PrefixArgs& a) {
   int it = blockIdx.x;
   w.own = it >= prompts;
   if (w.own) it -= prompts;
-  const int mt = w.own ? a.mto : a.mt, S = w.own ? a.So : a.S;
-  const int tile = it % mt, sp = (it / mt) % S;
-  w.u = it / mt / S;
+  const FastDiv by_mt = w.own ? a.by_mto : a.by_mt, by_S = w.own ? a.by_So : a.by_S;
+  const int x = fastdiv(it, by_mt), tile = it - x * (int)by_mt.d;
+  w.u = fastdiv(x, by_S);
+  const int sp = x - w.u * (int)by_S.d;
+  w.b = fastdiv(w.u, a.by_H);
+  w.h = w.u - w.b * a.H;
   w.part = w.own ? a.S + sp : sp;
   w.r0 = tile * kPrefixTcRows;
   w.nr = min(kPrefixTcRows, (w.own ? a.Ro : a.R) - w.r0);
   w.wide = w.nr > TM;
-  const int count = w.own ? own_count(a, w.u / a.H) : prompt_count(a, w.u / a.H);
+  return w;
+}
+__device__ __forceinline__ void keys_of(const PrefixArgs& a, Item& w) {
+  const int S = w.own ? a.So : a.S, sp = w.own ? w.part - a.S : w.part;
+  const int count = w.own ? own_count(a, w.b) : prompt_count(a, w.b);
   const int tiles = (count + TM - 1) / TM, per = (tiles + S - 1) / S;
   w.k0 = min(count, sp * per * TM);
   w.k1 = min(count, (sp + 1) * per * TM);
   w.T = (w.k1 - w.k0 + TM - 1) / TM;
-  return w;
 }
 
 // The ring of stages: position p of the order below is in stage p % n.
@@ -160,10 +169,12 @@ struct Ring {
 // L + 2 (t - A) + 1, and V_j position L + 2 j (j < T - L) or T + j.
 template <typename F>
 __device__ __forceinline__ void in_order(int T, int A, F f) {
-  for (int t = 0; t < min(A, T); ++t) f(t, false);
-  for (int j = 0; j < T; ++j) {
-    f(j, true);
-    if (j + A < T) f(j + A, false);
+  const int lead = min(A, T), paired = 2 * T - lead;  // positions [lead, paired) are V_j, K_(j+A) in turn
+#pragma unroll 1
+  for (int p = 0; p < 2 * T; ++p) {  // one call, so that f's code is there once
+    const int o = p - lead;
+    const bool v = o >= 0 && (p >= paired || !(o & 1));
+    f(o < 0 ? p : p >= paired ? p - T : o / 2 + ((o & 1) ? A : 0), v);
   }
 }
 
@@ -215,21 +226,33 @@ __device__ __forceinline__ void copy_tile(uint32_t st, const bf16* base, int64_t
   }
 }
 
+__device__ __forceinline__ RowAt row_at(const PrefixArgs& a, const Item& w, int r) {
+  return w.own ? own_row(a, w.b, w.h, w.r0 + r) : prompt_row(a, w.b, w.h, w.r0 + r);
+}
+__device__ __forceinline__ int64_t q_offset(const PrefixArgs& a, const Item& w, int r) {
+  const RowAt at = row_at(a, w, r);
+  return at.b * a.qsb + at.hq * a.qsh + at.i * a.qss;
+}
+
 template <int D, int FMT>
 __device__ void produce(const PrefixArgs& a, const Item& w, uint32_t sq, const Ring& ring, uint32_t raw, Bars& s, int tid) {
   typedef Cfg<D, FMT> C;
   constexpr int CH = D / 8, NPT = C::NPT;
-  // The query rows, K-major; rows past the last are zero.
-  const int rows = w.wide ? 2 * TM : TM;
-  for (int e = tid; e < rows * CH; e += NPT) {
-    const int r = e / CH, ch = e % CH;
+  if (w.T == 0) return;
+  // The query rows, K-major; rows past the last are zero.  Where a row lies takes
+  // two divisions, so each is found once and shared.
+  if (tid < w.nr) s.row[tid] = q_offset(a, w, tid);
+  if (NPT < kPrefixTcRows && tid + NPT < w.nr) s.row[tid + NPT] = q_offset(a, w, tid + NPT);
+  named_sync(2, NPT);
+  const int tiles = w.wide ? 2 : 1;
+  for (int i = 0; i < tiles * TM * CH / NPT; ++i) {
+    const int r = tid / CH + NPT / CH * i, ch = tid % CH;
     const bool ok = r < w.nr;
-    const RowAt at = w.own ? own_row(a, w.u, w.r0 + (ok ? r : 0)) : prompt_row(a, w.u, w.r0 + (ok ? r : 0));
-    const bf16* q = static_cast<const bf16*>(a.Q) + at.b * a.qsb + at.hq * a.qsh + at.i * a.qss + ch * 8;
-    cp_async16_zfill(sq + (r / TM) * C::TILE + swizzled(r % TM, ch), q, ok);
+    cp_async16_zfill(sq + (r / TM) * C::TILE + swizzled(r % TM, ch),
+                     static_cast<const bf16*>(a.Q) + (ok ? s.row[r] : 0) + ch * 8, ok);
   }
   cp_async_arrive_noinc(bar(s.qfull));
-  const int64_t b = w.u / a.H, h = w.u % a.H;
+  const int64_t b = w.b, h = w.h;
   const int A = w.wide ? 1 : 2;
   if (!C::CODES || w.own) {
     const int64_t sb = w.own ? a.gsb : a.ksb, sh = w.own ? a.gsh : a.ksh, ss = w.own ? a.gss : a.kss;
@@ -316,7 +339,7 @@ template <int D, int FMT>
 __device__ void load_codes(const PrefixArgs& a, const Item& w, uint32_t raw, Bars& s, int warp, int lane) {
   typedef Cfg<D, FMT> C;
   constexpr int CR = C::CR, RP = 32 / CR, NI = 64 / RP, SR = D / kMxBlock;  // rows a pass of the warp, passes
-  const int64_t b = w.u / a.H, h = w.u % a.H;
+  const int64_t b = w.b, h = w.h;
   const int x = lane % CR;
   const int32_t* idx = a.idx ? a.idx + (int64_t)w.u * a.k : nullptr;
   const uint8_t* kbase = static_cast<const uint8_t*>(a.K) + b * a.ksb + h * a.ksh + x * 16;
@@ -401,6 +424,7 @@ __device__ __forceinline__ bool elect() {
 template <int D, int FMT>
 __device__ void multiply(const PrefixArgs& a, const Item& w, uint32_t sq, const Ring& ring, Bars& s, int g) {
   typedef Cfg<D, FMT> C;
+  if (w.T == 0) return;
   const uint32_t tm = __shfl_sync(0xffffffffu, s.tmem, 0);
   constexpr uint32_t qk = idesc_bf16(TM, TM, 0, 0), pv = idesc_bf16(TM, D, 0, 1);
   constexpr int T4 = C::TILE >> 4, H4 = HALF >> 4;  // in units of a descriptor's address
@@ -550,7 +574,7 @@ __device__ __forceinline__ void soften_tile(const PrefixArgs& a, uint32_t sc, ui
 }
 
 template <int D, int FMT>
-__device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* ring, Bars& s, int g, int r) {
+__device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* stages, Bars& s, int g, int r) {
   typedef Cfg<D, FMT> C;
   const uint32_t lanes = (uint32_t)(r & ~31) << 16;  // the warp's quarter of the TMEM lanes
   const uint32_t tm = s.tmem, sc = tm + TM * g + lanes, oc = tm + 2 * TM + D * g + lanes;
@@ -574,81 +598,86 @@ __device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* ring, Bars& 
       if ((r & 31) == 0) mbar_arrive(bar(s.pready[g]));
     }
   }
-  // The last products: of both warpgroups, whose stages are the exchange below.
-  if (ok && w.T > 0 && (w.wide || w.T > 1 || g == 0)) ok = warp_wait(bar(s.odone[g]), 0, s, a);
-  if (ok && !w.wide && (g == 0 ? w.T > 1 : w.T > 0)) ok = warp_wait(bar(s.odone[g ^ 1]), 0, s, a);
-  tc_fence_after();
-  const bool have = w.T > first;  // this warpgroup had a tile
   const int row = rt + r;
-  float* ex = reinterpret_cast<float*>(ring);  // [128][D + 4]: O of the second warpgroup, m and l
-  if (!w.wide && w.T > 1) {
-    if (g == 1 && active) {
+  // The offsets in Q are not read any more: this warpgroup has seen an S, or no
+  // row of Q is (an empty range).
+  if (ok && row < w.nr && (w.wide || g == 0)) {
+    const RowAt at = row_at(a, w, row);
+    s.row[row] = a.whole ? at.b * a.osb + at.hq * a.osh + at.i * a.oss : (int64_t)w.part * a.rows + flat_row(a, at);
+  }
+  // The last products of both warpgroups: the exchange below is in their stages.
+  if (ok && w.T > 0) ok = warp_wait(bar(s.odone[0]), 0, s, a);
+  if (ok && w.T > step - 1) ok = warp_wait(bar(s.odone[1]), 0, s, a);
+  tc_fence_after();
+  // The rows go out through the stages, which nothing reads any more, 64 channels
+  // at a time: a thread has a row, a store to memory wants a row's 256 bytes
+  // from consecutive lanes (32 rows' 16 bytes a store took 5 us a CTA).  Two
+  // warpgroups on one row tile scale their O to the larger maximum and the
+  // sum is formed on the way out.
+  const bool have = w.T > first;  // this warpgroup had a tile
+  float* buf = reinterpret_cast<float*>(stages);                        // [2][128][64], 16-byte chunks swizzled
+  float2* ml = reinterpret_cast<float2*>(stages + 2 * TM * 64 * 4);  // [2][128]
+  float f = have ? 1.f : 0.f;
+  if (!w.wide) {
+    ml[g * TM + r] = make_float2(m, l);
+    named_sync(1, 256);
+    const float2 y = ml[(g ^ 1) * TM + r];
+    const float M = fmaxf(m, y.x);
+    f *= ex2(m - M);
+    l = g ? y.y * ex2(y.x - M) + l * ex2(m - M) : l * ex2(m - M) + y.y * ex2(y.x - M);  // in one order for both
+    m = M;
+  }
+  if (a.whole) f = l == 0.f ? 0.f : f / l;
+  const bool none = !have || l == 0.f;
+  const bool gone = abort_set(smem_u32(&s.abort));
+  const int lane = r & 31, warp = g * 4 + (r >> 5), cc = lane & 15;
 #pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
-        float o[32];
-        tmem_ld32(oc + 32 * c, o);
+  for (int ch = 0; ch < D / 64; ++ch) {
+    if (active) {
+      float* row = buf + (g * TM + r) * 64;
 #pragma unroll
-        for (int e = 0; e < 32; e += 4)
-          *reinterpret_cast<float4*>(ex + r * (D + 4) + 32 * c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+      for (int c = 0; c < 4; ++c) {
+        uint32_t o[16];
+        if (have) {
+          get(oc + 64 * ch + 16 * c, o);
+          got(o);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[e] = none ? 0u : __float_as_uint(__uint_as_float(o[e]) * f);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<uint4*>(row + (((4 * c + e) ^ (r & 7)) << 2)) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
       }
-      ex[r * (D + 4) + D] = m;
-      ex[r * (D + 4) + D + 1] = l;
     }
     named_sync(1, 256);
-  }
-  if (!w.wide && g == 1) return;
-  if (!active || abort_set(smem_u32(&s.abort))) return;
-  float f0 = 1.f, f1 = 0.f;
-  if (!w.wide && w.T > 1) {
-    const float m1 = ex[r * (D + 4) + D], l1 = ex[r * (D + 4) + D + 1];
-    const float M = fmaxf(m, m1);
-    f0 = ex2(m - M);
-    f1 = ex2(m1 - M);
-    m = M;
-    l = l * f0 + l1 * f1;
-  }
-  const RowAt at = row < w.nr ? (w.own ? own_row(a, w.u, w.r0 + row) : prompt_row(a, w.u, w.r0 + row)) : RowAt{0, 0, 0};
-  const bool whole = a.whole;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int64_t flat = (int64_t)w.part * a.rows + flat_row(a, at);
-  bf16* op = static_cast<bf16*>(a.O) + at.b * a.osb + at.hq * a.osh + at.i * a.oss;
-#pragma unroll 1
-  for (int c = 0; c < D / 32; ++c) {
-    float o[32];
-    if (have) tmem_ld32(oc + 32 * c, o);
-#pragma unroll
-    for (int e = 0; e < 32; ++e) {
-      if (!have || l == 0.f) o[e] = 0.f;
-      else if (!w.wide && w.T > 1) o[e] = o[e] * f0 + f1 * ex[r * (D + 4) + 32 * c + e];
-    }
-    if (row >= w.nr) continue;
-    if (whole) {
-#pragma unroll
-      for (int e = 0; e < 32; e += 8) {
-        float y[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) y[k] = o[e + k] * inv;
-        st_vec(op + 32 * c + e, y);
+#pragma unroll 4
+    for (int q = 2 * warp + (lane >> 4); q < w.nr && !gone; q += 16) {
+      const float* row = buf + q * 64 + ((cc ^ (q & 7)) << 2);
+      float4 y = *reinterpret_cast<const float4*>(row);
+      if (!w.wide) {
+        const float4 z = *reinterpret_cast<const float4*>(row + TM * 64);
+        y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
       }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 32; e += 4) st_vec(a.part_o + flat * D + 32 * c + e, o + e);
+      if (a.whole)
+        *reinterpret_cast<uint2*>(static_cast<bf16*>(a.O) + s.row[q] + 64 * ch + 4 * cc) =
+            make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+      else
+        *reinterpret_cast<float4*>(a.part_o + s.row[q] * D + 64 * ch + 4 * cc) = y;
     }
+    if (ch + 1 < D / 64) named_sync(1, 256);
   }
-  if (!whole && row < w.nr) a.part_ml[flat] = make_float2(m, l);
+  if (!a.whole && !gone && row < w.nr && (w.wide || g == 0)) a.part_ml[s.row[row]] = make_float2(m, l);
 }
 
 template <int D, int FMT>
 __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_constant__ PrefixArgs a) {
   typedef Cfg<D, FMT> C;
-  extern __shared__ uint8_t raw_smem[];
-  uint8_t* sm = raw_smem + ((1024u - (smem_u32(raw_smem) & 1023u)) & 1023u);
+  extern __shared__ __align__(1024) uint8_t sm[];
   uint8_t* raw = sm + (2 + C::STAGES) * C::TILE;
   Bars& s = *reinterpret_cast<Bars*>(raw + C::RAW);
   const int tid = threadIdx.x, warp = tid >> 5;
   constexpr int MMA_WARP = 8 + C::NPT / 32;
-  grid_dep_wait();
-  const Item w = item_of(a);
+  Item w = item_of(a);
   uint8_t* stages = sm + (w.wide ? 2 : 1) * C::TILE;
   const int ns = C::STAGES + (w.wide ? 0 : 1);
   const Ring ring = {smem_u32(stages), ns, 0xffffffffu / ns + 1};
@@ -678,6 +707,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
     s.abort = 0;
     fence_mbar_init();
   }
+  grid_dep_wait();
+  keys_of(a, w);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
