@@ -279,7 +279,9 @@ __device__ void produce(const PrefixArgs& a, const Item& w, uint32_t sq, const R
     constexpr bool FP4 = FMT == WF_MXFP4;
     constexpr int CR = C::CR, PX = C::PX, NG = NPT / 2, CPT = TM * CR / NG, RS = NG / CR;
     constexpr int EL = FP4 ? 32 : 16, OUT = EL / 8;  // channels a chunk, bf16 chunks they make
-    static_assert(RS % 8 == 0, "a thread's rows share their swizzle and place");
+    constexpr int U = CPT < 4 ? CPT : 4;
+    static_assert(RS % 8 == 0 && CPT % U == 0, "a thread's rows share their swizzle and place");
+    bool given_up = false;
     const int group = tid / NG, gt = tid % NG;
     const int x = gt % PX + PX * (gt / 8 % (CR / PX)), rr = gt / PX % (8 / PX) + 8 / PX * (gt / (8 * CR / PX));
     const uint32_t chunk = (uint32_t)(rr * CR + C::place(x, rr)) * 16;
@@ -288,40 +290,46 @@ __device__ void produce(const PrefixArgs& a, const Item& w, uint32_t sq, const R
     for (int p = group; p < 2 * w.T; p += 2) {
       const int slot = p % C::DEPTH, st = ring.stage(p), n = ring.turn(p);
       if (!warp_wait(bar(s.raw_full[slot]), p / C::DEPTH & 1, s, a)) break;
-      // The tile's codes go to registers and the slot back to the loaders at once,
-      // so that a copy's latency covers one tile's widening and not two.
+      // U chunks at a time: fewer instructions to fetch on a CTA's first tile.  The
+      // slot goes back to the loaders with the last chunk's load, so that a copy's
+      // latency covers one tile's widening and not two.
       const uint32_t src = raw + slot * C::SLOT, dst = ring.base + st * C::TILE;
-      uint4 code[CPT];
-      uint32_t byte[CPT];
-      bool large = false;  // a scale that takes a second factor
+#pragma unroll 1
+      for (int i0 = 0; i0 < CPT; i0 += U) {
+        uint4 code[U];
+        uint32_t byte[U];
+        bool large = false;  // a scale that takes a second factor
 #pragma unroll
-      for (int i = 0; i < CPT; ++i) {
-        code[i] = lds_v4(src + chunk + NG * 16 * i);
-        byte[i] = lds_u8(src + scale + RS * 4 * i);
-      }
-#pragma unroll
-      for (int i = 0; i < CPT; ++i) large |= byte[i] > kMxOne<FP4>;
-      large = __any_sync(0xffffffffu, large);
-      if ((gt & 31) == 0) mbar_arrive(bar(s.raw_empty[slot]));
-      if (n > 0 && !warp_wait(bar(s.empty[st]), (n - 1) & 1, s, a)) break;
-#pragma unroll
-      for (int i = 0; i < CPT; ++i) {
-        const uint32_t cw[4] = {code[i].x, code[i].y, code[i].z, code[i].w};
-        const uint32_t f = mx_factor<FP4>(byte[i]);
-        uint32_t y[OUT * 4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) mx_pairs<FP4>(cw[e], y + e * OUT);
-#pragma unroll
-        for (int e = 0; e < OUT * 4; ++e) y[e] = mul_bf16x2(y[e], f);
-        if (large) {
-          const uint32_t f2 = mx_second_factor<FP4>(byte[i]);
-#pragma unroll
-          for (int e = 0; e < OUT * 4; ++e) y[e] = mul_bf16x2(y[e], f2);
+        for (int i = 0; i < U; ++i) {
+          code[i] = lds_v4(src + chunk + NG * 16 * (i0 + i));
+          byte[i] = lds_u8(src + scale + RS * 4 * (i0 + i));
         }
 #pragma unroll
-        for (int o = 0; o < OUT; ++o)
-          sts_v4(dst + swizzled(rr + RS * i, x * OUT + o), make_uint4(y[4 * o], y[4 * o + 1], y[4 * o + 2], y[4 * o + 3]));
+        for (int i = 0; i < U; ++i) large |= byte[i] > kMxOne<FP4>;
+        large = __any_sync(0xffffffffu, large);
+        if (i0 + U == CPT && (gt & 31) == 0) mbar_arrive(bar(s.raw_empty[slot]));
+        if (i0 == 0 && n > 0 && !warp_wait(bar(s.empty[st]), (n - 1) & 1, s, a)) { given_up = true; break; }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const uint32_t cw[4] = {code[i].x, code[i].y, code[i].z, code[i].w};
+          const uint32_t f = mx_factor<FP4>(byte[i]);
+          uint32_t y[OUT * 4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx_pairs<FP4>(cw[e], y + e * OUT);
+#pragma unroll
+          for (int e = 0; e < OUT * 4; ++e) y[e] = mul_bf16x2(y[e], f);
+          if (large) {
+            const uint32_t f2 = mx_second_factor<FP4>(byte[i]);
+#pragma unroll
+            for (int e = 0; e < OUT * 4; ++e) y[e] = mul_bf16x2(y[e], f2);
+          }
+#pragma unroll
+          for (int o = 0; o < OUT; ++o)
+            sts_v4(dst + swizzled(rr, x * OUT + o) + RS * 128 * (i0 + i),
+                   make_uint4(y[4 * o], y[4 * o + 1], y[4 * o + 2], y[4 * o + 3]));
+        }
       }
+      if (given_up) break;
       fence_proxy_async();
       __syncwarp();
       if ((gt & 31) == 0) mbar_arrive(bar(s.full[st]));
@@ -512,8 +520,8 @@ __device__ __forceinline__ void got(uint32_t* v) {
 // P of one tile from S: one pass over chunks of CW columns, the next chunk on its
 // way while one is worked on, with the maximum of the tiles before as m.  P
 // stays in registers until the tile's own maximum is known; where that is more
-// than 2^kLazy above m (the first tile, seldom later) m is raised, O and l are
-// rescaled and the pass runs again, S being still there.  P goes to the upper
+// than 2^kLazy above m (seldom) m is raised, O and l are rescaled and the pass
+// runs again, S being still there.  P goes to the upper
 // half of S's columns.
 constexpr int CW = 16;
 template <int D, bool MASK>
@@ -523,6 +531,18 @@ __device__ __forceinline__ void soften_tile(const PrefixArgs& a, uint32_t sc, ui
   const f32x2 sl = pk2(a.sl2, a.sl2);
   uint32_t p[TM / 2];
   f32x2 sum[2];
+  if (!have_o) {  // the first tile: its maximum first, in a short pass
+    float top = -INFINITY;
+#pragma unroll 1
+    for (int c = 0; c < NC; ++c) {
+      uint32_t x[CW];
+      get(sc + CW * c, x);
+      got(x);
+#pragma unroll
+      for (int e = 0; e < CW; ++e) top = fmaxf(top, !MASK || CW * c + e < nk ? __uint_as_float(x[e]) : -INFINITY);
+    }
+    m = fmaxf(m, top * a.sl2);
+  }
 #pragma unroll 1
   for (;;) {
     const f32x2 nm = pk2(-m, -m);
@@ -685,44 +705,41 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
     tmem_alloc(smem_u32(&s.tmem), 512);
     tmem_relinquish();
   }
-  if (tid == 0) {
-    for (int i = 0; i < ns; ++i) {
-      mbar_init(bar(s.full[i]), C::CODES && !w.own ? C::NPT / 64 : C::NPT);
-      mbar_init(bar(s.empty[i]), w.wide ? 2 : 1);  // a commit of every MMA warp that reads the stage
-    }
-    for (int i = 0; i < C::DEPTH && C::CODES; ++i) {
-      mbar_init(bar(s.raw_full[i]), D == 128 ? 64 : 128);
-      mbar_init(bar(s.raw_empty[i]), C::NPT / 64);
-    }
+  // A barrier a thread: one after the other they took 0.4 us.
+  if (tid < 2 * kMaxStages) {
+    const int arrivals = C::CODES && !w.own ? C::NPT / 64 : C::NPT;
+    // A stage is free with a commit of every MMA warp that reads it.
+    mbar_init(bar(tid < kMaxStages ? s.full[tid] : s.empty[tid - kMaxStages]), tid < kMaxStages ? arrivals : w.wide ? 2 : 1);
+  } else if (tid >= 32 && tid < 40) {
+    const int i = tid & 3;
+    mbar_init(bar(tid < 36 ? s.raw_full[i] : s.raw_empty[i]), tid < 36 ? (D == 128 ? 64 : 128) : C::NPT / 64);
+  } else if (tid >= 64 && tid < 66) {
+    const int g = tid - 64, rows = w.wide ? w.nr - g * TM : w.nr;
+    mbar_init(bar(s.sfull[g]), 1);
+    mbar_init(bar(s.pready[g]), (min(rows, TM) + 31) / 32);
+    mbar_init(bar(s.odone[g]), 1);
+  } else if (tid >= 96 && tid < 98) {
+    mbar_init(bar(s.turn[tid - 96]), 1);
+    mbar_init(bar(s.drain[tid - 96]), 1);
+  } else if (tid == 128) {
     mbar_init(bar(s.qfull), C::NPT);
-    for (int g = 0; g < 2; ++g) {
-      const int rows = w.wide ? w.nr - g * TM : w.nr;
-      mbar_init(bar(s.sfull[g]), 1);
-      mbar_init(bar(s.pready[g]), (min(rows, TM) + 31) / 32);
-      mbar_init(bar(s.odone[g]), 1);
-      mbar_init(bar(s.drain[g]), 1);
-      mbar_init(bar(s.turn[g]), 1);
-    }
     mbar_init(bar(s.stall), 1);
     s.abort = 0;
-    fence_mbar_init();
   }
+  fence_mbar_init();
   grid_dep_wait();
   keys_of(a, w);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   grid_dep_launch();  // after the barrier that publishes the tensor memory (see Launch)
-  // Registers of the 20 warps with codes: 96 each at launch, 5 warps a quarter of
-  // the SM; 2 x 128 + 2 x 80 + 64 = 5 x 96.
+  // (Moving registers from the producers to the softmax warps was slower with
+  // codes: 93 against 90 us for a token at 128K.)
   if (warp < 8) {
-    if (C::CODES) asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
     soften<D, FMT>(a, w, stages, s, warp >> 2, tid & 127);
   } else if (warp < MMA_WARP) {
-    if (C::CODES) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     produce<D, FMT>(a, w, smem_u32(sm), ring, smem_u32(raw), s, tid - 256);
   } else {
-    if (C::CODES) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp < MMA_WARP + 2) multiply<D, FMT>(a, w, smem_u32(sm), ring, s, warp - MMA_WARP);
     else if (!w.own) load_codes<D, FMT>(a, w, smem_u32(raw), s, warp - MMA_WARP - 2, tid & 31);
   }
