@@ -12,6 +12,8 @@
 // weights 2^(m - M), and O is written here.
 #include <float.h>
 
+#include <type_traits>
+
 #include "wf_prefix.cuh"
 #include "wf_sm100.cuh"
 
@@ -62,7 +64,7 @@ size_t own_smem(int rows, int S, int ng) {
 
 // WR warps along the rows, 4 / WR along the keys.
 template <int D, int WR>
-__global__ void __launch_bounds__(NTH) own_join_kernel(const __grid_constant__ PrefixArgs a) {
+__global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __grid_constant__ PrefixArgs a) {
   constexpr int WK = 4 / WR, RB = 16 * WR, CH = D / 8, KW = KT / WK, TILE = KT * D * 2, PO = D + 4;
   extern __shared__ __align__(128) uint8_t smem[];
   uint8_t* sq = smem;
@@ -74,14 +76,22 @@ __global__ void __launch_bounds__(NTH) own_join_kernel(const __grid_constant__ P
   const int nb = (a.Ro + a.ob - 1) / a.ob, u = blockIdx.x / nb, r0 = (blockIdx.x % nb) * a.ob, nr = min(a.ob, a.Ro - r0);
   const int b = u / a.H, h = u % a.H;
   const int NP = WK + a.S;
+  // Where the block's rows lie, found once.
+  __shared__ int64_t row_q[RB], row_o[RB], row_flat[RB];
+  if (tid < nr) {
+    const RowAt w = own_row(a, b, h, r0 + tid);
+    row_q[tid] = w.b * a.qsb + w.hq * a.qsh + w.i * a.qss;
+    row_o[tid] = w.b * a.osb + w.hq * a.osh + w.i * a.oss;
+    row_flat[tid] = flat_row(a, w);
+  }
   grid_dep_wait();
   const int nk = own_count(a, b);
+  __syncthreads();
   // The parts' m and l and the query rows are on their way first: neither waits
   // for the length.
-  for (int e = tid; e < nr * a.S; e += NTH) {
-    const int r = e / a.S, j = e - r * a.S;
-    cp_async8(smem_u32(sml + r * NP + WK + j), a.part_ml + j * a.rows + flat_row(a, own_row(a, b, h, r0 + r)));
-  }
+  for (int r = warp; r < nr; r += 4)
+    for (int j = lane; j < a.S; j += 32)
+      cp_async8(smem_u32(sml + r * NP + WK + j), a.part_ml + j * a.rows + row_flat[r]);
   const bf16* K = static_cast<const bf16*>(a.Kg) + b * a.gsb + h * a.gsh;
   const bf16* V = static_cast<const bf16*>(a.Vg) + b * a.gsb + h * a.gsh;
 
@@ -101,9 +111,8 @@ __global__ void __launch_bounds__(NTH) own_join_kernel(const __grid_constant__ P
   if (a.ng > 0) {
     for (int e = tid; e < RB * CH; e += NTH) {
       const int r = e / CH, ch = e % CH;
-      const RowAt w = own_row(a, b, h, r0 + min(r, nr - 1));
-      cp_async16_zfill(smem_u32(sq) + at<D>(r, ch),
-                       static_cast<const bf16*>(a.Q) + w.b * a.qsb + w.hq * a.qsh + w.i * a.qss + ch * 8, r < nr);
+      cp_async16_zfill(smem_u32(sq) + at<D>(r, ch), static_cast<const bf16*>(a.Q) + row_q[min(r, nr - 1)] + ch * 8,
+                       r < nr);
     }
   }
   fetch(0);
@@ -193,68 +202,70 @@ __global__ void __launch_bounds__(NTH) own_join_kernel(const __grid_constant__ P
     if ((lane & 3) == 0 && r < nr) sml[r * (WK + a.S) + kw] = make_float2(m[i], l[i]);
   }
   __syncthreads();
-  // Weights 2^(m - M) / sum of 2^(m - M) l of a row's parts, a warp a row; a part
+  // Weights 2^(m - M) / sum of 2^(m - M) l of a row's parts, 4 lanes a row; a part
   // without a key (l = 0) has weight 0.
-  for (int r = warp; r < nr; r += 4) {
-    float2* ml = sml + r * NP;
+  for (int r = tid >> 2; r < RB; r += NTH / 4) {
+    float2* ml = sml + min(r, nr - 1) * NP;
+    const int c = tid & 3;
     float M = -FLT_MAX, L = 0.f;
-    for (int j = lane; j < NP; j += 32)
-      if (ml[j].y != 0.f) M = fmaxf(M, ml[j].x);
-#pragma unroll
-    for (int x = 1; x < 32; x *= 2) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, x));
-    for (int j = lane; j < NP; j += 32)
-      if (ml[j].y != 0.f) L += ex2(ml[j].x - M) * ml[j].y;
-#pragma unroll
-    for (int x = 1; x < 32; x *= 2) L += __shfl_xor_sync(0xffffffffu, L, x);
+    for (int j = c; j < NP; j += 4) M = fmaxf(M, ml[j].y != 0.f ? ml[j].x : -FLT_MAX);
+    M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, 1));
+    M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, 2));
+    for (int j = c; j < NP; j += 4) L += ml[j].y != 0.f ? ex2(ml[j].x - M) * ml[j].y : 0.f;
+    L += __shfl_xor_sync(0xffffffffu, L, 1);
+    L += __shfl_xor_sync(0xffffffffu, L, 2);
     const float inv = L == 0.f ? 0.f : 1.f / L;
-    for (int j = lane; j < NP; j += 32) ml[j].x = ml[j].y == 0.f ? 0.f : ex2(ml[j].x - M) * inv;
+    if (r < nr)
+      for (int j = c; j < NP; j += 4) ml[j].x = ml[j].y != 0.f ? ex2(ml[j].x - M) * inv : 0.f;
   }
   __syncthreads();
-  // O: EB groups of 4 channels a thread, so that the loads of several parts and
-  // groups are in flight together.
-  constexpr int EB = 4;
+  // O, a group of 4 channels a thread or 4 of them, with 16 loads of parts in
+  // flight either way.
   const int items = nr * (D / 4);
-  for (int e0 = tid; e0 < items; e0 += EB * NTH) {
-    float4 y[EB];
-    const float* po[EB];
-    int r[EB];
+  auto out = [&](auto groups) {
+    constexpr int EB = decltype(groups)::value, PB = 16 / EB;
+    for (int e0 = tid; e0 < items; e0 += EB * NTH) {
+      float4 y[EB];
+      const float* po[EB];
+      const float2* wt[EB];
 #pragma unroll
-    for (int x = 0; x < EB; ++x) {
-      const int e = min(e0 + x * NTH, items - 1), c = e % (D / 4);
-      r[x] = e / (D / 4);
-      po[x] = a.part_o + flat_row(a, own_row(a, b, h, r0 + r[x])) * D + 4 * c;
-      y[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int x = 0; x < EB; ++x) {
+        const int e = min(e0 + x * NTH, items - 1), r = e / (D / 4), c = e % (D / 4);
+        po[x] = a.part_o + row_flat[r] * D + 4 * c;
+        wt[x] = sml + r * NP;
+        y[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      auto add = [&](int x, float f, const float4& v) {
+        y[x].x = fmaf(f, v.x, y[x].x); y[x].y = fmaf(f, v.y, y[x].y);
+        y[x].z = fmaf(f, v.z, y[x].z); y[x].w = fmaf(f, v.w, y[x].w);
+      };
+      for (int j = 0; j < a.S; j += PB) {
+        float4 v[PB][EB];
+#pragma unroll
+        for (int k = 0; k < PB; ++k)
+#pragma unroll
+          for (int x = 0; x < EB; ++x)
+            v[k][x] = j + k < a.S ? *reinterpret_cast<const float4*>(po[x] + (j + k) * a.rows * D)
+                                  : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < PB; ++k)
+#pragma unroll
+          for (int x = 0; x < EB; ++x) add(x, j + k < a.S ? wt[x][WK + j + k].x : 0.f, v[k][x]);
+      }
+#pragma unroll
+      for (int x = 0; x < EB; ++x) {
+        const int e = e0 + x * NTH, r = e / (D / 4), c = e % (D / 4);
+        if (e >= items) break;
+#pragma unroll
+        for (int j = 0; j < WK; ++j)
+          add(x, wt[x][j].x, *reinterpret_cast<const float4*>(so + (j * RB + r) * PO + 4 * c));
+        *reinterpret_cast<uint2*>(static_cast<bf16*>(a.O) + row_o[r] + 4 * c) =
+            make_uint2(pack_bf16(y[x].x, y[x].y), pack_bf16(y[x].z, y[x].w));
+      }
     }
-    auto add = [&](int x, float f, const float4& v) {
-      y[x].x = fmaf(f, v.x, y[x].x); y[x].y = fmaf(f, v.y, y[x].y);
-      y[x].z = fmaf(f, v.z, y[x].z); y[x].w = fmaf(f, v.w, y[x].w);
-    };
-    for (int j = 0; j < a.S; j += 4) {
-      float4 v[4][EB];
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int x = 0; x < EB; ++x)
-          v[k][x] = j + k < a.S && e0 + x * NTH < items ? *reinterpret_cast<const float4*>(po[x] + (j + k) * a.rows * D)
-                                                        : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int x = 0; x < EB; ++x) add(x, j + k < a.S ? sml[r[x] * NP + WK + j + k].x : 0.f, v[k][x]);
-    }
-#pragma unroll
-    for (int x = 0; x < EB; ++x) {
-      const int e = e0 + x * NTH;
-      if (e >= items) break;
-      const int c = e % (D / 4);
-#pragma unroll
-      for (int j = 0; j < WK; ++j)
-        add(x, sml[r[x] * NP + j].x, *reinterpret_cast<const float4*>(so + (j * RB + r[x]) * PO + 4 * c));
-      const RowAt w = own_row(a, b, h, r0 + r[x]);
-      *reinterpret_cast<uint2*>(static_cast<bf16*>(a.O) + w.b * a.osb + w.hq * a.osh + w.i * a.oss + 4 * c) =
-          make_uint2(pack_bf16(y[x].x, y[x].y), pack_bf16(y[x].z, y[x].w));
-    }
-  }
+  };
+  if (items <= NTH) out(std::integral_constant<int, 1>());
+  else out(std::integral_constant<int, 4>());
 }
 
 template <int D, int WR>
