@@ -22,145 +22,198 @@ namespace {
 
 using namespace sm100;
 
-constexpr int NTH = 256;
 constexpr int TK = 64;  // keys a tile
 
 // How prompt rows are kept: like the own rows, or in codes.
 enum Cache { kPlain, kFp8, kFp4 };
 
-// 4 consecutive channels (4 c ..) of a row, in fp32.
-__device__ __forceinline__ float4 row4(const float* p, int c) { return __ldg(reinterpret_cast<const float4*>(p) + c); }
-template <bool FP4>
-__device__ __forceinline__ float4 code4(const uint8_t* p, const uint8_t* scales, int c) {
-  const uint32_t w = FP4 ? __ldg(reinterpret_cast<const uint16_t*>(p) + c) : __ldg(reinterpret_cast<const uint32_t*>(p) + c);
-  const float s = mx_scale(__ldg(scales + c / 8));
-  const float2 x = mx_decode2<FP4>(FP4 ? w & 0xffu : w & 0xffffu), y = mx_decode2<FP4>(FP4 ? w >> 8 : w >> 16);
-  return make_float4(x.x * s, x.y * s, y.x * s, y.y * s);
-}
-
+// The threads of a CTA of TR rows, and its shared memory: query rows, one K and
+// one V tile, P.
+template <int TR> constexpr int kThreads = TR == 128 ? 512 : 256;
+constexpr int PP = TK + 4;  // pitch of P
 template <int D, int TR>
 constexpr size_t simt_smem() {
-  return sizeof(float) * (TR * (D + 4) + TK * (D + 4) + TK * D + TR * (TK + 4));
+  return sizeof(float) * (TR * D + 2 * TK * D + TR * PP);
 }
 
-// Thread (ty, tx) = (tid / 16, tid % 16) owns rows ty RT .. + RT of the tile,
-// keys tx + 16 j of a key tile and channels 4 tx + 64 j of O.
-template <typename T, int CACHE, int D, int TR>
-__global__ void __launch_bounds__(NTH, 2) simt_kernel(const __grid_constant__ PrefixArgs a) {
-  constexpr int RT = TR / 16, PITCH = D + 4, PP = TK + 4, C = D / 64;
+// 16-byte chunk c of row r of a [rows][D] fp32 tile, chunks XOR-permuted by the
+// row: eight consecutive rows' chunks lie in different banks.
+template <int D>
+__device__ __forceinline__ int at(int r, int c) { return r * D + ((c ^ (r & 7)) << 2); }
+
+// Thread (ty, tx) = (tid / 16, tid % 16) owns rows ty RT .. + RT of the tile, keys
+// tx + 16 j of a key tile and channels 4 tx + 64 c of O.  A key tile's V is copied
+// while its logits are formed and the next tile's K while O is, so one buffer
+// each is enough; codes come into registers a phase ahead and are widened into
+// the buffer when it is free.
+//
+// 64 x 64 logits of 128 channels and their products with V are 2 x 4096 cycles of
+// the fp32 pipe, and the corrections of the logits' sums (below) 2560 more; the
+// shared-memory reads stay below that with 4 rows x 4 keys a thread.
+template <int CACHE, int D, int TR>
+__global__ void __launch_bounds__(kThreads<TR>, TR == 128 ? 1 : 2) simt_kernel(const __grid_constant__ PrefixArgs a) {
+  constexpr int NTH = kThreads<TR>, RT = TR * 16 / NTH, C = D / 64;
+  constexpr bool FP4 = CACHE == kFp4;
+  constexpr int IT = TK * D / 16 / NTH > 0 ? TK * D / 16 / NTH : 1;  // groups of 16 codes a thread
   extern __shared__ __align__(16) float sm[];
-  float* sq = sm;                // [TR][PITCH]
-  float* sk = sq + TR * PITCH;   // [TK][PITCH]
-  float* sv = sk + TK * PITCH;   // [TK][D]
-  float* sp = sv + TK * D;       // [TR][PP]
+  float* sq = sm;            // [TR][D]
+  float* sk = sq + TR * D;   // [TK][D]
+  float* sv = sk + TK * D;   // [TK][D]
+  float* sp = sv + TK * D;   // [TR][PP]
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   // The CTA's unit, row tile and part.
   const int prompts = a.P * a.H * a.mt * a.S;
   int it = blockIdx.x;
   const bool own = it >= prompts;
   if (own) it -= prompts;
-  const int mt = own ? a.mto : a.mt, S = own ? a.So : a.S;
-  const int tile = it % mt, sp_i = (it / mt) % S, u = it / mt / S;
+  const FastDiv by_mt = own ? a.by_mto : a.by_mt, by_S = own ? a.by_So : a.by_S;
+  const int x0 = fastdiv(it, by_mt), tile = it - x0 * (int)by_mt.d, u = fastdiv(x0, by_S), sp_i = x0 - u * (int)by_S.d;
+  const int b = fastdiv(u, a.by_H), h = u - b * a.H, S = by_S.d;
   const int r0 = tile * TR, nr = min(TR, (own ? a.Ro : a.R) - r0);
   grid_dep_wait();
-  const int count = own ? own_count(a, u / a.H) : prompt_count(a, u / a.H);
+  const int count = own ? own_count(a, b) : prompt_count(a, b);
   const int tiles = (count + TK - 1) / TK, per = (tiles + S - 1) / S;
   const int k0 = min(count, sp_i * per * TK), k1 = min(count, (sp_i + 1) * per * TK);
+  const bool coded = CACHE != kPlain && !own;
+  const int32_t* idx = a.idx && !own ? a.idx + (int64_t)u * a.k : nullptr;
+  auto row_of = [&](int j) { return idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j; };
+
+  // Rows t0 .. of K or V as they are, by cp.async.
+  auto copy = [&](bool v, int t0) {
+    const float* base = static_cast<const float*>(v ? (own ? a.Vg : a.V) : (own ? a.Kg : a.K)) +
+                        b * (own ? a.gsb : a.ksb) + h * (own ? a.gsh : a.ksh);
+    const int64_t ss = own ? a.gss : a.kss;
+    const uint32_t dst = smem_u32(v ? sv : sk);
+#pragma unroll 4
+    for (int e = tid; e < TK * (D / 4); e += NTH) {
+      const int r = e / (D / 4), c = e % (D / 4);
+      const bool ok = t0 + r < k1;
+      cp_async16_zfill(dst + 4 * at<D>(r, c), base + (ok ? row_of(t0 + r) * ss : 0) + 4 * c, ok);
+    }
+    cp_async_commit();
+  };
+  // The same of codes: into registers, and from there widened into the buffer.
+  uint4 code[IT];
+  uint32_t byte[IT];
+  auto fetch = [&](bool v, int t0) {
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const int e = tid + NTH * i, r = e / (D / 16), c = e % (D / 16);
+      code[i] = make_uint4(0, 0, 0, 0);
+      byte[i] = 0;
+      if (r < TK && t0 + r < k1) {
+        const int64_t row = row_of(t0 + r);
+        const uint8_t* p = static_cast<const uint8_t*>(v ? a.V : a.K) + b * a.ksb + h * a.ksh + row * a.kss;
+        if (FP4) {
+          const uint2 w = __ldg(reinterpret_cast<const uint2*>(p) + c);
+          code[i].x = w.x;
+          code[i].y = w.y;
+        } else {
+          code[i] = __ldg(reinterpret_cast<const uint4*>(p) + c);
+        }
+        byte[i] = __ldg((v ? a.Vs : a.Ks) + ((int64_t)u * a.n + row) * (D / kMxBlock) + c / 2);
+      }
+    }
+  };
+  auto widen = [&](bool v) {
+    float* dst = v ? sv : sk;
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const int e = tid + NTH * i, r = e / (D / 16), c = e % (D / 16);
+      if (r >= TK) break;
+      const uint32_t w[4] = {code[i].x, code[i].y, code[i].z, code[i].w};
+      const float s = mx_scale(byte[i]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t q = FP4 ? w[k / 2] >> (16 * (k & 1)) : w[k];
+        const float2 lo = mx_decode2<FP4>(FP4 ? q & 0xffu : q & 0xffffu), hi = mx_decode2<FP4>(FP4 ? q >> 8 & 0xffu : q >> 16);
+        *reinterpret_cast<float4*>(dst + at<D>(r, 4 * c + k)) = make_float4(lo.x * s, lo.y * s, hi.x * s, hi.y * s);
+      }
+    }
+  };
 
   for (int e = tid; e < TR * (D / 4); e += NTH) {
     const int r = e / (D / 4), c = e % (D / 4);
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (r < nr) {
-      const RowAt w = own ? own_row(a, u / a.H, u % a.H, r0 + r) : prompt_row(a, u / a.H, u % a.H, r0 + r);
-      v = row4(static_cast<const T*>(a.Q) + w.b * a.qsb + w.hq * a.qsh + w.i * a.qss, c);
-    }
-    *reinterpret_cast<float4*>(sq + r * PITCH + 4 * c) = v;
+    const bool ok = r < nr;
+    const RowAt w = own ? own_row(a, b, h, r0 + (ok ? r : 0)) : prompt_row(a, b, h, r0 + (ok ? r : 0));
+    cp_async16_zfill(smem_u32(sq) + 4 * at<D>(r, c),
+                     static_cast<const float*>(a.Q) + w.b * a.qsb + w.hq * a.qsh + w.i * a.qss + 4 * c, ok);
+  }
+  if (coded) {
+    cp_async_commit();
+    fetch(false, k0);
+    widen(false);
+    fetch(true, k0);
+  } else {
+    copy(false, k0);
   }
 
-  float m[RT], l[RT], o[RT][4 * C];
+  float m[RT], l[RT];
+  f32x2 o[RT][2 * C];
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
     m[i] = -FLT_MAX;  // finite, so that logits of -inf add 0 and not 2^(-inf + inf)
     l[i] = 0.f;
 #pragma unroll
-    for (int c = 0; c < 4 * C; ++c) o[i][c] = 0.f;
+    for (int c = 0; c < 2 * C; ++c) o[i][c] = 0ull;
   }
 #pragma unroll 1
   for (int t0 = k0; t0 < k1; t0 += TK) {
     const int nk = min(TK, k1 - t0);
-    __syncthreads();  // the last tile's readers
-    for (int e = tid; e < TK * (D / 4); e += NTH) {
-      const int r = e / (D / 4), c = e % (D / 4);
-      float4 kv = make_float4(0.f, 0.f, 0.f, 0.f), vv = kv;
-      if (r < nk) {
-        if (own) {
-          const int64_t at = (int64_t)(u / a.H) * a.gsb + (int64_t)(u % a.H) * a.gsh + (int64_t)(t0 + r) * a.gss;
-          kv = row4(static_cast<const T*>(a.Kg) + at, c);
-          vv = row4(static_cast<const T*>(a.Vg) + at, c);
-        } else {
-          int row = t0 + r;
-          if (a.idx) row = min(max(__ldg(a.idx + (int64_t)u * a.k + row), 0), a.n - 1);
-          const int64_t at = (int64_t)(u / a.H) * a.ksb + (int64_t)(u % a.H) * a.ksh + (int64_t)row * a.kss;
-          if (CACHE == kPlain) {
-            kv = row4(static_cast<const T*>(a.K) + at, c);
-            vv = row4(static_cast<const T*>(a.V) + at, c);
-          } else {
-            const int64_t sa = ((int64_t)u * a.n + row) * (D / kMxBlock);
-            kv = code4<CACHE == kFp4>(static_cast<const uint8_t*>(a.K) + at, a.Ks + sa, c);
-            vv = code4<CACHE == kFp4>(static_cast<const uint8_t*>(a.V) + at, a.Vs + sa, c);
-          }
-        }
-      }
-      *reinterpret_cast<float4*>(sk + r * PITCH + 4 * c) = kv;
-      *reinterpret_cast<float4*>(sv + r * D + 4 * c) = vv;
+    const bool more = t0 + TK < k1;
+    cp_async_wait_all();
+    __syncthreads();  // K has arrived, V is free
+    if (coded) {
+      widen(true);
+      if (more) fetch(false, t0 + TK);
+    } else {
+      copy(true, t0);
     }
-    __syncthreads();
-    // Logits: even and odd channels in packed FMAs, chains of four of them
-    // summed with a running correction.  A logit of 100 has a unit of 2^-17 in
-    // fp32; a plain sum of 128 products would leave an error of several of them,
-    // and the softmax turns it into a relative error of the weights.
-    f32x2 s2[RT][4], e2[RT][4];
+    // Logits: even and odd channels in packed FMAs, chains of four of them, eight
+    // channels, added to a sum with a running correction.  A logit of 100 has a
+    // unit of 2^-17 in fp32; a plain sum of 128 products would leave an error of
+    // several of them, and the softmax turns it into a relative error of the
+    // weights.
+    float s[RT][4], low[RT][4];
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s2[i][j] = e2[i][j] = 0ull;
+      for (int j = 0; j < 4; ++j) s[i][j] = low[i][j] = 0.f;
 #pragma unroll 1
-    for (int c = 0; c < D; c += 8) {
+    for (int c = 0; c < D / 4; c += 2) {
       ulonglong2 ka[4], kb[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float* kr = sk + (tx + 16 * j) * PITCH + c;
-        ka[j] = *reinterpret_cast<const ulonglong2*>(kr);
-        kb[j] = *reinterpret_cast<const ulonglong2*>(kr + 4);
+        ka[j] = *reinterpret_cast<const ulonglong2*>(sk + at<D>(tx + 16 * j, c));
+        kb[j] = *reinterpret_cast<const ulonglong2*>(sk + at<D>(tx + 16 * j, c + 1));
       }
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
-        const float* qr = sq + (ty * RT + i) * PITCH + c;
-        const ulonglong2 qa = *reinterpret_cast<const ulonglong2*>(qr), qb = *reinterpret_cast<const ulonglong2*>(qr + 4);
+        const ulonglong2 qa = *reinterpret_cast<const ulonglong2*>(sq + at<D>(ty * RT + i, c));
+        const ulonglong2 qb = *reinterpret_cast<const ulonglong2*>(sq + at<D>(ty * RT + i, c + 1));
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const f32x2 x = fma2(qb.y, kb[j].y, fma2(qb.x, kb[j].x, fma2(qa.y, ka[j].y, mul2(qa.x, ka[j].x))));
-          const f32x2 y = add2(x, e2[i][j]), t = add2(s2[i][j], y);
-          e2[i][j] = sub2(y, sub2(t, s2[i][j]));
-          s2[i][j] = t;
+          const float2 x = up2(fma2(qb.y, kb[j].y, fma2(qb.x, kb[j].x, fma2(qa.y, ka[j].y, mul2(qa.x, ka[j].x)))));
+          const float y = __fadd_rn(__fadd_rn(x.x, x.y), low[i][j]), t = __fadd_rn(s[i][j], y);
+          low[i][j] = __fsub_rn(y, __fsub_rn(t, s[i][j]));
+          s[i][j] = t;
         }
       }
     }
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
-      float s[4], low[4], top = -INFINITY;
+      float top = -INFINITY;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float2 v = up2(s2[i][j]), e = up2(e2[i][j]);
-        float h = v.x + v.y;
-        const float z = h - v.x;
-        low[j] = ((v.x - (h - z)) + (v.y - z)) + (e.x + e.y);  // what h has not got
-        if (!(fabsf(h) <= FLT_MAX)) {  // an infinity in the rows makes the correction NaN: the plain sum
-          h = low[j] = 0.f;
-          for (int c = 0; c < D; ++c) h = fmaf(sq[(ty * RT + i) * PITCH + c], sk[(tx + 16 * j) * PITCH + c], h);
+        float h2 = s[i][j];
+        if (!(fabsf(h2) <= FLT_MAX)) {  // an infinity in the rows makes the correction NaN: the plain sum
+          h2 = low[i][j] = 0.f;
+#pragma unroll 1
+          for (int c = 0; c < D; ++c)
+            h2 = fmaf(sq[at<D>(ty * RT + i, c / 4) + c % 4], sk[at<D>(tx + 16 * j, c / 4) + c % 4], h2);
         }
-        s[j] = tx + 16 * j < nk ? h : -INFINITY;
-        top = fmaxf(top, s[j]);
+        s[i][j] = tx + 16 * j < nk ? h2 : -INFINITY;
+        top = fmaxf(top, s[i][j]);
       }
 #pragma unroll
       for (int w = 1; w < 16; w *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
@@ -169,64 +222,78 @@ __global__ void __launch_bounds__(NTH, 2) simt_kernel(const __grid_constant__ Pr
       float sum = 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float p = s[j] == -INFINITY ? 0.f : exp2f(fmaf(low[j], a.sl2, fmaf(s[j], a.sl2, -mn)));
+        const float p = s[i][j] == -INFINITY ? 0.f : exp2f(fmaf(low[i][j], a.sl2, fmaf(s[i][j], a.sl2, -mn)));
         sum += p;
         sp[(ty * RT + i) * PP + tx + 16 * j] = p;
       }
       l[i] = l[i] * f + sum;  // this thread's keys; the 16 threads of the row are summed at the end
 #pragma unroll
-      for (int c = 0; c < 4 * C; ++c) o[i][c] *= f;
+      for (int c = 0; c < 2 * C; ++c) o[i][c] = mul2(o[i][c], pk2(f, f));
     }
-    __syncwarp();  // a row's P is written and read by one half-warp
-#pragma unroll 2
-    for (int j = 0; j < TK; ++j) {
-      float4 vv[C];
+    cp_async_wait_all();
+    __syncthreads();  // V has arrived, K is free (and a row's P, which one half-warp writes and reads)
+    if (more) {
+      if (coded) {
+        widen(false);
+        fetch(true, t0 + TK);
+      } else {
+        copy(false, t0 + TK);
+      }
+    }
+#pragma unroll 1
+    for (int j = 0; j < TK; j += 4) {
+      float4 p[RT];
 #pragma unroll
-      for (int c = 0; c < C; ++c) vv[c] = *reinterpret_cast<const float4*>(sv + j * D + 4 * tx + 64 * c);
+      for (int i = 0; i < RT; ++i) p[i] = *reinterpret_cast<const float4*>(sp + (ty * RT + i) * PP + j);
 #pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        const float p = sp[(ty * RT + i) * PP + j];
+      for (int k = 0; k < 4; ++k) {
+        ulonglong2 vv[C];
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          o[i][4 * c] = fmaf(p, vv[c].x, o[i][4 * c]);
-          o[i][4 * c + 1] = fmaf(p, vv[c].y, o[i][4 * c + 1]);
-          o[i][4 * c + 2] = fmaf(p, vv[c].z, o[i][4 * c + 2]);
-          o[i][4 * c + 3] = fmaf(p, vv[c].w, o[i][4 * c + 3]);
+        for (int c = 0; c < C; ++c) vv[c] = *reinterpret_cast<const ulonglong2*>(sv + at<D>(j + k, tx + 16 * c));
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+          const float pi = k == 0 ? p[i].x : k == 1 ? p[i].y : k == 2 ? p[i].z : p[i].w;
+          const f32x2 pp = pk2(pi, pi);
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            o[i][2 * c] = fma2(pp, vv[c].x, o[i][2 * c]);
+            o[i][2 * c + 1] = fma2(pp, vv[c].y, o[i][2 * c + 1]);
+          }
         }
       }
     }
   }
   grid_dep_launch();
+  cp_async_wait_all();
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
 #pragma unroll
     for (int w = 1; w < 16; w *= 2) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
     const int r = ty * RT + i;
     if (r >= nr) continue;
-    const RowAt w = own ? own_row(a, u / a.H, u % a.H, r0 + r) : prompt_row(a, u / a.H, u % a.H, r0 + r);
-    if (a.whole) {
-      const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
-      T* op = static_cast<T*>(a.O) + w.b * a.osb + w.hq * a.osh + w.i * a.oss;
+    const RowAt w = own ? own_row(a, b, h, r0 + r) : prompt_row(a, b, h, r0 + r);
+    const bool none = l[i] == 0.f;
+    const float f = none ? 0.f : a.whole ? 1.f / l[i] : 1.f;
+    const int64_t flat = (int64_t)(own ? a.S + sp_i : sp_i) * a.rows + flat_row(a, w);
+    float* op = a.whole ? static_cast<float*>(a.O) + w.b * a.osb + w.hq * a.osh + w.i * a.oss : a.part_o + flat * D;
 #pragma unroll
-      for (int c = 0; c < 4 * C; ++c) from_f32(op[4 * tx + 64 * (c / 4) + c % 4], l[i] == 0.f ? 0.f : o[i][c] * inv);
-    } else {
-      const int64_t at = (int64_t)(own ? a.S + sp_i : sp_i) * a.rows + flat_row(a, w);
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-        *reinterpret_cast<float4*>(a.part_o + at * D + 4 * tx + 64 * c) =
-            make_float4(o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]);
-      if (tx == 0) a.part_ml[at] = make_float2(m[i], l[i]);
+    for (int c = 0; c < C; ++c) {
+      const float2 y0 = up2(o[i][2 * c]), y1 = up2(o[i][2 * c + 1]);
+      const float4 y = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(y0.x * f, y0.y * f, y1.x * f, y1.y * f);
+      *reinterpret_cast<float4*>(op + 4 * tx + 64 * c) = y;
     }
+    if (!a.whole && tx == 0) a.part_ml[flat] = make_float2(m[i], l[i]);
   }
 }
 
 // O of every query row from its parts: with M the largest m, the sum of
 // 2^(m - M) O over that of 2^(m - M) l.  A part without a key (l = 0) adds
 // nothing, and a row without any is 0.  D / 4 threads a row.
+constexpr int JTH = 256;
 template <typename T, int D>
-__global__ void __launch_bounds__(NTH) join_kernel(const __grid_constant__ PrefixArgs a) {
+__global__ void __launch_bounds__(JTH) join_kernel(const __grid_constant__ PrefixArgs a) {
   const int c = threadIdx.x % (D / 4);
-  const int64_t row = (int64_t)blockIdx.x * (NTH / (D / 4)) + threadIdx.x / (D / 4);
+  const int64_t row = (int64_t)blockIdx.x * (JTH / (D / 4)) + threadIdx.x / (D / 4);
   grid_dep_wait();
   grid_dep_launch();
   if (row >= a.rows) return;
@@ -252,15 +319,26 @@ __global__ void __launch_bounds__(NTH) join_kernel(const __grid_constant__ Prefi
   for (int e = 0; e < 4; ++e) from_f32(op[e], l == 0.f ? 0.f : o[e] * inv);
 }
 
+// Rows a CTA of the fp32 kernel: enough for the unit's rows, up to 128.
+int simt_rows(const PrefixArgs& a) {
+  const int r = std::max(a.R, a.Ro);
+  return r <= 16 ? 16 : r <= 64 ? 64 : 128;
+}
+
+template <int CACHE, int D, int TR>
+cudaError_t launch_rows(const PrefixArgs& a, unsigned items, cudaStream_t s) {
+  const auto k = simt_kernel<CACHE, D, TR>;
+  const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(k), simt_smem<D, TR>());
+  return e != cudaSuccess ? e : Launch(dim3(items), kThreads<TR>, simt_smem<D, TR>(), s)(k, a);
+}
 template <int CACHE, int D>
 cudaError_t launch_simt(const PrefixArgs& a, cudaStream_t s) {
   const int64_t items = (int64_t)a.P * a.H * a.mt * a.S + (int64_t)a.B * a.H * a.mto * a.So;
   if (!items) return cudaSuccess;
-  const bool few = (a.R > a.Ro ? a.R : a.Ro) <= 16;
-  const auto k = few ? simt_kernel<float, CACHE, D, 16> : simt_kernel<float, CACHE, D, 64>;
-  const size_t smem = few ? simt_smem<D, 16>() : simt_smem<D, 64>();
-  const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(k), smem);
-  return e != cudaSuccess ? e : Launch(dim3((unsigned)items), NTH, smem, s)(k, a);
+  const int tr = simt_rows(a);
+  return tr == 16 ? launch_rows<CACHE, D, 16>(a, (unsigned)items, s)
+         : tr == 64 ? launch_rows<CACHE, D, 64>(a, (unsigned)items, s)
+                    : launch_rows<CACHE, D, 128>(a, (unsigned)items, s);
 }
 
 cudaError_t launch_parts(const PrefixPlan& p, cudaStream_t s) {
@@ -273,8 +351,8 @@ cudaError_t launch_parts(const PrefixPlan& p, cudaStream_t s) {
 
 template <typename T, int D>
 cudaError_t launch_join(const PrefixArgs& a, cudaStream_t s) {
-  const int per = NTH / (D / 4);
-  return Launch(dim3((unsigned)((a.rows + per - 1) / per)), NTH, 0, s)(join_kernel<T, D>, a);
+  const int per = JTH / (D / 4);
+  return Launch(dim3((unsigned)((a.rows + per - 1) / per)), JTH, 0, s)(join_kernel<T, D>, a);
 }
 
 }  // namespace
@@ -293,12 +371,12 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   p.dtype = q.dtype;
   p.fmt = kv.dtype;
   const bool tc = p.dtype == WF_BF16;
-  const int tr = tc ? kPrefixTcRows : (a.R > a.Ro ? a.R : a.Ro) <= 16 ? 16 : 64;
+  const int tr = tc ? kPrefixTcRows : simt_rows(a);
   a.mt = (a.R + tr - 1) / tr;
   a.mto = (a.Ro + tr - 1) / tr;
   // Splits: as many parts as fill the SMs once (one CTA an SM, two of the fp32
-  // kernel), of at least two tiles of 128 keys each.
-  const int slots = tc ? 152 : 304;
+  // kernel with few rows), of at least 256 keys each.
+  const int slots = tc || tr == 128 ? 152 : 304;
   auto split = [&](int64_t units, int keys) {
     if (!keys) return 0;
     const int64_t most = std::max(1, (keys + 255) / 256);
