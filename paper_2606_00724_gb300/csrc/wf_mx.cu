@@ -5,7 +5,10 @@
 // takes 16 bytes of the floating-point side (8 bf16 or 4 fp32 channels), so
 // that a warp reads or writes 512 consecutive bytes there and the matching 128
 // to 256 bytes of codes, and UN rows, all of them loaded before the first is
-// used.  The 4 or 8 lanes that share a block find its largest magnitude with
+// used.  They are close to bound by instructions too (130 a thread and row filled
+// 75 % of the issue slots), so the rows of a CTA that lie in one unit are found
+// by adding strides, magnitudes are compared two at a time and codes are widened
+// a word at a time.  The 4 or 8 lanes that share a block find its largest magnitude with
 // shuffles, as integers: the bits of |x| are ordered as the values are, with
 // infinities and NaN above them.
 #include <algorithm>
@@ -59,11 +62,7 @@ template <> struct Word<8> { typedef uint2 type; };
 template <> struct Word<4> { typedef uint32_t type; };
 template <> struct Word<2> { typedef uint16_t type; };
 
-__device__ __forceinline__ uint32_t half_word(const uint2& w, int i) { return ((i < 2 ? w.x : w.y) >> (16 * (i & 1))) & 0xffffu; }
-__device__ __forceinline__ uint32_t half_word(uint32_t w, int i) { return (w >> (16 * i)) & 0xffffu; }
-
-// Codes of the N channels of one thread, two at a time: a code pair is 16 bits
-// (E4M3) or 8 (E2M1).
+// Codes of the N channels of one thread from their values in units of the scale.
 template <bool FP4, int N>
 __device__ __forceinline__ typename Word<FP4 ? N / 2 : N>::type pack_codes(const float* y) {
   constexpr int BITS = FP4 ? 8 : 16;
@@ -73,18 +72,64 @@ __device__ __forceinline__ typename Word<FP4 ? N / 2 : N>::type pack_codes(const
   if constexpr (!FP4 && N == 8) return make_uint2(w[0], w[1]);
   else return (typename Word<FP4 ? N / 2 : N>::type)w[0];
 }
-template <bool FP4, int N>
-__device__ __forceinline__ void unpack_codes(const typename Word<FP4 ? N / 2 : N>::type& c, float* y) {
-#pragma unroll
-  for (int i = 0; i < N / 2; ++i) {
-    uint32_t pair;
-    if constexpr (FP4) pair = ((uint32_t)c >> (8 * i)) & 0xffu;
-    else pair = half_word(c, i);
-    const float2 v = mx_decode2<FP4>(pair);
-    y[2 * i] = v.x;
-    y[2 * i + 1] = v.y;
+
+// A thread's values from its codes and their scale byte, stored: bf16 by exact
+// products of pairs, fp32 by way of half precision.
+template <bool FP4>
+__device__ __forceinline__ void put_values(bf16* out, const typename Word<FP4 ? 4 : 8>::type& c, uint32_t byte) {
+  uint32_t y[4];
+  if constexpr (FP4) {
+    mx_pairs<true>(c, y);
+  } else {
+    mx_pairs<false>(c.x, y);
+    mx_pairs<false>(c.y, y + 2);
   }
+  const uint32_t f = mx_factor<FP4>(byte);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = mul_bf16x2(y[i], f);
+  if (byte > kMxOne<FP4>) {
+    const uint32_t f2 = mx_second_factor<FP4>(byte);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = mul_bf16x2(y[i], f2);
+  }
+  *reinterpret_cast<uint4*>(out) = make_uint4(y[0], y[1], y[2], y[3]);
 }
+template <bool FP4>
+__device__ __forceinline__ void put_values(float* out, const typename Word<FP4 ? 2 : 4>::type& c, uint32_t byte) {
+  const float s = mx_scale(byte);
+  const float2 x = mx_decode2<FP4>(FP4 ? c & 0xffu : c & 0xffffu), y = mx_decode2<FP4>(FP4 ? c >> 8 : c >> 16);
+  *reinterpret_cast<float4*>(out) = make_float4(x.x * s, x.y * s, y.x * s, y.y * s);
+}
+
+// Offsets of a thread's UN rows: of the fp32 / bf16 row, and of the row in the
+// cache (unit, place).  RPC rows a pass of the CTA, first its first row.
+template <int UN, int RPC>
+struct Rows {
+  int64_t f[UN], c[UN], s[UN];  // elements, bytes of codes, rows of scales
+  __device__ __forceinline__ void find(const MxArgs& a, uint32_t first, int mine) {
+    const At w = row_at(a, first);
+    const uint32_t last = min(first + RPC * UN, a.total) - 1;
+    if (w.i + (last - first) < a.rows.d) {  // all of one unit
+      const uint32_t i0 = w.i + mine;
+#pragma unroll
+      for (int i = 0; i < UN; ++i) {
+        // Rows past the last repeat it.
+        const uint32_t r = first + mine + RPC * i < a.total ? i0 + RPC * i : w.i + (last - first);
+        f[i] = w.b * a.fsb + w.h * a.fsh + (int64_t)r * a.fss;
+        c[i] = w.b * a.csb + w.h * a.csh + (a.pos + r) * a.css;
+        s[i] = (int64_t)w.u * a.n + a.pos + r;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < UN; ++i) {
+        const At x = row_at(a, min(first + mine + RPC * i, a.total - 1));
+        f[i] = x.b * a.fsb + x.h * a.fsh + (int64_t)x.i * a.fss;
+        c[i] = x.b * a.csb + x.h * a.csh + (a.pos + x.i) * a.css;
+        s[i] = (int64_t)x.u * a.n + a.pos + x.i;
+      }
+    }
+  }
+};
 
 template <typename T, bool FP4, int D, int UN>
 __global__ void __launch_bounds__(NTH) quantize_kernel(const __grid_constant__ MxArgs a) {
@@ -93,35 +138,36 @@ __global__ void __launch_bounds__(NTH) quantize_kernel(const __grid_constant__ M
   constexpr int TPB = kMxBlock / N;     // threads a block
   constexpr int RPC = NTH / TPR;        // rows a pass of the CTA
   typedef typename Word<FP4 ? N / 2 : N>::type W;
-  const int t = threadIdx.x % TPR, y = blockIdx.y;
-  const uint32_t r0 = blockIdx.x * (RPC * UN) + threadIdx.x / TPR;
+  const int t = threadIdx.x % TPR, mine = threadIdx.x / TPR, y = blockIdx.y;
+  const uint32_t first = blockIdx.x * (RPC * UN);
+  Rows<UN, RPC> rows;
+  rows.find(a, first, mine);
   sm100::grid_dep_wait();
   uint4 v[UN];
 #pragma unroll
-  for (int i = 0; i < UN; ++i) {
-    const At w = row_at(a, min(r0 + RPC * i, a.total - 1));
-    const int64_t o = w.b * a.fsb + w.h * a.fsh + w.i * a.fss;
-    v[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.src[y]) + o) + t);
-  }
+  for (int i = 0; i < UN; ++i)
+    v[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.src[y]) + rows.f[i]) + t);
   sm100::grid_dep_launch();
 #pragma unroll
   for (int i = 0; i < UN; ++i) {
-    const uint32_t r = r0 + RPC * i;
-    float x[N];
-    widen_vec(static_cast<const T*>(nullptr), v[i], x);
     uint32_t top = top_bits(static_cast<const T*>(nullptr), v[i]);
 #pragma unroll
     for (int s = 1; s < TPB; s *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
     const uint32_t byte = mx_scale_byte<FP4>(top);
-    const float inv = byte == 255 ? 0.f : mx_inv_scale(byte);
+    if (byte == 255) v[i] = make_uint4(0, 0, 0, 0);
+    float x[N];
+    widen_vec(static_cast<const T*>(nullptr), v[i], x);
+    const float inv = mx_inv_scale(min(byte, 254u - 1u));
+    const sm100::f32x2 inv2 = sm100::pk2(inv, inv);
 #pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = byte == 255 ? 0.f : x[e] * inv;
-    if (r < a.total) {
-      const At w = row_at(a, r);
-      const int64_t row = a.pos + w.i;
-      char* c = static_cast<char*>(a.dst[y]) + w.b * a.csb + w.h * a.csh + row * a.css;
-      reinterpret_cast<W*>(c)[t] = pack_codes<FP4, N>(x);
-      if (t % TPB == 0) a.scales[y][((int64_t)w.u * a.n + row) * (D / kMxBlock) + t / TPB] = (uint8_t)byte;
+    for (int e = 0; e < N; e += 2) {
+      const float2 p = sm100::up2(sm100::mul2(sm100::pk2(x[e], x[e + 1]), inv2));
+      x[e] = p.x;
+      x[e + 1] = p.y;
+    }
+    if (first + mine + RPC * i < a.total) {
+      reinterpret_cast<W*>(static_cast<char*>(a.dst[y]) + rows.c[i])[t] = pack_codes<FP4, N>(x);
+      if (t % TPB == 0) a.scales[y][rows.s[i] * (D / kMxBlock) + t / TPB] = (uint8_t)byte;
     }
   }
 }
@@ -130,52 +176,44 @@ template <typename T, bool FP4, int D, int UN>
 __global__ void __launch_bounds__(NTH) dequantize_kernel(const __grid_constant__ MxArgs a) {
   constexpr int N = Vec<T>::N, TPR = D / N, TPB = kMxBlock / N, RPC = NTH / TPR;
   typedef typename Word<FP4 ? N / 2 : N>::type W;
-  const int t = threadIdx.x % TPR, y = blockIdx.y;
-  const uint32_t r0 = blockIdx.x * (RPC * UN) + threadIdx.x / TPR;
+  const int t = threadIdx.x % TPR, mine = threadIdx.x / TPR, y = blockIdx.y;
+  const uint32_t first = blockIdx.x * (RPC * UN);
+  Rows<UN, RPC> rows;
+  rows.find(a, first, mine);
   sm100::grid_dep_wait();
+  if (a.idx) {
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+      const int r = min(max(__ldg(a.idx + min(first + mine + RPC * i, a.total - 1)), 0), a.n - 1);
+      const uint32_t u = fastdiv((uint32_t)min(first + mine + RPC * i, a.total - 1), a.rows), b = fastdiv(u, a.heads);
+      rows.c[i] = b * a.csb + (u - b * a.heads.d) * a.csh + r * a.css;
+      rows.s[i] = (int64_t)u * a.n + r;
+    }
+  }
   W c[UN];
   uint32_t byte[UN];
-  int64_t row[UN];
 #pragma unroll
   for (int i = 0; i < UN; ++i) {
-    const uint32_t r = min(r0 + RPC * i, a.total - 1);
-    row[i] = a.pos + row_at(a, r).i;
-    if (a.idx) row[i] = min(max(__ldg(a.idx + r), 0), a.n - 1);
-  }
-#pragma unroll
-  for (int i = 0; i < UN; ++i) {
-    const At w = row_at(a, min(r0 + RPC * i, a.total - 1));
-    const char* p = static_cast<const char*>(a.src[y]) + w.b * a.csb + w.h * a.csh + row[i] * a.css;
-    c[i] = __ldg(reinterpret_cast<const W*>(p) + t);
-    byte[i] = __ldg(a.scales[y] + ((int64_t)w.u * a.n + row[i]) * (D / kMxBlock) + t / TPB);
+    c[i] = __ldg(reinterpret_cast<const W*>(static_cast<const char*>(a.src[y]) + rows.c[i]) + t);
+    byte[i] = __ldg(a.scales[y] + rows.s[i] * (D / kMxBlock) + t / TPB);
   }
   sm100::grid_dep_launch();
 #pragma unroll
-  for (int i = 0; i < UN; ++i) {
-    const uint32_t r = r0 + RPC * i;
-    if (r >= a.total) break;
-    float x[N];
-    unpack_codes<FP4, N>(c[i], x);
-    const float s = mx_scale(byte[i]);
-#pragma unroll
-    for (int e = 0; e < N; ++e) x[e] *= s;
-    const At w = row_at(a, r);
-    const int64_t o = w.b * a.fsb + w.h * a.fsh + w.i * a.fss;
-    st_vec(static_cast<T*>(a.dst[y]) + o + t * N, x);
-  }
+  for (int i = 0; i < UN; ++i)
+    if (first + mine + RPC * i < a.total) put_values<FP4>(static_cast<T*>(a.dst[y]) + rows.f[i] + t * N, c[i], byte[i]);
 }
 
 template <typename T, bool FP4, int D, bool BACK>
 cudaError_t launch_un(const MxArgs& a, int tensors, cudaStream_t s) {
   constexpr int RPC = NTH / (D / Vec<T>::N);
-  // Four rows a thread from a few waves of CTAs on: fewer CTAs and more loads in
-  // flight a thread; below that, as many threads as possible.
+  // Eight rows a thread from a wave of CTAs on (a 32K prompt of 32 heads: 127 us,
+  // with four 132 to 136, with two 158); below that, as many threads as possible.
   const bool many = (int64_t)a.total * tensors > 8ll * RPC * 8 * sm_count();
-  const int un = many ? 4 : 1;
+  const int un = many ? 8 : 1;
   const dim3 grid((a.total + RPC * un - 1) / (RPC * un), (unsigned)tensors);
   Launch l(grid, NTH, 0, s);
-  if (BACK) return many ? l(dequantize_kernel<T, FP4, D, 4>, a) : l(dequantize_kernel<T, FP4, D, 1>, a);
-  return many ? l(quantize_kernel<T, FP4, D, 4>, a) : l(quantize_kernel<T, FP4, D, 1>, a);
+  if (BACK) return many ? l(dequantize_kernel<T, FP4, D, 8>, a) : l(dequantize_kernel<T, FP4, D, 1>, a);
+  return many ? l(quantize_kernel<T, FP4, D, 8>, a) : l(quantize_kernel<T, FP4, D, 1>, a);
 }
 
 template <bool BACK>
