@@ -117,19 +117,26 @@ def desc(t: torch.Tensor) -> wf_tensor:
     return wf_tensor(B, H, S, D, sb, sh, ss, code)
 
 
-def code_desc(codes: torch.Tensor, fmt: int) -> wf_tensor:
-    """wf_tensor for the codes of a quantised cache: [B, H, rows, d] bytes
-    (WF_MXFP8) or [B, H, rows, d / 2] (WF_MXFP4), last axis contiguous."""
-    if codes.dim() != 4 or codes.element_size() != 1:
+def _code_desc(shape, stride, size: int, fmt: int) -> wf_tensor:
+    if len(shape) != 4 or size != 1:
         raise ValueError("expected a [B, H, rows, bytes] tensor of 8-bit codes")
-    if fmt not in (WF_MXFP8, WF_MXFP4):
+    if fmt == WF_MXFP4:
+        per = 2
+    elif fmt == WF_MXFP8:
+        per = 1
+    else:
         raise ValueError(f"unknown format {fmt}")
-    per = 2 if fmt == WF_MXFP4 else 1
-    sb, sh, ss, sd = codes.stride()
-    B, H, S, W = codes.shape
+    B, H, S, W = shape
+    sb, sh, ss, sd = stride
     if W > 1 and sd != 1:
         raise ValueError("head_dim axis must be contiguous")
     return wf_tensor(B, H, S, W * per, sb * per, sh * per, ss * per, fmt)
+
+
+def code_desc(codes: torch.Tensor, fmt: int) -> wf_tensor:
+    """wf_tensor for the codes of a quantised cache: [B, H, rows, d] bytes
+    (WF_MXFP8) or [B, H, rows, d / 2] (WF_MXFP4), last axis contiguous."""
+    return _code_desc(codes.shape, codes.stride(), codes.element_size(), fmt)
 
 
 def _scales(K_scales, V_scales):
@@ -137,9 +144,10 @@ def _scales(K_scales, V_scales):
     size = 0
     for s in (K_scales, V_scales):
         if s is not None:
-            if s.element_size() != 1 or not s.is_contiguous():
+            n = s.nbytes
+            if n != s.numel() or not s.is_contiguous():
                 raise ValueError("scales must be contiguous bytes")
-            size = min(size, s.nbytes) if size else s.nbytes
+            size = n if size == 0 or n < size else size
     return size
 
 
@@ -149,10 +157,13 @@ def _on_gpu(*tensors):
             raise ValueError("expected tensors on the GPU")
 
 
-def _pair(K, V, what: str):
-    """V, where it is given, lies as K does."""
-    if K is not None and V is not None and not (_same_layout(V, K) and V.dtype == K.dtype):
+def _pair_desc(K, V, what: str, fmt=None) -> wf_tensor:
+    """Descriptor of K (codes of the format fmt where that is given); V, where
+    there is one, lies as K does."""
+    shape, stride, dtype = K.shape, K.stride(), K.dtype
+    if V is not None and (V.stride() != stride or V.shape != shape or V.dtype != dtype):
         raise ValueError(f"{what} must share dtype, shape and strides")
+    return desc(K) if fmt is None else _code_desc(shape, stride, dtype.itemsize, fmt)
 
 
 def _ptr(t):
@@ -364,31 +375,24 @@ def wf_cache_quantize(Knew, Vnew, Kc, Ks, Vc, Vs, fmt: int, pos: int, stream=Non
     """Quantise Knew (and Vnew) into the caches' codes and scales at
     [pos, pos + count) (see the C header; Vnew, Vc, Vs all None: keys alone)."""
     _on_gpu(Knew, Vnew, Kc, Ks, Vc, Vs)
-    _pair(Knew, Vnew, "Knew and Vnew")
-    _pair(Kc, Vc, "Kc and Vc")
-    _check(lib().wf_cache_quantize(_ptr(Knew), _ptr(Vnew), desc(Knew), _ptr(Kc), _ptr(Ks), _ptr(Vc), _ptr(Vs),
-                                   code_desc(Kc, fmt), _scales(Ks, Vs), pos, _stream(stream)), "wf_cache_quantize")
+    dn, dk = _pair_desc(Knew, Vnew, "Knew and Vnew"), _pair_desc(Kc, Vc, "Kc and Vc", fmt)
+    _check(lib().wf_cache_quantize(_ptr(Knew), _ptr(Vnew), dn, _ptr(Kc), _ptr(Ks), _ptr(Vc), _ptr(Vs), dk,
+                                   _scales(Ks, Vs), pos, _stream(stream)), "wf_cache_quantize")
 
 
 def wf_cache_dequantize(Kc, Ks, Vc, Vs, fmt: int, Kout, Vout, pos: int = 0, idx=None, stream=None) -> None:
     """Rows [pos, pos + m), or the rows idx ([B*H][m] int32), of the caches
     into Kout (and Vout) ([B, H, m, d]) (see the C header)."""
     _on_gpu(Kc, Ks, Vc, Vs, Kout, Vout, idx)
-    _pair(Kout, Vout, "Kout and Vout")
-    _pair(Kc, Vc, "Kc and Vc")
+    do, dk = _pair_desc(Kout, Vout, "Kout and Vout"), _pair_desc(Kc, Vc, "Kc and Vc", fmt)
     if idx is not None and tuple(idx.shape) != (Kout.shape[0] * Kout.shape[1], Kout.shape[2]):
         raise ValueError("idx must be [B*H, m]")
-    _check(lib().wf_cache_dequantize(_ptr(Kc), _ptr(Ks), _ptr(Vc), _ptr(Vs), code_desc(Kc, fmt), _scales(Ks, Vs),
-                                     _ints(idx), pos, _ptr(Kout), _ptr(Vout), desc(Kout), _stream(stream)),
-           "wf_cache_dequantize")
-
-
-def _prefix_desc(K, fmt):
-    return desc(K) if fmt is None else code_desc(K, fmt)
+    _check(lib().wf_cache_dequantize(_ptr(Kc), _ptr(Ks), _ptr(Vc), _ptr(Vs), dk, _scales(Ks, Vs), _ints(idx), pos,
+                                     _ptr(Kout), _ptr(Vout), do, _stream(stream)), "wf_cache_dequantize")
 
 
 def wf_prefix_attn_workspace_bytes(Q: torch.Tensor, K: torch.Tensor, k: int, n_g: int, fmt=None) -> int:
-    return int(lib().wf_prefix_attn_workspace_bytes(desc(Q), _prefix_desc(K, fmt), k, n_g))
+    return int(lib().wf_prefix_attn_workspace_bytes(desc(Q), _pair_desc(K, None, "", fmt), k, n_g))
 
 
 def wf_prefix_attn(Q, K, V, k: int, Kg, Vg, O, ws, idx=None, prefix_len=None, gen_len=None, Ks=None, Vs=None,
@@ -397,20 +401,18 @@ def wf_prefix_attn(Q, K, V, k: int, Kg, Vg, O, ws, idx=None, prefix_len=None, ge
     first k rows or the rows idx [P*H, k] of each, and each sequence's own rows
     Kg, Vg [B, H, n_g, d] (see the C header).  fmt (WF_MXFP8, WF_MXFP4): K and V
     are codes, with scales Ks and Vs."""
-    dq, dk, do = desc(Q), _prefix_desc(K, fmt), desc(O)
-    dg = desc(Kg) if Kg is not None else None
     _on_gpu(Q, K, V, Kg, Vg, O, ws, idx, prefix_len, gen_len, Ks, Vs)
-    _pair(K, V, "K and V")
-    _pair(Kg, Vg, "Kg and Vg")
+    dq, do = desc(Q), desc(O)
+    dk = _pair_desc(K, V, "K and V", fmt)
+    dg = _pair_desc(Kg, Vg, "Kg and Vg") if Kg is not None else None
     if fmt is not None:
-        need = K.shape[0] * K.shape[1] * K.shape[2] * (Q.shape[3] // 32)
-        if Ks is None or Vs is None or _scales(Ks, Vs) < need:
+        if Ks is None or Vs is None or _scales(Ks, Vs) < dk.batch * dk.heads * dk.seq * (dk.head_dim // 32):
             raise ValueError("a quantised prompt needs the scales of its K and V")
-    if idx is not None and tuple(idx.shape) != (K.shape[0] * K.shape[1], k):
+    if idx is not None and tuple(idx.shape) != (dk.batch * dk.heads, k):
         raise ValueError("idx must be [P*H, k]")
-    if prefix_len is not None and prefix_len.numel() != K.shape[0]:
+    if prefix_len is not None and prefix_len.numel() != dk.batch:
         raise ValueError("prefix_len must have an entry a prompt")
-    if gen_len is not None and gen_len.numel() != Q.shape[0]:
+    if gen_len is not None and gen_len.numel() != dq.batch:
         raise ValueError("gen_len must have an entry a sequence")
     _check(lib().wf_prefix_attn(_ptr(Q), dq, _ptr(K), _ptr(V), dk, _ptr(Ks), _ptr(Vs), _ints(idx), k,
                                 _ints(prefix_len), _ptr(Kg), _ptr(Vg), dg, _ints(gen_len), _ptr(O), do, float(scale),
