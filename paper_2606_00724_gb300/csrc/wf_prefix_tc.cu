@@ -42,13 +42,16 @@ using namespace sm100;
 constexpr int TM = kPrefixTcRows / 2;  // rows of a row tile, keys of a key tile
 constexpr int HALF = TM * 128;         // 64 channels of a tile of bf16 rows
 constexpr float kLazy = 8.f;
-constexpr int kPCol = TM / 2;            // P's columns among S's
 
 constexpr int kMaxStages = 9;
 struct Bars {
   unsigned long long full[kMaxStages], empty[kMaxStages], raw_full[4], raw_empty[4], qfull, sfull[2], pready[2], odone[2], turn[2], drain[2], stall;
   uint32_t tmem, abort;
-  int64_t row[kPrefixTcRows];  // a row's offset in Q while the rows are read, then in the output
+  // Between the two warps that share 32 rows of a tile: whether the tile is
+  // there, whether a maximum rises, and the rows' maxima.
+  int go[2][4], raise[2][2][4];
+  float top[2][TM];
+  uint32_t row[kPrefixTcRows];  // a row's number among all, for the way out
 };
 
 template <int D, int FMT>
@@ -56,7 +59,7 @@ struct Cfg {
   static constexpr bool CODES = FMT != WF_BF16;
   static constexpr int NPT = CODES ? 256 : 128;          // producer threads
   // Softmax warps, producers, two MMA warps and, with codes, two loader warps.
-  static constexpr int NTH = 256 + NPT + (CODES ? 128 : 64);
+  static constexpr int NTH = 512 + NPT + (CODES ? 128 : 64);
   static constexpr int TILE = TM * D * 2;                // a stage
   static constexpr int ROWB = FMT == WF_MXFP4 ? D / 2 : D;  // bytes of a row of codes
   static constexpr int DEPTH = FMT == WF_MXFP8 ? 3 : 4;  // tiles of codes in flight
@@ -72,6 +75,7 @@ struct Cfg {
   static constexpr int ROOM = 232448 - (int)sizeof(Bars) - 2 * TILE - RAW;
   // Stages beside two tiles of query rows; with one tile its place is a stage more.
   static constexpr int STAGES = ROOM / TILE > kMaxStages - 1 ? kMaxStages - 1 : ROOM / TILE;
+  static_assert(STAGES * TILE + RAW >= 2 * TM * D * 4, "the rows go out through the stages");
   static constexpr size_t SMEM = 2 * TILE + RAW + (size_t)STAGES * TILE + sizeof(Bars);
 };
 
@@ -229,29 +233,10 @@ __device__ __forceinline__ void copy_tile(uint32_t st, const bf16* base, int64_t
 __device__ __forceinline__ RowAt row_at(const PrefixArgs& a, const Item& w, int r) {
   return w.own ? own_row(a, w.b, w.h, w.r0 + r) : prompt_row(a, w.b, w.h, w.r0 + r);
 }
-__device__ __forceinline__ int64_t q_offset(const PrefixArgs& a, const Item& w, int r) {
-  const RowAt at = row_at(a, w, r);
-  return at.b * a.qsb + at.hq * a.qsh + at.i * a.qss;
-}
-
 template <int D, int FMT>
-__device__ void produce(const PrefixArgs& a, const Item& w, uint32_t sq, const Ring& ring, uint32_t raw, Bars& s, int tid) {
+__device__ void produce(const PrefixArgs& a, const Item& w, const Ring& ring, uint32_t raw, Bars& s, int tid) {
   typedef Cfg<D, FMT> C;
-  constexpr int CH = D / 8, NPT = C::NPT;
-  if (w.T == 0) return;
-  // The query rows, K-major; rows past the last are zero.  Where a row lies takes
-  // two divisions, so each is found once and shared.
-  if (tid < w.nr) s.row[tid] = q_offset(a, w, tid);
-  if (NPT < kPrefixTcRows && tid + NPT < w.nr) s.row[tid + NPT] = q_offset(a, w, tid + NPT);
-  named_sync(2, NPT);
-  const int tiles = w.wide ? 2 : 1;
-  for (int i = 0; i < tiles * TM * CH / NPT; ++i) {
-    const int r = tid / CH + NPT / CH * i, ch = tid % CH;
-    const bool ok = r < w.nr;
-    cp_async16_zfill(sq + (r / TM) * C::TILE + swizzled(r % TM, ch),
-                     static_cast<const bf16*>(a.Q) + (ok ? s.row[r] : 0) + ch * 8, ok);
-  }
-  cp_async_arrive_noinc(bar(s.qfull));
+  constexpr int NPT = C::NPT;
   const int64_t b = w.b, h = w.h;
   const int A = w.wide ? 1 : 2;
   if (!C::CODES || w.own) {
@@ -477,7 +462,7 @@ __device__ void multiply(const PrefixArgs& a, const Item& w, uint32_t sq, const 
       const uint64_t v = v0 + sv * T4;
 #pragma unroll
       for (int kq = 0; kq < TM / 16; ++kq)
-        mma_bf16_ts(tm + 2 * TM + D * g, tm + TM * g + kPCol + 8 * kq, v + kq * (2048 >> 4), pv, i > 0 || kq > 0);
+        mma_bf16_ts(tm + 2 * TM + D * g, tm + TM * g + (kq / 4) * 64 + (kq % 4) * 8, v + kq * (2048 >> 4), pv, i > 0 || kq > 0);
       mma_commit(bar(s.empty[sv]));
       if (!more) mma_commit(bar(s.odone[g]));
     }
@@ -517,19 +502,28 @@ __device__ __forceinline__ void got(uint32_t* v) {
                  "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
 }
 
-// P of one tile from S: one pass over chunks of CW columns, the next chunk on its
-// way while one is worked on, with the maximum of the tiles before as m.  P
-// stays in registers until the tile's own maximum is known; where that is more
-// than 2^kLazy above m (seldom) m is raised, O and l are rescaled and the pass
-// runs again, S being still there.  P goes to the upper
-// half of S's columns.
+// The larger of the two halves' maxima of row r.
+__device__ __forceinline__ float row_top(Bars& s, int g, int half, int r, int pair, float top) {
+  if (half) s.top[g][r] = top;
+  named_sync(pair, 64);
+  if (!half) s.top[g][r] = top = fmaxf(top, s.top[g][r]);
+  named_sync(pair, 64);
+  return half ? s.top[g][r] : top;
+}
+
+// P of half a tile (64 keys) from S: one pass over chunks of CW columns, the next
+// chunk on its way while one is worked on, with the maximum of the tiles before
+// as m.  P stays in registers until the tile's own maximum is known; where that
+// is more than 2^kLazy above m in either half (seldom) m is raised, O and l are
+// rescaled and the pass runs again, S being still there.  P takes the first 32
+// of its half's columns.
 constexpr int CW = 16;
 template <int D, bool MASK>
-__device__ __forceinline__ void soften_tile(const PrefixArgs& a, uint32_t sc, uint32_t oc, bool have_o, int nk, float& m,
-                                            float& l) {
-  constexpr int NC = TM / CW;
+__device__ __forceinline__ void soften_tile(const PrefixArgs& a, Bars& s, uint32_t sc, uint32_t oc, bool have_o, int nk,
+                                            int g, int half, int r, int pair, float& m, float& l) {
+  constexpr int NC = TM / 2 / CW;
   const f32x2 sl = pk2(a.sl2, a.sl2);
-  uint32_t p[TM / 2];
+  uint32_t p[TM / 4];
   f32x2 sum[2];
   if (!have_o) {  // the first tile: its maximum first, in a short pass
     float top = -INFINITY;
@@ -541,7 +535,7 @@ __device__ __forceinline__ void soften_tile(const PrefixArgs& a, uint32_t sc, ui
 #pragma unroll
       for (int e = 0; e < CW; ++e) top = fmaxf(top, !MASK || CW * c + e < nk ? __uint_as_float(x[e]) : -INFINITY);
     }
-    m = fmaxf(m, top * a.sl2);
+    m = fmaxf(m, row_top(s, g, half, r, pair, top) * a.sl2);
   }
 #pragma unroll 1
   for (;;) {
@@ -569,15 +563,18 @@ __device__ __forceinline__ void soften_tile(const PrefixArgs& a, uint32_t sc, ui
         p[(CW * c + e) / 2] = pack_bf16(p0, p1);
       }
     }
-    const float mt = top * a.sl2;
+    const bool mine = __any_sync(0xffffffffu, top * a.sl2 > m + kLazy);
+    if ((r & 31) == 0) s.raise[g][half][r >> 5] = mine;
+    named_sync(pair, 64);
+    if (!(mine | s.raise[g][half ^ 1][r >> 5])) break;
+    const float mt = row_top(s, g, half, r, pair, top) * a.sl2;
     const bool raise = mt > m + kLazy;
-    if (!__any_sync(0xffffffffu, raise)) break;
-    const float f = raise ? ex2(m - mt) : 1.f;  // 0 on the first tile
+    const float f = raise ? ex2(m - mt) : 1.f;
     m = raise ? mt : m;
     l *= f;
-    if (have_o) {  // the products into O are done: this S was issued behind them
+    if (have_o) {  // half of O's columns; the products into it are done: this S was issued behind them
 #pragma unroll 1
-      for (int c = 0; c < D / CW; ++c) {
+      for (int c = 0; c < D / 2 / CW; ++c) {
         uint32_t o[CW];
         get(oc + CW * c, o);
         got(o);
@@ -587,106 +584,129 @@ __device__ __forceinline__ void soften_tile(const PrefixArgs& a, uint32_t sc, ui
       }
     }
   }
-#pragma unroll
-  for (int c = 0; c < TM / 32; ++c) tmem_st16(sc + kPCol + 16 * c, p + 16 * c);
+  tmem_st16(sc, p);
+  tmem_st16(sc + 16, p + 16);
   const float2 z = up2(add2(sum[0], sum[1]));
   l += z.x + z.y;
 }
 
+// Warpgroup wg of four: half wg % 2 of the columns of S and O of row tile (or
+// key tile parity) wg / 2.  Thread r has TMEM lane r.
 template <int D, int FMT>
-__device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* stages, Bars& s, int g, int r) {
+__device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* sm, uint8_t* stages, Bars& s, int tid) {
   typedef Cfg<D, FMT> C;
+  constexpr int CH = D / 8;
+  const int g = tid >> 8, half = (tid >> 7) & 1, r = tid & 127, lane = tid & 31;
+  const int pair = 3 + g * 4 + (r >> 5);             // the named barrier of the two warps with these rows
   const uint32_t lanes = (uint32_t)(r & ~31) << 16;  // the warp's quarter of the TMEM lanes
-  const uint32_t tm = s.tmem, sc = tm + TM * g + lanes, oc = tm + 2 * TM + D * g + lanes;
-  const int rt = w.wide ? g * TM : 0;                // first row of the warpgroup's tile
+  const uint32_t tm = s.tmem, sc = tm + TM * g + TM / 2 * half + lanes, oc = tm + 2 * TM + D * g + D / 2 * half + lanes;
+  const int rt = w.wide ? g * TM : 0;                // first row of the row tile
   const bool active = rt + (r & ~31) < w.nr;         // the warp has a row
   const int step = w.wide ? 1 : 2, first = w.wide ? 0 : g;
+  if (w.T > 0) {
+    // The query rows, K-major; rows past the last are zero.
+    const uint32_t sq = smem_u32(sm);
+    const int tiles = w.wide ? 2 : 1;
+    for (int i = 0; i < tiles * TM * CH / 512; ++i) {
+      const int q = tid / CH + 512 / CH * i, ch = tid % CH;
+      const bool ok = q < w.nr;
+      const RowAt at = row_at(a, w, ok ? q : 0);
+      cp_async16_zfill(sq + (q / TM) * C::TILE + swizzled(q % TM, ch),
+                       static_cast<const bf16*>(a.Q) + at.b * a.qsb + at.hq * a.qsh + at.i * a.qss + ch * 8, ok);
+    }
+    cp_async_arrive_noinc(bar(s.qfull));
+  }
+  if (tid < w.nr) s.row[tid] = (uint32_t)flat_row(a, row_at(a, w, tid));
   float m = -FLT_MAX, l = 0.f;  // finite, so that logits of -inf add 0 and not 2^(-inf + inf)
   bool ok = true;
   if (active) {
     int i = 0;
 #pragma unroll 1
     for (int t = first; t < w.T; t += step, ++i) {
-      if (!(ok = warp_wait(bar(s.sfull[g]), i & 1, s, a))) break;
+      // One warp of a pair waits and tells the other: a wait that gives up must
+      // not leave one of them at the barriers below.
+      if (!half) {
+        ok = warp_wait(bar(s.sfull[g]), i & 1, s, a);
+        if (lane == 0) s.go[g][r >> 5] = ok;
+      }
+      named_sync(pair, 64);
+      ok = s.go[g][r >> 5];
+      if (!ok) break;
       tc_fence_after();
       const int nk = w.k1 - (w.k0 + t * TM);  // keys of the tile
-      if (nk >= TM) soften_tile<D, false>(a, sc, oc, i > 0, TM, m, l);
-      else soften_tile<D, true>(a, sc, oc, i > 0, nk, m, l);
+      if (nk >= TM) soften_tile<D, false>(a, s, sc, oc, i > 0, TM, g, half, r, pair, m, l);
+      else soften_tile<D, true>(a, s, sc, oc, i > 0, nk - TM / 2 * half, g, half, r, pair, m, l);
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if ((r & 31) == 0) mbar_arrive(bar(s.pready[g]));
+      if (lane == 0) mbar_arrive(bar(s.pready[g]));
     }
   }
-  const int row = rt + r;
-  // The offsets in Q are not read any more: this warpgroup has seen an S, or no
-  // row of Q is (an empty range).
-  if (ok && row < w.nr && (w.wide || g == 0)) {
-    const RowAt at = row_at(a, w, row);
-    s.row[row] = a.whole ? at.b * a.osb + at.hq * a.osh + at.i * a.oss : (int64_t)w.part * a.rows + flat_row(a, at);
-  }
-  // The last products of both warpgroups: the exchange below is in their stages.
+  cp_async_wait_all();
+  // The last products of both row tiles: the exchange below is in their stages.
   if (ok && w.T > 0) ok = warp_wait(bar(s.odone[0]), 0, s, a);
   if (ok && w.T > step - 1) ok = warp_wait(bar(s.odone[1]), 0, s, a);
   tc_fence_after();
-  // The rows go out through the stages, which nothing reads any more, 64 channels
-  // at a time: a thread has a row, a store to memory wants a row's 256 bytes
-  // from consecutive lanes (32 rows' 16 bytes a store took 5 us a CTA).  Two
-  // warpgroups on one row tile scale their O to the larger maximum and the
-  // sum is formed on the way out.
-  const bool have = w.T > first;  // this warpgroup had a tile
-  float* buf = reinterpret_cast<float*>(stages);                        // [2][128][64], 16-byte chunks swizzled
-  float2* ml = reinterpret_cast<float2*>(stages + 2 * TM * 64 * 4);  // [2][128]
+  // The rows go out through the stages, which nothing reads any more: a thread has
+  // a row, a store to memory wants a row's bytes from consecutive lanes (32
+  // rows' 16 bytes a store took 5 us a CTA).  Two warpgroups on one row tile
+  // scale their O to the larger maximum and the sum is formed on the way out.
+  const bool have = w.T > first;  // this row tile (parity) had a key tile
+  float* buf = reinterpret_cast<float*>(stages);   // [2][128][D], 16-byte chunks swizzled
+  float2* ml = reinterpret_cast<float2*>(sm);      // [2][2][128], in Q's place
+  ml[tid] = make_float2(m, l);
+  named_sync(1, 512);
+  l = ml[g * 256 + r].y + ml[g * 256 + 128 + r].y;
   float f = have ? 1.f : 0.f;
   if (!w.wide) {
-    ml[g * TM + r] = make_float2(m, l);
-    named_sync(1, 256);
-    const float2 y = ml[(g ^ 1) * TM + r];
-    const float M = fmaxf(m, y.x);
+    const float m0 = ml[r].x, m1 = ml[256 + r].x, M = fmaxf(m0, m1);
+    const float l0 = ml[r].y + ml[128 + r].y, l1 = ml[256 + r].y + ml[384 + r].y;
     f *= ex2(m - M);
-    l = g ? y.y * ex2(y.x - M) + l * ex2(m - M) : l * ex2(m - M) + y.y * ex2(y.x - M);  // in one order for both
+    l = l0 * ex2(m0 - M) + l1 * ex2(m1 - M);
     m = M;
   }
   if (a.whole) f = l == 0.f ? 0.f : f / l;
   const bool none = !have || l == 0.f;
   const bool gone = abort_set(smem_u32(&s.abort));
-  const int lane = r & 31, warp = g * 4 + (r >> 5), cc = lane & 15;
-#pragma unroll 1
-  for (int ch = 0; ch < D / 64; ++ch) {
-    if (active) {
-      float* row = buf + (g * TM + r) * 64;
+  if (active) {
+    float* row = buf + (g * TM + r) * D;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t o[16];
-        if (have) {
-          get(oc + 64 * ch + 16 * c, o);
-          got(o);
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[e] = none ? 0u : __float_as_uint(__uint_as_float(o[e]) * f);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          *reinterpret_cast<uint4*>(row + (((4 * c + e) ^ (r & 7)) << 2)) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+    for (int c = 0; c < D / 32; ++c) {
+      uint32_t o[16];
+      if (have) {
+        get(oc + 16 * c, o);
+        got(o);
       }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[e] = none ? 0u : __float_as_uint(__uint_as_float(o[e]) * f);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<uint4*>(row + (((D / 8 * half + 4 * c + e) ^ (r & 7)) << 2)) =
+            make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
     }
-    named_sync(1, 256);
-#pragma unroll 4
-    for (int q = 2 * warp + (lane >> 4); q < w.nr && !gone; q += 16) {
-      const float* row = buf + q * 64 + ((cc ^ (q & 7)) << 2);
-      float4 y = *reinterpret_cast<const float4*>(row);
-      if (!w.wide) {
-        const float4 z = *reinterpret_cast<const float4*>(row + TM * 64);
-        y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
-      }
-      if (a.whole)
-        *reinterpret_cast<uint2*>(static_cast<bf16*>(a.O) + s.row[q] + 64 * ch + 4 * cc) =
-            make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
-      else
-        *reinterpret_cast<float4*>(a.part_o + s.row[q] * D + 64 * ch + 4 * cc) = y;
-    }
-    if (ch + 1 < D / 64) named_sync(1, 256);
   }
-  if (!a.whole && !gone && row < w.nr && (w.wide || g == 0)) a.part_ml[s.row[row]] = make_float2(m, l);
+  named_sync(1, 512);
+  constexpr int LPR = D / 4, RPW = 32 / LPR;  // lanes a row, rows a warp
+  const int cc = lane % LPR;
+#pragma unroll 4
+  for (int q = tid / LPR; q < w.nr && !gone; q += 16 * RPW) {
+    const float* row = buf + q * D + ((cc ^ (q & 7)) << 2);
+    float4 y = *reinterpret_cast<const float4*>(row);
+    if (!w.wide) {
+      const float4 z = *reinterpret_cast<const float4*>(row + TM * D);
+      y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
+    }
+    if (a.whole) {
+      const RowAt at = row_at(a, w, q);
+      *reinterpret_cast<uint2*>(static_cast<bf16*>(a.O) + at.b * a.osb + at.hq * a.osh + at.i * a.oss + 4 * cc) =
+          make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+    } else {
+      *reinterpret_cast<float4*>(a.part_o + ((int64_t)w.part * a.rows + s.row[q]) * D + 4 * cc) = y;
+    }
+  }
+  const int row = rt + r;
+  if (!a.whole && !gone && row < w.nr && !half && (w.wide || g == 0))
+    a.part_ml[(int64_t)w.part * a.rows + s.row[row]] = make_float2(m, l);
 }
 
 template <int D, int FMT>
@@ -696,7 +716,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   uint8_t* raw = sm + (2 + C::STAGES) * C::TILE;
   Bars& s = *reinterpret_cast<Bars*>(raw + C::RAW);
   const int tid = threadIdx.x, warp = tid >> 5;
-  constexpr int MMA_WARP = 8 + C::NPT / 32;
+  constexpr int MMA_WARP = 16 + C::NPT / 32;
   Item w = item_of(a);
   uint8_t* stages = sm + (w.wide ? 2 : 1) * C::TILE;
   const int ns = C::STAGES + (w.wide ? 0 : 1);
@@ -716,13 +736,13 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   } else if (tid >= 64 && tid < 66) {
     const int g = tid - 64, rows = w.wide ? w.nr - g * TM : w.nr;
     mbar_init(bar(s.sfull[g]), 1);
-    mbar_init(bar(s.pready[g]), (min(rows, TM) + 31) / 32);
+    mbar_init(bar(s.pready[g]), (min(rows, TM) + 31) / 32 * 2);
     mbar_init(bar(s.odone[g]), 1);
   } else if (tid >= 96 && tid < 98) {
     mbar_init(bar(s.turn[tid - 96]), 1);
     mbar_init(bar(s.drain[tid - 96]), 1);
   } else if (tid == 128) {
-    mbar_init(bar(s.qfull), C::NPT);
+    mbar_init(bar(s.qfull), 512);
     mbar_init(bar(s.stall), 1);
     s.abort = 0;
   }
@@ -735,10 +755,10 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   grid_dep_launch();  // after the barrier that publishes the tensor memory (see Launch)
   // (Moving registers from the producers to the softmax warps was slower with
   // codes: 93 against 90 us for a token at 128K.)
-  if (warp < 8) {
-    soften<D, FMT>(a, w, stages, s, warp >> 2, tid & 127);
+  if (warp < 16) {
+    soften<D, FMT>(a, w, sm, stages, s, tid);
   } else if (warp < MMA_WARP) {
-    produce<D, FMT>(a, w, smem_u32(sm), ring, smem_u32(raw), s, tid - 256);
+    produce<D, FMT>(a, w, ring, smem_u32(raw), s, tid - 512);
   } else {
     if (warp < MMA_WARP + 2) multiply<D, FMT>(a, w, smem_u32(sm), ring, s, warp - MMA_WARP);
     else if (!w.own) load_codes<D, FMT>(a, w, smem_u32(raw), s, warp - MMA_WARP - 2, tid & 31);
