@@ -288,35 +288,63 @@ __global__ void __launch_bounds__(kThreads<TR>, TR == 128 ? 1 : 2) simt_kernel(c
 
 // O of every query row from its parts: with M the largest m, the sum of
 // 2^(m - M) O over that of 2^(m - M) l.  A part without a key (l = 0) adds
-// nothing, and a row without any is 0.  D / 4 threads a row.
+// nothing, and a row without any is 0.  D / 4 threads hold a row's channels; GR
+// groups of them take every GR-th part (many parts one after the other were 30
+// us for one row) and the first puts the groups together, in their order.
 constexpr int JTH = 256;
-template <typename T, int D>
+template <typename T, int D, int GR>
 __global__ void __launch_bounds__(JTH) join_kernel(const __grid_constant__ PrefixArgs a) {
-  const int c = threadIdx.x % (D / 4);
-  const int64_t row = (int64_t)blockIdx.x * (JTH / (D / 4)) + threadIdx.x / (D / 4);
+  constexpr int LPR = D / 4;
+  __shared__ float4 so[GR > 1 ? JTH : 1];
+  __shared__ float2 sml[GR > 1 ? JTH / LPR : 1];
+  const int c = threadIdx.x % LPR, slot = threadIdx.x / LPR, gr = slot % GR;
+  const int64_t row = (int64_t)blockIdx.x * (JTH / LPR / GR) + slot / GR;
+  const bool ok = row < a.rows;
   grid_dep_wait();
   grid_dep_launch();
-  if (row >= a.rows) return;
-  const int parts = a.S + a.So;
-  float M = -FLT_MAX;
-  for (int j = 0; j < parts; ++j) {
-    const float2 ml = a.part_ml[j * a.rows + row];
-    if (ml.y != 0.f) M = fmaxf(M, ml.x);
+  const int parts = ok ? a.S + a.So : 0;
+  const float2* ml = a.part_ml + (ok ? row : 0);
+  const float* po = a.part_o + (ok ? row : 0) * D + 4 * c;
+  float M = -FLT_MAX, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int j = gr; j < parts; j += GR) {
+    const float2 x = ml[j * a.rows];
+    M = fmaxf(M, x.y != 0.f ? x.x : -FLT_MAX);
   }
-  float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int j = 0; j < parts; ++j) {
-    const float2 ml = a.part_ml[j * a.rows + row];
-    if (ml.y == 0.f) continue;
-    const float w = exp2f(ml.x - M);
-    const float4 v = *reinterpret_cast<const float4*>(a.part_o + (j * a.rows + row) * D + 4 * c);
-    l = fmaf(w, ml.y, l);
-    o[0] = fmaf(w, v.x, o[0]); o[1] = fmaf(w, v.y, o[1]); o[2] = fmaf(w, v.z, o[2]); o[3] = fmaf(w, v.w, o[3]);
+#pragma unroll 4
+  for (int j = gr; j < parts; j += GR) {
+    const float2 x = ml[j * a.rows];
+    const float4 v = *reinterpret_cast<const float4*>(po + j * a.rows * D);
+    const float w = x.y != 0.f ? exp2f(x.x - M) : 0.f;
+    l = fmaf(w, x.y, l);
+    o.x = fmaf(w, v.x, o.x); o.y = fmaf(w, v.y, o.y); o.z = fmaf(w, v.z, o.z); o.w = fmaf(w, v.w, o.w);
   }
+  if (GR > 1) {
+    so[threadIdx.x] = o;
+    if (c == 0) sml[slot] = make_float2(M, l);
+    __syncthreads();
+    if (gr == 0) {
+      const float2* g = sml + slot;
+#pragma unroll
+      for (int j = 1; j < GR; ++j) M = fmaxf(M, g[j].y != 0.f ? g[j].x : -FLT_MAX);
+      l = 0.f;
+      o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int j = 0; j < GR; ++j) {
+        const float w = g[j].y != 0.f ? exp2f(g[j].x - M) : 0.f;
+        const float4 v = so[threadIdx.x + j * LPR];
+        l = fmaf(w, g[j].y, l);
+        o.x = fmaf(w, v.x, o.x); o.y = fmaf(w, v.y, o.y); o.z = fmaf(w, v.z, o.z); o.w = fmaf(w, v.w, o.w);
+      }
+    }
+  }
+  if (!ok || gr) return;
   const int64_t b = row / (a.q * a.H * a.G), hq = row / a.q % (a.H * a.G), i = row % a.q;
   T* op = static_cast<T*>(a.O) + b * a.osb + hq * a.osh + i * a.oss + 4 * c;
-  const float inv = 1.f / l;
+  const float inv = l == 0.f ? 0.f : 1.f / l, y[4] = {o.x, o.y, o.z, o.w};
 #pragma unroll
-  for (int e = 0; e < 4; ++e) from_f32(op[e], l == 0.f ? 0.f : o[e] * inv);
+  for (int e = 0; e < 4; ++e) from_f32(op[e], l == 0.f ? 0.f : y[e] * inv);
 }
 
 // Rows a CTA of the fp32 kernel: enough for the unit's rows, up to 128.
@@ -351,8 +379,11 @@ cudaError_t launch_parts(const PrefixPlan& p, cudaStream_t s) {
 
 template <typename T, int D>
 cudaError_t launch_join(const PrefixArgs& a, cudaStream_t s) {
-  const int per = JTH / (D / 4);
-  return Launch(dim3((unsigned)((a.rows + per - 1) / per)), JTH, 0, s)(join_kernel<T, D>, a);
+  constexpr int SLOTS = JTH / (D / 4);
+  const bool many = a.S + a.So > 4;
+  const int per = many ? 1 : SLOTS;
+  Launch l(dim3((unsigned)((a.rows + per - 1) / per)), JTH, 0, s);
+  return many ? l(join_kernel<T, D, SLOTS>, a) : l(join_kernel<T, D, 1>, a);
 }
 
 }  // namespace
@@ -374,17 +405,32 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   const int tr = tc ? kPrefixTcRows : simt_rows(a);
   a.mt = (a.R + tr - 1) / tr;
   a.mto = (a.Ro + tr - 1) / tr;
-  // Splits: as many parts as fill the SMs once (one CTA an SM, two of the fp32
-  // kernel with few rows), of at least 256 keys each.
-  const int slots = tc || tr == 128 ? 152 : 304;
-  auto split = [&](int64_t units, int keys) {
+  // Parts: the count with the least estimated time, in us: waves of CTAs, each a
+  // set-up and its key tiles, and the parts' way through memory to the joining
+  // kernel.  Measured at d = 128: a CTA's set-up, first tile and way out 7 us, a
+  // key tile 1.5 us with a row tile of 256 (products) or of 128 (the rows' bytes),
+  // a 64-key tile of the fp32 kernel 13 us for 128 rows; parts move at 5 TB/s.
+  const int tk = tc ? kPrefixTcRows / 2 : TK, slots = tc || tr == 128 ? 152 : 304;
+  const double wide = a.d / 128.0, tile_us = wide * (tc ? 1.5 : tr == 128 ? 13.0 : tr == 64 ? 10.0 : 4.0);
+  const double set_up = tc ? 7.0 : 4.0, part_us = (double)a.rows * a.d * 8 / 5e6;
+  auto split = [&](int64_t units, int keys, double move) {
     if (!keys) return 0;
-    const int64_t most = std::max(1, (keys + 255) / 256);
-    return (int)std::min(most, std::max<int64_t>(1, slots / units));
+    const int tiles = (keys + tk - 1) / tk;
+    int best = 1;
+    double least = 1e30;
+    // The counts that fill one to four waves, and halves of them.
+    for (int w = 1; w <= 4; ++w)
+      for (int64_t most = std::max<int64_t>(1, w * slots / units); most; most /= 2) {
+        const int per = (tiles + (int)std::min<int64_t>(most, tiles) - 1) / (int)std::min<int64_t>(most, tiles);
+        const int S = (tiles + per - 1) / per;
+        const double t = (double)((units * S + slots - 1) / slots) * (set_up + per * tile_us) + (S > 1 || n_g ? S * move : 0.0);
+        if (t < least) { least = t; best = S; }
+      }
+    return best;
   };
-  a.S = split((int64_t)a.P * a.H * a.mt, k);
+  a.S = split((int64_t)a.P * a.H * a.mt, k, part_us);
   p.fold = tc && n_g > 0 && n_g <= kPrefixFold;
-  a.So = p.fold ? 0 : split((int64_t)a.B * a.H * a.mto, n_g);
+  a.So = p.fold ? 0 : split((int64_t)a.B * a.H * a.mto, n_g, part_us);
   p.parts = a.S + a.So;
   a.by_H = make_fastdiv(a.H);
   a.by_S = make_fastdiv(std::max(1, a.S));
