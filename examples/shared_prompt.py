@@ -1,0 +1,101 @@
+"""Several answers to one long prompt, from an 8-bit or 4-bit cache.
+
+A prompt's keys and values are turned into the filter's pyramid and a quantised
+cache once, and the 16-bit tensors can go.  Every denoising step then selects
+prompt rows for all answers together (their query blocks form one group a key
+head, so the selection is one row list a head) and attends each answer's block
+to the selected rows of the quantised cache, read once for all, and to the
+answer's own rows.  A stretch of the prompt that changed is quantised into its
+place.
+
+    python examples/shared_prompt.py [--tokens 32768] [--answers 4] [--heads 32] [--four-bit]
+"""
+from __future__ import annotations
+
+import argparse
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+from paper_2606_00724_gb300 import wf  # noqa: E402
+
+
+class SharedPrompt:
+    """One prompt's keys and values [H, n, d] (bf16), kept quantised with the pyramid of its keys."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, levels: int, kept: int, fmt: int):
+        H, n, d = K.shape
+        self.levels, self.fmt = levels, fmt
+        self.keep = wf.wf_default_schedule(n, levels, kept)
+        if self.keep[0] != 2 * self.keep[1]:
+            raise ValueError("an odd count would score raw keys, which are not kept")
+        self.pyramid = torch.empty(H, n - (n >> levels), d, dtype=K.dtype, device=K.device)
+        wf.wf_dwt_build(K[None], levels, self.pyramid)
+        width = d // 2 if fmt == wf.WF_MXFP4 else d
+        self.Kc, self.Vc = (torch.empty(1, H, n, width, dtype=torch.uint8, device=K.device) for _ in range(2))
+        self.Ks, self.Vs = (torch.empty(wf.wf_scales_bytes(self.Kc, fmt), dtype=torch.uint8, device=K.device)
+                            for _ in range(2))
+        self.write(K, V, 0)
+        # The filter takes the keys for their shape; with every kept pair of tokens selected it reads the pyramid
+        # alone, so one head's worth of memory stands for all of them.
+        self.shape = K.new_empty(1, 1, n, d).expand(1, H, n, d)
+        self.idx = torch.empty(H, self.keep[0], dtype=torch.int32, device=K.device)
+        self.ws = self.attn_ws = None
+
+    def write(self, K: torch.Tensor, V: torch.Tensor, pos: int) -> None:
+        """Rows [pos, pos + count) of the cache from K, V [H, count, d].  (The pyramid of a changed stretch is
+        rebuilt from its rows by the caller that still has them.)"""
+        wf.wf_cache_quantize(K[None], V[None], self.Kc, self.Ks, self.Vc, self.Vs, self.fmt, pos)
+
+    def attend(self, Q: torch.Tensor, Kg: torch.Tensor, Vg: torch.Tensor, gen_len=None) -> torch.Tensor:
+        """Q [H, B, q, d]: the query blocks of B answers, head by head; Kg, Vg [B, H, ng, d] the answers' own rows,
+        of which the first gen_len[b] count.  The answers' outputs, [H, B, q, d]."""
+        H, B, q, d = Q.shape
+        grouped, by_answer = Q.view(1, H * B, q, d), Q.transpose(0, 1)
+        O = torch.empty_like(Q)
+        if self.ws is None:
+            size = wf.wf_filter_workspace_bytes(grouped, self.shape, self.levels, self.keep)
+            self.ws = torch.zeros(size, dtype=torch.uint8, device=Q.device)
+            size = wf.wf_prefix_attn_workspace_bytes(by_answer, self.Kc, self.keep[0], Kg.shape[2], fmt=self.fmt)
+            self.attn_ws = torch.zeros(size, dtype=torch.uint8, device=Q.device)
+        wf.wf_filter(grouped, self.pyramid, self.shape, self.levels, self.keep, self.idx, self.ws)
+        wf.wf_prefix_attn(by_answer, self.Kc, self.Vc, self.keep[0], Kg, Vg, O.transpose(0, 1), self.attn_ws,
+                          idx=self.idx, gen_len=gen_len, Ks=self.Ks, Vs=self.Vs, fmt=self.fmt)
+        return O
+
+
+def main(argv=None) -> dict:
+    p = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    p.add_argument("--tokens", type=int, default=32768)
+    p.add_argument("--answers", type=int, default=4)
+    p.add_argument("--heads", type=int, default=32)
+    p.add_argument("--steps", type=int, default=3)
+    p.add_argument("--four-bit", action="store_true")
+    a = p.parse_args(argv)
+    n, B, H, q, d, levels = a.tokens, a.answers, a.heads, 32, 128, 4
+    fmt = wf.WF_MXFP4 if a.four_bit else wf.WF_MXFP8
+    g = torch.Generator(device="cuda").manual_seed(0)
+
+    def draw(*shape):
+        return torch.randn(*shape, generator=g, device="cuda").bfloat16()
+    K, V = draw(H, n, d), draw(H, n, d)
+    prompt = SharedPrompt(K, V, levels, n // 16, fmt)
+    Kg, Vg = draw(B, H, q, d), draw(B, H, q, d)
+    gen_len = torch.tensor([q - b % 3 for b in range(B)], dtype=torch.int32, device="cuda")
+    for _ in range(a.steps):
+        Q = draw(H, B, q, d)
+        O = prompt.attend(Q, Kg, Vg, gen_len)
+    wf.wf_workspace_status(prompt.ws)
+    wf.wf_workspace_status(prompt.attn_ws)
+    kept = prompt.Kc.nbytes * 2 + prompt.Ks.nbytes * 2
+    result = {"cache_bytes": kept, "bf16_bytes": K.nbytes + V.nbytes, "rows": prompt.keep[0], "Q": Q, "O": O,
+              "K": K, "V": V, "Kg": Kg, "Vg": Vg, "gen_len": gen_len, "prompt": prompt}
+    print(f"{n} tokens, {H} heads: {kept / 1e6:.1f} MB quantised, {result['bf16_bytes'] / 1e6:.1f} MB in bf16; "
+          f"{B} answers attend to {prompt.keep[0]} rows a head")
+    return result
+
+
+if __name__ == "__main__":
+    main()

@@ -296,3 +296,29 @@ def test_every_code_and_scale_is_read_exactly(dtype, fmt):
     got = O.double().cpu()[:, :, 0]
     assert torch.equal(got[normal], want[normal])
     assert normal.double().mean() > 0.9
+
+
+@pytest.mark.parametrize("cache", [None, "mxfp8"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B", [2, 8])
+def test_nan_key_reaches_every_row_that_attends_to_it(B, dtype, cache):
+    # A key row with a NaN (a NaN scale in a quantised prompt) makes every query row of its key head NaN and no other.
+    c = Case(B, 2, 2, 1, 32, 128, 500, 10, dtype, cache, seed=15)
+    before = c.run()
+    if cache:
+        c.Ks[0, 1, 300, 2] = 255
+    else:
+        c.K[0, 1, 300, 70] = float("nan")
+    after = c.run()
+    assert torch.isnan(after[:B // 2, 1]).all()
+    assert torch.equal(after[B // 2:], before[B // 2:]) and torch.equal(after[:, 0], before[:, 0])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rising_logits(dtype):
+    # Keys ordered so that a row's maximum rises from tile to tile, by little and by much, up to logits of about 80.
+    c = Case(3, 1, 1, 1, 64, 128, 1100, 100, dtype, seed=16)
+    rise = torch.linspace(0, 1, 1100).pow(3) * 7 + 0.3
+    c.K[0, 0] = (f := c.Q[0, 0, 0].float())[None] / f.norm() * 11.3 * rise.cuda()[:, None] + 0.05 * c.K[0, 0].float()
+    c.K64 = f64(c.K)
+    c.check()
