@@ -402,7 +402,8 @@ def wf_prefix_attn(Q, K, V, k: int, Kg, Vg, O, ws, idx=None, prefix_len=None, ge
     Kg, Vg [B, H, n_g, d] (see the C header).  fmt (WF_MXFP8, WF_MXFP4): K and V
     are codes, with scales Ks and Vs."""
     _on_gpu(Q, K, V, Kg, Vg, O, ws, idx, prefix_len, gen_len, Ks, Vs)
-    dq, do = desc(Q), desc(O)
+    dq = desc(Q)
+    do = dq if O.stride() == Q.stride() and O.shape == Q.shape and O.dtype == Q.dtype else desc(O)
     dk = _pair_desc(K, V, "K and V", fmt)
     dg = _pair_desc(Kg, Vg, "Kg and Vg") if Kg is not None else None
     if fmt is not None:
