@@ -406,31 +406,53 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   a.mt = (a.R + tr - 1) / tr;
   a.mto = (a.Ro + tr - 1) / tr;
   // Parts: the count with the least estimated time, in us: waves of CTAs, each a
-  // set-up and its key tiles, and the parts' way through memory to the joining
-  // kernel.  Measured at d = 128: a CTA's set-up, first tile and way out 7 us, a
-  // key tile 1.5 us with a row tile of 256 (products) or of 128 (the rows' bytes),
-  // a 64-key tile of the fp32 kernel 13 us for 128 rows; parts move at 5 TB/s.
+  // set-up and its key tiles, the parts' way through memory and, without own rows,
+  // the joining kernel.  Measured at d = 128: a call of one tile 6 us, a key tile 1.5
+  // with a row tile of 256 (products) or of 128 (the rows' bytes), a 64-key tile
+  // of the fp32 kernel 13 for 128 rows; parts move at 5 TB/s; joining 2.5.
   const int tk = tc ? kPrefixTcRows / 2 : TK, slots = tc || tr == 128 ? 152 : 304;
   const double wide = a.d / 128.0, tile_us = wide * (tc ? 1.5 : tr == 128 ? 13.0 : tr == 64 ? 10.0 : 4.0);
-  const double set_up = tc ? 7.0 : 4.0, part_us = (double)a.rows * a.d * 8 / 5e6;
-  auto split = [&](int64_t units, int keys, double move) {
+  const double set_up = tc ? 5.0 : 4.0, part_us = (double)a.rows * a.d * 8 / 5e6;
+  auto split = [&](int64_t units, int keys, double* least) {
+    *least = 0.0;
     if (!keys) return 0;
     const int tiles = (keys + tk - 1) / tk;
     int best = 1;
-    double least = 1e30;
+    *least = 1e30;
     // The counts that fill one to four waves, and halves of them.
     for (int w = 1; w <= 4; ++w)
       for (int64_t most = std::max<int64_t>(1, w * slots / units); most; most /= 2) {
         const int per = (tiles + (int)std::min<int64_t>(most, tiles) - 1) / (int)std::min<int64_t>(most, tiles);
         const int S = (tiles + per - 1) / per;
-        const double t = (double)((units * S + slots - 1) / slots) * (set_up + per * tile_us) + (S > 1 || n_g ? S * move : 0.0);
-        if (t < least) { least = t; best = S; }
+        const double t = (double)((units * S + slots - 1) / slots) * (set_up + per * tile_us) +
+                         (S > 1 || n_g ? S * part_us : 0.0) + (S > 1 && !n_g ? 2.5 : 0.0);
+        if (t < *least) { *least = t; best = S; }
       }
     return best;
   };
-  a.S = split((int64_t)a.P * a.H * a.mt, k, part_us);
+  double prompt_us, own_us;
+  a.S = split((int64_t)a.P * a.H * a.mt, k, &prompt_us);
   p.fold = tc && n_g > 0 && n_g <= kPrefixFold;
-  a.So = p.fold ? 0 : split((int64_t)a.B * a.H * a.mto, n_g, part_us);
+  a.So = p.fold ? 0 : split((int64_t)a.B * a.H * a.mto, n_g, &own_us);
+  // Room for the parts, whether or not the call below does without them.
+  const int kept = a.S + a.So == 1 && !p.fold ? 0 : a.S + a.So;
+  // Prompt rows that every sequence attends to for itself, where its own rows are
+  // (one launch): a 64-key tile takes 1.25 us, or its bytes for all blocks of
+  // query rows at the 2.4 TB/s that they come out of L2 with.  Measured, both ways:
+  // 4 heads' tokens, 128 rows and 32 own ones 6.0 against 9.5 us, 400 and 32 10.8
+  // against 10.1; blocks of 32 rows of 4 sequences and 16 heads on 128 rows 7.3
+  // against 12.8, of 32 sequences on 400 rows 36 against 26.
+  if (tc && p.fmt == WF_BF16 && k > 0 && n_g <= kPrefixFold) {
+    auto direct = [&](int keys) {
+      const double blocks = (double)a.B * a.H * ((a.Ro + prefix_own_rows(a, 0, keys) - 1) / prefix_own_rows(a, 0, keys));
+      return ((keys + 63) / 64) * std::max(1.25, blocks * 256 * a.d / 2.4e6);
+    };
+    if (2.6 + direct(k + n_g) < prompt_us + (n_g ? 3.2 + direct(n_g) : 0.0)) {
+      a.direct = 1;
+      a.S = a.So = 0;
+      p.fold = true;
+    }
+  }
   p.parts = a.S + a.So;
   a.by_H = make_fastdiv(a.H);
   a.by_S = make_fastdiv(std::max(1, a.S));
@@ -439,7 +461,6 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   a.by_mto = make_fastdiv(a.mto);
   a.whole = p.parts == 1 && !p.fold;
   p.off_ml = 256;
-  const int kept = a.whole ? 0 : p.parts;
   p.off_o = align_up(p.off_ml + sizeof(float2) * (size_t)a.rows * kept, 256);
   p.total = p.off_o + sizeof(float) * (size_t)a.rows * a.d * kept;
   return p;

@@ -35,6 +35,7 @@ struct PrefixArgs {
   int S, So;      // parts of the prompt, of the own rows
   int mt, mto;    // row tiles of a prompt unit, of an own unit
   int ob;         // query rows a CTA where the own rows are folded in
+  int direct;     // the prompt's rows are attended there too (S = 0)
   int whole;      // a part is the whole softmax: O goes out as it is
   int64_t rows;   // B Hq q
   float* part_o;  // [parts][rows][d], rows in [B, Hq, q] order
@@ -60,6 +61,8 @@ struct PrefixPlan {
 };
 PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g);
 cudaError_t launch_prefix(const PrefixPlan& p, cudaStream_t s);
+// Query rows a CTA of that kernel for S parts and so many keys.
+int prefix_own_rows(const PrefixArgs& a, int S, int keys);
 cudaError_t launch_prefix_own(const PrefixPlan& p, cudaStream_t s);  // own rows and the joining of parts, bf16
 cudaError_t launch_prefix_tc(const PrefixPlan& p, cudaStream_t s);  // the parts (or O) of bf16 queries
 

@@ -7,6 +7,8 @@
 // a small part of a 128-row tensor-memory tile and would pay its set-up, about
 // 4 us a CTA with one CTA an SM; warp-level products (m16n8k16, fp32
 // accumulators) keep S and O in registers, and four CTAs share an SM.
+// Few prompt rows are attended here too, by every sequence for itself: one launch
+// instead of two (see plan_prefix).
 // The softmax is that of the prompt's kernel (base 2, running maximum), so what
 // the warps found and the prompt's parts are put together with one set of
 // weights 2^(m - M), and O is written here.
@@ -56,8 +58,8 @@ __device__ __forceinline__ uint32_t at(int r, int ch) { return (uint32_t)(r * (2
 // Query rows; one or two stages of a K and a V tile, whose place the warps' O
 // take; the parts' m and l, then their weights.
 template <int D, int WR>
-size_t own_smem(int rows, int S, int ng) {
-  const size_t q = 16 * WR * D * 2, stages = (ng > KT ? 4 : 2) * KT * D * 2;
+size_t own_smem(int rows, int S, int keys) {
+  const size_t q = 16 * WR * D * 2, stages = (keys > KT ? 4 : 2) * KT * D * 2;
   const size_t o = (4 / WR) * 16 * WR * (D + 4) * sizeof(float);
   return q + (stages > o ? stages : o) + (size_t)rows * (S + 4 / WR) * sizeof(float2);
 }
@@ -70,7 +72,7 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
   uint8_t* sq = smem;
   uint8_t* st = smem + RB * D * 2;
   float* so = reinterpret_cast<float*>(st);                      // [WK][RB][PO]
-  const size_t room = max((size_t)(a.ng > KT ? 4 : 2) * TILE, WK * RB * PO * sizeof(float));
+  const size_t room = max((size_t)(a.ng + (a.direct ? a.k : 0) > KT ? 4 : 2) * TILE, WK * RB * PO * sizeof(float));
   float2* sml = reinterpret_cast<float2*>(st + room);            // [a.ob][WK + S]: m and l, then the weight
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rw = warp % WR, kw = warp / WR;
   const int nb = (a.Ro + a.ob - 1) / a.ob, u = blockIdx.x / nb, r0 = (blockIdx.x % nb) * a.ob, nr = min(a.ob, a.Ro - r0);
@@ -85,7 +87,8 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
     row_flat[tid] = flat_row(a, w);
   }
   grid_dep_wait();
-  const int nk = own_count(a, b);
+  // Keys: the prompt's rows where they are attended here, then the own rows.
+  const int p = b / a.each, np = a.direct ? prompt_count(a, p) : 0, nk = np + own_count(a, b);
   __syncthreads();
   // The parts' m and l and the query rows are on their way first: neither waits
   // for the length.
@@ -94,6 +97,8 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
       cp_async8(smem_u32(sml + r * NP + WK + j), a.part_ml + j * a.rows + row_flat[r]);
   const bf16* K = static_cast<const bf16*>(a.Kg) + b * a.gsb + h * a.gsh;
   const bf16* V = static_cast<const bf16*>(a.Vg) + b * a.gsb + h * a.gsh;
+  const int64_t prompt = p * a.ksb + h * a.ksh;
+  const int32_t* idx = a.idx ? a.idx + (int64_t)(p * a.H + h) * a.k : nullptr;
 
   auto fetch = [&](int t) {
     if (t * KT < nk) {
@@ -101,14 +106,26 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
 #pragma unroll
       for (int e = tid; e < KT * CH; e += NTH) {
         const int r = e / CH, ch = e % CH, j = t * KT + r;
-        const int64_t o = j < nk ? (int64_t)j * a.gss + ch * 8 : 0;
-        cp_async16_zfill(base + at<D>(r, ch), K + o, j < nk);
-        cp_async16_zfill(base + TILE + at<D>(r, ch), V + o, j < nk);
+        const bf16 *ka = K, *va = V;
+        if (j < np) {
+          const int64_t o = prompt + (idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j) * a.kss + ch * 8;
+          ka = static_cast<const bf16*>(a.K) + o;
+          va = static_cast<const bf16*>(a.V) + o;
+        } else if (j < nk) {
+          const int64_t o = (int64_t)(j - np) * a.gss + ch * 8;
+          ka += o;
+          va += o;
+        } else if (np) {  // no address is read past the last key; one that exists is given
+          ka = static_cast<const bf16*>(a.K) + prompt;
+          va = static_cast<const bf16*>(a.V) + prompt;
+        }
+        cp_async16_zfill(base + at<D>(r, ch), ka, j < nk);
+        cp_async16_zfill(base + TILE + at<D>(r, ch), va, j < nk);
       }
     }
     cp_async_commit();
   };
-  if (a.ng > 0) {
+  if (a.ng > 0 || a.direct) {
     for (int e = tid; e < RB * CH; e += NTH) {
       const int r = e / CH, ch = e % CH;
       cp_async16_zfill(smem_u32(sq) + at<D>(r, ch), static_cast<const bf16*>(a.Q) + row_q[min(r, nr - 1)] + ch * 8,
@@ -269,25 +286,33 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
 }
 
 template <int D, int WR>
-cudaError_t launch(PrefixArgs a, cudaStream_t s) {
-  // Query rows a CTA: all that its warps hold, fewer (down to 4) where that
-  // leaves SMs without a CTA and the parts' bytes to the others.
-  a.ob = 16 * WR;
-  const int64_t units = (int64_t)a.B * a.H;
-  while (a.ob > 4 && units * ((a.Ro + a.ob - 1) / a.ob) < 2 * sm_count()) a.ob /= 2;
-  const size_t smem = own_smem<D, WR>(a.ob, a.S, a.ng);
+cudaError_t launch(const PrefixArgs& a, cudaStream_t s) {
+  const size_t smem = own_smem<D, WR>(a.ob, a.S, a.ng + (a.direct ? a.k : 0));
   const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(own_join_kernel<D, WR>), smem);
   if (e != cudaSuccess) return e;
-  const int64_t blocks = units * ((a.Ro + a.ob - 1) / a.ob);
+  const int64_t blocks = (int64_t)a.B * a.H * ((a.Ro + a.ob - 1) / a.ob);
   return Launch(dim3((unsigned)blocks), NTH, smem, s)(own_join_kernel<D, WR>, a);
 }
 
 template <int D>
-cudaError_t launch_rows(const PrefixArgs& a, cudaStream_t s) {
-  return a.Ro <= 16 ? launch<D, 1>(a, s) : a.Ro <= 32 ? launch<D, 2>(a, s) : launch<D, 4>(a, s);
+cudaError_t launch_rows(PrefixArgs a, cudaStream_t s) {
+  a.ob = prefix_own_rows(a, a.S, a.ng + (a.direct ? a.k : 0));
+  return a.ob <= 16 ? launch<D, 1>(a, s) : a.ob == 32 ? launch<D, 2>(a, s) : launch<D, 4>(a, s);
 }
 
 }  // namespace
+
+// The unit's rows, up to 64; blocks of 16 where fewer CTAs than SMs were left; down
+// to 4 where the parts are more bytes than the keys that every block reads
+// again (one token of 28 heads on 4, 37 parts: 15 -> 6 us).
+int prefix_own_rows(const PrefixArgs& a, int S, int keys) {
+  constexpr int sms = 152;
+  int ob = a.Ro <= 16 ? 16 : a.Ro <= 32 ? 32 : 64;
+  auto blocks = [&] { return (int64_t)a.B * a.H * ((a.Ro + ob - 1) / ob); };
+  while (ob > 16 && blocks() < sms) ob /= 2;
+  while (ob > 4 && blocks() < 2 * sms && ob * S > keys) ob /= 2;
+  return ob;
+}
 
 cudaError_t launch_prefix_own(const PrefixPlan& p, cudaStream_t s) {
   return p.a.d == 128 ? launch_rows<128>(p.a, s) : launch_rows<64>(p.a, s);
