@@ -432,8 +432,9 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   };
   double prompt_us, own_us;
   a.S = split((int64_t)a.P * a.H * a.mt, k, &prompt_us);
-  p.fold = tc && n_g > 0 && n_g <= kPrefixFold;
-  a.So = p.fold ? 0 : split((int64_t)a.B * a.H * a.mto, n_g, &own_us);
+  const int64_t own = (int64_t)a.B * a.H * a.mto;
+  p.fold = tc && n_g > 0 && own >= kPrefixOwn && n_g <= std::min<int64_t>(2 * own, a.Ro <= 16 ? 512 : 256);
+  a.So = p.fold ? 0 : split(own, n_g, &own_us);
   // Room for the parts, whether or not the call below does without them.
   const int kept = a.S + a.So == 1 && !p.fold ? 0 : a.S + a.So;
   // Prompt rows that every sequence attends to for itself, where its own rows are
@@ -442,12 +443,12 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   // 4 heads' tokens, 128 rows and 32 own ones 6.0 against 9.5 us, 400 and 32 10.8
   // against 10.1; blocks of 32 rows of 4 sequences and 16 heads on 128 rows 7.3
   // against 12.8, of 32 sequences on 400 rows 36 against 26.
-  if (tc && p.fmt == WF_BF16 && k > 0 && n_g <= kPrefixFold) {
+  if (tc && p.fmt == WF_BF16 && k > 0 && k + n_g <= 1024) {
     auto direct = [&](int keys) {
       const double blocks = (double)a.B * a.H * ((a.Ro + prefix_own_rows(a, 0, keys) - 1) / prefix_own_rows(a, 0, keys));
       return ((keys + 63) / 64) * std::max(1.25, blocks * 256 * a.d / 2.4e6);
     };
-    if (2.6 + direct(k + n_g) < prompt_us + (n_g ? 3.2 + direct(n_g) : 0.0)) {
+    if (2.6 + direct(k + n_g) < prompt_us + (p.fold ? 3.2 + direct(n_g) : n_g ? 3.5 : 0.0)) {
       a.direct = 1;
       a.S = a.So = 0;
       p.fold = true;

@@ -46,9 +46,14 @@ struct PrefixArgs {
   int stall;             // test-only: its first wait is on a barrier that nothing completes
 };
 
-// Own rows up to which they are attended where the parts are joined, a CTA a
-// block of query rows; more are ranges of their own for the prompt's kernel.
-constexpr int kPrefixFold = 512;
+// With at least so many units of own rows, and not too many rows for them, they are
+// attended where the parts are joined; else they are units of the prompt's kernel, where
+// few of them fit beside the prompt's.  Measured in us, joined against units: 16
+// tokens' units of 100 rows 14.5, 11.5; 64 of 65 rows 21.0, 22.6, of 300 rows 34, 25;
+// 64 of 32 query rows and 32 own rows 14.4, 19.1; 128 of those 32.7, 39.9; 1024
+// tokens' units of 100 rows 47, 72, of 500 rows 81, 91, of 1000 rows 123, 120; 512
+// units of 32 query rows and 300 own rows 103, 95.
+constexpr int kPrefixOwn = 64;
 constexpr int kPrefixTcRows = 256;  // query rows a CTA of the tensor-core kernel
 
 // The workspace of a call: the status word, then the parts.
