@@ -753,7 +753,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   tc_fence_after();
   grid_dep_launch();  // after the barrier that publishes the tensor memory (see Launch)
   // (Moving registers from the producers to the softmax warps was slower with
-  // codes: 93 against 88 us for a token at 128K.)
+  // codes: 93 against 88-90 us for a token at 128K.)
   if (warp < 16) {
     soften<D, FMT>(a, w, sm, stages, s, tid);
   } else if (warp < MMA_WARP) {
