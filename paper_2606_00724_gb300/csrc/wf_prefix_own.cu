@@ -214,8 +214,11 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
     l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
     const int r = rw * 16 + (lane >> 2) + 8 * i;
     float* row = so + (kw * RB + r) * PO + 2 * (lane & 3);
+    // Without weight, O is 0 x V, which is NaN where V is not finite.
+    const bool none = l[i] == 0.f;
 #pragma unroll
-    for (int c = 0; c < D / 8; ++c) *reinterpret_cast<float2*>(row + 8 * c) = make_float2(o[c][2 * i], o[c][2 * i + 1]);
+    for (int c = 0; c < D / 8; ++c)
+      *reinterpret_cast<float2*>(row + 8 * c) = none ? make_float2(0.f, 0.f) : make_float2(o[c][2 * i], o[c][2 * i + 1]);
     if ((lane & 3) == 0 && r < nr) sml[r * (WK + a.S) + kw] = make_float2(m[i], l[i]);
   }
   __syncthreads();
