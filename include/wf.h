@@ -439,6 +439,7 @@ wf_status wf_cache_dequantize(const void* Kc, const void* Ks, const void* Vc, co
  * rows that attend to its row only.
  * bf16 queries run on the tensor cores, fp32 queries in fp32 arithmetic.  The
  * same inputs give the same bits.
+ * B Hq q, k and n_g below 2^30 each, else WF_ERR_UNSUPPORTED (n may be longer).
  * ws: device scratch of at least wf_prefix_attn_workspace_bytes() bytes,
  * 256-byte aligned; its first 4 bytes are wf_filter's status word (zero it
  * once, read it with wf_workspace_status).

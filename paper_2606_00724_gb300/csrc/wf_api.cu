@@ -558,6 +558,8 @@ wf_status check_prefix_args(const wf_tensor* q, const wf_tensor* kv, int k, int 
   if (kv->head_dim != q->head_dim || q->heads % kv->heads || q->batch % kv->batch) return WF_ERR_SHAPE;
   if (k < 0 || k > kv->seq || n_g < 0) return WF_ERR_INVALID_ARG;
   if (too_many_rows((int64_t)q->batch * q->heads, q->seq)) return WF_ERR_UNSUPPORTED;
+  // A range of keys ends at a multiple of its tiles, past the count.
+  if (too_many_rows(1, k) || too_many_rows(1, n_g)) return WF_ERR_UNSUPPORTED;
   return WF_OK;
 }
 
