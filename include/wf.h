@@ -442,7 +442,9 @@ wf_status wf_cache_dequantize(const void* Kc, const void* Ks, const void* Vc, co
  * B Hq q, k and n_g below 2^30 each, else WF_ERR_UNSUPPORTED (n may be longer).
  * ws: device scratch of at least wf_prefix_attn_workspace_bytes() bytes,
  * 256-byte aligned; its first 4 bytes are wf_filter's status word (zero it
- * once, read it with wf_workspace_status).
+ * once, read it with wf_workspace_status).  The size does not fall as B, P, H,
+ * G, q, k or n_g grows, so a workspace sized for the largest call of a dtype
+ * and head_dim serves the smaller ones.
  * ------------------------------------------------------------------------- */
 size_t wf_prefix_attn_workspace_bytes(const wf_tensor* q, const wf_tensor* kv, int k, int n_g);
 wf_status wf_prefix_attn(const void* Q, const wf_tensor* q, const void* K, const void* V, const wf_tensor* kv,

@@ -22,7 +22,9 @@ namespace {
 
 using namespace sm100;
 
-constexpr int TK = 64;  // keys a tile
+constexpr int TK = 64;      // keys a tile
+constexpr int kSms = 152;   // a wave of CTAs of the tensor-core kernel, one an SM
+constexpr int kWaves = 4;   // the parts of a call fill at most so many
 
 // How prompt rows are kept: like the own rows, or in codes.
 enum Cache { kPlain, kFp8, kFp4 };
@@ -410,7 +412,7 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   // the joining kernel.  Measured at d = 128: a call of one tile 6 us, a key tile 1.5
   // with a row tile of 256 (products) or of 128 (the rows' bytes), a 64-key tile
   // of the fp32 kernel 13 for 128 rows; parts move at 5 TB/s; joining 2.5.
-  const int tk = tc ? kPrefixTcRows / 2 : TK, slots = tc || tr == 128 ? 152 : 304;
+  const int tk = tc ? kPrefixTcRows / 2 : TK, slots = tc || tr == 128 ? kSms : 2 * kSms;
   const double wide = a.d / 128.0, tile_us = wide * (tc ? 1.5 : tr == 128 ? 13.0 : tr == 64 ? 10.0 : 4.0);
   const double set_up = tc ? 5.0 : 4.0, part_us = (double)a.rows * a.d * 8 / 5e6;
   auto split = [&](int64_t units, int keys, double* least) {
@@ -420,7 +422,7 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
     int best = 1;
     *least = 1e30;
     // The counts that fill one to four waves, and halves of them.
-    for (int w = 1; w <= 4; ++w)
+    for (int w = 1; w <= kWaves; ++w)
       for (int64_t most = std::max<int64_t>(1, w * slots / units); most; most /= 2) {
         const int per = (tiles + (int)std::min<int64_t>(most, tiles) - 1) / (int)std::min<int64_t>(most, tiles);
         const int S = (tiles + per - 1) / per;
@@ -435,8 +437,6 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   const int64_t own = (int64_t)a.B * a.H * a.mto;
   p.fold = tc && n_g > 0 && own >= kPrefixOwn && n_g <= std::min<int64_t>(2 * own, a.Ro <= 16 ? 512 : 256);
   a.So = p.fold ? 0 : split(own, n_g, &own_us);
-  // Room for the parts, whether or not the call below does without them.
-  const int kept = a.S + a.So == 1 && !p.fold ? 0 : a.S + a.So;
   // Prompt rows that every sequence attends to for itself, where its own rows are
   // (one launch): a 64-key tile takes 1.25 us, or its bytes for all blocks of
   // query rows at the 2.4 TB/s that they come out of L2 with.  Measured, both ways:
@@ -461,9 +461,19 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   a.by_mt = make_fastdiv(a.mt);
   a.by_mto = make_fastdiv(a.mto);
   a.whole = p.parts == 1 && !p.fold;
+  const int64_t kept = a.whole ? 0 : a.rows * p.parts;  // rows of parts
   p.off_ml = 256;
-  p.off_o = align_up(p.off_ml + sizeof(float2) * (size_t)a.rows * kept, 256);
-  p.total = p.off_o + sizeof(float) * (size_t)a.rows * a.d * kept;
+  p.off_o = align_up(p.off_ml + sizeof(float2) * (size_t)kept, 256);
+  // The size is the most that a call with as many keys and query rows, or fewer of
+  // any, can take, so that one workspace serves them all: S itself is not monotone.
+  // S units is at most kWaves slots where S > 1, and a unit has at most tr rows.
+  const int64_t most = (int64_t)kWaves * (tc ? kSms * kPrefixTcRows : 2 * kSms * 64);
+  auto room = [&](int keys, bool alone) {
+    const int64_t tiles = (keys + tk - 1) / tk;
+    return std::min(tiles * a.rows, alone ? most : std::max(a.rows, most));
+  };
+  const int64_t reserved = room(k, n_g == 0) + room(n_g, false);
+  p.total = align_up(p.off_ml + sizeof(float2) * (size_t)reserved, 256) + sizeof(float) * (size_t)reserved * a.d;
   return p;
 }
 
