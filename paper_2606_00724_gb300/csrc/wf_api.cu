@@ -9,6 +9,7 @@
 #include <utility>
 
 #include "wf_internal.cuh"
+#include "wf_mx.cuh"
 #include "wf_prefix.cuh"
 #include "wf_testing.h"
 

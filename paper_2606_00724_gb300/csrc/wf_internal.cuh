@@ -53,27 +53,6 @@ __device__ __forceinline__ float to_f32(bf16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ void from_f32(float& d, float x) { d = x; }
 __device__ __forceinline__ void from_f32(bf16& d, float x) { d = __float2bfloat16_rn(x); }
 
-// Quotient and remainder by an invariant divisor with a multiply and a shift
-// (Granlund and Montgomery, "Division by invariant integers using
-// multiplication", 1994): for 0 <= x < 2^31 and d >= 1, with
-// l = ceil(log2 d) and mul = floor(2^32 (2^l - d) / d) + 1,
-// x / d = (umulhi(mul, x) + x) >> l.
-struct FastDiv {
-  uint32_t d, mul, shift;
-};
-inline FastDiv make_fastdiv(uint32_t d) {
-  FastDiv f;
-  f.d = d;
-  uint32_t l = 0;
-  while ((1ull << l) < d) ++l;
-  f.shift = l;
-  f.mul = (uint32_t)((((1ull << l) - d) << 32) / d + 1);
-  return f;
-}
-__device__ __forceinline__ uint32_t fastdiv(uint32_t x, const FastDiv& f) {
-  return (__umulhi(f.mul, x) + x) >> f.shift;
-}
-
 // A [B, H, rows, d] row source: element (b, h, r, c) at
 // base + b*sb + h*sh + off + r*ss + c.
 struct RowSrc {
@@ -90,13 +69,6 @@ cudaError_t launch_dwt(const void* K, const wf_tensor& kv, int levels, void* coe
 // Cache update with the refresh of the touched pyramid blocks: see wf_cache_update.
 cudaError_t launch_cache_update(const void* Kn, const void* Vn, const wf_tensor& nt, void* K, void* V,
                                 const wf_tensor& kv, int64_t pos, int levels, void* coeffs, cudaStream_t s);
-
-// The quantised cache: see wf_cache_quantize, wf_cache_dequantize (Vn, Vo null: keys alone).
-cudaError_t launch_quantize(const void* Kn, const void* Vn, const wf_tensor& nt, void* Kc, void* Ks, void* Vc,
-                            void* Vs, const wf_tensor& kv, int64_t pos, cudaStream_t s);
-cudaError_t launch_dequantize(const void* Kc, const void* Ks, const void* Vc, const void* Vs, const wf_tensor& kv,
-                              const int32_t* idx, int64_t pos, void* Ko, void* Vo, const wf_tensor& out,
-                              cudaStream_t s);
 
 // Filter workspace plan for one call.  A unit is one (batch, KV head); its
 // query block is the qs rows of each of its G query heads, q = G qs rows.

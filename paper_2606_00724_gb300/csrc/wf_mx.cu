@@ -13,6 +13,7 @@
 // infinities and NaN above them.
 #include <algorithm>
 
+#include "wf_div.cuh"
 #include "wf_mx.cuh"
 #include "wf_sm100.cuh"
 

@@ -12,6 +12,13 @@ namespace wf {
 
 constexpr int kMxBlock = 32;
 
+// See wf_cache_quantize, wf_cache_dequantize (Vn, Vo null: keys alone).
+cudaError_t launch_quantize(const void* Kn, const void* Vn, const wf_tensor& nt, void* Kc, void* Ks, void* Vc,
+                            void* Vs, const wf_tensor& kv, int64_t pos, cudaStream_t s);
+cudaError_t launch_dequantize(const void* Kc, const void* Ks, const void* Vc, const void* Vs, const wf_tensor& kv,
+                              const int32_t* idx, int64_t pos, void* Ko, void* Vo, const wf_tensor& out,
+                              cudaStream_t s);
+
 // The scale byte of a block whose largest magnitude has the fp32 bits `top`:
 // with top = (1 + f) 2^E the least e with top <= 448 2^e is E - 8 for
 // 1 + f <= 1.75 and E - 7 above it (6 2^e: E - 2 for 1 + f <= 1.5, E - 1 above);

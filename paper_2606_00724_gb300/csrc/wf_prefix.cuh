@@ -1,6 +1,7 @@
 // Attention over shared prompts (wf_prefix_attn): what its kernels share.
 #pragma once
 
+#include "wf_div.cuh"
 #include "wf_internal.cuh"
 
 namespace wf {

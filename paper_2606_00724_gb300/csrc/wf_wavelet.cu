@@ -29,6 +29,7 @@
 #include <map>
 #include <mutex>
 
+#include "wf_div.cuh"
 #include "wf_internal.cuh"
 #include "wf_sm100.cuh"
 
