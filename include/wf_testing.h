@@ -1,6 +1,7 @@
 /* Test-only controls of libwf.  Not part of the library's interface: they
  * exist so that tests can drive the failure path of the tensor-core kernels'
- * bounded waits without faulting or hanging a GPU.
+ * bounded waits without faulting or hanging a GPU, and can tell which of its
+ * kernels a call takes.
  *
  * The fused step kernel (wf_step) and the tensor-core sparse attention
  * (wf_sparse_attn for bf16 / head_dim 128) wait on mbarriers for copies,
@@ -31,6 +32,20 @@ extern "C" {
  *   that drain work already issued keep the default bound.
  * Returns WF_ERR_INVALID_ARG for a negative limit. */
 wf_status wf_testing_set_wait_failure(int stall, long long wait_limit_cycles);
+
+/* How a wf_prefix_attn call of these shapes would be run (host only), so that a
+ * test can tell which kernels and loops it reaches. */
+typedef struct {
+  long long workspace_used; /* bytes of the workspace that the call writes, at most */
+  int prompt_parts;   /* ranges of the prompt's keys */
+  int own_parts;      /* ranges of the own rows that are units of the prompt's kernel */
+  int key_tile;       /* keys a tile of those ranges */
+  int prompt_rows;    /* query rows a CTA there, at most: 128 or fewer are one row tile */
+  int joined;         /* own rows are attended where the parts are joined */
+  int direct;         /* the prompt's rows are too */
+  int join_rows;      /* query rows a CTA of the joining kernel (0 unless joined) */
+} wf_testing_plan;
+wf_status wf_testing_prefix_plan(const wf_tensor* q, const wf_tensor* kv, int k, int n_g, wf_testing_plan* plan);
 
 #ifdef __cplusplus
 }

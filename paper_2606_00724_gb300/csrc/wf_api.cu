@@ -655,3 +655,20 @@ WF_API wf_status wf_testing_set_wait_failure(int stall, long long wait_limit_cyc
   g_test_stall.store(stall != 0, std::memory_order_relaxed);
   return WF_OK;
 }
+
+WF_API wf_status wf_testing_prefix_plan(const wf_tensor* q, const wf_tensor* kv, int k, int n_g,
+                                        wf_testing_plan* plan) {
+  const wf_status st = check_prefix_args(q, kv, k, n_g);
+  if (st != WF_OK) return st;
+  if (!plan) return WF_ERR_INVALID_ARG;
+  const wf::PrefixPlan p = wf::plan_prefix(*q, *kv, k, n_g);
+  plan->workspace_used = (long long)p.used;
+  plan->prompt_parts = p.a.S;
+  plan->own_parts = p.a.So;
+  plan->key_tile = p.tk;
+  plan->prompt_rows = p.tr < p.a.R ? p.tr : p.a.R;
+  plan->joined = p.fold;
+  plan->direct = p.a.direct;
+  plan->join_rows = p.fold ? wf::prefix_own_rows(p.a, p.a.S, n_g + (p.a.direct ? k : 0)) : 0;
+  return WF_OK;
+}

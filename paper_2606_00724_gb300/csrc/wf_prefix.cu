@@ -404,7 +404,7 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   p.dtype = q.dtype;
   p.fmt = kv.dtype;
   const bool tc = p.dtype == WF_BF16;
-  const int tr = tc ? kPrefixTcRows : simt_rows(a);
+  const int tr = p.tr = tc ? kPrefixTcRows : simt_rows(a);
   a.mt = (a.R + tr - 1) / tr;
   a.mto = (a.Ro + tr - 1) / tr;
   // Parts: the count with the least estimated time, in us: waves of CTAs, each a
@@ -412,7 +412,7 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   // the joining kernel.  Measured at d = 128: a call of one tile 6 us, a key tile 1.5
   // with a row tile of 256 (products) or of 128 (the rows' bytes), a 64-key tile
   // of the fp32 kernel 13 for 128 rows; parts move at 5 TB/s; joining 2.5.
-  const int tk = tc ? kPrefixTcRows / 2 : TK, slots = tc || tr == 128 ? kSms : 2 * kSms;
+  const int tk = p.tk = tc ? kPrefixTcRows / 2 : TK, slots = tc || tr == 128 ? kSms : 2 * kSms;
   const double wide = a.d / 128.0, tile_us = wide * (tc ? 1.5 : tr == 128 ? 13.0 : tr == 64 ? 10.0 : 4.0);
   const double set_up = tc ? 5.0 : 4.0, part_us = (double)a.rows * a.d * 8 / 5e6;
   auto split = [&](int64_t units, int keys, double* least) {
@@ -464,6 +464,7 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   const int64_t kept = a.whole ? 0 : a.rows * p.parts;  // rows of parts
   p.off_ml = 256;
   p.off_o = align_up(p.off_ml + sizeof(float2) * (size_t)kept, 256);
+  p.used = p.off_o + sizeof(float) * (size_t)kept * a.d;
   // The size is the most that a call with as many keys and query rows, or fewer of
   // any, can take, so that one workspace serves them all: S itself is not monotone.
   // S units is at most kWaves slots where S > 1, and a unit has at most tr rows.

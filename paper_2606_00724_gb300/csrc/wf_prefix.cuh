@@ -61,9 +61,11 @@ constexpr int kPrefixTcRows = 256;  // query rows a CTA of the tensor-core kerne
 struct PrefixPlan {
   PrefixArgs a;  // shapes and splits; pointers are filled in by the call
   int dtype, fmt;
+  int tr, tk;    // query rows a CTA, keys a tile
   int parts;     // 1: the kernel writes O itself
   bool fold;     // the own rows are attended where the parts are joined (So = 0)
-  size_t off_ml, off_o, total;
+  size_t off_ml, off_o, used;  // used: what this call writes
+  size_t total;                // what it asks for
 };
 PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g);
 cudaError_t launch_prefix(const PrefixPlan& p, cudaStream_t s);

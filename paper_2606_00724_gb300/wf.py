@@ -40,6 +40,12 @@ class wf_tensor(ctypes.Structure):
                 ("stride_s", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
 
+class wf_testing_plan(ctypes.Structure):
+    _fields_ = [("workspace_used", ctypes.c_longlong)] + [
+        (name, ctypes.c_int) for name in ("prompt_parts", "own_parts", "key_tile", "prompt_rows", "joined", "direct",
+                                          "join_rows")]
+
+
 _lib = None
 
 # Every symbol declared in include/wf.h, with its ctypes signature.
@@ -75,6 +81,7 @@ SIGNATURES = {
     "wf_workspace_status": (_I, [_P, _P]),
     # include/wf_testing.h (test-only)
     "wf_testing_set_wait_failure": (_I, [_I, ctypes.c_longlong]),
+    "wf_testing_prefix_plan": (_I, [_T, _T, _I, _I, ctypes.POINTER(wf_testing_plan)]),
 }
 
 
@@ -432,3 +439,11 @@ def wf_testing_set_wait_failure(stall: bool, wait_limit_cycles: int = 0):
     up by wait_limit_cycles (0: the default bound).  Reset with (False, 0)."""
     _check(lib().wf_testing_set_wait_failure(int(bool(stall)), int(wait_limit_cycles)),
            "wf_testing_set_wait_failure")
+
+
+def wf_testing_prefix_plan(q: wf_tensor, kv: wf_tensor, k: int, n_g: int) -> wf_testing_plan:
+    """Test-only (include/wf_testing.h): how a wf_prefix_attn call of these
+    shapes would be run."""
+    plan = wf_testing_plan()
+    _check(lib().wf_testing_prefix_plan(q, kv, k, n_g, plan), "wf_testing_prefix_plan")
+    return plan
