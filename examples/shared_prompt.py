@@ -42,12 +42,22 @@ class SharedPrompt:
         # alone, so one head's worth of memory stands for all of them.
         self.shape = K.new_empty(1, 1, n, d).expand(1, H, n, d)
         self.idx = torch.empty(H, self.keep[0], dtype=torch.int32, device=K.device)
-        self.ws = self.attn_ws = None
+        self.ws, self.attn_ws = (torch.zeros(256, dtype=torch.uint8, device=K.device) for _ in range(2))
 
     def write(self, K: torch.Tensor, V: torch.Tensor, pos: int) -> None:
         """Rows [pos, pos + count) of the cache from K, V [H, count, d].  (The pyramid of a changed stretch is
         rebuilt from its rows by the caller that still has them.)"""
         wf.wf_cache_quantize(K[None], V[None], self.Kc, self.Ks, self.Vc, self.Vs, self.fmt, pos)
+
+    @staticmethod
+    def _at_least(ws: torch.Tensor, size: int) -> torch.Tensor:
+        """ws, or a larger workspace in its place where a step has more answers or longer ones; the word in which
+        the calls report a wait that gave up goes along."""
+        if ws.nbytes >= size:
+            return ws
+        larger = torch.zeros(size, dtype=torch.uint8, device=ws.device)
+        larger[:4] = ws[:4]
+        return larger
 
     def attend(self, Q: torch.Tensor, Kg: torch.Tensor, Vg: torch.Tensor, gen_len=None) -> torch.Tensor:
         """Q [H, B, q, d]: the query blocks of B answers, head by head; Kg, Vg [B, H, ng, d] the answers' own rows,
@@ -55,11 +65,9 @@ class SharedPrompt:
         H, B, q, d = Q.shape
         grouped, by_answer = Q.view(1, H * B, q, d), Q.transpose(0, 1)
         O = torch.empty_like(Q)
-        if self.ws is None:
-            size = wf.wf_filter_workspace_bytes(grouped, self.shape, self.levels, self.keep)
-            self.ws = torch.zeros(size, dtype=torch.uint8, device=Q.device)
-            size = wf.wf_prefix_attn_workspace_bytes(by_answer, self.Kc, self.keep[0], Kg.shape[2], fmt=self.fmt)
-            self.attn_ws = torch.zeros(size, dtype=torch.uint8, device=Q.device)
+        self.ws = self._at_least(self.ws, wf.wf_filter_workspace_bytes(grouped, self.shape, self.levels, self.keep))
+        self.attn_ws = self._at_least(self.attn_ws, wf.wf_prefix_attn_workspace_bytes(
+            by_answer, self.Kc, self.keep[0], Kg.shape[2], fmt=self.fmt))
         wf.wf_filter(grouped, self.pyramid, self.shape, self.levels, self.keep, self.idx, self.ws)
         wf.wf_prefix_attn(by_answer, self.Kc, self.Vc, self.keep[0], Kg, Vg, O.transpose(0, 1), self.attn_ws,
                           idx=self.idx, gen_len=gen_len, Ks=self.Ks, Vs=self.Vs, fmt=self.fmt)
