@@ -6,7 +6,7 @@ prompt rows for all answers together (their query blocks form one group a key
 head, so the selection is one row list a head) and attends each answer's block
 to the selected rows of the quantised cache, read once for all, and to the
 answer's own rows.  A stretch of the prompt that changed is quantised into its
-place.
+place, and the pyramid over it is rebuilt.
 
     python examples/shared_prompt.py [--tokens 32768] [--answers 4] [--heads 32] [--four-bit]
 """
@@ -37,7 +37,7 @@ class SharedPrompt:
         self.Kc, self.Vc = (torch.empty(1, H, n, width, dtype=torch.uint8, device=K.device) for _ in range(2))
         self.Ks, self.Vs = (torch.empty(wf.wf_scales_bytes(self.Kc, fmt), dtype=torch.uint8, device=K.device)
                             for _ in range(2))
-        self.write(K, V, 0)
+        wf.wf_cache_quantize(K[None], V[None], self.Kc, self.Ks, self.Vc, self.Vs, fmt, 0)
         # The filter takes the keys for their shape; with every kept pair of tokens selected it reads the pyramid
         # alone, so one head's worth of memory stands for all of them.
         self.shape = K.new_empty(1, 1, n, d).expand(1, H, n, d)
@@ -45,9 +45,23 @@ class SharedPrompt:
         self.ws, self.attn_ws = (torch.zeros(256, dtype=torch.uint8, device=K.device) for _ in range(2))
 
     def write(self, K: torch.Tensor, V: torch.Tensor, pos: int) -> None:
-        """Rows [pos, pos + count) of the cache from K, V [H, count, d].  (The pyramid of a changed stretch is
-        rebuilt from its rows by the caller that still has them.)"""
+        """Rows [pos, pos + count) of the prompt from K, V [H, count, d]: into the cache, and into the pyramid's
+        coefficients over the blocks of 2^levels tokens that hold them.  The blocks' other rows are read back out of
+        the cache, the only place where they still are."""
+        H, count, d = K.shape
+        if count == 0:
+            return
         wf.wf_cache_quantize(K[None], V[None], self.Kc, self.Ks, self.Vc, self.Vs, self.fmt, pos)
+        n, L = self.Kc.shape[2], self.levels
+        lo, hi = pos >> L << L, -(-(pos + count) >> L) << L
+        rows = torch.empty(1, H, hi - lo, d, dtype=K.dtype, device=K.device)
+        wf.wf_cache_dequantize(self.Kc, self.Ks, None, None, self.fmt, rows, None, lo)
+        rows[0, :, pos - lo:pos - lo + count] = K
+        stretch = torch.empty(H, (hi - lo) - (hi - lo >> L), d, dtype=K.dtype, device=K.device)
+        wf.wf_dwt_build(rows, L, stretch)
+        for level in range(1, L + 1):  # n / 2^level rows from n - n / 2^(level - 1) on
+            to, at, m = n - (n >> level - 1), (hi - lo) - (hi - lo >> level - 1), hi - lo >> level
+            self.pyramid[:, to + (lo >> level):to + (hi >> level)] = stretch[:, at:at + m]
 
     @staticmethod
     def _at_least(ws: torch.Tensor, size: int) -> torch.Tensor:

@@ -39,3 +39,37 @@ def test_answers_and_generations_grow():
         wf.wf_workspace_status(prompt.attn_ws)
         fresh = SharedPrompt(K, V, LEVELS, KEPT, wf.WF_MXFP8).attend(Q, Kg, Vg)
         assert torch.equal(O, fresh) and torch.isfinite(O).all()
+
+
+@pytest.mark.parametrize("fmt", [wf.WF_MXFP8, wf.WF_MXFP4])
+@pytest.mark.parametrize("pos,count", [(100, 17), (0, 16), (2031, 17), (1024, 1), (5, 2000)])
+def test_rewritten_stretch_is_selected_by(pos, count, fmt):
+    # The pyramid after a write is that of the rows that the prompt now has: the new ones as given, in the blocks of
+    # 16 tokens around them the others as the cache holds them, and the first ones elsewhere.
+    g, K, V, prompt = prompt_of(1, fmt)
+    new = rn(g, H, count, D)
+    prompt.write(new, -new, pos)
+    kept = torch.empty(1, H, N, D, dtype=torch.bfloat16, device="cuda")
+    wf.wf_cache_dequantize(prompt.Kc, prompt.Ks, None, None, fmt, kept, None)
+    now = K.clone()
+    lo, hi = pos // 16 * 16, -(-(pos + count) // 16) * 16
+    now[:, lo:hi] = kept[0, :, lo:hi]
+    now[:, pos:pos + count] = new
+    want = torch.empty_like(prompt.pyramid)
+    wf.wf_dwt_build(now[None], LEVELS, want)
+    assert torch.equal(prompt.pyramid, want)
+
+
+def test_rewritten_rows_are_found():
+    # Rows that answer the queries much better than all others are written over: the next step selects them.
+    g, K, V, prompt = prompt_of(2)
+    Q, Kg, Vg = rn(g, H, 2, 8, D), rn(g, 2, H, 8, D), rn(g, 2, H, 8, D)
+    Q[:] = Q[:, :1, :1]
+    prompt.attend(Q, Kg, Vg)
+    stretch = torch.arange(640, 672, device="cuda")
+    assert not torch.isin(stretch, prompt.idx[0]).all()
+    new = Q[:, 0, :1].expand(H, 32, D).contiguous()
+    prompt.write(new, new, 640)
+    prompt.attend(Q, Kg, Vg)
+    for h in range(H):
+        assert torch.isin(stretch, prompt.idx[h]).all()
