@@ -111,10 +111,13 @@ def main(argv=None) -> dict:
         O = prompt.attend(Q, Kg, Vg, gen_len)
     wf.wf_workspace_status(prompt.ws)
     wf.wf_workspace_status(prompt.attn_ws)
-    kept = prompt.Kc.nbytes * 2 + prompt.Ks.nbytes * 2
-    result = {"cache_bytes": kept, "bf16_bytes": K.nbytes + V.nbytes, "rows": prompt.keep[0], "Q": Q, "O": O,
-              "K": K, "V": V, "Kg": Kg, "Vg": Vg, "gen_len": gen_len, "prompt": prompt}
-    print(f"{n} tokens, {H} heads: {kept / 1e6:.1f} MB quantised, {result['bf16_bytes'] / 1e6:.1f} MB in bf16; "
+    cache, pyramid = 2 * (prompt.Kc.nbytes + prompt.Ks.nbytes), prompt.pyramid.nbytes
+    result = {"cache_bytes": cache, "pyramid_bytes": pyramid, "bf16_bytes": K.nbytes + V.nbytes,
+              "rows": prompt.keep[0], "Q": Q, "O": O, "K": K, "V": V, "Kg": Kg, "Vg": Vg, "gen_len": gen_len,
+              "prompt": prompt}
+    print(f"{n} tokens, {H} heads, with a pyramid of {pyramid / 1e6:.1f} MB in bf16: "
+          f"{(cache + pyramid) / 1e6:.1f} MB with keys and values quantised, "
+          f"{(result['bf16_bytes'] + pyramid) / 1e6:.1f} MB with them in bf16; "
           f"{B} answers attend to {prompt.keep[0]} rows a head")
     return result
 

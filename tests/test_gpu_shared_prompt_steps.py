@@ -73,3 +73,15 @@ def test_rewritten_rows_are_found():
     prompt.attend(Q, Kg, Vg)
     for h in range(H):
         assert torch.isin(stretch, prompt.idx[h]).all()
+
+
+def test_bytes_that_are_reported(capsys):
+    # The pyramid stays in 16 bits and counts on both sides: 15/16 of the keys at four levels.
+    import shared_prompt
+    r = shared_prompt.main(["--tokens", "2048", "--answers", "2", "--heads", "2", "--steps", "1"])
+    keys = 2 * 2048 * 128
+    assert r["cache_bytes"] == 2 * (keys + keys // 32) and r["pyramid_bytes"] == 2 * keys * 15 // 16
+    said = capsys.readouterr().out
+    kept = r["cache_bytes"] + r["pyramid_bytes"]
+    assert f"{kept / 1e6:.1f} MB with keys and values quantised" in said
+    assert f"{(2 * 2 * keys + r['pyramid_bytes']) / 1e6:.1f} MB with them in bf16" in said
