@@ -8,6 +8,11 @@ to the selected rows of the quantised cache, read once for all, and to the
 answer's own rows.  A stretch of the prompt that changed is quantised into its
 place, and the pyramid over it is rebuilt.
 
+One selection serves at most 256 query rows of a key head (wf_filter's limit),
+eight answers' blocks of 32; more answers are attended in groups, each with a
+selection of its own.  Every query head has a key head here: with grouped heads
+the two calls want the queries in different orders.
+
     python examples/shared_prompt.py [--tokens 32768] [--answers 4] [--heads 32] [--four-bit]
 """
 from __future__ import annotations
@@ -24,6 +29,8 @@ from paper_2606_00724_gb300 import wf  # noqa: E402
 
 class SharedPrompt:
     """One prompt's keys and values [H, n, d] (bf16), kept quantised with the pyramid of its keys."""
+
+    MAX_ROWS = 256  # query rows a selection: wf_filter's limit a key head
 
     def __init__(self, K: torch.Tensor, V: torch.Tensor, levels: int, kept: int, fmt: int):
         H, n, d = K.shape
@@ -77,6 +84,10 @@ class SharedPrompt:
         """Q [H, B, q, d]: the query blocks of B answers, head by head; Kg, Vg [B, H, ng, d] the answers' own rows,
         of which the first gen_len[b] count.  The answers' outputs, [H, B, q, d]."""
         H, B, q, d = Q.shape
+        if H != self.Kc.shape[1]:
+            raise ValueError("a query head a key head")
+        if B * q > self.MAX_ROWS:
+            raise ValueError(f"one selection serves at most {self.MAX_ROWS} query rows: attend in groups of answers")
         grouped, by_answer = Q.view(1, H * B, q, d), Q.transpose(0, 1)
         O = torch.empty_like(Q)
         self.ws = self._at_least(self.ws, wf.wf_filter_workspace_bytes(grouped, self.shape, self.levels, self.keep))

@@ -85,3 +85,24 @@ def test_bytes_that_are_reported(capsys):
     kept = r["cache_bytes"] + r["pyramid_bytes"]
     assert f"{kept / 1e6:.1f} MB with keys and values quantised" in said
     assert f"{(2 * 2 * keys + r['pyramid_bytes']) / 1e6:.1f} MB with them in bf16" in said
+
+
+def test_answers_of_one_selection():
+    # 256 rows a key head are one selection; more are refused with what to do about it, and groups of them work.
+    g, K, V, prompt = prompt_of(3)
+    Q, Kg, Vg = rn(g, H, 16, 32, D), rn(g, 16, H, 32, D), rn(g, 16, H, 32, D)
+    with pytest.raises(ValueError, match="groups"):
+        prompt.attend(Q, Kg, Vg)
+    for at in (slice(0, 8), slice(8, 16)):
+        O = prompt.attend(Q[:, at].contiguous(), Kg[at], Vg[at])
+        assert O.shape == (H, 8, 32, D) and torch.isfinite(O).all()
+    with pytest.raises(ValueError, match="key head"):
+        prompt.attend(rn(g, 2 * H, 1, 32, D), Kg[:1], Vg[:1])
+
+
+def test_selection_reads_no_keys():
+    g, K, V, prompt = prompt_of(4)
+    Q, Kg, Vg = rn(g, H, 4, 32, D), rn(g, 4, H, 32, D), rn(g, 4, H, 32, D)
+    before = prompt.attend(Q, Kg, Vg), prompt.idx.clone()
+    prompt.shape[0, 0].fill_(float("nan"))  # the memory that stands in for the keys, in the filter's arguments alone
+    assert torch.equal(prompt.attend(Q, Kg, Vg), before[0]) and torch.equal(prompt.idx, before[1])
