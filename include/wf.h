@@ -42,7 +42,10 @@
  *   the same dtype); head_dim 64 or 128; 1 <= query rows <= 64 per query head
  *   (at most 256 per key head when query heads are grouped); prompt length
  *   n a multiple of 2^levels with 1 <= levels <= 10; base pointers and the
- *   three strides (in bytes) 16-byte aligned.
+ *   three strides (in bytes) 16-byte aligned.  Of these, the quantised cache
+ *   and the attention over shared prompts (sections 5 and 6) keep head_dim and
+ *   alignment only: they take any prompt length and any number of query rows,
+ *   and prompts of the dtypes that they name.
  */
 #ifndef WF_H
 #define WF_H
@@ -385,15 +388,18 @@ wf_status wf_step_wavelet(const void* Q, const wf_tensor* q, const void* top, co
  * are bytes e + 127 (255: NaN), contiguous [B][H][rows][head_dim / 32], 4-byte
  * aligned.  K and V have code and scale tensors of the same shape and strides.
  * The E4M3 codes 0x7f and 0xff (that format's NaN) are never written; a caller
- * who makes codes of its own must not use them.
+ * who makes codes of its own must not use them: they read as NaN in fp32 and as
+ * 480 s where codes are widened to bf16.  A magnitude that rounds to 2^128 (the
+ * largest values of both types) reads back as an infinity.
  *
  * wf_scales_bytes: size of the scales of kv (0 if kv is not a valid quantised
  * cache).
  *
  * wf_cache_quantize: the count = nt->seq rows Knew (and Vnew), WF_F32 or
  * WF_BF16, into the caches at token positions [pos, pos + count), quantised
- * as they are written; no other row is touched.  count may be 0 (then Knew and Vnew may be NULL).  Vnew, Vc and Vs
- * are all NULL for keys alone.  The new rows must not overlap the caches.
+ * as they are written; no other row is touched.  count may be 0 (then Knew and
+ * Vnew may be NULL).  Vnew, Vc and Vs are all NULL for keys alone.  The new rows
+ * must not overlap the caches.
  *
  * wf_cache_dequantize: m = out->seq rows read back into Kout (and Vout), WF_F32
  * or WF_BF16 (code times scale, rounded once): with idx == NULL the rows
@@ -403,7 +409,8 @@ wf_status wf_step_wavelet(const void* Q, const wf_tensor* q, const void* top, co
  *
  * scales_bytes: the size of each scale tensor.  Errors: WF_ERR_INVALID_ARG for
  * a missing pointer, V given in part, or a window outside [0, n);
- * WF_ERR_WORKSPACE for scales that are too small; shape, dtype and alignment
+ * WF_ERR_WORKSPACE for scales that are too small; WF_ERR_UNSUPPORTED for 2^30
+ * rows of all units (B H count, B H m) and more; shape, dtype and alignment
  * errors as elsewhere.  Nothing is enqueued on an error.
  * ------------------------------------------------------------------------- */
 size_t wf_scales_bytes(const wf_tensor* kv);
@@ -420,8 +427,9 @@ wf_status wf_cache_dequantize(const void* Kc, const void* Ks, const void* Vc, co
  *
  * Q: [B,Hq,q,d] WF_F32 or WF_BF16, any q >= 1 (q = 1: one token a sequence).
  * K, V: the prompts [P,H,n,d] (kv), in Q's dtype, or quantised with their
- * scales Ks, Vs (else NULL).  P divides B: sequence b reads prompt
- * b / (B / P).  Hq = G H as in wf_filter: query head hq reads key head hq / G.
+ * scales Ks, Vs of wf_scales_bytes(kv) bytes each (else NULL).  P divides B:
+ * sequence b reads prompt b / (B / P).  Hq = G H as in wf_filter: query head hq
+ * reads key head hq / G.
  * The prompt rows of unit u = p H + h that are attended:
  *   idx == NULL: rows [0, k), 0 <= k <= n;
  *   idx (device, int32 [P*H][k]): the k rows idx[u][..], 0 <= k <= n, in any
@@ -437,8 +445,9 @@ wf_status wf_cache_dequantize(const void* Kc, const void* Ks, const void* Vc, co
  * written rounded to that dtype.  A query row with no row to attend to, or
  * whose logits are all -inf, gets O = 0.  A NaN or an infinity reaches the query
  * rows that attend to its row only.
- * bf16 queries run on the tensor cores, fp32 queries in fp32 arithmetic.  The
- * same inputs give the same bits.
+ * bf16 queries run on the tensor cores, with the softmax's weights rounded to
+ * bf16 (as wf_step's; wf_sparse_attn keeps 16 bits of them), fp32 queries in
+ * fp32 arithmetic.  The same inputs give the same bits.
  * B Hq q, k and n_g below 2^30 each, else WF_ERR_UNSUPPORTED (n may be longer).
  * ws: device scratch of at least wf_prefix_attn_workspace_bytes() bytes,
  * 256-byte aligned; its first 4 bytes are wf_filter's status word (zero it

@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(NTH) quantize_kernel(const __grid_constant__ M
     if (byte == 255) v[i] = make_uint4(0, 0, 0, 0);
     float x[N];
     widen_vec(static_cast<const T*>(nullptr), v[i], x);
-    const float inv = mx_inv_scale(min(byte, 254u - 1u));
+    const float inv = mx_inv_scale(min(byte, 253u));
     const sm100::f32x2 inv2 = sm100::pk2(inv, inv);
 #pragma unroll
     for (int e = 0; e < N; e += 2) {

@@ -30,7 +30,8 @@ __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t top) {
                     : (int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u);
   return (uint32_t)max(e, 0);
 }
-// 2^-e of a scale byte below 255 (at most 253 - 1, so never subnormal).
+// 2^-e of a scale byte up to 253, the largest of a finite block: 2^-126, the
+// least normal number.
 __device__ __forceinline__ float mx_inv_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 // 2^e of a scale byte: byte 0 is the subnormal 2^-127, byte 255 NaN.
 __device__ __forceinline__ float mx_scale(uint32_t byte) {

@@ -23,7 +23,6 @@ namespace {
 using namespace sm100;
 
 constexpr int TK = 64;      // keys a tile
-constexpr int kSms = 152;   // a wave of CTAs of the tensor-core kernel, one an SM
 constexpr int kWaves = 4;   // the parts of a call fill at most so many
 
 // How prompt rows are kept: like the own rows, or in codes.
@@ -412,7 +411,7 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   // the joining kernel.  Measured at d = 128: a call of one tile 6 us, a key tile 1.5
   // with a row tile of 256 (products) or of 128 (the rows' bytes), a 64-key tile
   // of the fp32 kernel 13 for 128 rows; parts move at 5 TB/s; joining 2.5.
-  const int tk = p.tk = tc ? kPrefixTcRows / 2 : TK, slots = tc || tr == 128 ? kSms : 2 * kSms;
+  const int tk = p.tk = tc ? kPrefixTcRows / 2 : TK, slots = tc || tr == 128 ? kPrefixSms : 2 * kPrefixSms;
   const double wide = a.d / 128.0, tile_us = wide * (tc ? 1.5 : tr == 128 ? 13.0 : tr == 64 ? 10.0 : 4.0);
   const double set_up = tc ? 5.0 : 4.0, part_us = (double)a.rows * a.d * 8 / 5e6;
   auto split = [&](int64_t units, int keys, double* least) {
@@ -468,7 +467,7 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   // The size is the most that a call with as many keys and query rows, or fewer of
   // any, can take, so that one workspace serves them all: S itself is not monotone.
   // S units is at most kWaves slots where S > 1, and a unit has at most tr rows.
-  const int64_t most = (int64_t)kWaves * (tc ? kSms * kPrefixTcRows : 2 * kSms * 64);
+  const int64_t most = (int64_t)kWaves * (tc ? kPrefixSms * kPrefixTcRows : 2 * kPrefixSms * 64);
   auto room = [&](int keys, bool alone) {
     const int64_t tiles = (keys + tk - 1) / tk;
     return std::min(tiles * a.rows, alone ? most : std::max(a.rows, most));

@@ -55,6 +55,9 @@ struct PrefixArgs {
 // tokens' units of 100 rows 47, 72, of 500 rows 81, 91, of 1000 rows 123, 120; 512
 // units of 32 query rows and 300 own rows 103, 95.
 constexpr int kPrefixOwn = 64;
+// SMs of the machine that the estimates of plan_prefix and prefix_own_rows are
+// of, with their times a tile; a call's split and size follow from its shapes alone.
+constexpr int kPrefixSms = 152;
 constexpr int kPrefixTcRows = 256;  // query rows a CTA of the tensor-core kernel
 
 // The workspace of a call: the status word, then the parts.

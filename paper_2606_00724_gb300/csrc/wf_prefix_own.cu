@@ -7,6 +7,7 @@
 // a small part of a 128-row tensor-memory tile and would pay its set-up, about
 // 4 us a CTA with one CTA an SM; warp-level products (m16n8k16, fp32
 // accumulators) keep S and O in registers, and four CTAs share an SM.
+// P is one bf16 term, as in the prompt's kernel.
 // Few prompt rows are attended here too, by every sequence for itself: one launch
 // instead of two (see plan_prefix).
 // The softmax is that of the prompt's kernel (base 2, running maximum), so what
@@ -309,11 +310,10 @@ cudaError_t launch_rows(PrefixArgs a, cudaStream_t s) {
 // to 4 where the parts are more bytes than the keys that every block reads
 // again (one token of 28 heads on 4, 37 parts: 15 -> 6 us).
 int prefix_own_rows(const PrefixArgs& a, int S, int keys) {
-  constexpr int sms = 152;
   int ob = a.Ro <= 16 ? 16 : a.Ro <= 32 ? 32 : 64;
   auto blocks = [&] { return (int64_t)a.B * a.H * ((a.Ro + ob - 1) / ob); };
-  while (ob > 16 && blocks() < sms) ob /= 2;
-  while (ob > 4 && blocks() < 2 * sms && ob * S > keys) ob /= 2;
+  while (ob > 16 && blocks() < kPrefixSms) ob /= 2;
+  while (ob > 4 && blocks() < 2 * kPrefixSms && ob * S > keys) ob /= 2;
   return ob;
 }
 
