@@ -20,8 +20,10 @@
  * with Eq. 11 taken literally (wf_wavelet_approx, wf_filter_wavelet), grouped
  * query heads (wf_filter, wf_sparse_attn, wf_step),
  * wf_sparse_attn_noalloc for callers that cannot pass a workspace, a cache in
- * 8-bit or 4-bit codes (wf_cache_quantize, wf_cache_dequantize), and the
- * attention of several sequences over one cached prompt (wf_prefix_attn).
+ * 8-bit or 4-bit codes (wf_cache_quantize, wf_cache_dequantize), the
+ * attention of several sequences over one cached prompt (wf_prefix_attn), and a
+ * cache in pages for drafted tokens: rotary positions (wf_rotary_apply), rows
+ * into pages (wf_paged_append) and the attention over both (wf_tree_attn).
  *
  * Conventions shared by every entry point
  * - A tensor is described by wf_tensor: [batch, heads, seq, head_dim] with
@@ -29,7 +31,8 @@
  *   contiguous.  BHSD and BSHD layouts are both expressible.
  * - Pointers named Q, K, V, Kg, Vg, O, coeffs, idx, level_sets, ws are DEVICE
  *   pointers owned by the caller; libwf allocates no device memory and keeps
- *   no state between calls.  Arrays named keep and m are HOST arrays.
+ *   no state between calls.  Arrays named keep and m are HOST arrays, and so are
+ *   those of wf_rotary_plan.
  * - `stream` is a cudaStream_t passed as void* (NULL = the legacy default
  *   stream).  Every call only enqueues work on that stream and returns; the
  *   outputs are valid once the stream reaches that point.
@@ -42,10 +45,10 @@
  *   the same dtype); head_dim 64 or 128; 1 <= query rows <= 64 per query head
  *   (at most 256 per key head when query heads are grouped); prompt length
  *   n a multiple of 2^levels with 1 <= levels <= 10; base pointers and the
- *   three strides (in bytes) 16-byte aligned.  Of these, the quantised cache
- *   and the attention over shared prompts (sections 5 and 6) keep head_dim and
- *   alignment only: they take any prompt length and any number of query rows,
- *   and prompts of the dtypes that they name.
+ *   three strides (in bytes) 16-byte aligned.  Of these, the quantised cache,
+ *   the attention over shared prompts and the cache in pages (sections 5 to 7)
+ *   keep head_dim and alignment only: they take any prompt length and any number
+ *   of query rows, and prompts of the dtypes that they name.
  */
 #ifndef WF_H
 #define WF_H
@@ -460,6 +463,89 @@ wf_status wf_prefix_attn(const void* Q, const wf_tensor* q, const void* K, const
                          const void* Ks, const void* Vs, const int32_t* idx, int k, const int32_t* prefix_len,
                          const void* Kg, const void* Vg, const wf_tensor* g, const int32_t* gen_len, void* O,
                          const wf_tensor* o, float scale, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * 7. A cache in pages, for sequences of unequal and growing lengths and for
+ * drafted tokens of which some are accepted.
+ *
+ * A pool holds pages of ps rows: K, V [pages, H, ps, d] (descriptor pool, whose
+ * batch counts the pages and whose seq is ps, any number from 1 on), WF_F32,
+ * WF_BF16, or quantised with scales Ks, Vs of wf_scales_bytes(pool) bytes each
+ * (wf_cache_dequantize and wf_cache_quantize take a pool as they take a cache).
+ * Row j of sequence b is row j % ps of page pages[b][j / ps] (device, int32
+ * [B][table]); a page may serve several sequences.  pages x ps and table x ps
+ * are below 2^31.
+ *
+ * Rotary positions.  With f_i the radians a position of pair i and p the
+ * position on its axis, (x, y) becomes
+ *   (x cos(p f_i) - y sin(p f_i), y cos(p f_i) + x sin(p f_i)),
+ * where pair i is channels (i, i + pairs), or (2 i, 2 i + 1) if adjacent != 0;
+ * the other channels, from 2 pairs on, stay.  The angle is formed in whole
+ * numbers (the position times a plan's turn, modulo 2^64), so a far position is
+ * as exact as a near one; its cosine and sine, the products and sums are fp32
+ * (for bf16 rows the cosine and sine are within 2^-19), rounded once at the end.
+ * The rotation by -p undoes that by p, and is its gradient's.
+ *
+ * wf_rotary_plan: freq (f_i) and axis (NULL: all 0) of `pairs` pairs into plan,
+ * 2 pairs numbers: the turn 2^64 f_i / (2 pi) modulo 2^64, rounded, and the
+ * axis.  All are HOST arrays; the caller copies the plan to the device once.
+ * Errors: WF_ERR_INVALID_ARG for pairs < 1, an axis outside [0, 64) or a
+ * frequency that is not finite or 2^32 and above in magnitude.
+ *
+ * wf_rotary_apply: the rows of Q [B,Hq,rows,d] and K [B,Hk,rows,d] (K, k, Kout,
+ * ko may be NULL) into Qout and Kout of the same shape and dtype, which are Q and
+ * K themselves (same address and strides) or do not overlap them.  plan: device;
+ * pairs: a multiple of 8, at most d / 2; pos: device, int32 [axes][B][rows], any
+ * values (an axis of the plan from `axes` on takes the last).  No row: nothing
+ * is done.
+ *
+ * wf_paged_append: m new rows of every sequence, Knew, Vnew [B,H,rows,d] (nt;
+ * Vnew, V, Vs NULL: keys alone), into K, V of the same dtype or quantised (as
+ * wf_cache_quantize defines).  Row i < min(m, count[b]) (count: device, int32
+ * [B], NULL: all m) goes to place start[b] + i of sequence b (start: device,
+ * int32 [B]).  rows_at (device, int32 [B][m]): new row rows_at[b][i] instead of
+ * row i, clamped to [0, rows), e.g. the accepted ones of a draft; without it
+ * m = rows.  With a plan (NULL: none) keys are rotated on the way, by
+ * pos[axis][b][new row] (int32 [axes][B][rows]) or, where pos is NULL, by their
+ * place, and rounded once.  A row whose place is outside the table or on a page
+ * outside the pool is left out; nothing else in the pool is touched.  Two rows
+ * for the same place of the same page: one of them is kept, which is not said.
+ * The new rows must not overlap the pool.
+ *
+ * wf_tree_attn: q query rows of each sequence, e.g. the nodes of a tree of
+ * drafted tokens (one token: a tree of one node; a denoising block: drafted rows
+ * that all see each other), over the sequence's cached rows and the drafted rows.
+ *   Q, O: [B,Hq,q,d], as in wf_prefix_attn; Hq = G H.
+ *   pool, pages, n: rows [0, min(n, cache_len[b])) of each sequence are attended
+ *     (cache_len: device, int32 [B], NULL: n; 0 <= n <= table ps); pages behind
+ *     them are not looked at, entries outside the pool are clamped into it.
+ *   Kt, Vt: the drafted rows [B,H,n_t,d] (t, Q's dtype; NULL when n_t = 0), of
+ *     which the first min(n_t, tree_len[b]) count (NULL: all).  They need not be
+ *     in the cache, and accepted ones get there with wf_paged_append.
+ *   mask: device, int32 [B][q][(n_t + 31) / 32]: query row i sees drafted row j
+ *     if bit j % 32 of word j / 32 is set (NULL: it sees all).
+ *   O = softmax(scale Q [K_b; Kt_b]^T) [V_b; Vt_b] over what a row sees, with
+ * wf_prefix_attn's arithmetic, scale, workspace rules, limits and status word.  A
+ * row that sees nothing gets O = 0.  Rows past a length are never read, and a
+ * drafted row does not touch the query rows that do not see it, whatever it
+ * holds.
+ *
+ * Errors: as elsewhere; WF_ERR_INVALID_ARG for n outside [0, table ps].
+ * ------------------------------------------------------------------------- */
+wf_status wf_rotary_plan(const double* freq, const int32_t* axis, int pairs, int64_t* plan);
+wf_status wf_rotary_apply(const void* Q, const wf_tensor* q, const void* K, const wf_tensor* k, const int64_t* plan,
+                          int pairs, int adjacent, const int32_t* pos, int axes, void* Qout, const wf_tensor* qo,
+                          void* Kout, const wf_tensor* ko, void* stream);
+wf_status wf_paged_append(const void* Knew, const void* Vnew, const wf_tensor* nt, const int32_t* rows_at, int m,
+                          const int32_t* start, const int32_t* count, const int64_t* plan, int pairs, int adjacent,
+                          const int32_t* pos, int axes, void* K, void* V, void* Ks, void* Vs, const wf_tensor* pool,
+                          size_t scales_bytes, const int32_t* pages, int table, void* stream);
+size_t wf_tree_attn_workspace_bytes(const wf_tensor* q, const wf_tensor* pool, int n, int n_t);
+wf_status wf_tree_attn(const void* Q, const wf_tensor* q, const void* K, const void* V, const wf_tensor* pool,
+                       const void* Ks, const void* Vs, const int32_t* pages, int table, int n,
+                       const int32_t* cache_len, const void* Kt, const void* Vt, const wf_tensor* t,
+                       const int32_t* tree_len, const int32_t* mask, void* O, const wf_tensor* o, float scale, void* ws,
+                       size_t ws_bytes, void* stream);
 
 /* Device status of the last wf_step calls that used workspace ws: waits for
  * `stream`, returns WF_ERR_TIMEOUT (and clears the word) if a bounded device

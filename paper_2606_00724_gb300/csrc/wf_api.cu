@@ -11,6 +11,7 @@
 #include "wf_internal.cuh"
 #include "wf_mx.cuh"
 #include "wf_prefix.cuh"
+#include "wf_rows.cuh"
 #include "wf_testing.h"
 
 #define WF_API extern "C" __attribute__((visibility("default")))
@@ -564,6 +565,41 @@ wf_status check_prefix_args(const wf_tensor* q, const wf_tensor* kv, int k, int 
   return WF_OK;
 }
 
+// Outputs and, where there are any, own rows (g) of the queries q over key heads kv.
+wf_status check_attn_rows(const wf_tensor* q, const wf_tensor* kv, const wf_tensor* g, const wf_tensor* o) {
+  wf_status st;
+  if ((st = check_desc(o, false)) != WF_OK) return st;
+  if (!same_units(q, o) || o->seq != q->seq) return WF_ERR_SHAPE;
+  if (o->dtype != q->dtype) return WF_ERR_DTYPE;
+  if (g) {
+    if ((st = check_desc(g, true)) != WF_OK) return st;
+    if (g->batch != q->batch || g->heads != kv->heads || g->head_dim != q->head_dim) return WF_ERR_SHAPE;
+    if (g->dtype != q->dtype) return WF_ERR_DTYPE;
+  }
+  return WF_OK;
+}
+
+void fill_prefix(wf::PrefixPlan& p, const void* Q, const wf_tensor* q, const void* K, const void* V,
+                 const wf_tensor* kv, const void* Ks, const void* Vs, const void* Kg, const void* Vg,
+                 const wf_tensor* g, void* O, const wf_tensor* o, float scale, void* ws) {
+  wf::PrefixArgs& a = p.a;
+  const int64_t code = kv->dtype == WF_MXFP4 ? 2 : 1;  // elements a byte of the codes' strides
+  a.Q = Q; a.qsb = q->stride_b; a.qsh = q->stride_h; a.qss = q->stride_s;
+  a.K = K; a.V = V;
+  a.ksb = kv->stride_b / code; a.ksh = kv->stride_h / code; a.kss = kv->stride_s / code;
+  a.Ks = static_cast<const uint8_t*>(Ks); a.Vs = static_cast<const uint8_t*>(Vs);
+  a.Kg = Kg; a.Vg = Vg;
+  if (a.ng > 0) { a.gsb = g->stride_b; a.gsh = g->stride_h; a.gss = g->stride_s; }
+  a.O = O; a.osb = o->stride_b; a.osh = o->stride_h; a.oss = o->stride_s;
+  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + p.off_ml);
+  a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + p.off_o);
+  a.sl2 = 1.4426950408889634f * (scale == 0.f ? 1.0f / sqrtf((float)q->head_dim) : scale);
+  a.status = static_cast<int*>(ws);
+  const wf::WaitControls wc = wf::wait_controls();
+  a.wait_limit = wc.limit;
+  a.stall = wc.stall;
+}
+
 }  // namespace
 
 WF_API size_t wf_prefix_attn_workspace_bytes(const wf_tensor* q, const wf_tensor* kv, int k, int n_g) {
@@ -578,14 +614,7 @@ WF_API wf_status wf_prefix_attn(const void* Q, const wf_tensor* q, const void* K
   const int n_g = g ? g->seq : 0;
   wf_status st = check_prefix_args(q, kv, k, n_g);
   if (st != WF_OK) return st;
-  if ((st = check_desc(o, false)) != WF_OK) return st;
-  if (!same_units(q, o) || o->seq != q->seq) return WF_ERR_SHAPE;
-  if (o->dtype != q->dtype) return WF_ERR_DTYPE;
-  if (g) {
-    if ((st = check_desc(g, true)) != WF_OK) return st;
-    if (g->batch != q->batch || g->heads != kv->heads || g->head_dim != q->head_dim) return WF_ERR_SHAPE;
-    if (g->dtype != q->dtype) return WF_ERR_DTYPE;
-  }
+  if ((st = check_attn_rows(q, kv, g, o)) != WF_OK) return st;
   if (!Q || !K || !V || !O || !ws) return WF_ERR_INVALID_ARG;
   if (quantised(kv) ? (!Ks || !Vs) : (Ks || Vs)) return WF_ERR_INVALID_ARG;
   if (n_g > 0 && (!Kg || !Vg)) return WF_ERR_INVALID_ARG;
@@ -597,24 +626,214 @@ WF_API wf_status wf_prefix_attn(const void* Q, const wf_tensor* q, const void* K
     return WF_ERR_ALIGN;
   wf::PrefixPlan p = wf::plan_prefix(*q, *kv, k, n_g);
   if (ws_bytes < p.total) return WF_ERR_WORKSPACE;
-  wf::PrefixArgs& a = p.a;
-  const int64_t code = kv->dtype == WF_MXFP4 ? 2 : 1;  // elements a byte of the codes' strides
-  a.Q = Q; a.qsb = q->stride_b; a.qsh = q->stride_h; a.qss = q->stride_s;
-  a.K = K; a.V = V;
-  a.ksb = kv->stride_b / code; a.ksh = kv->stride_h / code; a.kss = kv->stride_s / code;
-  a.Ks = static_cast<const uint8_t*>(Ks); a.Vs = static_cast<const uint8_t*>(Vs);
-  a.Kg = Kg; a.Vg = Vg;
-  if (n_g > 0) { a.gsb = g->stride_b; a.gsh = g->stride_h; a.gss = g->stride_s; }
-  a.O = O; a.osb = o->stride_b; a.osh = o->stride_h; a.oss = o->stride_s;
-  a.idx = idx; a.plen = prefix_len; a.glen = gen_len;
-  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + p.off_ml);
-  a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + p.off_o);
-  a.sl2 = 1.4426950408889634f * (scale == 0.f ? 1.0f / sqrtf((float)q->head_dim) : scale);
-  a.status = static_cast<int*>(ws);
-  const wf::WaitControls wc = wf::wait_controls();
-  a.wait_limit = wc.limit;
-  a.stall = wc.stall;
+  fill_prefix(p, Q, q, K, V, kv, Ks, Vs, Kg, Vg, g, O, o, scale, ws);
+  p.a.idx = idx; p.a.plen = prefix_len; p.a.glen = gen_len;
   return cuda_status(wf::launch_prefix(p, static_cast<cudaStream_t>(stream)));
+}
+
+// ---------------------------------------------------------------------------
+// A cache in pages.
+// ---------------------------------------------------------------------------
+namespace {
+
+// 2^192 / (2 pi) rounded down, in 32-bit digits, the most significant first.
+constexpr uint32_t kTurn[] = {0x28be60dbu, 0x9391054au, 0x7f09d5f4u, 0x7d4d3770u, 0x36d8a566u, 0x4f10e410u};
+
+// f / (2 pi) modulo 1, as a fraction of 2^64, to nearest.  f = m 2^e with a whole m of 53
+// bits, so the fraction is m times the digits above, shifted; of |f| < 2^32 no
+// digit that counts is left out.
+uint64_t turns_of(double f) {
+  int e;
+  const double x = frexp(fabs(f), &e);
+  const uint64_t m = (uint64_t)ldexp(x, 53);
+  e -= 53;  // f = m 2^e, e <= -21
+  // m / (2 pi) in units of 2^-192, eight digits, the least significant first.
+  uint32_t y[9] = {0};
+  for (int part = 0; part < 2; ++part) {
+    const uint64_t d = part ? m >> 32 : m & 0xffffffffu;
+    uint64_t carry = 0;
+    for (int i = 0; i < 6; ++i) {
+      const uint64_t t = d * kTurn[5 - i] + y[i + part] + carry;
+      y[i + part] = (uint32_t)t;
+      carry = t >> 32;
+    }
+    y[6 + part] += (uint32_t)carry;
+  }
+  // 2^64 f / (2 pi) = y 2^(e - 128): bits [s, s + 64) of y, s = 128 - e, rounded at bit s - 1.
+  const int s = 128 - e;
+  if (s > 256) return 0;
+  auto bit = [&](int i) { return i < 0 || i >= 288 ? 0u : y[i >> 5] >> (i & 31) & 1u; };
+  uint64_t r = 0;
+  for (int i = 0; i < 64; ++i) r |= (uint64_t)bit(s + i) << i;
+  r += bit(s - 1);
+  return f < 0 ? 0 - r : r;
+}
+
+wf_status check_plan(const int64_t* plan, int pairs, int d) {
+  if (!plan) return WF_ERR_INVALID_ARG;
+  if (pairs < 8 || pairs % 8 || pairs > d / 2) return WF_ERR_SHAPE;
+  return aligned16(plan) ? WF_OK : WF_ERR_ALIGN;
+}
+
+// A pool of pages and the tables of its sequences.
+wf_status check_pool(const wf_tensor* pool, int table) {
+  if (!pool) return WF_ERR_INVALID_ARG;
+  const wf_status st = quantised(pool) ? check_codes(pool) : check_desc(pool, false);
+  if (st != WF_OK) return st;
+  if (table < 1) return WF_ERR_INVALID_ARG;
+  const int64_t most = (int64_t)1 << 31;
+  if ((int64_t)pool->batch * pool->seq >= most || (int64_t)table * pool->seq >= most) return WF_ERR_UNSUPPORTED;
+  return WF_OK;
+}
+
+void fill_rows(wf::RowsArgs& a, int x, const void* src, const wf_tensor* from, void* dst, const wf_tensor* to) {
+  const int64_t code = to->dtype == WF_MXFP4 ? 2 : 1;
+  a.src[x] = src;
+  a.ssb[x] = from->stride_b; a.ssh[x] = from->stride_h; a.sss[x] = from->stride_s;
+  a.dst[x] = dst;
+  a.dsb[x] = to->stride_b / code; a.dsh[x] = to->stride_h / code; a.dss[x] = to->stride_s / code;
+  a.heads[x] = from->heads;
+}
+
+// The shapes of a wf_tree_attn call, and what wf_prefix_attn's plan takes for them: a
+// cache of n rows a sequence.
+wf_status check_tree(const wf_tensor* q, const wf_tensor* pool, int n, int n_t, wf_tensor* cache) {
+  wf_status st;
+  if ((st = check_desc(q, false)) != WF_OK) return st;
+  if ((st = check_pool(pool, 1)) != WF_OK) return st;
+  if (!quantised(pool) && pool->dtype != q->dtype) return WF_ERR_DTYPE;
+  if (pool->head_dim != q->head_dim || q->heads % pool->heads) return WF_ERR_SHAPE;
+  if (n < 0 || n_t < 0) return WF_ERR_INVALID_ARG;
+  if (too_many_rows((int64_t)q->batch * q->heads, q->seq) || too_many_rows(1, n) || too_many_rows(1, n_t))
+    return WF_ERR_UNSUPPORTED;
+  *cache = *pool;
+  cache->batch = q->batch;
+  cache->seq = n;
+  return WF_OK;
+}
+
+}  // namespace
+
+WF_API wf_status wf_rotary_plan(const double* freq, const int32_t* axis, int pairs, int64_t* plan) {
+  if (!freq || !plan || pairs < 1) return WF_ERR_INVALID_ARG;
+  for (int i = 0; i < pairs; ++i) {
+    if (!(fabs(freq[i]) < 4294967296.0) || (axis && (axis[i] < 0 || axis[i] >= 64))) return WF_ERR_INVALID_ARG;
+  }
+  for (int i = 0; i < pairs; ++i) {
+    plan[2 * i] = (int64_t)turns_of(freq[i]);
+    plan[2 * i + 1] = axis ? axis[i] : 0;
+  }
+  return WF_OK;
+}
+
+WF_API wf_status wf_rotary_apply(const void* Q, const wf_tensor* q, const void* K, const wf_tensor* k,
+                                 const int64_t* plan, int pairs, int adjacent, const int32_t* pos, int axes,
+                                 void* Qout, const wf_tensor* qo, void* Kout, const wf_tensor* ko, void* stream) {
+  wf_status st;
+  if ((st = check_desc(q, true)) != WF_OK || (st = check_desc(qo, true)) != WF_OK) return st;
+  if ((K != nullptr) != (Kout != nullptr)) return WF_ERR_INVALID_ARG;
+  if (!same_units(q, qo) || q->seq != qo->seq) return WF_ERR_SHAPE;
+  if (q->dtype != qo->dtype) return WF_ERR_DTYPE;
+  if (K) {
+    if ((st = check_desc(k, true)) != WF_OK || (st = check_desc(ko, true)) != WF_OK) return st;
+    if (!same_units(k, ko) || k->seq != ko->seq || k->batch != q->batch || k->head_dim != q->head_dim ||
+        k->seq != q->seq)
+      return WF_ERR_SHAPE;
+    if (k->dtype != q->dtype || ko->dtype != q->dtype) return WF_ERR_DTYPE;
+  }
+  if (too_many_rows((int64_t)q->batch * (q->heads + (int64_t)(K ? k->heads : 0)), q->seq)) return WF_ERR_UNSUPPORTED;
+  if ((st = check_plan(plan, pairs, q->head_dim)) != WF_OK) return st;
+  if (axes < 1) return WF_ERR_INVALID_ARG;
+  if (q->seq == 0) return WF_OK;
+  if (!Q || !Qout || !pos) return WF_ERR_INVALID_ARG;
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(Qout) || !aligned16(Kout) || !aligned4(pos)) return WF_ERR_ALIGN;
+  wf::RowsArgs a = {};
+  fill_rows(a, 0, Q, q, Qout, qo);
+  if (K) fill_rows(a, 1, K, k, Kout, ko);
+  a.both = 1;
+  a.plan = reinterpret_cast<const wf::RotaryPair*>(plan);
+  a.pairs = pairs; a.adjacent = adjacent != 0;
+  a.pos = pos; a.axes = axes; a.B = q->batch; a.rows = q->seq;
+  a.by_m = wf::make_fastdiv((uint32_t)q->seq);
+  a.total = (uint32_t)q->batch * (uint32_t)q->seq;
+  return cuda_status(wf::launch_rotate(a, q->dtype, q->head_dim, static_cast<cudaStream_t>(stream)));
+}
+
+WF_API wf_status wf_paged_append(const void* Knew, const void* Vnew, const wf_tensor* nt, const int32_t* rows_at, int m,
+                                 const int32_t* start, const int32_t* count, const int64_t* plan, int pairs,
+                                 int adjacent, const int32_t* pos, int axes, void* K, void* V, void* Ks, void* Vs,
+                                 const wf_tensor* pool, size_t scales_bytes, const int32_t* pages, int table,
+                                 void* stream) {
+  wf_status st;
+  if ((st = check_pool(pool, table)) != WF_OK || (st = check_desc(nt, true)) != WF_OK) return st;
+  if (!quantised(pool) && pool->dtype != nt->dtype) return WF_ERR_DTYPE;
+  if (nt->heads != pool->heads || nt->head_dim != pool->head_dim) return WF_ERR_SHAPE;
+  if (m < 0 || (rows_at ? nt->seq < 1 && m > 0 : m != nt->seq)) return WF_ERR_INVALID_ARG;
+  if (too_many_rows((int64_t)nt->batch * nt->heads * 2, nt->seq) || too_many_rows((int64_t)nt->batch * nt->heads * 2, m))
+    return WF_ERR_UNSUPPORTED;
+  if (quantised(pool) && scales_bytes < wf_scales_bytes(pool)) return WF_ERR_WORKSPACE;
+  if (plan && (st = check_plan(plan, pairs, nt->head_dim)) != WF_OK) return st;
+  if (pos && axes < 1) return WF_ERR_INVALID_ARG;
+  if (m == 0) return WF_OK;
+  if (!Knew || !K || !start || !pages) return WF_ERR_INVALID_ARG;
+  if ((Vnew != nullptr) != (V != nullptr)) return WF_ERR_INVALID_ARG;
+  if (quantised(pool) ? (!Ks || (Vs != nullptr) != (V != nullptr)) : (Ks || Vs)) return WF_ERR_INVALID_ARG;
+  if (!aligned16(Knew) || !aligned16(Vnew) || !aligned16(K) || !aligned16(V) || !aligned4(Ks) || !aligned4(Vs) ||
+      !aligned4(rows_at) || !aligned4(start) || !aligned4(count) || !aligned4(pos) || !aligned4(pages))
+    return WF_ERR_ALIGN;
+  wf::RowsArgs a = {};
+  fill_rows(a, 0, Knew, nt, K, pool);
+  if (V) fill_rows(a, 1, Vnew, nt, V, pool);
+  a.scales[0] = static_cast<uint8_t*>(Ks); a.scales[1] = static_cast<uint8_t*>(Vs);
+  a.plan = reinterpret_cast<const wf::RotaryPair*>(plan);
+  a.pairs = pairs; a.adjacent = adjacent != 0;
+  a.pos = pos; a.axes = pos ? axes : 64; a.B = nt->batch; a.rows = nt->seq;
+  a.pages = pages; a.start = start; a.rows_at = rows_at; a.count = count;
+  a.table = table; a.pool = pool->batch;
+  a.by_ps = wf::make_fastdiv((uint32_t)pool->seq);
+  a.by_m = wf::make_fastdiv((uint32_t)m);
+  a.total = (uint32_t)nt->batch * (uint32_t)m;
+  return cuda_status(wf::launch_append(a, nt->dtype, pool->dtype, nt->head_dim, static_cast<cudaStream_t>(stream)));
+}
+
+WF_API size_t wf_tree_attn_workspace_bytes(const wf_tensor* q, const wf_tensor* pool, int n, int n_t) {
+  wf_tensor cache;
+  if (check_tree(q, pool, n, n_t, &cache) != WF_OK) return 0;
+  return wf::plan_prefix(*q, cache, n, n_t, true).total;
+}
+
+WF_API wf_status wf_tree_attn(const void* Q, const wf_tensor* q, const void* K, const void* V, const wf_tensor* pool,
+                              const void* Ks, const void* Vs, const int32_t* pages, int table, int n,
+                              const int32_t* cache_len, const void* Kt, const void* Vt, const wf_tensor* t,
+                              const int32_t* tree_len, const int32_t* mask, void* O, const wf_tensor* o, float scale,
+                              void* ws, size_t ws_bytes, void* stream) {
+  const int n_t = t ? t->seq : 0;
+  wf_tensor cache;
+  wf_status st = check_tree(q, pool, n, n_t, &cache);
+  if (st != WF_OK || (st = check_pool(pool, table)) != WF_OK) return st;
+  if (n > (int64_t)table * pool->seq) return WF_ERR_INVALID_ARG;
+  if ((st = check_attn_rows(q, pool, t, o)) != WF_OK) return st;
+  if (!Q || !K || !V || !O || !ws || !pages) return WF_ERR_INVALID_ARG;
+  if (quantised(pool) ? (!Ks || !Vs) : (Ks || Vs)) return WF_ERR_INVALID_ARG;
+  if (n_t > 0 && (!Kt || !Vt)) return WF_ERR_INVALID_ARG;
+  if (!(scale >= 0.f) || isinf(scale)) return WF_ERR_INVALID_ARG;
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned4(Ks) || !aligned4(Vs))
+    return WF_ERR_ALIGN;
+  if (n_t > 0 && (!aligned16(Kt) || !aligned16(Vt))) return WF_ERR_ALIGN;
+  if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0 || !aligned4(pages) || !aligned4(cache_len) ||
+      !aligned4(tree_len) || !aligned4(mask))
+    return WF_ERR_ALIGN;
+  wf::PrefixPlan p = wf::plan_prefix(*q, cache, n, n_t, true);
+  if (ws_bytes < p.total) return WF_ERR_WORKSPACE;
+  fill_prefix(p, Q, q, K, V, pool, Ks, Vs, Kt, Vt, t, O, o, scale, ws);
+  wf::PrefixArgs& a = p.a;
+  a.plen = cache_len; a.glen = tree_len;
+  a.pages = pages; a.table = table; a.pool = pool->batch;
+  a.by_ps = wf::make_fastdiv((uint32_t)pool->seq);
+  a.kx = a.ksb - (int64_t)pool->seq * a.kss;
+  a.mask = n_t > 0 ? reinterpret_cast<const uint32_t*>(mask) : nullptr;
+  a.mw = (n_t + 31) / 32;
+  return cuda_status(wf::launch_tree(p, static_cast<cudaStream_t>(stream)));
 }
 
 WF_API wf_status wf_workspace_status(void* ws, void* stream) {

@@ -58,22 +58,6 @@ __device__ __forceinline__ uint32_t top_bits(const bf16*, const uint4& v) {
   return max(m & 0xffff0000u, m << 16);
 }
 
-template <int BYTES> struct Word;
-template <> struct Word<8> { typedef uint2 type; };
-template <> struct Word<4> { typedef uint32_t type; };
-template <> struct Word<2> { typedef uint16_t type; };
-
-// Codes of the N channels of one thread from their values in units of the scale.
-template <bool FP4, int N>
-__device__ __forceinline__ typename Word<FP4 ? N / 2 : N>::type pack_codes(const float* y) {
-  constexpr int BITS = FP4 ? 8 : 16;
-  uint32_t w[2] = {0, 0};
-#pragma unroll
-  for (int i = 0; i < N / 2; ++i) w[i * BITS / 32] |= mx_encode2<FP4>(y[2 * i], y[2 * i + 1]) << (i * BITS % 32);
-  if constexpr (!FP4 && N == 8) return make_uint2(w[0], w[1]);
-  else return (typename Word<FP4 ? N / 2 : N>::type)w[0];
-}
-
 // A thread's values from its codes and their scale byte, stored: bf16 by exact
 // products of pairs, fp32 by way of half precision.
 template <bool FP4>

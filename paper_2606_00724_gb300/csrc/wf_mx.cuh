@@ -44,6 +44,22 @@ __device__ __forceinline__ uint32_t mx_encode2(float a, float b) {
   if (FP4) return __nv_cvt_float2_to_fp4x2(make_float2(a, b), __NV_E2M1, cudaRoundNearest);
   return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
+template <int BYTES> struct Word;
+template <> struct Word<8> { typedef uint2 type; };
+template <> struct Word<4> { typedef uint32_t type; };
+template <> struct Word<2> { typedef uint16_t type; };
+
+// Codes of the N channels of one thread from their values in units of the scale.
+template <bool FP4, int N>
+__device__ __forceinline__ typename Word<FP4 ? N / 2 : N>::type pack_codes(const float* y) {
+  constexpr int BITS = FP4 ? 8 : 16;
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) w[i * BITS / 32] |= mx_encode2<FP4>(y[2 * i], y[2 * i + 1]) << (i * BITS % 32);
+  if constexpr (!FP4 && N == 8) return make_uint2(w[0], w[1]);
+  else return (typename Word<FP4 ? N / 2 : N>::type)w[0];
+}
+
 // Two fp32 values from two codes (in the low bits of c).
 template <bool FP4>
 __device__ __forceinline__ float2 mx_decode2(uint32_t c) {

@@ -51,7 +51,7 @@ __device__ __forceinline__ int at(int r, int c) { return r * D + ((c ^ (r & 7)) 
 // 64 x 64 logits of 128 channels and their products with V are 2 x 4096 cycles of
 // the fp32 pipe, and the corrections of the logits' sums (below) 2560 more; the
 // shared-memory reads stay below that with 4 rows x 4 keys a thread.
-template <int CACHE, int D, int TR>
+template <int CACHE, int D, int TR, bool PAGED>
 __global__ void __launch_bounds__(kThreads<TR>, TR == 128 ? 1 : 2) simt_kernel(const __grid_constant__ PrefixArgs a) {
   constexpr int NTH = kThreads<TR>, RT = TR * 16 / NTH, C = D / 64;
   constexpr bool FP4 = CACHE == kFp4;
@@ -77,19 +77,31 @@ __global__ void __launch_bounds__(kThreads<TR>, TR == 128 ? 1 : 2) simt_kernel(c
   const int k0 = min(count, sp_i * per * TK), k1 = min(count, (sp_i + 1) * per * TK);
   const bool coded = CACHE != kPlain && !own;
   const int32_t* idx = a.idx && !own ? a.idx + (int64_t)u * a.k : nullptr;
-  auto row_of = [&](int j) { return idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j; };
+  // Elements, or bytes of codes, from row 0 to row j of the prompt, and its row of scales.
+  const int64_t cached = PAGED ? h * a.ksh : b * a.ksb + h * a.ksh;
+  auto row_of = [&](int j, int64_t* scales) {
+    if (PAGED) {
+      const PagedRow w = paged_row(a, b, j);
+      *scales = paged_scale(a, w, h);
+      return paged_offset(a, w);
+    }
+    const int64_t row = idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j;
+    *scales = (int64_t)u * a.n + row;
+    return row * a.kss;
+  };
 
   // Rows t0 .. of K or V as they are, by cp.async.
   auto copy = [&](bool v, int t0) {
     const float* base = static_cast<const float*>(v ? (own ? a.Vg : a.V) : (own ? a.Kg : a.K)) +
-                        b * (own ? a.gsb : a.ksb) + h * (own ? a.gsh : a.ksh);
-    const int64_t ss = own ? a.gss : a.kss;
+                        (own ? b * a.gsb + h * a.gsh : cached);
     const uint32_t dst = smem_u32(v ? sv : sk);
 #pragma unroll 4
     for (int e = tid; e < TK * (D / 4); e += NTH) {
       const int r = e / (D / 4), c = e % (D / 4);
       const bool ok = t0 + r < k1;
-      cp_async16_zfill(dst + 4 * at<D>(r, c), base + (ok ? row_of(t0 + r) * ss : 0) + 4 * c, ok);
+      int64_t scales;
+      const int64_t o = !ok ? 0 : own ? (t0 + r) * a.gss : row_of(t0 + r, &scales);
+      cp_async16_zfill(dst + 4 * at<D>(r, c), base + o + 4 * c, ok);
     }
     cp_async_commit();
   };
@@ -103,8 +115,8 @@ __global__ void __launch_bounds__(kThreads<TR>, TR == 128 ? 1 : 2) simt_kernel(c
       code[i] = make_uint4(0, 0, 0, 0);
       byte[i] = 0;
       if (r < TK && t0 + r < k1) {
-        const int64_t row = row_of(t0 + r);
-        const uint8_t* p = static_cast<const uint8_t*>(v ? a.V : a.K) + b * a.ksb + h * a.ksh + row * a.kss;
+        int64_t scales;
+        const uint8_t* p = static_cast<const uint8_t*>(v ? a.V : a.K) + cached + row_of(t0 + r, &scales);
         if (FP4) {
           const uint2 w = __ldg(reinterpret_cast<const uint2*>(p) + c);
           code[i].x = w.x;
@@ -112,7 +124,7 @@ __global__ void __launch_bounds__(kThreads<TR>, TR == 128 ? 1 : 2) simt_kernel(c
         } else {
           code[i] = __ldg(reinterpret_cast<const uint4*>(p) + c);
         }
-        byte[i] = __ldg((v ? a.Vs : a.Ks) + ((int64_t)u * a.n + row) * (D / kMxBlock) + c / 2);
+        byte[i] = __ldg((v ? a.Vs : a.Ks) + scales * (D / kMxBlock) + c / 2);
       }
     }
   };
@@ -204,6 +216,7 @@ __global__ void __launch_bounds__(kThreads<TR>, TR == 128 ? 1 : 2) simt_kernel(c
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
       float top = -INFINITY;
+      const int block_row = PAGED && own && a.mask ? own_row(a, b, h, min(r0 + ty * RT + i, a.Ro - 1)).i : 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float h2 = s[i][j];
@@ -214,6 +227,7 @@ __global__ void __launch_bounds__(kThreads<TR>, TR == 128 ? 1 : 2) simt_kernel(c
             h2 = fmaf(sq[at<D>(ty * RT + i, c / 4) + c % 4], sk[at<D>(tx + 16 * j, c / 4) + c % 4], h2);
         }
         s[i][j] = tx + 16 * j < nk ? h2 : -INFINITY;
+        if (PAGED && own && a.mask && tx + 16 * j < nk && !sees(a, b, block_row, t0 + tx + 16 * j)) s[i][j] = -INFINITY;
         top = fmaxf(top, s[i][j]);
       }
 #pragma unroll
@@ -254,6 +268,8 @@ __global__ void __launch_bounds__(kThreads<TR>, TR == 128 ? 1 : 2) simt_kernel(c
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
           const float pi = k == 0 ? p[i].x : k == 1 ? p[i].y : k == 2 ? p[i].z : p[i].w;
+          // A masked row of V may hold anything: 0 times it is not 0.
+          if (PAGED && own && pi == 0.f) continue;
           const f32x2 pp = pk2(pi, pi);
 #pragma unroll
           for (int c = 0; c < C; ++c) {
@@ -354,28 +370,27 @@ int simt_rows(const PrefixArgs& a) {
   return r <= 16 ? 16 : r <= 64 ? 64 : 128;
 }
 
-template <int CACHE, int D, int TR>
+template <int CACHE, int D, int TR, bool PAGED>
 cudaError_t launch_rows(const PrefixArgs& a, unsigned items, cudaStream_t s) {
-  const auto k = simt_kernel<CACHE, D, TR>;
+  const auto k = simt_kernel<CACHE, D, TR, PAGED>;
   const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(k), simt_smem<D, TR>());
   return e != cudaSuccess ? e : Launch(dim3(items), kThreads<TR>, simt_smem<D, TR>(), s)(k, a);
 }
-template <int CACHE, int D>
+template <int CACHE, int D, bool PAGED>
 cudaError_t launch_simt(const PrefixArgs& a, cudaStream_t s) {
   const int64_t items = (int64_t)a.P * a.H * a.mt * a.S + (int64_t)a.B * a.H * a.mto * a.So;
   if (!items) return cudaSuccess;
   const int tr = simt_rows(a);
-  return tr == 16 ? launch_rows<CACHE, D, 16>(a, (unsigned)items, s)
-         : tr == 64 ? launch_rows<CACHE, D, 64>(a, (unsigned)items, s)
-                    : launch_rows<CACHE, D, 128>(a, (unsigned)items, s);
+  return tr == 16 ? launch_rows<CACHE, D, 16, PAGED>(a, (unsigned)items, s)
+         : tr == 64 ? launch_rows<CACHE, D, 64, PAGED>(a, (unsigned)items, s)
+                    : launch_rows<CACHE, D, 128, PAGED>(a, (unsigned)items, s);
 }
-
-cudaError_t launch_parts(const PrefixPlan& p, cudaStream_t s) {
+template <bool PAGED>
+cudaError_t launch_cached(const PrefixPlan& p, cudaStream_t s) {
   const bool wide = p.a.d == 128;
-  if (p.dtype == WF_BF16) return launch_prefix_tc(p, s);
-  if (p.fmt == WF_MXFP8) return wide ? launch_simt<kFp8, 128>(p.a, s) : launch_simt<kFp8, 64>(p.a, s);
-  if (p.fmt == WF_MXFP4) return wide ? launch_simt<kFp4, 128>(p.a, s) : launch_simt<kFp4, 64>(p.a, s);
-  return wide ? launch_simt<kPlain, 128>(p.a, s) : launch_simt<kPlain, 64>(p.a, s);
+  if (p.fmt == WF_MXFP8) return wide ? launch_simt<kFp8, 128, PAGED>(p.a, s) : launch_simt<kFp8, 64, PAGED>(p.a, s);
+  if (p.fmt == WF_MXFP4) return wide ? launch_simt<kFp4, 128, PAGED>(p.a, s) : launch_simt<kFp4, 64, PAGED>(p.a, s);
+  return wide ? launch_simt<kPlain, 128, PAGED>(p.a, s) : launch_simt<kPlain, 64, PAGED>(p.a, s);
 }
 
 template <typename T, int D>
@@ -389,7 +404,7 @@ cudaError_t launch_join(const PrefixArgs& a, cudaStream_t s) {
 
 }  // namespace
 
-PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) {
+PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g, bool paged) {
   PrefixPlan p = {};
   PrefixArgs& a = p.a;
   a.B = q.batch; a.P = kv.batch; a.H = kv.heads; a.G = q.heads / kv.heads;
@@ -434,7 +449,7 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   double prompt_us, own_us;
   a.S = split((int64_t)a.P * a.H * a.mt, k, &prompt_us);
   const int64_t own = (int64_t)a.B * a.H * a.mto;
-  p.fold = tc && n_g > 0 && own >= kPrefixOwn && n_g <= std::min<int64_t>(2 * own, a.Ro <= 16 ? 512 : 256);
+  p.fold = tc && n_g > 0 && paged ? true : tc && n_g > 0 && own >= kPrefixOwn && n_g <= std::min<int64_t>(2 * own, a.Ro <= 16 ? 512 : 256);
   a.So = p.fold ? 0 : split(own, n_g, &own_us);
   // Prompt rows that every sequence attends to for itself, where its own rows are
   // (one launch): a 64-key tile takes 1.25 us, or its bytes for all blocks of
@@ -442,7 +457,7 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   // 4 heads' tokens, 128 rows and 32 own ones 6.0 against 9.5 us, 400 and 32 10.8
   // against 10.1; blocks of 32 rows of 4 sequences and 16 heads on 128 rows 7.3
   // against 12.8, of 32 sequences on 400 rows 36 against 26.
-  if (tc && p.fmt == WF_BF16 && k > 0 && k + n_g <= 1024) {
+  if (tc && !paged && p.fmt == WF_BF16 && k > 0 && k + n_g <= 1024) {
     auto direct = [&](int keys) {
       const double blocks = (double)a.B * a.H * ((a.Ro + prefix_own_rows(a, 0, keys) - 1) / prefix_own_rows(a, 0, keys));
       return ((keys + 63) / 64) * std::max(1.25, blocks * 256 * a.d / 2.4e6);
@@ -477,12 +492,23 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) 
   return p;
 }
 
-cudaError_t launch_prefix(const PrefixPlan& p, cudaStream_t s) {
-  const cudaError_t e = launch_parts(p, s);
-  if (e != cudaSuccess || p.a.whole) return e;
-  if (p.fold) return launch_prefix_own(p, s);
+namespace {
+cudaError_t join(const PrefixPlan& p, cudaStream_t s) {
   if (p.dtype == WF_BF16) return p.a.d == 128 ? launch_join<bf16, 128>(p.a, s) : launch_join<bf16, 64>(p.a, s);
   return p.a.d == 128 ? launch_join<float, 128>(p.a, s) : launch_join<float, 64>(p.a, s);
+}
+}  // namespace
+
+cudaError_t launch_prefix(const PrefixPlan& p, cudaStream_t s) {
+  const cudaError_t e = p.dtype == WF_BF16 ? launch_prefix_tc(p, s) : launch_cached<false>(p, s);
+  if (e != cudaSuccess || p.a.whole) return e;
+  return p.fold ? launch_prefix_own(p, s) : join(p, s);
+}
+
+cudaError_t launch_tree(const PrefixPlan& p, cudaStream_t s) {
+  const cudaError_t e = p.dtype == WF_BF16 ? launch_tree_tc(p, s) : launch_cached<true>(p, s);
+  if (e != cudaSuccess || p.a.whole) return e;
+  return p.fold ? launch_tree_own(p, s) : join(p, s);
 }
 
 }  // namespace wf

@@ -45,6 +45,15 @@ struct PrefixArgs {
   int* status;
   long long wait_limit;  // bound of the tensor-core kernel's waits (cycles)
   int stall;             // test-only: its first wait is on a barrier that nothing completes
+  // A cache in pages (wf_tree_attn; else null): row j of a sequence is row j % ps
+  // of page pages[b][j / ps], and ksb is the stride between pages.
+  const int32_t* pages;
+  int table, pool;       // entries a sequence, pages of the pool
+  FastDiv by_ps;
+  int64_t kx;            // ksb - ps kss: what a page adds to the rows before it
+  // The drafted rows that a query row sees (null: all): bit j of mask[b][i].
+  const uint32_t* mask;
+  int mw;                // words a row
 };
 
 // With at least so many units of own rows, and not too many rows for them, they are
@@ -70,12 +79,18 @@ struct PrefixPlan {
   size_t off_ml, off_o, used;  // used: what this call writes
   size_t total;                // what it asks for
 };
-PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g);
+// paged: for wf_tree_attn, whose own rows (the drafted ones) are joined where the
+// queries are bf16.
+PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g, bool paged = false);
 cudaError_t launch_prefix(const PrefixPlan& p, cudaStream_t s);
+cudaError_t launch_tree(const PrefixPlan& p, cudaStream_t s);
 // Query rows a CTA of that kernel for S parts and so many keys.
 int prefix_own_rows(const PrefixArgs& a, int S, int keys);
 cudaError_t launch_prefix_own(const PrefixPlan& p, cudaStream_t s);  // own rows and the joining of parts, bf16
 cudaError_t launch_prefix_tc(const PrefixPlan& p, cudaStream_t s);  // the parts (or O) of bf16 queries
+// The same for caches in pages and masks.
+cudaError_t launch_tree_own(const PrefixPlan& p, cudaStream_t s);
+cudaError_t launch_tree_tc(const PrefixPlan& p, cudaStream_t s);
 
 // Sequence, query head and block row of row r of the unit of prompt p (or of
 // sequence b) and key head h.
@@ -99,6 +114,27 @@ __device__ __forceinline__ int prompt_count(const PrefixArgs& a, int p) {
 }
 __device__ __forceinline__ int own_count(const PrefixArgs& a, int b) {
   return a.glen ? min(a.ng, max(0, __ldg(a.glen + b))) : a.ng;
+}
+
+// A row of a cache in pages: its number in the pool, and its page.
+struct PagedRow {
+  int flat, page;
+};
+__device__ __forceinline__ PagedRow paged_row(const PrefixArgs& a, int b, int j) {
+  const int entry = fastdiv((uint32_t)j, a.by_ps);
+  const int page = min(max(__ldg(a.pages + (int64_t)b * a.table + entry), 0), a.pool - 1);
+  return {page * (int)a.by_ps.d + (j - entry * (int)a.by_ps.d), page};
+}
+__device__ __forceinline__ int64_t paged_offset(const PrefixArgs& a, const PagedRow& r) {
+  return r.flat * a.kss + r.page * a.kx;
+}
+// Its row among the scales of key head h.
+__device__ __forceinline__ int64_t paged_scale(const PrefixArgs& a, const PagedRow& r, int h) {
+  return r.flat + ((int64_t)r.page * (a.H - 1) + h) * a.by_ps.d;
+}
+// Whether query row i of sequence b sees drafted row j.
+__device__ __forceinline__ bool sees(const PrefixArgs& a, int b, int i, int j) {
+  return !a.mask || (__ldg(a.mask + ((int64_t)b * a.q + i) * a.mw + (j >> 5)) >> (j & 31) & 1);
 }
 
 }  // namespace wf

@@ -204,7 +204,26 @@ __device__ __forceinline__ uint32_t swizzled(int r, int ch) {
 
 // One tile of bf16 rows, NPT threads: chunk tid % CH of rows tid / CH + RS i.
 // With idx, lane ch of the CH lanes that share a row looks up rows
-// tid / CH + RS (ch + CH k) and the lanes pass them on.
+// tid / CH + RS (ch + CH k) and the lanes pass them on; of a cache in pages that
+// is look_up's, a tile ahead.
+template <int D, int NPT>
+__device__ __forceinline__ PagedRow look_up(const PrefixArgs& a, int b, int t0, int k1, int tid) {
+  constexpr int CH = D / 8, RS = NPT / CH, NI = TM / RS;
+  static_assert(NI <= CH, "one row a lane");
+  const int ch = tid % CH, j = t0 + tid / CH + RS * ch;
+  return ch < NI && j < k1 ? paged_row(a, b, j) : PagedRow{-1, 0};
+}
+template <int D, int NPT>
+__device__ __forceinline__ void copy_paged(uint32_t st, const PrefixArgs& a, const bf16* base, const PagedRow& at, int tid) {
+  constexpr int CH = D / 8, RS = NPT / CH, NI = TM / RS;
+  const int ch = tid % CH, rr = tid / CH;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const PagedRow w = {__shfl_sync(0xffffffffu, at.flat, i, CH), __shfl_sync(0xffffffffu, at.page, i, CH)};
+    const bool ok = w.flat >= 0;
+    cp_async16_zfill(st + swizzled(rr + RS * i, ch), base + ch * 8 + (ok ? paged_offset(a, w) : 0), ok);
+  }
+}
 template <int D, int NPT>
 __device__ __forceinline__ void copy_tile(uint32_t st, const bf16* base, int64_t stride, const int32_t* idx, int n, int t0,
                                           int k1, int tid) {
@@ -245,12 +264,35 @@ __device__ __forceinline__ void copy_tile(uint32_t st, const bf16* base, int64_t
 __device__ __forceinline__ RowAt row_at(const PrefixArgs& a, const Item& w, int r) {
   return w.own ? own_row(a, w.b, w.h, w.r0 + r) : prompt_row(a, w.b, w.h, w.r0 + r);
 }
-template <int D, int FMT>
+template <int D, int FMT, bool PAGED>
 __device__ void produce(const PrefixArgs& a, const Item& w, const Ring& ring, uint32_t raw, Bars& s, int tid) {
   typedef Cfg<D, FMT> C;
   constexpr int NPT = C::NPT;
   const int64_t b = w.b, h = w.h;
   const int A = w.wide ? 1 : 2;
+  if constexpr (PAGED && !C::CODES) {
+    const bf16 *K = static_cast<const bf16*>(a.K) + h * a.ksh, *V = static_cast<const bf16*>(a.V) + h * a.ksh;
+    int pos = -1, tile = -1;
+    bool ok = true, kind = false;
+    PagedRow row = {-1, 0};
+    auto bring = [&] {
+      const int st = ring.stage(pos), n = ring.turn(pos);
+      if (ok && n > 0) ok = warp_wait(bar(s.empty[st]), (n - 1) & 1, s, a);
+      if (ok) copy_paged<D, NPT>(ring.base + st * C::TILE, a, kind ? V : K, row, tid);
+      cp_async_arrive_noinc(bar(s.full[st]));
+    };
+    in_order(w.T, A, [&](int t, bool v) {
+      const PagedRow next = look_up<D, NPT>(a, w.b, w.k0 + t * TM, w.k1, tid);
+      if (tile >= 0) bring();
+      row = next;
+      kind = v;
+      tile = t;
+      ++pos;
+    });
+    if (tile >= 0) bring();
+    cp_async_wait_all();
+    return;
+  }
   if (!C::CODES || w.own) {
     const int64_t sb = w.own ? a.gsb : a.ksb, sh = w.own ? a.gsh : a.ksh, ss = w.own ? a.gss : a.kss;
     const bf16* K = static_cast<const bf16*>(w.own ? a.Kg : a.K) + b * sb + h * sh;
@@ -334,35 +376,42 @@ __device__ void produce(const PrefixArgs& a, const Item& w, const Ring& ring, ui
 // their scales, and the lanes pass the rows on for the chunks.  A row's scale
 // bytes have 4 bytes of a slot; where they are 2, they are stored by the thread,
 // since the smallest copy is 4 bytes on 4.
-template <int D, int FMT>
+template <int D, int FMT, bool PAGED>
 __device__ void load_codes(const PrefixArgs& a, const Item& w, uint32_t raw, Bars& s, int warp, int lane) {
   typedef Cfg<D, FMT> C;
   constexpr int CR = C::CR, RP = 32 / CR, NI = 64 / RP, SR = D / kMxBlock;  // rows a pass of the warp, passes
   const int64_t b = w.b, h = w.h;
   const int x = lane % CR;
-  const int32_t* idx = a.idx ? a.idx + (int64_t)w.u * a.k : nullptr;
-  const uint8_t* kbase = static_cast<const uint8_t*>(a.K) + b * a.ksb + h * a.ksh + x * 16;
-  const uint8_t* vbase = static_cast<const uint8_t*>(a.V) + b * a.ksb + h * a.ksh + x * 16;
-  const int64_t srow = (int64_t)w.u * a.n * SR;
+  const int32_t* idx = !PAGED && a.idx ? a.idx + (int64_t)w.u * a.k : nullptr;
+  const int64_t unit = (PAGED ? 0 : b * a.ksb) + h * a.ksh + x * 16;
+  const uint8_t* kbase = static_cast<const uint8_t*>(a.K) + unit;
+  const uint8_t* vbase = static_cast<const uint8_t*>(a.V) + unit;
+  const int64_t srow = PAGED ? 0 : (int64_t)w.u * a.n * SR;
   // Row q of the warp's half is row 64 warp + q of the tile; -1 past the last.
-  auto look_up = [&](int t, int* row) {
+  auto look_up = [&](int t, int* row, int* page) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const int j = w.k0 + t * TM + 64 * warp + lane + 32 * k;
-      row[k] = j >= w.k1 ? -1 : idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j;
+      if (PAGED) {
+        const PagedRow r = j >= w.k1 ? PagedRow{-1, 0} : paged_row(a, w.b, j);
+        row[k] = r.flat;
+        page[k] = r.page;
+      } else {
+        row[k] = j >= w.k1 ? -1 : idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j;
+      }
     }
   };
   int slot = 0, n = 0;
   bool ok = true;
   const uint32_t first = (uint32_t)((64 * warp + lane / CR) * CR) * 16;  // this lane's first row in a slot
-  auto bring = [&](int t, const int* row, bool v) {
+  auto bring = [&](int t, const int* row, const int* page, bool v) {
     if (ok && n > 0) ok = warp_wait(bar(s.raw_empty[slot]), (n - 1) & 1, s, a);
     if (ok) {
       const uint32_t dst = raw + slot * C::SLOT;
       const uint8_t* base = v ? vbase : kbase;
       const uint8_t* sc = (v ? a.Vs : a.Ks) + srow;
       const bool full = w.k0 + (t + 1) * TM <= w.k1;
-      if (!idx && full) {
+      if (!PAGED && !idx && full) {
         const uint8_t* p = base + (w.k0 + t * TM + 64 * warp + lane / CR) * a.kss;
 #pragma unroll
         for (int i = 0; i < NI; ++i, p += RP * a.kss)
@@ -371,14 +420,15 @@ __device__ void load_codes(const PrefixArgs& a, const Item& w, uint32_t raw, Bar
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
           const int at = __shfl_sync(0xffffffffu, row[RP * i / 32], (RP * i + lane / CR) % 32);
-          cp_async16_zfill(dst + first + RP * CR * 16 * i + C::place(x, lane / CR + RP * i) * 16,
-                           base + max(at, 0) * a.kss, at >= 0);
+          int64_t from = max(at, 0) * a.kss;
+          if (PAGED) from += __shfl_sync(0xffffffffu, page[RP * i / 32], (RP * i + lane / CR) % 32) * a.kx;
+          cp_async16_zfill(dst + first + RP * CR * 16 * i + C::place(x, lane / CR + RP * i) * 16, base + from, at >= 0);
         }
       }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const uint32_t at = dst + TM * C::ROWB + (uint32_t)(64 * warp + lane + 32 * k) * 4;
-        const uint8_t* p = sc + (int64_t)max(row[k], 0) * SR;
+        const uint8_t* p = sc + (PAGED ? paged_scale(a, {max(row[k], 0), page[k]}, w.h) : max(row[k], 0)) * SR;
         if (SR == 4) cp_async4(at, p, row[k] < 0 ? 0 : 4);  // rows past the last: scale 2^-127 of zeros
         else sts_u32(at, row[k] < 0 ? 0u : __ldg(reinterpret_cast<const uint16_t*>(p)));
       }
@@ -387,17 +437,20 @@ __device__ void load_codes(const PrefixArgs& a, const Item& w, uint32_t raw, Bar
     cp_async_arrive_noinc(bar(s.raw_full[slot]));
     if (++slot == C::DEPTH) { slot = 0; ++n; }
   };
-  int row[2], ahead[2], tile = -1;
+  int row[2], ahead[2], page[2], page_ahead[2], tile = -1;
   bool kind = false;
   in_order(w.T, w.wide ? 1 : 2, [&](int t, bool v) {
-    look_up(t, ahead);
-    if (tile >= 0) bring(tile, row, kind);
-    row[0] = ahead[0];
-    row[1] = ahead[1];
+    look_up(t, ahead, page_ahead);
+    if (tile >= 0) bring(tile, row, page, kind);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      row[k] = ahead[k];
+      page[k] = page_ahead[k];
+    }
     kind = v;
     tile = t;
   });
-  if (tile >= 0) bring(tile, row, kind);
+  if (tile >= 0) bring(tile, row, page, kind);
   cp_async_wait_all();
 }
 
@@ -715,7 +768,7 @@ __device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* sm, uint8_t*
     a.part_ml[(int64_t)w.part * a.rows + s.row[row]] = make_float2(m, l);
 }
 
-template <int D, int FMT>
+template <int D, int FMT, bool PAGED>
 __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_constant__ PrefixArgs a) {
   typedef Cfg<D, FMT> C;
   extern __shared__ __align__(1024) uint8_t sm[];
@@ -764,10 +817,10 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   if (warp < 16) {
     soften<D, FMT>(a, w, sm, stages, s, tid);
   } else if (warp < MMA_WARP) {
-    produce<D, FMT>(a, w, ring, smem_u32(raw), s, tid - 512);
+    produce<D, FMT, PAGED>(a, w, ring, smem_u32(raw), s, tid - 512);
   } else {
     if (warp < MMA_WARP + 2) multiply<D, FMT>(a, w, smem_u32(sm), ring, s, warp - MMA_WARP);
-    else if (!w.own) load_codes<D, FMT>(a, w, smem_u32(raw), s, warp - MMA_WARP - 2, tid & 31);
+    else if (!w.own) load_codes<D, FMT, PAGED>(a, w, smem_u32(raw), s, warp - MMA_WARP - 2, tid & 31);
   }
   tc_fence_before();
   __syncthreads();
@@ -777,23 +830,30 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   }
 }
 
-template <int D, int FMT>
+template <int D, int FMT, bool PAGED>
 cudaError_t launch(const PrefixArgs& a, cudaStream_t s) {
   typedef Cfg<D, FMT> C;
   const int64_t items = (int64_t)a.P * a.H * a.mt * a.S + (int64_t)a.B * a.H * a.mto * a.So;
   if (!items) return cudaSuccess;
-  const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(tc_kernel<D, FMT>), C::SMEM);
-  if (e != cudaSuccess) return e;
-  return Launch(dim3((unsigned)items), C::NTH, C::SMEM, s)(tc_kernel<D, FMT>, a);
+  const auto k = tc_kernel<D, FMT, PAGED>;
+  const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(k), C::SMEM);
+  return e != cudaSuccess ? e : Launch(dim3((unsigned)items), C::NTH, C::SMEM, s)(k, a);
+}
+template <bool PAGED>
+cudaError_t launch_cached(const PrefixPlan& p, cudaStream_t s) {
+  const bool wide = p.a.d == 128;
+  if (p.fmt == WF_MXFP8) return wide ? launch<128, WF_MXFP8, PAGED>(p.a, s) : launch<64, WF_MXFP8, PAGED>(p.a, s);
+  if (p.fmt == WF_MXFP4) return wide ? launch<128, WF_MXFP4, PAGED>(p.a, s) : launch<64, WF_MXFP4, PAGED>(p.a, s);
+  return wide ? launch<128, WF_BF16, PAGED>(p.a, s) : launch<64, WF_BF16, PAGED>(p.a, s);
 }
 
 }  // namespace
 
-cudaError_t launch_prefix_tc(const PrefixPlan& p, cudaStream_t s) {
-  const bool wide = p.a.d == 128;
-  if (p.fmt == WF_MXFP8) return wide ? launch<128, WF_MXFP8>(p.a, s) : launch<64, WF_MXFP8>(p.a, s);
-  if (p.fmt == WF_MXFP4) return wide ? launch<128, WF_MXFP4>(p.a, s) : launch<64, WF_MXFP4>(p.a, s);
-  return wide ? launch<128, WF_BF16>(p.a, s) : launch<64, WF_BF16>(p.a, s);
-}
+// wf_tree_tc.cu compiles this file for caches in pages.
+#ifdef WF_TREE
+cudaError_t launch_tree_tc(const PrefixPlan& p, cudaStream_t s) { return launch_cached<true>(p, s); }
+#else
+cudaError_t launch_prefix_tc(const PrefixPlan& p, cudaStream_t s) { return launch_cached<false>(p, s); }
+#endif
 
 }  // namespace wf

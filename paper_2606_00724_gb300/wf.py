@@ -7,7 +7,7 @@ kernels; if libwf.so is missing this module raises on import of the library
 (there is no fallback).
 
 Tensors are [B, H, rows, d] views whose last axis is contiguous (BHSD or
-BSHD strides both work); idx / level_sets are int32.
+BSHD strides both work); idx, level_sets, tables, lengths and masks are int32.
 
 A short call is bound by the time spent here, so the marshalling avoids what
 costs most: addresses and descriptors go to ctypes as they are (the argtypes
@@ -78,6 +78,12 @@ SIGNATURES = {
     "wf_prefix_attn_workspace_bytes": (_SZ, [_T, _T, _I, _I]),
     "wf_prefix_attn": (_I, [_P, _T, _P, _P, _T, _P, _P, _P, _I, _P, _P, _P, _T, _P, _P, _T, ctypes.c_float, _P, _SZ,
                             _P]),
+    "wf_rotary_plan": (_I, [_P, _P, _I, _P]),
+    "wf_rotary_apply": (_I, [_P, _T, _P, _T, _P, _I, _I, _P, _I, _P, _T, _P, _T, _P]),
+    "wf_paged_append": (_I, [_P, _P, _T, _P, _I, _P, _P, _P, _I, _I, _P, _I, _P, _P, _P, _P, _T, _SZ, _P, _I, _P]),
+    "wf_tree_attn_workspace_bytes": (_SZ, [_T, _T, _I, _I]),
+    "wf_tree_attn": (_I, [_P, _T, _P, _P, _T, _P, _P, _P, _I, _I, _P, _P, _P, _T, _P, _P, _P, _T, ctypes.c_float, _P,
+                          _SZ, _P]),
     "wf_workspace_status": (_I, [_P, _P]),
     # include/wf_testing.h (test-only)
     "wf_testing_set_wait_failure": (_I, [_I, ctypes.c_longlong]),
@@ -425,6 +431,101 @@ def wf_prefix_attn(Q, K, V, k: int, Kg, Vg, O, ws, idx=None, prefix_len=None, ge
     _check(lib().wf_prefix_attn(_ptr(Q), dq, _ptr(K), _ptr(V), dk, _ptr(Ks), _ptr(Vs), _ints(idx), k,
                                 _ints(prefix_len), _ptr(Kg), _ptr(Vg), dg, _ints(gen_len), _ptr(O), do, float(scale),
                                 _ptr(ws), ws.nbytes, _stream(stream)), "wf_prefix_attn")
+
+
+def wf_rotary_plan(freq: torch.Tensor, axis: torch.Tensor | None = None) -> torch.Tensor:
+    """The plan of a rotation, [pairs, 2] int64 on the host, from the radians a
+    position of each pair (float64) and its axis (int32, None: all 0); both are
+    tensors on the host (see the C header).  Copy it to the GPU once."""
+    if freq.dtype != torch.float64 or freq.dim() != 1 or not freq.is_contiguous() or freq.is_cuda:
+        raise ValueError("frequencies must be a contiguous float64 vector on the host")
+    if axis is not None and (axis.is_cuda or axis.shape != freq.shape):
+        raise ValueError("axes must be a vector on the host, one a pair")
+    plan = torch.empty(freq.shape[0], 2, dtype=torch.int64)
+    _check(lib().wf_rotary_plan(_ptr(freq), _ints(axis), freq.shape[0], _ptr(plan)), "wf_rotary_plan")
+    return plan
+
+
+def _plan(plan):
+    """Pairs of a plan on the GPU (0 where there is none)."""
+    if plan is None:
+        return 0
+    if plan.dtype != torch.int64 or plan.dim() != 2 or plan.shape[1] != 2 or not plan.is_contiguous():
+        raise ValueError("expected a plan of wf_rotary_plan")
+    return plan.shape[0]
+
+
+def wf_rotary_apply(Q, K, plan, pos, Qout, Kout, adjacent: bool = False, stream=None) -> None:
+    """Q [B, Hq, rows, d] and K [B, Hk, rows, d] (None: Q alone) rotated by pos
+    [axes, B, rows] into Qout and Kout, which may be Q and K (see the C header)."""
+    _on_gpu(Q, K, plan, pos, Qout, Kout)
+    dq, do = desc(Q), desc(Qout)
+    dk, dl = (desc(K), desc(Kout)) if K is not None and Kout is not None else (None, None)
+    if pos.dim() != 3 or tuple(pos.shape[1:]) != (dq.batch, dq.seq):
+        raise ValueError("positions must be [axes, B, rows]")
+    _check(lib().wf_rotary_apply(_ptr(Q), dq, _ptr(K), dk, _ptr(plan), _plan(plan), int(adjacent), _ints(pos),
+                                 pos.shape[0], _ptr(Qout), do, _ptr(Kout), dl, _stream(stream)), "wf_rotary_apply")
+
+
+def _table(pages, batch: int) -> int:
+    """Entries a sequence of a page table [B, entries]."""
+    if pages.dim() != 2 or pages.shape[0] != batch:
+        raise ValueError("a page table has a row a sequence")
+    return pages.shape[1]
+
+
+def wf_paged_append(Knew, Vnew, K, V, pages, start, Ks=None, Vs=None, fmt=None, rows=None, count=None, plan=None,
+                    pos=None, adjacent: bool = False, stream=None) -> None:
+    """Knew (and Vnew) [B, H, rows, d] into the pages of K (and V) [pages, H,
+    page rows, d] from place start [B] on by the table pages [B, entries] (see
+    the C header).  fmt: K and V are codes with scales Ks, Vs.  rows [B, m]: those
+    new rows; count [B]: how many of them.  plan: the keys are rotated by pos
+    [axes, B, rows], or by their place."""
+    _on_gpu(Knew, Vnew, K, V, pages, start, Ks, Vs, rows, count, plan, pos)
+    dn, dk = _pair_desc(Knew, Vnew, "Knew and Vnew"), _pair_desc(K, V, "K and V", fmt)
+    B, m = dn.batch, dn.seq
+    if rows is not None:
+        if rows.dim() != 2 or rows.shape[0] != B:
+            raise ValueError("rows must be [B, m]")
+        m = rows.shape[1]
+    if start.numel() != B or (count is not None and count.numel() != B):
+        raise ValueError("start and count must have an entry a sequence")
+    if pos is not None and (pos.dim() != 3 or tuple(pos.shape[1:]) != (B, dn.seq)):
+        raise ValueError("positions must be [axes, B, rows]")
+    _check(lib().wf_paged_append(_ptr(Knew), _ptr(Vnew), dn, _ints(rows), m, _ints(start), _ints(count), _ptr(plan),
+                                 _plan(plan), int(adjacent), _ints(pos), 0 if pos is None else pos.shape[0], _ptr(K),
+                                 _ptr(V), _ptr(Ks), _ptr(Vs), dk, _scales(Ks, Vs), _ints(pages), _table(pages, B),
+                                 _stream(stream)), "wf_paged_append")
+
+
+def wf_tree_attn_workspace_bytes(Q: torch.Tensor, K: torch.Tensor, n: int, n_t: int, fmt=None) -> int:
+    return int(lib().wf_tree_attn_workspace_bytes(desc(Q), _pair_desc(K, None, "", fmt), n, n_t))
+
+
+def wf_tree_attn(Q, K, V, pages, n: int, Kt, Vt, O, ws, cache_len=None, tree_len=None, mask=None, Ks=None, Vs=None,
+                 fmt=None, scale: float = 0.0, stream=None) -> None:
+    """Attention of Q [B, Hq, q, d] over the first n rows, or cache_len [B] of
+    them, that the table pages [B, entries] finds in the pool K, V [pages, H, page
+    rows, d], and over the drafted rows Kt, Vt [B, H, n_t, d] (None: none), the first
+    tree_len [B] of them, that mask [B, q, words] lets each query row see (see the C
+    header).  fmt: K and V are codes, with scales Ks and Vs."""
+    _on_gpu(Q, K, V, pages, Kt, Vt, O, ws, cache_len, tree_len, mask, Ks, Vs)
+    dq = desc(Q)
+    do = dq if O.stride() == Q.stride() and O.shape == Q.shape and O.dtype == Q.dtype else desc(O)
+    dk = _pair_desc(K, V, "K and V", fmt)
+    dt = _pair_desc(Kt, Vt, "Kt and Vt") if Kt is not None else None
+    if fmt is not None:
+        if Ks is None or Vs is None or _scales(Ks, Vs) < dk.batch * dk.heads * dk.seq * (dk.head_dim // 32):
+            raise ValueError("a quantised cache needs the scales of its K and V")
+    for t in (cache_len, tree_len):
+        if t is not None and t.numel() != dq.batch:
+            raise ValueError("lengths must have an entry a sequence")
+    if mask is not None and tuple(mask.shape) != (dq.batch, dq.seq, ((dt.seq if dt else 0) + 31) // 32):
+        raise ValueError("the mask must be [B, q, words of 32 drafted rows]")
+    _check(lib().wf_tree_attn(_ptr(Q), dq, _ptr(K), _ptr(V), dk, _ptr(Ks), _ptr(Vs), _ints(pages),
+                              _table(pages, dq.batch), n, _ints(cache_len), _ptr(Kt), _ptr(Vt), dt, _ints(tree_len),
+                              _ints(mask), _ptr(O), do, float(scale), _ptr(ws), ws.nbytes, _stream(stream)),
+           "wf_tree_attn")
 
 
 def wf_workspace_status(ws: torch.Tensor, stream=None):
