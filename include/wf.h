@@ -482,8 +482,8 @@ wf_status wf_prefix_attn(const void* Q, const wf_tensor* q, const void* K, const
  * where pair i is channels (i, i + pairs), or (2 i, 2 i + 1) if adjacent != 0;
  * the other channels, from 2 pairs on, stay.  The angle is formed in whole
  * numbers (the position times a plan's turn, modulo 2^64), so a far position is
- * as exact as a near one; its cosine and sine, the products and sums are fp32
- * (for bf16 rows the cosine and sine are within 2^-19), rounded once at the end.
+ * as exact as a near one; its cosine and sine, the products and sums are fp32,
+ * rounded once at the end.
  * The rotation by -p undoes that by p, and is its gradient's.
  *
  * wf_rotary_plan: freq (f_i) and axis (NULL: all 0) of `pairs` pairs into plan,

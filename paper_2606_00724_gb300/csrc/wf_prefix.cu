@@ -468,6 +468,15 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g, 
       p.fold = true;
     }
   }
+  if (paged && tc && a.Ro <= kFewRows) {
+    p.few = p.fold = true;
+    a.tk = kFewKeys;
+    a.tr = a.Ro;
+    a.mt = 1;
+    a.C = (int)std::min<int64_t>(kFewCtas, (int64_t)a.B * a.H * ((k + kFewKeys - 1) / kFewKeys));
+    a.S = a.C ? spread_parts(a) : 0;
+    a.So = 0;
+  }
   p.parts = a.S + a.So;
   a.by_H = make_fastdiv(a.H);
   a.by_S = make_fastdiv(std::max(1, a.S));
@@ -475,7 +484,7 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g, 
   a.by_mt = make_fastdiv(a.mt);
   a.by_mto = make_fastdiv(a.mto);
   a.whole = p.parts == 1 && !p.fold;
-  const int64_t kept = a.whole ? 0 : a.rows * p.parts;  // rows of parts
+  const int64_t kept = a.whole ? 0 : a.C ? ((int64_t)a.C + a.B * a.H * a.mt) * a.tr : a.rows * p.parts;  // rows of parts
   p.off_ml = 256;
   p.off_o = align_up(p.off_ml + sizeof(float2) * (size_t)kept, 256);
   p.used = p.off_o + sizeof(float) * (size_t)kept * a.d;
@@ -487,7 +496,8 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g, 
     const int64_t tiles = (keys + tk - 1) / tk;
     return std::min(tiles * a.rows, alone ? most : std::max(a.rows, most));
   };
-  const int64_t reserved = room(k, n_g == 0) + room(n_g, false);
+  int64_t reserved = room(k, n_g == 0) + room(n_g, false);
+  if (paged && tc) reserved = std::max(reserved, kFewCtas * (int64_t)std::min(a.Ro, kFewRows) + a.rows);
   p.total = align_up(p.off_ml + sizeof(float2) * (size_t)reserved, 256) + sizeof(float) * (size_t)reserved * a.d;
   return p;
 }
@@ -506,7 +516,7 @@ cudaError_t launch_prefix(const PrefixPlan& p, cudaStream_t s) {
 }
 
 cudaError_t launch_tree(const PrefixPlan& p, cudaStream_t s) {
-  const cudaError_t e = p.dtype == WF_BF16 ? launch_tree_tc(p, s) : launch_cached<true>(p, s);
+  const cudaError_t e = p.few ? launch_tree_few(p, s) : p.dtype == WF_BF16 ? launch_tree_tc(p, s) : launch_cached<true>(p, s);
   if (e != cudaSuccess || p.a.whole) return e;
   return p.fold ? launch_tree_own(p, s) : join(p, s);
 }

@@ -54,6 +54,10 @@ struct PrefixArgs {
   // The drafted rows that a query row sees (null: all): bit j of mask[b][i].
   const uint32_t* mask;
   int mw;                // words a row
+  // Where C > 0 the key tiles (tk keys each) that the sequences really have are spread
+  // over C CTAs evenly, see Spread: parts are slots of tr rows then, S is the
+  // most of them that a unit has, and there are no own units.
+  int C, tk, tr;
 };
 
 // With at least so many units of own rows, and not too many rows for them, they are
@@ -76,6 +80,7 @@ struct PrefixPlan {
   int tr, tk;    // query rows a CTA, keys a tile
   int parts;     // 1: the kernel writes O itself
   bool fold;     // the own rows are attended where the parts are joined (So = 0)
+  bool few;      // wf_tree_attn's kernel for few query rows a unit
   size_t off_ml, off_o, used;  // used: what this call writes
   size_t total;                // what it asks for
 };
@@ -91,6 +96,10 @@ cudaError_t launch_prefix_tc(const PrefixPlan& p, cudaStream_t s);  // the parts
 // The same for caches in pages and masks.
 cudaError_t launch_tree_own(const PrefixPlan& p, cudaStream_t s);
 cudaError_t launch_tree_tc(const PrefixPlan& p, cudaStream_t s);
+cudaError_t launch_tree_few(const PrefixPlan& p, cudaStream_t s);
+// Query rows of a unit that the kernel for few of them takes, keys of its tiles, and
+// its CTAs.
+constexpr int kFewRows = 16, kFewKeys = 64, kFewCtas = 2 * kPrefixSms;
 
 // Sequence, query head and block row of row r of the unit of prompt p (or of
 // sequence b) and key head h.
@@ -132,6 +141,95 @@ __device__ __forceinline__ int64_t paged_offset(const PrefixArgs& a, const Paged
 __device__ __forceinline__ int64_t paged_scale(const PrefixArgs& a, const PagedRow& r, int h) {
   return r.flat + ((int64_t)r.page * (a.H - 1) + h) * a.by_ps.d;
 }
+// Work in pages spread over C CTAs: the key tiles of all items, an item being a
+// row tile of tr rows of a unit, lie in one line, items in the order [sequence][key
+// head][row tile]; CTA c takes tiles [c per, (c + 1) per), which are ranges of one item
+// or of several that follow each other.  The lengths are known on the device
+// alone, so every warp finds its place in the line from them.  A range is a part, and its
+// slot is c + item: along the line either grows by one from range to range, so no
+// two ranges share a slot and those of an item follow each other.
+struct Spread {
+  int64_t total, per;
+  __device__ __forceinline__ static int tiles_of(const PrefixArgs& a, int b) {
+    return b < a.B ? (prompt_count(a, b) + a.tk - 1) / a.tk : 0;
+  }
+  // By a whole warp.
+  __device__ __forceinline__ void measure(const PrefixArgs& a) {
+    int64_t t = 0;
+    for (int b = threadIdx.x & 31; b < a.B; b += 32) t += tiles_of(a, b);
+#pragma unroll
+    for (int w = 1; w < 32; w *= 2) t += __shfl_xor_sync(0xffffffffu, t, w);
+    total = t * a.H * a.mt;
+    per = max((int64_t)1, (total + a.C - 1) / a.C);
+  }
+  // The sequence whose items hold tile x < total, and its first tile in the line; by a
+  // whole warp.
+  __device__ __forceinline__ int find(const PrefixArgs& a, int64_t x, int64_t* first) const {
+    const int lane = threadIdx.x & 31;
+    int64_t before = 0;
+    for (int b0 = 0;; b0 += 32) {
+      const int64_t mine = (int64_t)tiles_of(a, b0 + lane) * a.H * a.mt;
+      int64_t sum = mine;
+#pragma unroll
+      for (int w = 1; w < 32; w *= 2) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, sum, w);
+        if (lane >= w) sum += y;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, x < before + sum);
+      if (past || b0 + 32 >= a.B) {
+        const int at = past ? __ffs(past) - 1 : 31;
+        *first = before + __shfl_sync(0xffffffffu, sum - mine, at);
+        return min(b0 + at, a.B - 1);
+      }
+      before += __shfl_sync(0xffffffffu, sum, 31);
+    }
+  }
+  // The first tile of sequence b in the line; by a whole warp.
+  __device__ __forceinline__ int64_t first_of(const PrefixArgs& a, int b) const {
+    int64_t t = 0;
+    for (int x = threadIdx.x & 31; x < b; x += 32) t += tiles_of(a, x);
+#pragma unroll
+    for (int w = 1; w < 32; w *= 2) t += __shfl_xor_sync(0xffffffffu, t, w);
+    return t * a.H * a.mt;
+  }
+};
+
+// The ranges of one CTA, one after the other.
+struct Walk {
+  int64_t x, end, first;  // next tile, end of the CTA's; first tile of sequence b
+  int b, tiles;           // tiles of an item of b
+  int item, t0, t1;       // the range: item of b, tiles [t0, t1)
+  // By a whole warp; false if the CTA has nothing to do.
+  __device__ __forceinline__ bool start(const PrefixArgs& a, const Spread& s) {
+    x = blockIdx.x * s.per;
+    end = min(x + s.per, s.total);
+    if (x >= end) return false;
+    b = s.find(a, x, &first);
+    tiles = Spread::tiles_of(a, b);
+    return true;
+  }
+  // To the next range; false behind the last.
+  __device__ __forceinline__ bool next(const PrefixArgs& a) {
+    if (x >= end) return false;
+    while (x >= first + (int64_t)tiles * a.H * a.mt) {  // a sequence without tiles has no range
+      first += (int64_t)tiles * a.H * a.mt;
+      tiles = Spread::tiles_of(a, ++b);
+    }
+    const uint32_t in = (uint32_t)min(x - first, (int64_t)0x7fffffff);
+    item = in == 0x7fffffffu ? (int)((x - first) / tiles) : (int)(in / (uint32_t)tiles);
+    t0 = (int)(x - first - (int64_t)item * tiles);
+    t1 = (int)min((int64_t)tiles, t0 + (end - x));
+    x += t1 - t0;
+    return true;
+  }
+  __device__ __forceinline__ int64_t slot(const PrefixArgs& a) const {
+    return blockIdx.x + (int64_t)b * a.H * a.mt + item;
+  }
+};
+// The most ranges of an item: the items of a sequence are equally long, and there are H mt
+// of them.
+inline int spread_parts(const PrefixArgs& a) { return a.C / (a.H * a.mt) + 2; }
+
 // Whether query row i of sequence b sees drafted row j.
 __device__ __forceinline__ bool sees(const PrefixArgs& a, int b, int i, int j) {
   return !a.mask || (__ldg(a.mask + ((int64_t)b * a.q + i) * a.mw + (j >> 5)) >> (j & 31) & 1);

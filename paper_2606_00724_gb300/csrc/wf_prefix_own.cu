@@ -86,7 +86,6 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rw = warp % WR, kw = warp / WR;
   const int nb = (a.Ro + a.ob - 1) / a.ob, u = blockIdx.x / nb, r0 = (blockIdx.x % nb) * a.ob, nr = min(a.ob, a.Ro - r0);
   const int b = u / a.H, h = u % a.H;
-  const int NP = WK + a.S;
   // Where the block's rows lie, found once.
   __shared__ int64_t row_q[RB], row_o[RB], row_flat[RB];
   if (tid < nr) {
@@ -96,14 +95,27 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
     row_flat[tid] = flat_row(a, w);
   }
   grid_dep_wait();
+  // Parts, and the rows from one to the next: of slots, what the lengths make them.
+  int S = a.S;
+  int64_t pitch = a.rows;
+  if (TREE && a.C) {
+    const int tile = r0 / a.tr, items = a.H * a.mt, item = h * a.mt + tile, tiles = Spread::tiles_of(a, b);
+    Spread sp;
+    sp.measure(a);
+    const int64_t x = sp.first_of(a, b) + (int64_t)item * tiles, c0 = x / sp.per;
+    S = tiles ? (int)((x + tiles - 1) / sp.per - c0) + 1 : 0;
+    pitch = a.tr;
+    if (tid < nr) row_flat[tid] = (c0 + (int64_t)b * items + item) * a.tr + (r0 + tid - tile * a.tr);
+  }
   // Keys: the prompt's rows where they are attended here, then the own rows.
   const int p = b / a.each, np = a.direct ? prompt_count(a, p) : 0, nk = np + own_count(a, b);
   __syncthreads();
   // The parts' m and l and the query rows are on their way first: neither waits
   // for the length.
+  const int NP = WK + S;
   for (int r = warp; r < nr; r += 4)
-    for (int j = lane; j < a.S; j += 32)
-      cp_async8(smem_u32(sml + r * NP + WK + j), a.part_ml + j * a.rows + row_flat[r]);
+    for (int j = lane; j < S; j += 32)
+      cp_async8(smem_u32(sml + r * NP + WK + j), a.part_ml + j * pitch + row_flat[r]);
   const bf16* K = static_cast<const bf16*>(a.Kg) + b * a.gsb + h * a.gsh;
   const bf16* V = static_cast<const bf16*>(a.Vg) + b * a.gsb + h * a.gsh;
   const int64_t prompt = p * a.ksb + h * a.ksh;
@@ -276,7 +288,7 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
 #pragma unroll
     for (int c = 0; c < D / 8; ++c)
       *reinterpret_cast<float2*>(row + 8 * c) = none ? make_float2(0.f, 0.f) : make_float2(o[c][2 * i], o[c][2 * i + 1]);
-    if ((lane & 3) == 0 && r < nr) sml[r * (WK + a.S) + kw] = make_float2(m[i], l[i]);
+    if ((lane & 3) == 0 && r < nr) sml[r * NP + kw] = make_float2(m[i], l[i]);
   }
   __syncthreads();
   // Weights 2^(m - M) / sum of 2^(m - M) l of a row's parts, 4 lanes a row; a part
@@ -316,18 +328,18 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
         y[x].x = fmaf(f, v.x, y[x].x); y[x].y = fmaf(f, v.y, y[x].y);
         y[x].z = fmaf(f, v.z, y[x].z); y[x].w = fmaf(f, v.w, y[x].w);
       };
-      for (int j = 0; j < a.S; j += PB) {
+      for (int j = 0; j < S; j += PB) {
         float4 v[PB][EB];
 #pragma unroll
         for (int k = 0; k < PB; ++k)
 #pragma unroll
           for (int x = 0; x < EB; ++x)
-            v[k][x] = j + k < a.S ? *reinterpret_cast<const float4*>(po[x] + (j + k) * a.rows * D)
+            v[k][x] = j + k < S ? *reinterpret_cast<const float4*>(po[x] + (j + k) * pitch * D)
                                   : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < PB; ++k)
 #pragma unroll
-          for (int x = 0; x < EB; ++x) add(x, j + k < a.S ? wt[x][WK + j + k].x : 0.f, v[k][x]);
+          for (int x = 0; x < EB; ++x) add(x, j + k < S ? wt[x][WK + j + k].x : 0.f, v[k][x]);
       }
 #pragma unroll
       for (int x = 0; x < EB; ++x) {

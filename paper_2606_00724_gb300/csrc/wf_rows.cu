@@ -22,20 +22,22 @@ namespace {
 
 constexpr int NTH = 256;
 
-// Cosine and sine of a fraction t / 2^64 of a turn.
-__device__ __forceinline__ void turned(unsigned long long t, const float*, float& c, float& s) {
+// Cosine and sine of a fraction t / 2^64 of a turn: of the part beyond the nearest
+// quarter turn, at most pi / 4 = x, by their series in x^2 (the first terms left
+// out are x^12 / 12! < 2^-33 and x^11 / 11! < 2^-29).
+__device__ __forceinline__ void turned(unsigned long long t, float& c, float& s) {
   const uint32_t hi = (uint32_t)(t >> 32), q = (hi + 0x20000000u) >> 30;
-  sincospif((float)(int32_t)(hi - (q << 30)) * 0x1p-31f, &s, &c);
-  const float c0 = c, s0 = s;
-  if (q & 1) { c = -s0; s = c0; }
-  if (q & 2) { c = -c; s = -s; }
-}
-// For rows that are rounded to 8 bits or fewer, the special-function unit's, 2^-20
-// off at these angles.
-__device__ __forceinline__ void turned(unsigned long long t, const bf16*, float& c, float& s) {
-  const uint32_t hi = (uint32_t)(t >> 32), q = (hi + 0x20000000u) >> 30;
-  const float y = (float)(int32_t)(hi - (q << 30)) * (0x1p-31f * 3.14159265f);
-  const float c0 = __cosf(y), s0 = __sinf(y);
+  const float x = (float)(int32_t)(hi - (q << 30)) * (0x1p-31f * 3.14159265358979f), y = x * x;
+  float c0 = -1.f / 3628800.f, s0 = 1.f / 362880.f;
+  c0 = fmaf(c0, y, 1.f / 40320.f);
+  s0 = fmaf(s0, y, -1.f / 5040.f);
+  c0 = fmaf(c0, y, -1.f / 720.f);
+  s0 = fmaf(s0, y, 1.f / 120.f);
+  c0 = fmaf(c0, y, 1.f / 24.f);
+  s0 = fmaf(s0, y, -1.f / 6.f);
+  c0 = fmaf(c0, y, -0.5f);
+  s0 = fmaf(s0 * y, x, x);
+  c0 = fmaf(c0, y, 1.f);
   c = q & 1 ? -s0 : c0;
   s = q & 1 ? c0 : s0;
   if (q & 2) { c = -c; s = -s; }
@@ -88,7 +90,7 @@ __global__ void __launch_bounds__(NTH) rows_kernel(const __grid_constant__ RowsA
         const ulonglong2 p = __ldg(reinterpret_cast<const ulonglong2*>(a.plan) + first + e);
         const int axis = min(max((int)p.y, 0), a.axes - 1);
         const long long pos = a.pos ? __ldg(a.pos + ((int64_t)axis * a.B + b) * a.rows + row) : place;
-        turned((unsigned long long)pos * p.x, type, c[e], s[e]);
+        turned((unsigned long long)pos * p.x, c[e], s[e]);
         if (!a.adjacent && t < half) s[e] = -s[e];
       }
     }

@@ -1,0 +1,395 @@
+// Drafted tokens over pages for few query rows: at most 16 a (sequence, key head), as
+// one token of a group of heads makes them (wf_tree_attn, bf16 queries).
+//
+// So few rows use every cached byte once and hardly compute, so the rows' way in is
+// all that counts, and a 128-row tensor-memory tile would stand seven eighths empty
+// behind barriers and a set-up of 5 us.  Here a warp is on its own: it takes 16 keys a
+// step, forms their logits and weights in registers (m16n8k16, fp32 accumulators) and
+// adds their share of O, without a barrier.  Each lane copies the bytes that it will
+// itself use, QD steps ahead, by cp.async into slots that no other lane reads:
+// shared memory as an extension of its registers.  A contraction may go through its
+// channels in any order, so a lane's operands of K are 16 consecutive bytes of a row;
+// V's pairs of keys are put together by byte permutes.
+//
+// The CTAs share all the sequences' keys evenly (Spread), a range's four warps
+// taking every fourth 16 keys of it; the ranges are joined where the drafted rows
+// are attended (own_join_kernel).  m is raised lazily, by more than 2^8, as in the
+// kernels for more rows; P is one bf16 term, l is summed before the rounding.
+#include <float.h>
+
+#include "wf_mx.cuh"
+#include "wf_prefix.cuh"
+#include "wf_sm100.cuh"
+
+namespace wf {
+namespace {
+
+using namespace sm100;
+
+constexpr int NTH = 128, NW = NTH / 32;
+constexpr int SK = kFewKeys / NW;  // keys a step
+constexpr float kLazy = 8.f;
+static_assert(SK == 16 && kFewRows == 16, "one m16n8k16 operand each");
+
+__device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// BYTES (4, 8 or 16) from global to shared memory; zeros if !valid.
+template <int BYTES>
+__device__ __forceinline__ void copy(uint32_t dst, const void* src, bool valid) {
+  if constexpr (BYTES == 16) {
+    cp_async16_zfill(dst, src, valid);
+  } else {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(valid ? BYTES : 0)
+                 : "memory");
+  }
+}
+template <int BYTES>
+__device__ __forceinline__ void fetch(uint32_t* w, uint32_t a) {
+  if constexpr (BYTES == 16) {
+    const uint4 v = lds_v4(a);
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+  } else if constexpr (BYTES == 8) {
+    const uint2 v = lds_v2(a);
+    w[0] = v.x; w[1] = v.y;
+  } else {
+    w[0] = lds_u32(a);
+  }
+}
+
+// A lane's bytes of a row: as an operand of K, KN chunks of KB bytes of four lanes' share;
+// of V, VN of VB of eight lanes'.
+template <int D, int FMT>
+struct Few {
+  static constexpr bool CODES = FMT != WF_BF16, FP4 = FMT == WF_MXFP4;
+  static constexpr int ROWB = FMT == WF_BF16 ? 2 * D : FP4 ? D / 2 : D;
+  static constexpr int KB = ROWB / 4 < 16 ? ROWB / 4 : 16, KN = ROWB / 4 / KB, KE = KB * D / ROWB;  // KE: elements
+  static constexpr int VB = ROWB / 8 < 16 ? ROWB / 8 : 16, VN = ROWB / 8 / VB, VE = VB * D / ROWB;
+  static constexpr int STEP = 2 * SK * ROWB + (CODES ? 128 : 0);
+  static constexpr int QD = 24576 / STEP > 8 ? 8 : 24576 / STEP;
+  static constexpr int PO = D + 4;
+  static constexpr size_t QUEUE = (size_t)NW * QD * STEP, SMEM = QUEUE + 2 * 16 * (PO + 2) * sizeof(float);
+};
+
+// N bytes of codes (or of bf16) to pairs of bf16; byte: their scale.
+template <int D, int FMT, int BYTES>
+__device__ __forceinline__ void pairs_of(const uint32_t* w, uint32_t byte, uint32_t* y) {
+  typedef Few<D, FMT> C;
+  if constexpr (!C::CODES) {
+#pragma unroll
+    for (int i = 0; i < BYTES / 4; ++i) y[i] = w[i];
+  } else {
+    constexpr int P = C::FP4 ? 4 : 2;  // pairs a word
+    const uint32_t f = mx_factor<C::FP4>(byte);
+#pragma unroll
+    for (int i = 0; i < BYTES / 4; ++i) mx_pairs<C::FP4>(w[i], y + P * i);
+#pragma unroll
+    for (int i = 0; i < BYTES / 4 * P; ++i) y[i] = mul_bf16x2(y[i], f);
+    if (byte > kMxOne<C::FP4>) {
+      const uint32_t f2 = mx_second_factor<C::FP4>(byte);
+#pragma unroll
+      for (int i = 0; i < BYTES / 4 * P; ++i) y[i] = mul_bf16x2(y[i], f2);
+    }
+  }
+}
+
+template <int D, int FMT>
+__global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ PrefixArgs a) {
+  typedef Few<D, FMT> C;
+  extern __shared__ __align__(128) uint8_t sm[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
+  const uint32_t queue = smem_u32(sm) + warp * C::QD * C::STEP;
+  float* const so = reinterpret_cast<float*>(sm + C::QUEUE);        // [2][16][PO]
+  float2* const sml = reinterpret_cast<float2*>(so + 2 * 16 * C::PO);  // [2][16]
+  grid_dep_wait();
+  Spread sp;
+  sp.measure(a);
+  Walk in;  // the range of the next step to be copied
+  bool more = in.start(a, sp);
+  if (!more) {
+    grid_dep_launch();
+    return;
+  }
+  Walk now = in;  // the range at work
+  const bool in_page = a.by_ps.d % SK == 0;
+  const int SR = D / kMxBlock;
+
+  // The next step: its place is looked up a step before it is copied, since a table's
+  // entry takes as long to come as a row.
+  int t = 0;
+  PagedRow at = {0, 0};
+  more = in.next(a);
+  t = in.t0;
+  auto look_up = [&] {
+    if (!more) return;
+    const int j = t * kFewKeys + warp * SK + (in_page ? 0 : lane % SK);
+    at = j < prompt_count(a, in.b) ? paged_row(a, in.b, j) : PagedRow{0, 0};
+  };
+  uint32_t odd = 0;  // D = 64: whether the scales that this lane copied are the second half of their word
+  auto bring = [&](uint32_t slot) {
+    if (more) {
+      const int left = prompt_count(a, in.b) - (t * kFewKeys + warp * SK);
+      const int64_t head = (int64_t)in.item * a.ksh;
+      const uint8_t* K = static_cast<const uint8_t*>(a.K) + head * (C::CODES ? 1 : 2);
+      const uint8_t* V = static_cast<const uint8_t*>(a.V) + head * (C::CODES ? 1 : 2);
+      auto row = [&](int r) -> int64_t {  // bytes to row r of the step
+        if (in_page) return (paged_offset(a, at) + r * a.kss) * (C::CODES ? 1 : 2);
+        const PagedRow w = {__shfl_sync(0xffffffffu, at.flat, r), __shfl_sync(0xffffffffu, at.page, r)};
+        return paged_offset(a, w) * (C::CODES ? 1 : 2);
+      };
+      uint32_t dst = slot + lane * C::KB;
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const int r = 8 * n + g;
+        const int64_t o = row(r);
+#pragma unroll
+        for (int j = 0; j < C::KN; ++j, dst += 32 * C::KB)
+          copy<C::KB>(dst, K + (r < left ? o : 0) + (4 * j + c) * C::KB, r < left);
+      }
+      dst = slot + SK * C::ROWB + lane * C::VB;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const int r = 2 * c + (n & 1) + 8 * (n >> 1);
+        const int64_t o = row(r);
+#pragma unroll
+        for (int j = 0; j < C::VN; ++j, dst += 32 * C::VB)
+          copy<C::VB>(dst, V + (r < left ? o : 0) + (8 * j + g) * C::VB, r < left);
+      }
+      if constexpr (C::CODES) {  // lanes 0 to 15: scales of K's rows, 16 to 31: of V's
+        const int r = lane & 15;
+        PagedRow w = at;
+        if (in_page) w.flat += r;
+        else w = {__shfl_sync(0xffffffffu, at.flat, r), __shfl_sync(0xffffffffu, at.page, r)};
+        const int64_t s = r < left ? paged_scale(a, w, in.item) : 0;
+        const uint8_t* p = (lane < 16 ? a.Ks : a.Vs) + s * SR;
+        const uint32_t to = slot + 2 * SK * C::ROWB + lane * 4;
+        if (D == 128) {
+          copy<4>(to, p, r < left);
+        } else {  // the smallest copy is 4 bytes on 4; the word's other half is another row's, or nobody's
+          const bool second = s & 1;
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(p - (second ? 2 : 0)),
+                       "r"(r < left ? (second ? 4 : 2) : 0)
+                       : "memory");
+          odd = odd << 1 | (uint32_t)second;
+        }
+      }
+      if (++t == in.t1) {
+        more = in.next(a);
+        t = in.t0;
+      }
+      look_up();
+    } else if (D == 64) {
+      odd <<= 1;
+    }
+    cp_async_commit();
+  };
+  look_up();
+#pragma unroll 1
+  for (int i = 0; i < C::QD; ++i) bring(queue + i * C::STEP);
+
+  int stage = 0;
+#pragma unroll 1
+  while (now.next(a)) {
+    const int count = prompt_count(a, now.b);
+    // Query rows g and g + 8, the channels in the order in which a lane has those of K.
+    uint32_t q[D / 16][4];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const int r = g + 8 * n;
+      const RowAt w = own_row(a, now.b, now.item, r < a.Ro ? r : 0);
+      const bf16* p = static_cast<const bf16*>(a.Q) + w.b * a.qsb + w.hq * a.qsh + w.i * a.qss;
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {  // runs of 8 channels
+        constexpr int RUNS = C::KE / 8;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (r < a.Ro) v = __ldg(reinterpret_cast<const uint4*>(p + (4 * (j / RUNS) + c) * C::KE + 8 * (j % RUNS)));
+        q[2 * j][n] = v.x; q[2 * j][2 + n] = v.y;
+        q[2 * j + 1][n] = v.z; q[2 * j + 1][2 + n] = v.w;
+      }
+    }
+    float o[D / 8][4], m[2] = {-FLT_MAX, -FLT_MAX}, l[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+#pragma unroll 1
+    for (int tile = now.t0; tile < now.t1; ++tile) {
+      const uint32_t slot = queue + stage * C::STEP;
+      const int left = count - (tile * kFewKeys + warp * SK);
+      cp_async_wait<C::QD - 1>();
+      if constexpr (C::CODES) {
+        if (D == 64) {  // every lane puts the scales that it copied in the word's first half
+          const uint32_t w = slot + 2 * SK * C::ROWB + lane * 4;
+          if (odd >> (C::QD - 1) & 1) sts_u32(w, lds_u32(w) >> 16);
+        }
+        __syncwarp();
+      }
+      if (left > 0) {
+        float s[2][4];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+          const uint32_t scale = C::CODES ? lds_u32(slot + 2 * SK * C::ROWB + (8 * n + g) * 4) : 0;
+          uint32_t k[D / 8];
+#pragma unroll
+          for (int j = 0; j < C::KN; ++j) {
+            uint32_t w[C::KB / 4];
+            fetch<C::KB>(w, slot + ((n * C::KN + j) * 32 + lane) * C::KB);
+            pairs_of<D, FMT, C::KB>(w, scale >> 8 * ((4 * j + c) * C::KE / kMxBlock) & 0xffu, k + j * C::KE / 2);
+          }
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) mma16816(s[n], q[i], k[2 * i], k[2 * i + 1]);
+        }
+        if (left < SK) {
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (8 * n + 2 * c + (e & 1) >= left) s[n][e] = -INFINITY;
+        }
+        float top[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          top[i] = fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1])) * a.sl2;
+        if (__any_sync(0xffffffffu, top[0] > m[0] + kLazy || top[1] > m[1] + kLazy)) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+            top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+            const float mn = fmaxf(m[i], top[i]), f = ex2(m[i] - mn);
+            m[i] = mn;
+            l[i] *= f;
+#pragma unroll
+            for (int e = 0; e < D / 8; ++e) {
+              o[e][2 * i] *= f;
+              o[e][2 * i + 1] *= f;
+            }
+          }
+        }
+        uint32_t p[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {  // rows g (even x), g + 8; keys 0-7 (x < 2), 8-15
+          const float* v = s[x >> 1] + 2 * (x & 1);
+          const float p0 = ex2(fmaf(v[0], a.sl2, -m[x & 1])), p1 = ex2(fmaf(v[1], a.sl2, -m[x & 1]));
+          l[x & 1] += p0 + p1;
+          p[x] = pack_bf16(p0, p1);
+        }
+#pragma unroll
+        for (int j = 0; j < C::VN; ++j) {
+          uint32_t v[4][C::VE / 2];
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            const int r = 2 * c + (n & 1) + 8 * (n >> 1);
+            uint32_t w[C::VB / 4], byte = 0;
+            fetch<C::VB>(w, slot + SK * C::ROWB + ((n * C::VN + j) * 32 + lane) * C::VB);
+            if (C::CODES)
+              byte = lds_u32(slot + 2 * SK * C::ROWB + (16 + r) * 4) >> 8 * ((8 * j + g) * C::VE / kMxBlock) & 0xffu;
+            pairs_of<D, FMT, C::VB>(w, byte, v[n]);
+          }
+#pragma unroll
+          for (int e = 0; e < C::VE / 2; ++e) {
+            mma16816(o[j * C::VE + 2 * e], p, __byte_perm(v[0][e], v[1][e], 0x5410), __byte_perm(v[2][e], v[3][e], 0x5410));
+            mma16816(o[j * C::VE + 2 * e + 1], p, __byte_perm(v[0][e], v[1][e], 0x7632),
+                     __byte_perm(v[2][e], v[3][e], 0x7632));
+          }
+        }
+      }
+      if (C::CODES) __syncwarp();  // every lane has read the scales
+      bring(slot);
+      if (++stage == C::QD) stage = 0;
+    }
+
+    // The four warps' O: 2 and 3 go to 0 and 1, then 1 to 0, which writes the part.
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+    }
+    auto channel = [&](int e, int x) { return (8 * (e / C::VE) + 2 * c + x) * C::VE + e % C::VE; };
+    auto put = [&](int to) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = g + 8 * i;
+        if (r >= a.Ro) continue;
+        if (c == 0) sml[to * 16 + r] = make_float2(m[i], l[i]);
+#pragma unroll
+        for (int e = 0; e < D / 8; e += 4)
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+            *reinterpret_cast<float4*>(so + (to * 16 + r) * C::PO + channel(e, x)) =
+                make_float4(o[e][2 * i + x], o[e + 1][2 * i + x], o[e + 2][2 * i + x], o[e + 3][2 * i + x]);
+      }
+    };
+    auto take = [&](int from) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = g + 8 * i;
+        if (r >= a.Ro) continue;
+        // Without weight (l = 0) O is 0 x V, which is NaN where V is not finite.
+        const float2 y = sml[from * 16 + r];
+        const bool have = l[i] != 0.f, add = y.y != 0.f;
+        if (!add) continue;
+        const float M = have ? fmaxf(m[i], y.x) : y.x, f0 = have ? ex2(m[i] - M) : 0.f, f1 = ex2(y.x - M);
+        m[i] = M;
+        l[i] = (have ? l[i] * f0 : 0.f) + y.y * f1;
+#pragma unroll
+        for (int e = 0; e < D / 8; e += 4)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const float4 v = *reinterpret_cast<const float4*>(so + (from * 16 + r) * C::PO + channel(e, x));
+            const float w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int z = 0; z < 4; ++z)
+              o[e + z][2 * i + x] = have ? fmaf(o[e + z][2 * i + x], f0, w[z] * f1) : w[z] * f1;
+          }
+      }
+    };
+    __syncthreads();  // the last range's exchange is over
+    if (warp >= 2) put(warp - 2);
+    __syncthreads();
+    if (warp < 2) take(warp);
+    if (warp == 1) put(1);
+    __syncthreads();
+    if (warp == 0) {
+      take(1);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = g + 8 * i;
+        if (r >= a.Ro) continue;
+        const int64_t row = now.slot(a) * a.tr + r;
+        const bool none = l[i] == 0.f;
+        if (c == 0) a.part_ml[row] = make_float2(m[i], l[i]);
+#pragma unroll
+        for (int e = 0; e < D / 8; e += 4)
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+            *reinterpret_cast<float4*>(a.part_o + row * D + channel(e, x)) =
+                none ? make_float4(0.f, 0.f, 0.f, 0.f)
+                     : make_float4(o[e][2 * i + x], o[e + 1][2 * i + x], o[e + 2][2 * i + x], o[e + 3][2 * i + x]);
+      }
+    }
+  }
+  grid_dep_launch();
+  cp_async_wait_all();
+}
+
+template <int D, int FMT>
+cudaError_t launch(const PrefixArgs& a, cudaStream_t s) {
+  if (!a.C) return cudaSuccess;
+  const auto k = few_kernel<D, FMT>;
+  const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(k), Few<D, FMT>::SMEM);
+  return e != cudaSuccess ? e : Launch(dim3((unsigned)a.C), NTH, Few<D, FMT>::SMEM, s)(k, a);
+}
+
+}  // namespace
+
+cudaError_t launch_tree_few(const PrefixPlan& p, cudaStream_t s) {
+  const bool wide = p.a.d == 128;
+  if (p.fmt == WF_MXFP8) return wide ? launch<128, WF_MXFP8>(p.a, s) : launch<64, WF_MXFP8>(p.a, s);
+  if (p.fmt == WF_MXFP4) return wide ? launch<128, WF_MXFP4>(p.a, s) : launch<64, WF_MXFP4>(p.a, s);
+  return wide ? launch<128, WF_BF16>(p.a, s) : launch<64, WF_BF16>(p.a, s);
+}
+
+}  // namespace wf
