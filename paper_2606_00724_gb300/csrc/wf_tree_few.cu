@@ -5,9 +5,8 @@
 // all that counts, and a 128-row tensor-memory tile would stand seven eighths empty
 // behind barriers and a set-up of 5 us.  Here a warp is on its own: it takes 16 keys a
 // step, forms their logits and weights in registers (m16n8k16, fp32 accumulators) and
-// adds their share of O, without a barrier.  Each lane copies the bytes that it will
-// itself use, QD steps ahead, by cp.async into slots that no other lane reads:
-// shared memory as an extension of its registers.  A contraction may go through its
+// adds their share of O, with no barrier but the warp's.  It copies its own rows, QD
+// steps ahead, by cp.async into slots of its own.  A contraction may go through its
 // channels in any order, so a lane's operands of K are 16 consecutive bytes of a row;
 // V's pairs of keys are put together by byte permutes.
 //
@@ -38,16 +37,6 @@ __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// BYTES (4, 8 or 16) from global to shared memory; zeros if !valid.
-template <int BYTES>
-__device__ __forceinline__ void copy(uint32_t dst, const void* src, bool valid) {
-  if constexpr (BYTES == 16) {
-    cp_async16_zfill(dst, src, valid);
-  } else {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(valid ? BYTES : 0)
-                 : "memory");
-  }
-}
 template <int BYTES>
 __device__ __forceinline__ void fetch(uint32_t* w, uint32_t a) {
   if constexpr (BYTES == 16) {
@@ -69,6 +58,14 @@ struct Few {
   static constexpr int ROWB = FMT == WF_BF16 ? 2 * D : FP4 ? D / 2 : D;
   static constexpr int KB = ROWB / 4 < 16 ? ROWB / 4 : 16, KN = ROWB / 4 / KB, KE = KB * D / ROWB;  // KE: elements
   static constexpr int VB = ROWB / 8 < 16 ? ROWB / 8 : 16, VN = ROWB / 8 / VB, VE = VB * D / ROWB;
+  // A slot holds the rows of K and of V with their 16-byte chunks permuted by the row, so that the
+  // lanes of a phase read from different banks: of K, rows g and g + 1 and chunks c; of V,
+  // rows 2 c and chunks g and g + 1.
+  static constexpr int CPR = ROWB / 16, RPI = 32 / CPR;  // chunks a row, rows a copying instruction of the warp
+  __device__ static int k_place(int r, int ch) { return r * ROWB + (CPR >= 8 ? ch ^ (r & 1) * 4 : ch) * 16; }
+  __device__ static int v_place(int r, int ch) {
+    return r * ROWB + (CPR >= 8 ? ch ^ (r >> 1 & 3) * 2 : CPR == 4 ? ch ^ (r >> 1 & 3) : ch) * 16;
+  }
   static constexpr int STEP = 2 * SK * ROWB + (CODES ? 128 : 0);
   static constexpr int QD = 24576 / STEP > 8 ? 8 : 24576 / STEP;
   static constexpr int PO = D + 4;
@@ -119,45 +116,43 @@ __global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ Pre
   const int SR = D / kMxBlock;
 
   // The next step: its place is looked up a step before it is copied, since a table's
-  // entry takes as long to come as a row.
-  int t = 0;
+  // entry takes as long to come as a row.  What a range fixes is found once.
+  constexpr int EB = C::CODES ? 1 : 2;  // bytes of a stride's unit
+  int t = 0, count_in = 0;
   PagedRow at = {0, 0};
-  more = in.next(a);
-  t = in.t0;
-  auto look_up = [&] {
+  const uint8_t *K = nullptr, *V = nullptr;
+  const int64_t kss = a.kss * EB, kx = a.kx * EB;
+  auto enter = [&] {
+    more = in.next(a);
     if (!more) return;
+    t = in.t0;
+    count_in = prompt_count(a, in.b);
+    K = static_cast<const uint8_t*>(a.K) + in.item * a.ksh * EB + lane % C::CPR * 16;
+    V = static_cast<const uint8_t*>(a.V) + in.item * a.ksh * EB + lane % C::CPR * 16;
+  };
+  auto look_up = [&] {
     const int j = t * kFewKeys + warp * SK + (in_page ? 0 : lane % SK);
-    at = j < prompt_count(a, in.b) ? paged_row(a, in.b, j) : PagedRow{0, 0};
+    at = more && j < count_in ? paged_row(a, in.b, j) : PagedRow{0, 0};
   };
   uint32_t odd = 0;  // D = 64: whether the scales that this lane copied are the second half of their word
   auto bring = [&](uint32_t slot) {
     if (more) {
-      const int left = prompt_count(a, in.b) - (t * kFewKeys + warp * SK);
-      const int64_t head = (int64_t)in.item * a.ksh;
-      const uint8_t* K = static_cast<const uint8_t*>(a.K) + head * (C::CODES ? 1 : 2);
-      const uint8_t* V = static_cast<const uint8_t*>(a.V) + head * (C::CODES ? 1 : 2);
-      auto row = [&](int r) -> int64_t {  // bytes to row r of the step
-        if (in_page) return (paged_offset(a, at) + r * a.kss) * (C::CODES ? 1 : 2);
-        const PagedRow w = {__shfl_sync(0xffffffffu, at.flat, r), __shfl_sync(0xffffffffu, at.page, r)};
-        return paged_offset(a, w) * (C::CODES ? 1 : 2);
-      };
-      uint32_t dst = slot + lane * C::KB;
+      const int left = count_in - (t * kFewKeys + warp * SK);
+      const bool full = left >= SK;
+      const int64_t first = at.flat * kss + at.page * kx;  // bytes to the step's first row, where that finds them all
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const int r = 8 * n + g;
-        const int64_t o = row(r);
-#pragma unroll
-        for (int j = 0; j < C::KN; ++j, dst += 32 * C::KB)
-          copy<C::KB>(dst, K + (r < left ? o : 0) + (4 * j + c) * C::KB, r < left);
-      }
-      dst = slot + SK * C::ROWB + lane * C::VB;
-#pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const int r = 2 * c + (n & 1) + 8 * (n >> 1);
-        const int64_t o = row(r);
-#pragma unroll
-        for (int j = 0; j < C::VN; ++j, dst += 32 * C::VB)
-          copy<C::VB>(dst, V + (r < left ? o : 0) + (8 * j + g) * C::VB, r < left);
+      for (int n = 0; n < SK / C::RPI; ++n) {
+        const int r = C::RPI * n + lane / C::CPR;
+        const bool ok = full || r < left;
+        int64_t o;
+        if (in_page) {
+          o = ok ? first + r * kss : 0;
+        } else {
+          const PagedRow w = {__shfl_sync(0xffffffffu, at.flat, r), __shfl_sync(0xffffffffu, at.page, r)};
+          o = w.flat * kss + w.page * kx;
+        }
+        cp_async16_zfill(slot + C::k_place(r, lane % C::CPR), K + o, ok);
+        cp_async16_zfill(slot + SK * C::ROWB + C::v_place(r, lane % C::CPR), V + o, ok);
       }
       if constexpr (C::CODES) {  // lanes 0 to 15: scales of K's rows, 16 to 31: of V's
         const int r = lane & 15;
@@ -168,7 +163,7 @@ __global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ Pre
         const uint8_t* p = (lane < 16 ? a.Ks : a.Vs) + s * SR;
         const uint32_t to = slot + 2 * SK * C::ROWB + lane * 4;
         if (D == 128) {
-          copy<4>(to, p, r < left);
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(p), "r"(r < left ? 4 : 0) : "memory");
         } else {  // the smallest copy is 4 bytes on 4; the word's other half is another row's, or nobody's
           const bool second = s & 1;
           asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(p - (second ? 2 : 0)),
@@ -177,16 +172,14 @@ __global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ Pre
           odd = odd << 1 | (uint32_t)second;
         }
       }
-      if (++t == in.t1) {
-        more = in.next(a);
-        t = in.t0;
-      }
+      if (++t == in.t1) enter();
       look_up();
     } else if (D == 64) {
       odd <<= 1;
     }
     cp_async_commit();
   };
+  enter();
   look_up();
 #pragma unroll 1
   for (int i = 0; i < C::QD; ++i) bring(queue + i * C::STEP);
@@ -224,8 +217,8 @@ __global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ Pre
           const uint32_t w = slot + 2 * SK * C::ROWB + lane * 4;
           if (odd >> (C::QD - 1) & 1) sts_u32(w, lds_u32(w) >> 16);
         }
-        __syncwarp();
       }
+      __syncwarp();  // every lane's copies are there
       if (left > 0) {
         float s[2][4];
 #pragma unroll
@@ -236,7 +229,8 @@ __global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ Pre
 #pragma unroll
           for (int j = 0; j < C::KN; ++j) {
             uint32_t w[C::KB / 4];
-            fetch<C::KB>(w, slot + ((n * C::KN + j) * 32 + lane) * C::KB);
+            const int at = (4 * j + c) * C::KB;
+            fetch<C::KB>(w, slot + C::k_place(8 * n + g, at / 16) + at % 16);
             pairs_of<D, FMT, C::KB>(w, scale >> 8 * ((4 * j + c) * C::KE / kMxBlock) & 0xffu, k + j * C::KE / 2);
           }
 #pragma unroll
@@ -283,7 +277,8 @@ __global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ Pre
           for (int n = 0; n < 4; ++n) {
             const int r = 2 * c + (n & 1) + 8 * (n >> 1);
             uint32_t w[C::VB / 4], byte = 0;
-            fetch<C::VB>(w, slot + SK * C::ROWB + ((n * C::VN + j) * 32 + lane) * C::VB);
+            const int at = (8 * j + g) * C::VB;
+            fetch<C::VB>(w, slot + SK * C::ROWB + C::v_place(r, at / 16) + at % 16);
             if (C::CODES)
               byte = lds_u32(slot + 2 * SK * C::ROWB + (16 + r) * 4) >> 8 * ((8 * j + g) * C::VE / kMxBlock) & 0xffu;
             pairs_of<D, FMT, C::VB>(w, byte, v[n]);
@@ -296,7 +291,7 @@ __global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ Pre
           }
         }
       }
-      if (C::CODES) __syncwarp();  // every lane has read the scales
+      __syncwarp();  // every lane has read the slot
       bring(slot);
       if (++stage == C::QD) stage = 0;
     }
