@@ -799,7 +799,7 @@ WF_API wf_status wf_paged_append(const void* Knew, const void* Vnew, const wf_te
 WF_API size_t wf_tree_attn_workspace_bytes(const wf_tensor* q, const wf_tensor* pool, int n, int n_t) {
   wf_tensor cache;
   if (check_tree(q, pool, n, n_t, &cache) != WF_OK) return 0;
-  return wf::plan_prefix(*q, cache, n, n_t, true).total;
+  return wf::plan_tree(*q, cache, n, n_t).total;
 }
 
 WF_API wf_status wf_tree_attn(const void* Q, const wf_tensor* q, const void* K, const void* V, const wf_tensor* pool,
@@ -823,7 +823,7 @@ WF_API wf_status wf_tree_attn(const void* Q, const wf_tensor* q, const void* K, 
   if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0 || !aligned4(pages) || !aligned4(cache_len) ||
       !aligned4(tree_len) || !aligned4(mask))
     return WF_ERR_ALIGN;
-  wf::PrefixPlan p = wf::plan_prefix(*q, cache, n, n_t, true);
+  wf::PrefixPlan p = wf::plan_tree(*q, cache, n, n_t);
   if (ws_bytes < p.total) return WF_ERR_WORKSPACE;
   fill_prefix(p, Q, q, K, V, pool, Ks, Vs, Kt, Vt, t, O, o, scale, ws);
   wf::PrefixArgs& a = p.a;
@@ -833,6 +833,11 @@ WF_API wf_status wf_tree_attn(const void* Q, const wf_tensor* q, const void* K, 
   a.kx = a.ksb - (int64_t)pool->seq * a.kss;
   a.mask = n_t > 0 ? reinterpret_cast<const uint32_t*>(mask) : nullptr;
   a.mw = (n_t + 31) / 32;
+  if (p.off_info) {
+    const size_t items = (size_t)a.B * a.H * a.mt;
+    a.info = reinterpret_cast<int2*>(static_cast<char*>(ws) + p.off_info);
+    a.flags = reinterpret_cast<int*>(a.info + items);
+  }
   return cuda_status(wf::launch_tree(p, static_cast<cudaStream_t>(stream)));
 }
 

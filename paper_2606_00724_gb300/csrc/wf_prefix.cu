@@ -404,7 +404,7 @@ cudaError_t launch_join(const PrefixArgs& a, cudaStream_t s) {
 
 }  // namespace
 
-PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g, bool paged) {
+PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g) {
   PrefixPlan p = {};
   PrefixArgs& a = p.a;
   a.B = q.batch; a.P = kv.batch; a.H = kv.heads; a.G = q.heads / kv.heads;
@@ -449,7 +449,7 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g, 
   double prompt_us, own_us;
   a.S = split((int64_t)a.P * a.H * a.mt, k, &prompt_us);
   const int64_t own = (int64_t)a.B * a.H * a.mto;
-  p.fold = tc && n_g > 0 && paged ? true : tc && n_g > 0 && own >= kPrefixOwn && n_g <= std::min<int64_t>(2 * own, a.Ro <= 16 ? 512 : 256);
+  p.fold = tc && n_g > 0 && own >= kPrefixOwn && n_g <= std::min<int64_t>(2 * own, a.Ro <= 16 ? 512 : 256);
   a.So = p.fold ? 0 : split(own, n_g, &own_us);
   // Prompt rows that every sequence attends to for itself, where its own rows are
   // (one launch): a 64-key tile takes 1.25 us, or its bytes for all blocks of
@@ -457,7 +457,7 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g, 
   // 4 heads' tokens, 128 rows and 32 own ones 6.0 against 9.5 us, 400 and 32 10.8
   // against 10.1; blocks of 32 rows of 4 sequences and 16 heads on 128 rows 7.3
   // against 12.8, of 32 sequences on 400 rows 36 against 26.
-  if (tc && !paged && p.fmt == WF_BF16 && k > 0 && k + n_g <= 1024) {
+  if (tc && p.fmt == WF_BF16 && k > 0 && k + n_g <= 1024) {
     auto direct = [&](int keys) {
       const double blocks = (double)a.B * a.H * ((a.Ro + prefix_own_rows(a, 0, keys) - 1) / prefix_own_rows(a, 0, keys));
       return ((keys + 63) / 64) * std::max(1.25, blocks * 256 * a.d / 2.4e6);
@@ -468,15 +468,6 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g, 
       p.fold = true;
     }
   }
-  if (paged && tc && a.Ro <= kFewRows) {
-    p.few = p.fold = true;
-    a.tk = kFewKeys;
-    a.tr = a.Ro;
-    a.mt = 1;
-    a.C = (int)std::min<int64_t>(kFewCtas, (int64_t)a.B * a.H * ((k + kFewKeys - 1) / kFewKeys));
-    a.S = a.C ? spread_parts(a) : 0;
-    a.So = 0;
-  }
   p.parts = a.S + a.So;
   a.by_H = make_fastdiv(a.H);
   a.by_S = make_fastdiv(std::max(1, a.S));
@@ -484,7 +475,7 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g, 
   a.by_mt = make_fastdiv(a.mt);
   a.by_mto = make_fastdiv(a.mto);
   a.whole = p.parts == 1 && !p.fold;
-  const int64_t kept = a.whole ? 0 : a.C ? ((int64_t)a.C + a.B * a.H * a.mt) * a.tr : a.rows * p.parts;  // rows of parts
+  const int64_t kept = a.whole ? 0 : a.rows * p.parts;  // rows of parts
   p.off_ml = 256;
   p.off_o = align_up(p.off_ml + sizeof(float2) * (size_t)kept, 256);
   p.used = p.off_o + sizeof(float) * (size_t)kept * a.d;
@@ -496,8 +487,7 @@ PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g, 
     const int64_t tiles = (keys + tk - 1) / tk;
     return std::min(tiles * a.rows, alone ? most : std::max(a.rows, most));
   };
-  int64_t reserved = room(k, n_g == 0) + room(n_g, false);
-  if (paged && tc) reserved = std::max(reserved, kFewCtas * (int64_t)std::min(a.Ro, kFewRows) + a.rows);
+  const int64_t reserved = room(k, n_g == 0) + room(n_g, false);
   p.total = align_up(p.off_ml + sizeof(float2) * (size_t)reserved, 256) + sizeof(float) * (size_t)reserved * a.d;
   return p;
 }
@@ -515,10 +505,42 @@ cudaError_t launch_prefix(const PrefixPlan& p, cudaStream_t s) {
   return p.fold ? launch_prefix_own(p, s) : join(p, s);
 }
 
+PrefixPlan plan_tree(const wf_tensor& q, const wf_tensor& kv, int k, int n_t) {
+  // fp32 queries: ranges and own units as wf_prefix_attn's.
+  PrefixPlan p = plan_prefix(q, kv, k, n_t);
+  if (p.dtype != WF_BF16) return p;
+  PrefixArgs& a = p.a;
+  a.S = a.So = a.direct = a.whole = 0;
+  p.few = a.Ro <= kFewRows;
+  a.tk = p.few ? kFewKeys : kPrefixTcRows / 2;
+  a.mt = (a.Ro + kPrefixTcRows - 1) / kPrefixTcRows;
+  // Row tiles of equal height, whole warps of them.
+  a.tr = a.mt == 1 ? a.Ro : ((a.Ro + a.mt - 1) / a.mt + 31) / 32 * 32;
+  const int64_t U = (int64_t)a.B * a.H, items = U * a.mt;
+  const int64_t tiles = std::max<int64_t>(1, ((int64_t)k + a.tk - 1) / a.tk + ((int64_t)n_t + a.tk - 1) / a.tk);
+  a.C = (int)std::min<int64_t>(p.few ? kFewCtas : kPrefixSms, items * tiles);
+  p.join = tiles > 1;
+  const size_t slots = (size_t)(a.C + items) * a.tr;
+  p.off_info = 256;
+  p.off_ml = align_up(p.off_info + (size_t)items * sizeof(int2) + (size_t)(a.C + items) * sizeof(int), 256);
+  p.off_o = align_up(p.off_ml + sizeof(float2) * slots, 256);
+  p.used = p.off_o + sizeof(float) * slots * a.d;
+  // The size is the most that a call with as many rows and keys, or fewer of any, can take:
+  // tr is R at most, or, with several row tiles, 256, and R + 32 mt in all.
+  const int64_t reserved = kFewCtas * (int64_t)std::min(a.Ro, kFewRows) +
+                           kPrefixSms * (int64_t)std::min(a.Ro, kPrefixTcRows) + U * (a.Ro + (a.mt > 1 ? 32 * (int64_t)a.mt : 0));
+  const size_t heads = align_up(p.off_info + (size_t)items * (sizeof(int2) + sizeof(int)) + kFewCtas * sizeof(int), 256);
+  p.total = align_up(heads + sizeof(float2) * (size_t)reserved, 256) + sizeof(float) * (size_t)reserved * a.d;
+  return p;
+}
+
 cudaError_t launch_tree(const PrefixPlan& p, cudaStream_t s) {
-  const cudaError_t e = p.few ? launch_tree_few(p, s) : p.dtype == WF_BF16 ? launch_tree_tc(p, s) : launch_cached<true>(p, s);
-  if (e != cudaSuccess || p.a.whole) return e;
-  return p.fold ? launch_tree_own(p, s) : join(p, s);
+  if (p.dtype == WF_BF16) {
+    const cudaError_t e = p.few ? launch_tree_few(p, s) : launch_tree_tc(p, s);
+    return e != cudaSuccess || !(p.join || p.a.mask) ? e : launch_tree_join(p, s);
+  }
+  const cudaError_t e = launch_cached<true>(p, s);
+  return e != cudaSuccess || p.a.whole ? e : join(p, s);
 }
 
 }  // namespace wf

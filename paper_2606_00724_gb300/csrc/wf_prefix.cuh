@@ -54,10 +54,13 @@ struct PrefixArgs {
   // The drafted rows that a query row sees (null: all): bit j of mask[b][i].
   const uint32_t* mask;
   int mw;                // words a row
-  // Where C > 0 the key tiles (tk keys each) that the sequences really have are spread
-  // over C CTAs evenly, see Spread: parts are slots of tr rows then, S is the
-  // most of them that a unit has, and there are no own units.
+  // bf16 queries over pages: the key tiles (tk keys each) that the sequences really have
+  // are spread over C CTAs evenly (see Spread), a unit's rows in mt tiles of tr.  A
+  // part is a slot of tr rows; info says where an item's are and how many, flags
+  // which of them left drafted values out that are not finite.
   int C, tk, tr;
+  int2* info;
+  int* flags;
 };
 
 // With at least so many units of own rows, and not too many rows for them, they are
@@ -81,25 +84,26 @@ struct PrefixPlan {
   int parts;     // 1: the kernel writes O itself
   bool fold;     // the own rows are attended where the parts are joined (So = 0)
   bool few;      // wf_tree_attn's kernel for few query rows a unit
-  size_t off_ml, off_o, used;  // used: what this call writes
+  bool join;     // an item may have several parts
+  size_t off_info, off_ml, off_o, used;  // used: what this call writes
   size_t total;                // what it asks for
 };
-// paged: for wf_tree_attn, whose own rows (the drafted ones) are joined where the
-// queries are bf16.
-PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g, bool paged = false);
+PrefixPlan plan_prefix(const wf_tensor& q, const wf_tensor& kv, int k, int n_g);
 cudaError_t launch_prefix(const PrefixPlan& p, cudaStream_t s);
+// The same for wf_tree_attn: k rows a sequence and n_t drafted ones.
+PrefixPlan plan_tree(const wf_tensor& q, const wf_tensor& kv, int k, int n_t);
 cudaError_t launch_tree(const PrefixPlan& p, cudaStream_t s);
 // Query rows a CTA of that kernel for S parts and so many keys.
 int prefix_own_rows(const PrefixArgs& a, int S, int keys);
 cudaError_t launch_prefix_own(const PrefixPlan& p, cudaStream_t s);  // own rows and the joining of parts, bf16
 cudaError_t launch_prefix_tc(const PrefixPlan& p, cudaStream_t s);  // the parts (or O) of bf16 queries
-// The same for caches in pages and masks.
-cudaError_t launch_tree_own(const PrefixPlan& p, cudaStream_t s);
+// The same of wf_tree_attn: of more query rows a unit, of few, and their joining.
 cudaError_t launch_tree_tc(const PrefixPlan& p, cudaStream_t s);
 cudaError_t launch_tree_few(const PrefixPlan& p, cudaStream_t s);
+cudaError_t launch_tree_join(const PrefixPlan& p, cudaStream_t s);
 // Query rows of a unit that the kernel for few of them takes, keys of its tiles, and
 // its CTAs.
-constexpr int kFewRows = 16, kFewKeys = 64, kFewCtas = 2 * kPrefixSms;
+constexpr int kFewRows = 16, kFewKeys = 64, kFewCtas = 3 * kPrefixSms;
 
 // Sequence, query head and block row of row r of the unit of prompt p (or of
 // sequence b) and key head h.
@@ -141,17 +145,18 @@ __device__ __forceinline__ int64_t paged_offset(const PrefixArgs& a, const Paged
 __device__ __forceinline__ int64_t paged_scale(const PrefixArgs& a, const PagedRow& r, int h) {
   return r.flat + ((int64_t)r.page * (a.H - 1) + h) * a.by_ps.d;
 }
-// Work in pages spread over C CTAs: the key tiles of all items, an item being a
+// Work over pages spread over C CTAs: the key tiles of all items, an item being a
 // row tile of tr rows of a unit, lie in one line, items in the order [sequence][key
-// head][row tile]; CTA c takes tiles [c per, (c + 1) per), which are ranges of one item
-// or of several that follow each other.  The lengths are known on the device
-// alone, so every warp finds its place in the line from them.  A range is a part, and its
-// slot is c + item: along the line either grows by one from range to range, so no
-// two ranges share a slot and those of an item follow each other.
+// head][row tile], an item's cached tiles before its drafted ones and one tile at
+// least; CTA c takes tiles [c per, (c + 1) per), which are ranges of one item or of
+// several that follow each other.  The lengths are known on the device alone, so
+// every warp finds its place in the line from them.  A range is a part, and its slot is
+// c + item: along the line either grows by one from range to range, so no two
+// ranges share a slot and those of an item follow each other.
 struct Spread {
   int64_t total, per;
   __device__ __forceinline__ static int tiles_of(const PrefixArgs& a, int b) {
-    return b < a.B ? (prompt_count(a, b) + a.tk - 1) / a.tk : 0;
+    return b < a.B ? max(1, (prompt_count(a, b) + a.tk - 1) / a.tk + (own_count(a, b) + a.tk - 1) / a.tk) : 0;
   }
   // By a whole warp.
   __device__ __forceinline__ void measure(const PrefixArgs& a) {
@@ -160,7 +165,7 @@ struct Spread {
 #pragma unroll
     for (int w = 1; w < 32; w *= 2) t += __shfl_xor_sync(0xffffffffu, t, w);
     total = t * a.H * a.mt;
-    per = max((int64_t)1, (total + a.C - 1) / a.C);
+    per = total < 0x7fffffff ? (int64_t)(((uint32_t)total + a.C - 1) / (uint32_t)a.C) : (total + a.C - 1) / a.C;
   }
   // The sequence whose items hold tile x < total, and its first tile in the line; by a
   // whole warp.
@@ -184,52 +189,66 @@ struct Spread {
       before += __shfl_sync(0xffffffffu, sum, 31);
     }
   }
-  // The first tile of sequence b in the line; by a whole warp.
-  __device__ __forceinline__ int64_t first_of(const PrefixArgs& a, int b) const {
-    int64_t t = 0;
-    for (int x = threadIdx.x & 31; x < b; x += 32) t += tiles_of(a, x);
-#pragma unroll
-    for (int w = 1; w < 32; w *= 2) t += __shfl_xor_sync(0xffffffffu, t, w);
-    return t * a.H * a.mt;
-  }
 };
 
 // The ranges of one CTA, one after the other.
 struct Walk {
-  int64_t x, end, first;  // next tile, end of the CTA's; first tile of sequence b
-  int b, tiles;           // tiles of an item of b
-  int item, t0, t1;       // the range: item of b, tiles [t0, t1)
+  int64_t x, end, first;      // next tile, end of the CTA's; first tile of sequence b
+  int64_t per;
+  int b, count, drafts;       // sequence, its cached and drafted rows
+  int cached, tiles;          // tiles of an item of b: cached ones, all
+  int item, t0, t1;           // the range: item of b, tiles [t0, t1)
+  __device__ __forceinline__ void enter(const PrefixArgs& a, int sequence) {
+    b = sequence;
+    count = prompt_count(a, b);
+    drafts = own_count(a, b);
+    cached = (count + a.tk - 1) / a.tk;
+    tiles = max(1, cached + (drafts + a.tk - 1) / a.tk);
+  }
   // By a whole warp; false if the CTA has nothing to do.
-  __device__ __forceinline__ bool start(const PrefixArgs& a, const Spread& s) {
-    x = blockIdx.x * s.per;
-    end = min(x + s.per, s.total);
+  __device__ __forceinline__ bool start(const PrefixArgs& a) {
+    Spread s;
+    s.measure(a);
+    per = s.per;
+    x = blockIdx.x * per;
+    end = min(x + per, s.total);
     if (x >= end) return false;
-    b = s.find(a, x, &first);
-    tiles = Spread::tiles_of(a, b);
+    enter(a, s.find(a, x, &first));
     return true;
   }
   // To the next range; false behind the last.
   __device__ __forceinline__ bool next(const PrefixArgs& a) {
     if (x >= end) return false;
-    while (x >= first + (int64_t)tiles * a.H * a.mt) {  // a sequence without tiles has no range
+    while (x >= first + (int64_t)tiles * a.H * a.mt) {
       first += (int64_t)tiles * a.H * a.mt;
-      tiles = Spread::tiles_of(a, ++b);
+      enter(a, b + 1);
     }
-    const uint32_t in = (uint32_t)min(x - first, (int64_t)0x7fffffff);
-    item = in == 0x7fffffffu ? (int)((x - first) / tiles) : (int)(in / (uint32_t)tiles);
-    t0 = (int)(x - first - (int64_t)item * tiles);
+    const int64_t in = x - first;
+    item = in < 0x7fffffff ? (int)((uint32_t)in / (uint32_t)tiles) : (int)(in / tiles);
+    t0 = (int)(in - (int64_t)item * tiles);
     t1 = (int)min((int64_t)tiles, t0 + (end - x));
     x += t1 - t0;
     return true;
   }
-  __device__ __forceinline__ int64_t slot(const PrefixArgs& a) const {
-    return blockIdx.x + (int64_t)b * a.H * a.mt + item;
+  __device__ __forceinline__ int64_t items(const PrefixArgs& a) const { return (int64_t)b * a.H * a.mt + item; }
+  __device__ __forceinline__ int64_t slot(const PrefixArgs& a) const { return blockIdx.x + items(a); }
+  // The whole item: there are no other parts.
+  __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == tiles; }
+  // The parts of the item whose first one this is.
+  __device__ __forceinline__ int parts() const {
+    return (int)((x - (t1 - t0) + tiles - 1) / per) - (int)blockIdx.x + 1;
   }
 };
-// The most ranges of an item: the items of a sequence are equally long, and there are H mt
-// of them.
-inline int spread_parts(const PrefixArgs& a) { return a.C / (a.H * a.mt) + 2; }
 
+// Whether one of a pair of bf16 is an infinity or a NaN; the pair with 0 there.  Drafted
+// values that some query rows do not see are left out of the products where they are
+// not finite, since 0 times them is not 0, and added by the joining kernel.
+__device__ __forceinline__ bool not_finite(uint32_t w) {
+  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+}
+__device__ __forceinline__ uint32_t finite_only(uint32_t w) {
+  return ((w & 0x7f80u) == 0x7f80u ? 0 : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0 : w & 0xffff0000u);
+}
 // Whether query row i of sequence b sees drafted row j.
 __device__ __forceinline__ bool sees(const PrefixArgs& a, int b, int i, int j) {
   return !a.mask || (__ldg(a.mask + ((int64_t)b * a.q + i) * a.mw + (j >> 5)) >> (j & 31) & 1);

@@ -51,14 +51,6 @@ __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Whether one of a pair of bf16 is an infinity or a NaN; the pair with 0 there.
-__device__ __forceinline__ bool not_finite(uint32_t w) {
-  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
-}
-__device__ __forceinline__ uint32_t finite_only(uint32_t w) {
-  return ((w & 0x7f80u) == 0x7f80u ? 0 : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0 : w & 0xffff0000u);
-}
-
 // Byte offset of 16-byte chunk ch of row r of a [rows][D] bf16 tile: chunks
 // XOR-permuted by the row, so that the 8 rows of a matrix lie in 8 banks.
 template <int D>
@@ -74,7 +66,7 @@ size_t own_smem(int rows, int S, int keys) {
 }
 
 // WR warps along the rows, 4 / WR along the keys.
-template <int D, int WR, bool TREE>
+template <int D, int WR>
 __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __grid_constant__ PrefixArgs a) {
   constexpr int WK = 4 / WR, RB = 16 * WR, CH = D / 8, KW = KT / WK, TILE = KT * D * 2, PO = D + 4;
   extern __shared__ __align__(128) uint8_t smem[];
@@ -86,6 +78,7 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rw = warp % WR, kw = warp / WR;
   const int nb = (a.Ro + a.ob - 1) / a.ob, u = blockIdx.x / nb, r0 = (blockIdx.x % nb) * a.ob, nr = min(a.ob, a.Ro - r0);
   const int b = u / a.H, h = u % a.H;
+  const int NP = WK + a.S;
   // Where the block's rows lie, found once.
   __shared__ int64_t row_q[RB], row_o[RB], row_flat[RB];
   if (tid < nr) {
@@ -95,27 +88,14 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
     row_flat[tid] = flat_row(a, w);
   }
   grid_dep_wait();
-  // Parts, and the rows from one to the next: of slots, what the lengths make them.
-  int S = a.S;
-  int64_t pitch = a.rows;
-  if (TREE && a.C) {
-    const int tile = r0 / a.tr, items = a.H * a.mt, item = h * a.mt + tile, tiles = Spread::tiles_of(a, b);
-    Spread sp;
-    sp.measure(a);
-    const int64_t x = sp.first_of(a, b) + (int64_t)item * tiles, c0 = x / sp.per;
-    S = tiles ? (int)((x + tiles - 1) / sp.per - c0) + 1 : 0;
-    pitch = a.tr;
-    if (tid < nr) row_flat[tid] = (c0 + (int64_t)b * items + item) * a.tr + (r0 + tid - tile * a.tr);
-  }
   // Keys: the prompt's rows where they are attended here, then the own rows.
   const int p = b / a.each, np = a.direct ? prompt_count(a, p) : 0, nk = np + own_count(a, b);
   __syncthreads();
   // The parts' m and l and the query rows are on their way first: neither waits
   // for the length.
-  const int NP = WK + S;
   for (int r = warp; r < nr; r += 4)
-    for (int j = lane; j < S; j += 32)
-      cp_async8(smem_u32(sml + r * NP + WK + j), a.part_ml + j * pitch + row_flat[r]);
+    for (int j = lane; j < a.S; j += 32)
+      cp_async8(smem_u32(sml + r * NP + WK + j), a.part_ml + j * a.rows + row_flat[r]);
   const bf16* K = static_cast<const bf16*>(a.Kg) + b * a.gsb + h * a.gsh;
   const bf16* V = static_cast<const bf16*>(a.Vg) + b * a.gsb + h * a.gsh;
   const int64_t prompt = p * a.ksb + h * a.ksh;
@@ -156,11 +136,6 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
   fetch(0);
   fetch(1);
 
-  int seen_by[2] = {0, 0};  // the rows of the block of queries that this thread's are, for the mask
-  if (TREE && a.mask) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) seen_by[i] = own_row(a, b, h, r0 + min(rw * 16 + (lane >> 2) + 8 * i, nr - 1)).i;
-  }
   uint32_t q[D / 16][4];
   float o[D / 8][4], m[2] = {-FLT_MAX, -FLT_MAX}, l[2] = {0.f, 0.f};
 #pragma unroll
@@ -193,8 +168,7 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
       for (int n = 0; n < KW / 8; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int j = j0 + 8 * n + 2 * (lane & 3) + (e & 1);
-          if (j >= nk || (TREE && a.mask && !sees(a, b, seen_by[e >> 1], j))) s[n][e] = -INFINITY;
+          if (j0 + 8 * n + 2 * (lane & 3) + (e & 1) >= nk) s[n][e] = -INFINITY;
           top[e >> 1] = fmaxf(top[e >> 1], s[n][e]);
         }
 #pragma unroll
@@ -210,64 +184,22 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
           o[c][2 * i + 1] *= f;
         }
       }
-      // A value that is not finite, in a row that some query rows do not see: 0 times it
-      // is not 0, so such values are left out of the products and added below, row by row.
-      bool bad = false;
-      if (TREE && a.mask) {
-        for (int e = lane; e < KW * CH; e += 32) {
-          const uint4 x = lds_v4(vt + at<D>(kw * KW + e / CH, e % CH));
-          bad |= not_finite(x.x) | not_finite(x.y) | not_finite(x.z) | not_finite(x.w);
-        }
-        bad = __any_sync(0xffffffffu, bad);
-      }
 #pragma unroll
       for (int n = 0; n < KW / 16; ++n) {
         uint32_t p[4];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {  // rows g (even x), g + 8; keys 0-7 (x < 2), 8-15
-          float* sv = s[2 * n + (x >> 1)] + 2 * (x & 1);
+          const float* sv = s[2 * n + (x >> 1)] + 2 * (x & 1);
           const float p0 = ex2(fmaf(sv[0], a.sl2, -m[x & 1])), p1 = ex2(fmaf(sv[1], a.sl2, -m[x & 1]));
           l[x & 1] += p0 + p1;
           p[x] = pack_bf16(p0, p1);
-          if (TREE) { sv[0] = p0; sv[1] = p1; }
         }
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
           uint32_t v4[4];  // channels 0-7: keys 0-7, 8-15; channels 8-15: the same
           ldsm4t(v4, vt + at<D>(kw * KW + 16 * n + (lane & 15), 2 * c + (lane >> 4)));
-          if (TREE && bad) {
-#pragma unroll
-            for (int x = 0; x < 4; ++x) v4[x] = finite_only(v4[x]);
-          }
           mma16816(o[2 * c], p, v4[0], v4[1]);
           mma16816(o[2 * c + 1], p, v4[2], v4[3]);
-        }
-      }
-      if (TREE && bad) {
-#pragma unroll 1
-        for (int j = 0; j < KW && j0 + j < nk; ++j) {
-          float pj[2];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            float mine = 0.f;  // the weight of key j, where this thread has it
-#pragma unroll
-            for (int x = 0; x < KW / 4; ++x)
-              if (x / 2 == j / 8 && x % 2 == j % 2) mine = s[x / 2][2 * i + x % 2];
-            pj[i] = __shfl_sync(0xffffffffu, mine, (lane & ~3) | (j % 8 / 2));
-            if (!sees(a, b, seen_by[i], j0 + j)) pj[i] = -1.f;
-          }
-#pragma unroll
-          for (int c = 0; c < D / 8; ++c) {
-            const uint32_t w = lds_u32(vt + at<D>(kw * KW + j, c) + 4 * (lane & 3));
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const float v = e ? bf16_hi(w) : bf16_lo(w);
-              if (fabsf(v) <= FLT_MAX) continue;
-#pragma unroll
-              for (int i = 0; i < 2; ++i)
-                if (pj[i] >= 0.f || isnan(pj[i])) o[c][2 * i + e] = fmaf(pj[i], v, o[c][2 * i + e]);
-            }
-          }
         }
       }
     }
@@ -288,7 +220,7 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
 #pragma unroll
     for (int c = 0; c < D / 8; ++c)
       *reinterpret_cast<float2*>(row + 8 * c) = none ? make_float2(0.f, 0.f) : make_float2(o[c][2 * i], o[c][2 * i + 1]);
-    if ((lane & 3) == 0 && r < nr) sml[r * NP + kw] = make_float2(m[i], l[i]);
+    if ((lane & 3) == 0 && r < nr) sml[r * (WK + a.S) + kw] = make_float2(m[i], l[i]);
   }
   __syncthreads();
   // Weights 2^(m - M) / sum of 2^(m - M) l of a row's parts, 4 lanes a row; a part
@@ -328,18 +260,18 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
         y[x].x = fmaf(f, v.x, y[x].x); y[x].y = fmaf(f, v.y, y[x].y);
         y[x].z = fmaf(f, v.z, y[x].z); y[x].w = fmaf(f, v.w, y[x].w);
       };
-      for (int j = 0; j < S; j += PB) {
+      for (int j = 0; j < a.S; j += PB) {
         float4 v[PB][EB];
 #pragma unroll
         for (int k = 0; k < PB; ++k)
 #pragma unroll
           for (int x = 0; x < EB; ++x)
-            v[k][x] = j + k < S ? *reinterpret_cast<const float4*>(po[x] + (j + k) * pitch * D)
+            v[k][x] = j + k < a.S ? *reinterpret_cast<const float4*>(po[x] + (j + k) * a.rows * D)
                                   : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < PB; ++k)
 #pragma unroll
-          for (int x = 0; x < EB; ++x) add(x, j + k < S ? wt[x][WK + j + k].x : 0.f, v[k][x]);
+          for (int x = 0; x < EB; ++x) add(x, j + k < a.S ? wt[x][WK + j + k].x : 0.f, v[k][x]);
       }
 #pragma unroll
       for (int x = 0; x < EB; ++x) {
@@ -357,20 +289,19 @@ __global__ void __launch_bounds__(NTH, WR == 4 ? 3 : 4) own_join_kernel(const __
   else out(std::integral_constant<int, 4>());
 }
 
-template <int D, int WR, bool TREE>
+template <int D, int WR>
 cudaError_t launch(const PrefixArgs& a, cudaStream_t s) {
   const size_t smem = own_smem<D, WR>(a.ob, a.S, a.ng + (a.direct ? a.k : 0));
-  const auto k = own_join_kernel<D, WR, TREE>;
-  const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(k), smem);
+  const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(own_join_kernel<D, WR>), smem);
   if (e != cudaSuccess) return e;
   const int64_t blocks = (int64_t)a.B * a.H * ((a.Ro + a.ob - 1) / a.ob);
-  return Launch(dim3((unsigned)blocks), NTH, smem, s)(k, a);
+  return Launch(dim3((unsigned)blocks), NTH, smem, s)(own_join_kernel<D, WR>, a);
 }
 
-template <int D, bool TREE>
+template <int D>
 cudaError_t launch_rows(PrefixArgs a, cudaStream_t s) {
   a.ob = prefix_own_rows(a, a.S, a.ng + (a.direct ? a.k : 0));
-  return a.ob <= 16 ? launch<D, 1, TREE>(a, s) : a.ob == 32 ? launch<D, 2, TREE>(a, s) : launch<D, 4, TREE>(a, s);
+  return a.ob <= 16 ? launch<D, 1>(a, s) : a.ob == 32 ? launch<D, 2>(a, s) : launch<D, 4>(a, s);
 }
 
 }  // namespace
@@ -387,10 +318,7 @@ int prefix_own_rows(const PrefixArgs& a, int S, int keys) {
 }
 
 cudaError_t launch_prefix_own(const PrefixPlan& p, cudaStream_t s) {
-  return p.a.d == 128 ? launch_rows<128, false>(p.a, s) : launch_rows<64, false>(p.a, s);
-}
-cudaError_t launch_tree_own(const PrefixPlan& p, cudaStream_t s) {
-  return p.a.d == 128 ? launch_rows<128, true>(p.a, s) : launch_rows<64, true>(p.a, s);
+  return p.a.d == 128 ? launch_rows<128>(p.a, s) : launch_rows<64>(p.a, s);
 }
 
 }  // namespace wf

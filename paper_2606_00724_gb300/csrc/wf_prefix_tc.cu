@@ -55,10 +55,46 @@ constexpr int TM = kPrefixTcRows / 2;  // rows of a row tile, keys of a key tile
 constexpr int HALF = TM * 128;         // 64 channels of a tile of bf16 rows
 constexpr float kLazy = 8.f;
 
+// What a CTA works on: from the launch alone, and its keys from the lengths.
+struct Item {
+  bool own, wide;
+  int u, b, h;          // unit: prompt or sequence, key head
+  int part, r0, nr;     // part, first row, rows
+  int k0, k1, T;        // keys [k0, k1), tiles
+  // A range of wf_tree_attn: its first tile, the cached ones and rows of the item, drafted
+  // rows; whether it is the whole item, and its slot.
+  int t0, cached, count, drafts;
+  bool whole;
+  int64_t slot;
+  __device__ __forceinline__ bool draft(int t) const { return t0 + t >= cached; }
+};
+// How far the barriers have gone in the ranges before this one (of wf_tree_attn; else 0):
+// ring positions modulo two turns, steps, turns passed, last products, tiles of codes.
+struct Gone {
+  int pos, step0, step1, turn0, turn1, done0, done1, range, raw;
+  __device__ __forceinline__ void by(const Item& w, int stages) {
+    const int n0 = w.wide ? w.T : (w.T + 1) / 2, n1 = w.wide ? w.T : w.T / 2;
+    pos = (pos + 2 * w.T) % (2 * stages);
+    step0 += n0; step1 += n1;
+    turn0 += n1; turn1 += n0;
+    done0 += n0 > 0; done1 += n1 > 0;
+    range += 1;
+    raw += 2 * max(0, min(w.T, w.cached - w.t0));
+  }
+  __device__ __forceinline__ int step(int g) const { return g ? step1 : step0; }
+  __device__ __forceinline__ int turn(int g) const { return g ? turn1 : turn0; }
+};
+
 constexpr int kMaxStages = 9;
 struct Bars {
   unsigned long long full[kMaxStages], empty[kMaxStages], raw_full[4], raw_empty[4], qfull, sfull[2], pready[2], odone[2], turn[2], drain[2], stall;
   uint32_t tmem, abort;
+  int flag;  // a drafted value of this range is not finite
+  // wf_tree_attn's ranges, which one thread moves along.
+  Walk walk;
+  Item range;
+  Gone gone;
+  int more;
   // Between the two warps that share 32 rows of a tile: whether the tile is
   // there, whether a maximum rises, and the rows' maxima.
   int go[2][4], raise[2][2][4];
@@ -135,14 +171,25 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, int byt
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
-// What a CTA works on: from the launch alone, and its keys from the lengths.
-struct Item {
-  bool own, wide;
-  int u, b, h;          // unit: prompt or sequence, key head
-  int part, r0, nr;     // part, first row, rows
-  int k0, k1, T;        // keys [k0, k1), tiles
-};
-
+// Query rows of the row tiles of wf_tree_attn's items (the last may have fewer).
+__device__ __forceinline__ int tree_rows(const PrefixArgs& a) { return a.mt > 1 ? a.tr : a.Ro; }
+__device__ __forceinline__ Item range_of(const PrefixArgs& a, const Walk& k) {
+  Item w = {};
+  const int tile = k.item % a.mt;
+  w.b = k.b;
+  w.h = k.item / a.mt;
+  w.r0 = tile * a.tr;
+  w.nr = min(a.tr, a.Ro - w.r0);
+  w.wide = tree_rows(a) > TM;
+  w.T = k.t1 - k.t0;
+  w.t0 = k.t0;
+  w.cached = k.cached;
+  w.count = k.count;
+  w.drafts = k.drafts;
+  w.whole = k.whole();
+  w.slot = k.slot(a);
+  return w;
+}
 __device__ __forceinline__ Item item_of(const PrefixArgs& a) {
   Item w;
   const int prompts = a.P * a.H * a.mt * a.S;
@@ -264,25 +311,57 @@ __device__ __forceinline__ void copy_tile(uint32_t st, const bf16* base, int64_t
 __device__ __forceinline__ RowAt row_at(const PrefixArgs& a, const Item& w, int r) {
   return w.own ? own_row(a, w.b, w.h, w.r0 + r) : prompt_row(a, w.b, w.h, w.r0 + r);
 }
+// A drafted tile of bf16 rows by NT threads.  Values that are not finite are left out
+// where there is a mask (see not_finite), which the threads that brought them see to.
+template <int D, int NT>
+__device__ __forceinline__ void bring_draft(const PrefixArgs& a, const Item& w, Bars& s, uint32_t st, int t, bool v, int tid) {
+  // Without drafted rows nothing is read, of an address that exists.
+  const bf16* base = w.drafts > 0 ? static_cast<const bf16*>(v ? a.Vg : a.Kg) + w.b * a.gsb + w.h * a.gsh
+                                  : static_cast<const bf16*>(a.K);
+  copy_tile<D, NT>(st, base, a.gss, nullptr, 0, (w.t0 + t - w.cached) * TM, w.drafts, tid);
+  cp_async_wait_all();
+  if (v && a.mask) {
+    constexpr int CH = D / 8, RS = NT / CH;
+    bool bad = false;
+#pragma unroll 1
+    for (int i = 0; i < TM / RS; ++i) {
+      const uint32_t at = st + swizzled(tid / CH + RS * i, tid % CH);
+      const uint4 x = lds_v4(at);
+      if (not_finite(x.x) | not_finite(x.y) | not_finite(x.z) | not_finite(x.w)) {
+        bad = true;
+        sts_v4(at, make_uint4(finite_only(x.x), finite_only(x.y), finite_only(x.z), finite_only(x.w)));
+      }
+    }
+    if (bad) atomicExch(&s.flag, 1);
+  }
+  fence_proxy_async();
+}
+
 template <int D, int FMT, bool PAGED>
-__device__ void produce(const PrefixArgs& a, const Item& w, const Ring& ring, uint32_t raw, Bars& s, int tid) {
+__device__ void produce(const PrefixArgs& a, const Item& w, const Gone& gone, const Ring& ring, uint32_t raw, Bars& s,
+                        int tid) {
   typedef Cfg<D, FMT> C;
   constexpr int NPT = C::NPT;
   const int64_t b = w.b, h = w.h;
   const int A = w.wide ? 1 : 2;
   if constexpr (PAGED && !C::CODES) {
     const bf16 *K = static_cast<const bf16*>(a.K) + h * a.ksh, *V = static_cast<const bf16*>(a.V) + h * a.ksh;
-    int pos = -1, tile = -1;
+    int pos = gone.pos - 1, tile = -1;
     bool ok = true, kind = false;
     PagedRow row = {-1, 0};
     auto bring = [&] {
-      const int st = ring.stage(pos), n = ring.turn(pos);
-      if (ok && n > 0) ok = warp_wait(bar(s.empty[st]), (n - 1) & 1, s, a);
-      if (ok) copy_paged<D, NPT>(ring.base + st * C::TILE, a, kind ? V : K, row, tid);
+      const int st = ring.stage(pos);
+      if (ok) ok = warp_wait(bar(s.empty[st]), (ring.turn(pos) + 1) & 1, s, a);
+      if (ok && w.draft(tile)) {
+        bring_draft<D, NPT>(a, w, s, ring.base + st * C::TILE, tile, kind, tid);
+      } else if (ok) {
+        copy_paged<D, NPT>(ring.base + st * C::TILE, a, kind ? V : K, row, tid);
+      }
       cp_async_arrive_noinc(bar(s.full[st]));
     };
     in_order(w.T, A, [&](int t, bool v) {
-      const PagedRow next = look_up<D, NPT>(a, w.b, w.k0 + t * TM, w.k1, tid);
+      const PagedRow next =
+          w.draft(t) ? PagedRow{-1, 0} : look_up<D, NPT>(a, w.b, (w.t0 + t) * TM, w.count, tid);
       if (tile >= 0) bring();
       row = next;
       kind = v;
@@ -323,10 +402,28 @@ __device__ void produce(const PrefixArgs& a, const Item& w, const Ring& ring, ui
     const int x = gt % PX + PX * (gt / 8 % (CR / PX)), rr = gt / PX % (8 / PX) + 8 / PX * (gt / (8 * CR / PX));
     const uint32_t chunk = (uint32_t)(rr * CR + C::place(x, rr)) * 16;
     const uint32_t scale = TM * C::ROWB + rr * 4 + x * EL / kMxBlock;
+    const int lead = min(A, w.T), paired = 2 * w.T - lead;
+    int raw_at = PAGED ? gone.raw : 0;
 #pragma unroll 1
-    for (int p = group; p < 2 * w.T; p += 2) {
-      const int slot = p % C::DEPTH, st = ring.stage(p), n = ring.turn(p);
-      if (!warp_wait(bar(s.raw_full[slot]), p / C::DEPTH & 1, s, a)) break;
+    for (int p0 = PAGED ? 0 : group; p0 < 2 * w.T; p0 += PAGED ? 1 : 2) {
+      const int p = (PAGED ? gone.pos : 0) + p0, st = ring.stage(p), n = ring.turn(p);
+      const int code_at = PAGED ? raw_at : p0, slot = code_at % C::DEPTH;
+      if (PAGED) {
+        const int o = p0 - lead;  // see in_order
+        const bool v = o >= 0 && (p0 >= paired || !(o & 1)), mine = (p0 & 1) == group;
+        const int t = o < 0 ? p0 : p0 >= paired ? p0 - w.T : o / 2 + ((o & 1) ? A : 0);
+        if (w.draft(t)) {
+          if (!mine) continue;
+          if (!warp_wait(bar(s.empty[st]), (n + 1) & 1, s, a)) break;
+          bring_draft<D, NG>(a, w, s, ring.base + st * C::TILE, t, v, gt);
+          __syncwarp();
+          if ((gt & 31) == 0) mbar_arrive(bar(s.full[st]));
+          continue;
+        }
+        ++raw_at;
+        if (!mine) continue;
+      }
+      if (!warp_wait(bar(s.raw_full[slot]), code_at / C::DEPTH & 1, s, a)) break;
       // All of the thread's codes first, and the slot back to the loaders, so that a
       // copy's latency covers one tile's widening and not two (82 against 85 us for
       // a token from 8 bits, with four chunks at a time).
@@ -344,7 +441,7 @@ __device__ void produce(const PrefixArgs& a, const Item& w, const Ring& ring, ui
       large = __any_sync(0xffffffffu, large);
       __syncwarp();  // every lane has read its chunks
       if ((gt & 31) == 0) mbar_arrive(bar(s.raw_empty[slot]));
-      if (n > 0 && !warp_wait(bar(s.empty[st]), (n - 1) & 1, s, a)) break;
+      if ((PAGED || n > 0) && !warp_wait(bar(s.empty[st]), (n + 1) & 1, s, a)) break;
 #pragma unroll
       for (int i = 0; i < CPT; ++i) {
         const uint32_t cw[4] = {code[i].x, code[i].y, code[i].z, code[i].w};
@@ -377,7 +474,7 @@ __device__ void produce(const PrefixArgs& a, const Item& w, const Ring& ring, ui
 // bytes have 4 bytes of a slot; where they are 2, they are stored by the thread,
 // since the smallest copy is 4 bytes on 4.
 template <int D, int FMT, bool PAGED>
-__device__ void load_codes(const PrefixArgs& a, const Item& w, uint32_t raw, Bars& s, int warp, int lane) {
+__device__ void load_codes(const PrefixArgs& a, const Item& w, const Gone& gone, uint32_t raw, Bars& s, int warp, int lane) {
   typedef Cfg<D, FMT> C;
   constexpr int CR = C::CR, RP = 32 / CR, NI = 64 / RP, SR = D / kMxBlock;  // rows a pass of the warp, passes
   const int64_t b = w.b, h = w.h;
@@ -391,9 +488,9 @@ __device__ void load_codes(const PrefixArgs& a, const Item& w, uint32_t raw, Bar
   auto look_up = [&](int t, int* row, int* page) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const int j = w.k0 + t * TM + 64 * warp + lane + 32 * k;
+      const int j = (PAGED ? w.t0 * TM : w.k0) + t * TM + 64 * warp + lane + 32 * k;
       if (PAGED) {
-        const PagedRow r = j >= w.k1 ? PagedRow{-1, 0} : paged_row(a, w.b, j);
+        const PagedRow r = j >= w.count ? PagedRow{-1, 0} : paged_row(a, w.b, j);
         row[k] = r.flat;
         page[k] = r.page;
       } else {
@@ -401,11 +498,11 @@ __device__ void load_codes(const PrefixArgs& a, const Item& w, uint32_t raw, Bar
       }
     }
   };
-  int slot = 0, n = 0;
+  int slot = PAGED ? gone.raw % C::DEPTH : 0, n = PAGED ? gone.raw / C::DEPTH : 0;
   bool ok = true;
   const uint32_t first = (uint32_t)((64 * warp + lane / CR) * CR) * 16;  // this lane's first row in a slot
   auto bring = [&](int t, const int* row, const int* page, bool v) {
-    if (ok && n > 0) ok = warp_wait(bar(s.raw_empty[slot]), (n - 1) & 1, s, a);
+    if (ok && (PAGED || n > 0)) ok = warp_wait(bar(s.raw_empty[slot]), (n + 1) & 1, s, a);
     if (ok) {
       const uint32_t dst = raw + slot * C::SLOT;
       const uint8_t* base = v ? vbase : kbase;
@@ -440,6 +537,7 @@ __device__ void load_codes(const PrefixArgs& a, const Item& w, uint32_t raw, Bar
   int row[2], ahead[2], page[2], page_ahead[2], tile = -1;
   bool kind = false;
   in_order(w.T, w.wide ? 1 : 2, [&](int t, bool v) {
+    if (PAGED && w.draft(t)) return;
     look_up(t, ahead, page_ahead);
     if (tile >= 0) bring(tile, row, page, kind);
 #pragma unroll
@@ -473,8 +571,9 @@ __device__ __forceinline__ bool elect() {
   return r != 0;
 }
 
-template <int D, int FMT>
-__device__ void multiply(const PrefixArgs& a, const Item& w, uint32_t sq, const Ring& ring, Bars& s, int g) {
+template <int D, int FMT, bool PAGED>
+__device__ void multiply(const PrefixArgs& a, const Item& w, const Gone& gone, uint32_t sq, const Ring& ring, Bars& s,
+                         int g) {
   typedef Cfg<D, FMT> C;
   if (w.T == 0) return;
   const uint32_t tm = __shfl_sync(0xffffffffu, s.tmem, 0);
@@ -483,9 +582,9 @@ __device__ void multiply(const PrefixArgs& a, const Item& w, uint32_t sq, const 
   const uint64_t q = smem_desc_sw128(sq, 16, 1024) + (w.wide ? g : 0) * T4, k0 = smem_desc_sw128(ring.base, 16, 1024),
                  v0 = smem_desc_sw128(ring.base, HALF, 1024);
   const int A = w.wide ? 1 : 2, first = w.wide ? 0 : g;
-  bool ok = warp_wait(bar(a.stall ? s.stall : s.qfull), 0, s, a);
+  bool ok = warp_wait(bar(a.stall ? s.stall : s.qfull), (PAGED ? gone.range : 0) & 1, s, a);
   // Ring position of key tile t and of value tile t: see in_order.
-  const int lead = min(A, w.T);
+  const int lead = min(A, w.T), base = PAGED ? gone.pos : 0;
   auto arrived = [&](int pos) {
     if (ok) ok = warp_wait(bar(s.full[ring.stage(pos)]), ring.turn(pos) & 1, s, a);
     fence_proxy_async();
@@ -503,17 +602,17 @@ __device__ void multiply(const PrefixArgs& a, const Item& w, uint32_t sq, const 
     __syncwarp();
   };
   if (first < w.T) {
-    arrived(first);
-    if (ok) scores(first);
+    arrived(base + first);
+    if (ok) scores(PAGED ? ring.stage(base + first) : first);
   }
 #pragma unroll 1
   for (int j = first, i = 0; j < w.T && ok; j += A, ++i) {
     const bool more = j + A < w.T;
-    const int pv_pos = j < w.T - lead ? lead + 2 * j : w.T + j, pk_pos = pv_pos + 1;
+    const int pv_pos = base + (j < w.T - lead ? lead + 2 * j : w.T + j), pk_pos = pv_pos + 1;
     arrived(pv_pos);
     if (more && w.wide) arrived(pk_pos);
-    if (ok) ok = warp_wait(bar(s.pready[g]), i & 1, s, a);
-    if (ok && (g || i > 0)) ok = warp_wait(bar(s.turn[g]), (g ? i : i - 1) & 1, s, a);
+    if (ok) ok = warp_wait(bar(s.pready[g]), ((PAGED ? gone.step(g) : 0) + i) & 1, s, a);
+    if (ok && (g || i > 0)) ok = warp_wait(bar(s.turn[g]), ((PAGED ? gone.turn(g) : 0) + (g ? i : i - 1)) & 1, s, a);
     tc_fence_after();
     if (!ok) break;
     const int sv = ring.stage(pv_pos);
@@ -577,9 +676,11 @@ __device__ __forceinline__ float row_top(Bars& s, int g, int half, int r, int pa
 // rescaled and the pass runs again, S being still there.  P takes the first 32
 // of its half's columns.
 constexpr int CW = 16;
-template <int D, bool MASK>
+// MASK: keys from nk on count for nothing; BITS: nor do those whose bit is not set.
+template <int D, bool MASK, bool BITS>
 __device__ __forceinline__ void soften_tile(const PrefixArgs& a, Bars& s, uint32_t sc, uint32_t oc, bool have_o, int nk,
-                                            int g, int half, int r, int pair, float& m, float& l) {
+                                            const uint32_t* bits, int g, int half, int r, int pair, float& m, float& l) {
+  auto seen = [&](int e) { return BITS ? (bits[e >> 5] >> (e & 31) & 1) != 0 : e < nk; };
   constexpr int NC = TM / 2 / CW;
   const f32x2 sl = pk2(a.sl2, a.sl2);
   uint32_t p[TM / 4];
@@ -592,7 +693,7 @@ __device__ __forceinline__ void soften_tile(const PrefixArgs& a, Bars& s, uint32
       get(sc + CW * c, x);
       got(x);
 #pragma unroll
-      for (int e = 0; e < CW; ++e) top = fmaxf(top, !MASK || CW * c + e < nk ? __uint_as_float(x[e]) : -INFINITY);
+      for (int e = 0; e < CW; ++e) top = fmaxf(top, !MASK || seen(CW * c + e) ? __uint_as_float(x[e]) : -INFINITY);
     }
     m = fmaxf(m, row_top(s, g, half, r, pair, top) * a.sl2);
   }
@@ -610,7 +711,7 @@ __device__ __forceinline__ void soften_tile(const PrefixArgs& a, Bars& s, uint32
       if (c + 1 < NC) get(sc + CW * (c + 1), v[(c + 1) & 1]);
       if (MASK) {
 #pragma unroll
-        for (int e = 0; e < CW; ++e) x[e] = CW * c + e < nk ? x[e] : __float_as_uint(-INFINITY);
+        for (int e = 0; e < CW; ++e) x[e] = seen(CW * c + e) ? x[e] : __float_as_uint(-INFINITY);
       }
 #pragma unroll
       for (int e = 0; e < CW; e += 2) {
@@ -651,8 +752,9 @@ __device__ __forceinline__ void soften_tile(const PrefixArgs& a, Bars& s, uint32
 
 // Warpgroup wg of four: half wg % 2 of the columns of S and O of row tile (or
 // key tile parity) wg / 2.  Thread r has TMEM lane r.
-template <int D, int FMT>
-__device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* sm, uint8_t* stages, Bars& s, int tid) {
+template <int D, int FMT, bool PAGED>
+__device__ void soften(const PrefixArgs& a, const Item& w, const Gone& gone, uint8_t* sm, uint8_t* stages, Bars& s,
+                       int tid) {
   typedef Cfg<D, FMT> C;
   constexpr int CH = D / 8;
   const int g = tid >> 8, half = (tid >> 7) & 1, r = tid & 127, lane = tid & 31;
@@ -660,7 +762,7 @@ __device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* sm, uint8_t*
   const uint32_t lanes = (uint32_t)(r & ~31) << 16;  // the warp's quarter of the TMEM lanes
   const uint32_t tm = s.tmem, sc = tm + TM * g + TM / 2 * half + lanes, oc = tm + 2 * TM + D * g + D / 2 * half + lanes;
   const int rt = w.wide ? g * TM : 0;                // first row of the row tile
-  const bool active = rt + (r & ~31) < w.nr;         // the warp has a row
+  const bool active = rt + (r & ~31) < (PAGED ? tree_rows(a) : w.nr);  // the warp has a row
   const int step = w.wide ? 1 : 2, first = w.wide ? 0 : g;
   if (w.T > 0) {
     // The query rows, K-major; rows past the last are zero.
@@ -675,7 +777,7 @@ __device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* sm, uint8_t*
     }
     cp_async_arrive_noinc(bar(s.qfull));
   }
-  if (tid < w.nr) s.row[tid] = (uint32_t)flat_row(a, row_at(a, w, tid));
+  if (!PAGED && tid < w.nr) s.row[tid] = (uint32_t)flat_row(a, row_at(a, w, tid));
   float m = -FLT_MAX, l = 0.f;  // finite, so that logits of -inf add 0 and not 2^(-inf + inf)
   bool ok = true;
   if (active) {
@@ -685,16 +787,33 @@ __device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* sm, uint8_t*
       // One warp of a pair waits and tells the other: a wait that gives up must
       // not leave one of them at the barriers below.
       if (!half) {
-        ok = warp_wait(bar(s.sfull[g]), i & 1, s, a);
+        ok = warp_wait(bar(s.sfull[g]), ((PAGED ? gone.step(g) : 0) + i) & 1, s, a);
         if (lane == 0) s.go[g][r >> 5] = ok;
       }
       named_sync(pair, 64);
       ok = s.go[g][r >> 5];
       if (!ok) break;
       tc_fence_after();
-      const int nk = w.k1 - (w.k0 + t * TM);  // keys of the tile
-      if (nk >= TM) soften_tile<D, false>(a, s, sc, oc, i > 0, TM, g, half, r, pair, m, l);
-      else soften_tile<D, true>(a, s, sc, oc, i > 0, nk - TM / 2 * half, g, half, r, pair, m, l);
+      const bool draft = PAGED && w.draft(t);
+      const int nk = !PAGED  ? w.k1 - (w.k0 + t * TM)  // keys of the tile
+                     : draft ? w.drafts - (w.t0 + t - w.cached) * TM
+                             : w.count - (w.t0 + t) * TM;
+      if (nk >= TM && !(draft && a.mask)) {
+        soften_tile<D, false, false>(a, s, sc, oc, i > 0, TM, nullptr, g, half, r, pair, m, l);
+      } else if (PAGED) {
+        uint32_t bits[2];
+        const int left = nk - TM / 2 * half, row = row_at(a, w, min(rt + r, w.nr - 1)).i;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int in = left - 32 * x;  // keys of this word
+          bits[x] = in >= 32 ? 0xffffffffu : in > 0 ? (1u << in) - 1 : 0u;
+          if (draft && a.mask && in > 0)
+            bits[x] &= __ldg(a.mask + ((int64_t)w.b * a.q + row) * a.mw + (w.t0 + t - w.cached) * (TM / 32) + 2 * half + x);
+        }
+        soften_tile<D, true, true>(a, s, sc, oc, i > 0, 0, bits, g, half, r, pair, m, l);
+      } else {
+        soften_tile<D, true, false>(a, s, sc, oc, i > 0, nk - TM / 2 * half, nullptr, g, half, r, pair, m, l);
+      }
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
@@ -703,8 +822,8 @@ __device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* sm, uint8_t*
   }
   cp_async_wait_all();
   // The last products of both row tiles: the exchange below is in their stages.
-  if (ok && w.T > 0) ok = warp_wait(bar(s.odone[0]), 0, s, a);
-  if (ok && w.T > step - 1) ok = warp_wait(bar(s.odone[1]), 0, s, a);
+  if (ok && w.T > 0) ok = warp_wait(bar(s.odone[0]), (PAGED ? gone.done0 : 0) & 1, s, a);
+  if (ok && w.T > step - 1) ok = warp_wait(bar(s.odone[1]), (PAGED ? gone.done1 : 0) & 1, s, a);
   tc_fence_after();
   // The rows go out through the stages, which nothing reads any more: a thread has
   // a row, a store to memory wants a row's bytes from consecutive lanes (32
@@ -724,9 +843,10 @@ __device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* sm, uint8_t*
     l = l0 * ex2(m0 - M) + l1 * ex2(m1 - M);
     m = M;
   }
-  if (a.whole) f = l == 0.f ? 0.f : f / l;
+  const bool whole = PAGED ? w.whole : a.whole;
+  if (whole) f = l == 0.f ? 0.f : f / l;
   const bool none = !have || l == 0.f;
-  const bool gone = abort_set(smem_u32(&s.abort));
+  const bool cut = abort_set(smem_u32(&s.abort));
   if (active) {
     float* row = buf + (g * TM + r) * D;
 #pragma unroll
@@ -748,24 +868,30 @@ __device__ void soften(const PrefixArgs& a, const Item& w, uint8_t* sm, uint8_t*
   constexpr int LPR = D / 4, RPW = 32 / LPR;  // lanes a row, rows a warp
   const int cc = lane % LPR;
 #pragma unroll 4
-  for (int q = tid / LPR; q < w.nr && !gone; q += 16 * RPW) {
+  for (int q = tid / LPR; q < w.nr && !cut; q += 16 * RPW) {
     const float* row = buf + q * D + ((cc ^ (q & 7)) << 2);
     float4 y = *reinterpret_cast<const float4*>(row);
     if (!w.wide) {
       const float4 z = *reinterpret_cast<const float4*>(row + TM * D);
       y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
     }
-    if (a.whole) {
+    if (whole) {
       const RowAt at = row_at(a, w, q);
       *reinterpret_cast<uint2*>(static_cast<bf16*>(a.O) + at.b * a.osb + at.hq * a.osh + at.i * a.oss + 4 * cc) =
           make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
     } else {
-      *reinterpret_cast<float4*>(a.part_o + ((int64_t)w.part * a.rows + s.row[q]) * D + 4 * cc) = y;
+      const int64_t to = PAGED ? w.slot * a.tr + q : (int64_t)w.part * a.rows + s.row[q];
+      *reinterpret_cast<float4*>(a.part_o + to * D + 4 * cc) = y;
     }
   }
   const int row = rt + r;
-  if (!a.whole && !gone && row < w.nr && !half && (w.wide || g == 0))
-    a.part_ml[(int64_t)w.part * a.rows + s.row[row]] = make_float2(m, l);
+  if ((PAGED || !whole) && !cut && row < w.nr && !half && (w.wide || g == 0))
+    a.part_ml[PAGED ? w.slot * a.tr + row : (int64_t)w.part * a.rows + s.row[row]] = make_float2(m, l);
+  if (PAGED && !cut && tid == 0) {
+    if (w.t0 == 0) a.info[s.walk.items(a)] = make_int2((int)w.slot, s.walk.parts());
+    a.flags[w.slot] = s.flag;
+    s.flag = 0;
+  }
 }
 
 template <int D, int FMT, bool PAGED>
@@ -776,9 +902,12 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   Bars& s = *reinterpret_cast<Bars*>(raw + C::RAW);
   const int tid = threadIdx.x, warp = tid >> 5;
   constexpr int MMA_WARP = 16 + C::NPT / 32;
-  Item w = item_of(a);
-  uint8_t* stages = sm + (w.wide ? 2 : 1) * C::TILE;
-  const int ns = C::STAGES + (w.wide ? 0 : 1);
+  Item w;
+  if (!PAGED) w = item_of(a);
+  const int rows = PAGED ? tree_rows(a) : w.nr;
+  const bool wide = rows > TM;
+  uint8_t* stages = sm + (wide ? 2 : 1) * C::TILE;
+  const int ns = C::STAGES + (wide ? 0 : 1);
   const Ring ring = {smem_u32(stages), ns, 0xffffffffu / ns + 1};
   if (warp == MMA_WARP) {
     tmem_alloc(smem_u32(&s.tmem), 512);
@@ -786,16 +915,16 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   }
   // A barrier a thread: one after the other they took 0.4 us.
   if (tid < 2 * kMaxStages) {
-    const int arrivals = C::CODES && !w.own ? C::NPT / 64 : C::NPT;
+    const int arrivals = C::CODES && (PAGED || !w.own) ? C::NPT / 64 : C::NPT;
     // A stage is free with a commit of every MMA warp that reads it.
-    mbar_init(bar(tid < kMaxStages ? s.full[tid] : s.empty[tid - kMaxStages]), tid < kMaxStages ? arrivals : w.wide ? 2 : 1);
+    mbar_init(bar(tid < kMaxStages ? s.full[tid] : s.empty[tid - kMaxStages]), tid < kMaxStages ? arrivals : wide ? 2 : 1);
   } else if (tid >= 32 && tid < 40) {
     const int i = tid & 3;
     mbar_init(bar(tid < 36 ? s.raw_full[i] : s.raw_empty[i]), tid < 36 ? (D == 128 ? 64 : 128) : C::NPT / 64);
   } else if (tid >= 64 && tid < 66) {
-    const int g = tid - 64, rows = w.wide ? w.nr - g * TM : w.nr;
+    const int g = tid - 64, mine = wide ? rows - g * TM : rows;
     mbar_init(bar(s.sfull[g]), 1);
-    mbar_init(bar(s.pready[g]), (min(rows, TM) + 31) / 32 * 2);
+    mbar_init(bar(s.pready[g]), (min(mine, TM) + 31) / 32 * 2);
     mbar_init(bar(s.odone[g]), 1);
   } else if (tid >= 96 && tid < 98) {
     mbar_init(bar(s.turn[tid - 96]), 1);
@@ -804,23 +933,52 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
     mbar_init(bar(s.qfull), 512);
     mbar_init(bar(s.stall), 1);
     s.abort = 0;
+    s.flag = 0;
   }
   fence_mbar_init();
   grid_dep_wait();
-  keys_of(a, w);
+  if (!PAGED) {
+    keys_of(a, w);
+  } else if (warp == 0) {
+    Walk walk;
+    const bool more = walk.start(a) && walk.next(a);
+    if (tid == 0) {
+      s.more = more;
+      s.walk = walk;
+      if (more) s.range = range_of(a, walk);
+      s.gone = Gone{};
+    }
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   grid_dep_launch();  // after the barrier that publishes the tensor memory (see Launch)
   // (Moving registers from the producers to the softmax warps was slower with
   // codes: 93 against 88-90 us for a token at 128K.)
-  if (warp < 16) {
-    soften<D, FMT>(a, w, sm, stages, s, tid);
-  } else if (warp < MMA_WARP) {
-    produce<D, FMT, PAGED>(a, w, ring, smem_u32(raw), s, tid - 512);
+  auto work = [&](const Item& w, const Gone& gone) {
+    if (warp < 16) {
+      soften<D, FMT, PAGED>(a, w, gone, sm, stages, s, tid);
+    } else if (warp < MMA_WARP) {
+      produce<D, FMT, PAGED>(a, w, gone, ring, smem_u32(raw), s, tid - 512);
+    } else {
+      if (warp < MMA_WARP + 2) multiply<D, FMT, PAGED>(a, w, gone, smem_u32(sm), ring, s, warp - MMA_WARP);
+      else if (PAGED || !w.own) load_codes<D, FMT, PAGED>(a, w, gone, smem_u32(raw), s, warp - MMA_WARP - 2, tid & 31);
+    }
+  };
+  if (!PAGED) {
+    work(w, Gone{});
   } else {
-    if (warp < MMA_WARP + 2) multiply<D, FMT>(a, w, smem_u32(sm), ring, s, warp - MMA_WARP);
-    else if (!w.own) load_codes<D, FMT, PAGED>(a, w, smem_u32(raw), s, warp - MMA_WARP - 2, tid & 31);
+#pragma unroll 1
+    while (s.more) {
+      work(s.range, s.gone);
+      __syncthreads();  // the range is over: its stages, and what the roles share, are free
+      if (tid == 0) {
+        s.gone.by(s.range, ns);
+        s.more = !s.abort && s.walk.next(a);
+        if (s.more) s.range = range_of(a, s.walk);
+      }
+      __syncthreads();
+    }
   }
   tc_fence_before();
   __syncthreads();
@@ -833,7 +991,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
 template <int D, int FMT, bool PAGED>
 cudaError_t launch(const PrefixArgs& a, cudaStream_t s) {
   typedef Cfg<D, FMT> C;
-  const int64_t items = (int64_t)a.P * a.H * a.mt * a.S + (int64_t)a.B * a.H * a.mto * a.So;
+  const int64_t items = PAGED ? a.C : (int64_t)a.P * a.H * a.mt * a.S + (int64_t)a.B * a.H * a.mto * a.So;
   if (!items) return cudaSuccess;
   const auto k = tc_kernel<D, FMT, PAGED>;
   const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(k), C::SMEM);

@@ -67,9 +67,9 @@ struct Few {
     return r * ROWB + (CPR >= 8 ? ch ^ (r >> 1 & 3) * 2 : CPR == 4 ? ch ^ (r >> 1 & 3) : ch) * 16;
   }
   static constexpr int STEP = 2 * SK * ROWB + (CODES ? 128 : 0);
-  static constexpr int QD = 24576 / STEP > 8 ? 8 : 24576 / STEP;
+  static constexpr int QD = 16896 / STEP > 8 ? 8 : 16896 / STEP;
   static constexpr int PO = D + 4;
-  static constexpr size_t QUEUE = (size_t)NW * QD * STEP, SMEM = QUEUE + 2 * 16 * (PO + 2) * sizeof(float);
+  static constexpr size_t QUEUE = (size_t)NW * QD * STEP, SMEM = QUEUE + 16 * (PO + 2) * sizeof(float);
 };
 
 // N bytes of codes (or of bf16) to pairs of bf16; byte: their scale.
@@ -95,22 +95,17 @@ __device__ __forceinline__ void pairs_of(const uint32_t* w, uint32_t byte, uint3
 }
 
 template <int D, int FMT>
-__global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ PrefixArgs a) {
+__global__ void __launch_bounds__(NTH, kFewCtas / kPrefixSms) few_kernel(const __grid_constant__ PrefixArgs a) {
   typedef Few<D, FMT> C;
   extern __shared__ __align__(128) uint8_t sm[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
   const uint32_t queue = smem_u32(sm) + warp * C::QD * C::STEP;
-  float* const so = reinterpret_cast<float*>(sm + C::QUEUE);        // [2][16][PO]
-  float2* const sml = reinterpret_cast<float2*>(so + 2 * 16 * C::PO);  // [2][16]
+  float* const so = reinterpret_cast<float*>(sm + C::QUEUE);        // [16][PO]
+  float2* const sml = reinterpret_cast<float2*>(so + 16 * C::PO);  // [16]
   grid_dep_wait();
-  Spread sp;
-  sp.measure(a);
+  grid_dep_launch();
   Walk in;  // the range of the next step to be copied
-  bool more = in.start(a, sp);
-  if (!more) {
-    grid_dep_launch();
-    return;
-  }
+  if (!in.start(a)) return;
   Walk now = in;  // the range at work
   const bool in_page = a.by_ps.d % SK == 0;
   const int SR = D / kMxBlock;
@@ -118,26 +113,28 @@ __global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ Pre
   // The next step: its place is looked up a step before it is copied, since a table's
   // entry takes as long to come as a row.  What a range fixes is found once.
   constexpr int EB = C::CODES ? 1 : 2;  // bytes of a stride's unit
-  int t = 0, count_in = 0;
+  int t = 0, t_end = 0;
+  bool more = true;
   PagedRow at = {0, 0};
   const uint8_t *K = nullptr, *V = nullptr;
   const int64_t kss = a.kss * EB, kx = a.kx * EB;
   auto enter = [&] {
-    more = in.next(a);
+    do more = in.next(a);
+    while (more && in.t0 >= in.cached);  // drafted rows alone
     if (!more) return;
     t = in.t0;
-    count_in = prompt_count(a, in.b);
+    t_end = min(in.t1, in.cached);
     K = static_cast<const uint8_t*>(a.K) + in.item * a.ksh * EB + lane % C::CPR * 16;
     V = static_cast<const uint8_t*>(a.V) + in.item * a.ksh * EB + lane % C::CPR * 16;
   };
   auto look_up = [&] {
     const int j = t * kFewKeys + warp * SK + (in_page ? 0 : lane % SK);
-    at = more && j < count_in ? paged_row(a, in.b, j) : PagedRow{0, 0};
+    at = more && j < in.count ? paged_row(a, in.b, j) : PagedRow{0, 0};
   };
   uint32_t odd = 0;  // D = 64: whether the scales that this lane copied are the second half of their word
   auto bring = [&](uint32_t slot) {
     if (more) {
-      const int left = count_in - (t * kFewKeys + warp * SK);
+      const int left = in.count - (t * kFewKeys + warp * SK);
       const bool full = left >= SK;
       const int64_t first = at.flat * kss + at.page * kx;  // bytes to the step's first row, where that finds them all
 #pragma unroll
@@ -172,7 +169,7 @@ __global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ Pre
           odd = odd << 1 | (uint32_t)second;
         }
       }
-      if (++t == in.t1) enter();
+      if (++t == t_end) enter();
       look_up();
     } else if (D == 64) {
       odd <<= 1;
@@ -187,13 +184,14 @@ __global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ Pre
   int stage = 0;
 #pragma unroll 1
   while (now.next(a)) {
-    const int count = prompt_count(a, now.b);
     // Query rows g and g + 8, the channels in the order in which a lane has those of K.
     uint32_t q[D / 16][4];
+    int block_row[2];
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       const int r = g + 8 * n;
       const RowAt w = own_row(a, now.b, now.item, r < a.Ro ? r : 0);
+      block_row[n] = w.i;
       const bf16* p = static_cast<const bf16*>(a.Q) + w.b * a.qsb + w.hq * a.qsh + w.i * a.qss;
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) {  // runs of 8 channels
@@ -204,34 +202,50 @@ __global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ Pre
         q[2 * j + 1][n] = v.z; q[2 * j + 1][2 + n] = v.w;
       }
     }
+    int flag = 0;
     float o[D / 8][4], m[2] = {-FLT_MAX, -FLT_MAX}, l[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
 #pragma unroll 1
     for (int tile = now.t0; tile < now.t1; ++tile) {
       const uint32_t slot = queue + stage * C::STEP;
-      const int left = count - (tile * kFewKeys + warp * SK);
-      cp_async_wait<C::QD - 1>();
-      if constexpr (C::CODES) {
-        if (D == 64) {  // every lane puts the scales that it copied in the word's first half
-          const uint32_t w = slot + 2 * SK * C::ROWB + lane * 4;
-          if (odd >> (C::QD - 1) & 1) sts_u32(w, lds_u32(w) >> 16);
+      const bool draft = tile >= now.cached;
+      const int first = (draft ? tile - now.cached : tile) * kFewKeys + warp * SK;
+      const int left = (draft ? now.drafts : now.count) - first;
+      if (!draft) {
+        cp_async_wait<C::QD - 1>();
+        if constexpr (C::CODES) {
+          if (D == 64) {  // every lane puts the scales that it copied in the word's first half
+            const uint32_t w = slot + 2 * SK * C::ROWB + lane * 4;
+            if (odd >> (C::QD - 1) & 1) sts_u32(w, lds_u32(w) >> 16);
+          }
         }
+        __syncwarp();  // every lane's copies are there
       }
-      __syncwarp();  // every lane's copies are there
+      const int64_t own = now.b * a.gsb + now.item * a.gsh;  // drafted rows come straight from memory
       if (left > 0) {
         float s[2][4];
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
           s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
-          const uint32_t scale = C::CODES ? lds_u32(slot + 2 * SK * C::ROWB + (8 * n + g) * 4) : 0;
+          const uint32_t scale = C::CODES && !draft ? lds_u32(slot + 2 * SK * C::ROWB + (8 * n + g) * 4) : 0;
           uint32_t k[D / 8];
+          if (draft) {
+            const bf16* p = static_cast<const bf16*>(a.Kg) + own + (int64_t)(first + min(8 * n + g, left - 1)) * a.gss;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) {
+              constexpr int RUNS = C::KE / 8;
+              const uint4 v = __ldg(reinterpret_cast<const uint4*>(p + (4 * (j / RUNS) + c) * C::KE + 8 * (j % RUNS)));
+              k[4 * j] = v.x; k[4 * j + 1] = v.y; k[4 * j + 2] = v.z; k[4 * j + 3] = v.w;
+            }
+          } else {
 #pragma unroll
           for (int j = 0; j < C::KN; ++j) {
             uint32_t w[C::KB / 4];
             const int at = (4 * j + c) * C::KB;
             fetch<C::KB>(w, slot + C::k_place(8 * n + g, at / 16) + at % 16);
             pairs_of<D, FMT, C::KB>(w, scale >> 8 * ((4 * j + c) * C::KE / kMxBlock) & 0xffu, k + j * C::KE / 2);
+          }
           }
 #pragma unroll
           for (int i = 0; i < D / 16; ++i) mma16816(s[n], q[i], k[2 * i], k[2 * i + 1]);
@@ -242,6 +256,16 @@ __global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ Pre
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               if (8 * n + 2 * c + (e & 1) >= left) s[n][e] = -INFINITY;
+        }
+        if (draft && a.mask) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t w =
+                __ldg(a.mask + ((int64_t)now.b * a.q + block_row[i]) * a.mw + (first >> 5)) >> ((first & 31) + 2 * c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (!(w >> (8 * (e >> 1) + (e & 1)) & 1)) s[e >> 1][2 * i + (e & 1)] = -INFINITY;
+          }
         }
         float top[2];
 #pragma unroll
@@ -276,6 +300,24 @@ __global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ Pre
 #pragma unroll
           for (int n = 0; n < 4; ++n) {
             const int r = 2 * c + (n & 1) + 8 * (n >> 1);
+            if (draft) {
+              const bf16* p = static_cast<const bf16*>(a.Vg) + own + (int64_t)(first + min(r, left - 1)) * a.gss +
+                              (8 * j + g) * C::VE;
+#pragma unroll
+              for (int i = 0; i < C::VE / 8; ++i) {
+                const uint4 w = __ldg(reinterpret_cast<const uint4*>(p) + i);
+                v[n][4 * i] = w.x; v[n][4 * i + 1] = w.y; v[n][4 * i + 2] = w.z; v[n][4 * i + 3] = w.w;
+              }
+#pragma unroll
+              for (int i = 0; i < C::VE / 2; ++i) {
+                if (r >= left) v[n][i] = 0;
+                if (a.mask && not_finite(v[n][i])) {
+                  flag = 1;
+                  v[n][i] = finite_only(v[n][i]);
+                }
+              }
+              continue;
+            }
             uint32_t w[C::VB / 4], byte = 0;
             const int at = (8 * j + g) * C::VB;
             fetch<C::VB>(w, slot + SK * C::ROWB + C::v_place(r, at / 16) + at % 16);
@@ -291,39 +333,41 @@ __global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ Pre
           }
         }
       }
-      __syncwarp();  // every lane has read the slot
-      bring(slot);
-      if (++stage == C::QD) stage = 0;
+      if (!draft) {
+        __syncwarp();  // every lane has read the slot
+        bring(slot);
+        if (++stage == C::QD) stage = 0;
+      }
     }
 
-    // The four warps' O: 2 and 3 go to 0 and 1, then 1 to 0, which writes the part.
+    // The four warps' O, added from the last to the first, which writes the part.
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
     }
     auto channel = [&](int e, int x) { return (8 * (e / C::VE) + 2 * c + x) * C::VE + e % C::VE; };
-    auto put = [&](int to) {
+    auto put = [&] {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int r = g + 8 * i;
         if (r >= a.Ro) continue;
-        if (c == 0) sml[to * 16 + r] = make_float2(m[i], l[i]);
+        if (c == 0) sml[r] = make_float2(m[i], l[i]);
 #pragma unroll
         for (int e = 0; e < D / 8; e += 4)
 #pragma unroll
           for (int x = 0; x < 2; ++x)
-            *reinterpret_cast<float4*>(so + (to * 16 + r) * C::PO + channel(e, x)) =
+            *reinterpret_cast<float4*>(so + r * C::PO + channel(e, x)) =
                 make_float4(o[e][2 * i + x], o[e + 1][2 * i + x], o[e + 2][2 * i + x], o[e + 3][2 * i + x]);
       }
     };
-    auto take = [&](int from) {
+    auto take = [&] {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int r = g + 8 * i;
         if (r >= a.Ro) continue;
         // Without weight (l = 0) O is 0 x V, which is NaN where V is not finite.
-        const float2 y = sml[from * 16 + r];
+        const float2 y = sml[r];
         const bool have = l[i] != 0.f, add = y.y != 0.f;
         if (!add) continue;
         const float M = have ? fmaxf(m[i], y.x) : y.x, f0 = have ? ex2(m[i] - M) : 0.f, f1 = ex2(y.x - M);
@@ -333,7 +377,7 @@ __global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ Pre
         for (int e = 0; e < D / 8; e += 4)
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const float4 v = *reinterpret_cast<const float4*>(so + (from * 16 + r) * C::PO + channel(e, x));
+            const float4 v = *reinterpret_cast<const float4*>(so + r * C::PO + channel(e, x));
             const float w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (int z = 0; z < 4; ++z)
@@ -341,38 +385,48 @@ __global__ void __launch_bounds__(NTH, 2) few_kernel(const __grid_constant__ Pre
           }
       }
     };
-    __syncthreads();  // the last range's exchange is over
-    if (warp >= 2) put(warp - 2);
-    __syncthreads();
-    if (warp < 2) take(warp);
-    if (warp == 1) put(1);
-    __syncthreads();
+#pragma unroll 1
+    for (int w = NW - 1; w > 0; --w) {
+      flag = __syncthreads_or(flag);  // the last exchange is over
+      if (warp == w) put();
+      __syncthreads();
+      if (warp == w - 1) take();
+    }
+    const bool whole = now.whole();
+    if (threadIdx.x == 0) {
+      if (now.t0 == 0) a.info[now.items(a)] = make_int2((int)now.slot(a), now.parts());
+      a.flags[now.slot(a)] = flag;
+    }
     if (warp == 0) {
-      take(1);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int r = g + 8 * i;
         if (r >= a.Ro) continue;
         const int64_t row = now.slot(a) * a.tr + r;
         const bool none = l[i] == 0.f;
+        const float f = whole ? 1.f / l[i] : 1.f;
         if (c == 0) a.part_ml[row] = make_float2(m[i], l[i]);
+        const RowAt w = own_row(a, now.b, now.item, r);
+        bf16* out = static_cast<bf16*>(a.O) + w.b * a.osb + w.hq * a.osh + w.i * a.oss;
 #pragma unroll
         for (int e = 0; e < D / 8; e += 4)
 #pragma unroll
-          for (int x = 0; x < 2; ++x)
-            *reinterpret_cast<float4*>(a.part_o + row * D + channel(e, x)) =
-                none ? make_float4(0.f, 0.f, 0.f, 0.f)
-                     : make_float4(o[e][2 * i + x], o[e + 1][2 * i + x], o[e + 2][2 * i + x], o[e + 3][2 * i + x]);
+          for (int x = 0; x < 2; ++x) {
+            const int at = channel(e, x);
+            float4 y = make_float4(o[e][2 * i + x], o[e + 1][2 * i + x], o[e + 2][2 * i + x], o[e + 3][2 * i + x]);
+            if (none) y = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (!whole) *reinterpret_cast<float4*>(a.part_o + row * D + at) = y;
+            else *reinterpret_cast<uint2*>(out + at) =
+                none ? make_uint2(0, 0) : make_uint2(pack_bf16(y.x * f, y.y * f), pack_bf16(y.z * f, y.w * f));
+          }
       }
     }
   }
-  grid_dep_launch();
   cp_async_wait_all();
 }
 
 template <int D, int FMT>
 cudaError_t launch(const PrefixArgs& a, cudaStream_t s) {
-  if (!a.C) return cudaSuccess;
   const auto k = few_kernel<D, FMT>;
   const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(k), Few<D, FMT>::SMEM);
   return e != cudaSuccess ? e : Launch(dim3((unsigned)a.C), NTH, Few<D, FMT>::SMEM, s)(k, a);
