@@ -59,6 +59,7 @@ struct PrefixArgs {
   // part is a slot of tr rows; info says where an item's are and how many, flags
   // which of them left drafted values out that are not finite.
   int C, tk, tr;
+  int box;               // rows of the pieces of pages that the copy engine brings; 0: not by it
   int2* info;
   int* flags;
 };

@@ -40,7 +40,11 @@
 // Every wait is bounded: one that gives up sets the status word and the
 // abort word, every role leaves its loops, work in flight is drained and the
 // tensor memory freed.
+#include <cuda.h>
 #include <float.h>
+
+#include <numeric>
+#include <type_traits>
 
 #include "wf_mx.cuh"
 #include "wf_prefix.cuh"
@@ -251,26 +255,7 @@ __device__ __forceinline__ uint32_t swizzled(int r, int ch) {
 
 // One tile of bf16 rows, NPT threads: chunk tid % CH of rows tid / CH + RS i.
 // With idx, lane ch of the CH lanes that share a row looks up rows
-// tid / CH + RS (ch + CH k) and the lanes pass them on; of a cache in pages that
-// is look_up's, a tile ahead.
-template <int D, int NPT>
-__device__ __forceinline__ PagedRow look_up(const PrefixArgs& a, int b, int t0, int k1, int tid) {
-  constexpr int CH = D / 8, RS = NPT / CH, NI = TM / RS;
-  static_assert(NI <= CH, "one row a lane");
-  const int ch = tid % CH, j = t0 + tid / CH + RS * ch;
-  return ch < NI && j < k1 ? paged_row(a, b, j) : PagedRow{-1, 0};
-}
-template <int D, int NPT>
-__device__ __forceinline__ void copy_paged(uint32_t st, const PrefixArgs& a, const bf16* base, const PagedRow& at, int tid) {
-  constexpr int CH = D / 8, RS = NPT / CH, NI = TM / RS;
-  const int ch = tid % CH, rr = tid / CH;
-#pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    const PagedRow w = {__shfl_sync(0xffffffffu, at.flat, i, CH), __shfl_sync(0xffffffffu, at.page, i, CH)};
-    const bool ok = w.flat >= 0;
-    cp_async16_zfill(st + swizzled(rr + RS * i, ch), base + ch * 8 + (ok ? paged_offset(a, w) : 0), ok);
-  }
-}
+// tid / CH + RS (ch + CH k) and the lanes pass them on.
 template <int D, int NPT>
 __device__ __forceinline__ void copy_tile(uint32_t st, const bf16* base, int64_t stride, const int32_t* idx, int n, int t0,
                                           int k1, int tid) {
@@ -311,10 +296,50 @@ __device__ __forceinline__ void copy_tile(uint32_t st, const bf16* base, int64_t
 __device__ __forceinline__ RowAt row_at(const PrefixArgs& a, const Item& w, int r) {
   return w.own ? own_row(a, w.b, w.h, w.r0 + r) : prompt_row(a, w.b, w.h, w.r0 + r);
 }
+// Pages.  Where the least common parts of pages and tiles are 8 rows or more (a.box,
+// their greatest common divisor), a tile is boxes of so many rows and 64 channels of
+// one page, which the copy engine brings: a warp's lanes look up a box each and ask for it
+// (with a copy instruction a 16-byte chunk and its address from the table, 256 rows a key head on
+// 32K took 150 us against the 118 of a contiguous prompt).  Pages of other sizes, and a
+// tile that ends inside, go by chunks: the lanes that share a row look up a row each, a
+// tile ahead, and pass the offsets on.
+struct TreeMaps {
+  CUtensorMap k, v;
+};
+struct NoMaps {};
+
+[[maybe_unused]] __device__ __forceinline__ void bring_box(uint32_t dst, const CUtensorMap* map, int x, int y, int h, int page,
+                                          uint32_t mbar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], "
+      "[%6];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(h), "r"(page), "r"(mbar)
+      : "memory");
+}
+template <int D, int NPT>
+__device__ __forceinline__ int64_t look_up(const PrefixArgs& a, int b, int t0, int k1, int tid) {
+  constexpr int CH = D / 8, RS = NPT / CH, NI = TM / RS;
+  static_assert(NI <= CH, "one row a lane");
+  const int ch = tid % CH, j = t0 + tid / CH + RS * ch;
+  return ch < NI && j < k1 ? paged_offset(a, paged_row(a, b, j)) : -1;
+}
+template <int D, int NPT>
+__device__ __forceinline__ void copy_paged(uint32_t st, const bf16* base, int64_t at, int tid) {
+  constexpr int CH = D / 8, RS = NPT / CH, NI = TM / RS;
+  const int ch = tid % CH, rr = tid / CH;
+  const int lo = (int)(uint32_t)at, hi = (int)(at >> 32);
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int64_t o =
+        (int64_t)__shfl_sync(0xffffffffu, hi, i, CH) << 32 | (uint32_t)__shfl_sync(0xffffffffu, lo, i, CH);
+    cp_async16_zfill(st + swizzled(rr + RS * i, ch), base + ch * 8 + max(o, (int64_t)0), o >= 0);
+  }
+}
+
 // A drafted tile of bf16 rows by NT threads.  Values that are not finite are left out
 // where there is a mask (see not_finite), which the threads that brought them see to.
 template <int D, int NT>
-__device__ __forceinline__ void bring_draft(const PrefixArgs& a, const Item& w, Bars& s, uint32_t st, int t, bool v, int tid) {
+__device__ __noinline__ void bring_draft(const PrefixArgs& a, const Item& w, Bars& s, uint32_t st, int t, bool v, int tid) {
   // Without drafted rows nothing is read, of an address that exists.
   const bf16* base = w.drafts > 0 ? static_cast<const bf16*>(v ? a.Vg : a.Kg) + w.b * a.gsb + w.h * a.gsh
                                   : static_cast<const bf16*>(a.K);
@@ -337,39 +362,75 @@ __device__ __forceinline__ void bring_draft(const PrefixArgs& a, const Item& w, 
   fence_proxy_async();
 }
 
-template <int D, int FMT, bool PAGED>
-__device__ void produce(const PrefixArgs& a, const Item& w, const Gone& gone, const Ring& ring, uint32_t raw, Bars& s,
-                        int tid) {
+template <int D, int FMT, bool PAGED, typename M>
+__device__ void produce(const PrefixArgs& a, const M& maps, const Item& w, const Gone& gone, const Ring& ring, uint32_t raw,
+                        Bars& s, int tid) {
   typedef Cfg<D, FMT> C;
   constexpr int NPT = C::NPT;
   const int64_t b = w.b, h = w.h;
   const int A = w.wide ? 1 : 2;
   if constexpr (PAGED && !C::CODES) {
     const bf16 *K = static_cast<const bf16*>(a.K) + h * a.ksh, *V = static_cast<const bf16*>(a.V) + h * a.ksh;
-    int pos = gone.pos - 1, tile = -1;
+    constexpr int HV = D / 64;  // boxes side by side
+    int pos = gone.pos - 1, tile = -1, page = 0, y = 0, last = pos;
     bool ok = true, kind = false;
-    PagedRow row = {-1, 0};
-    auto bring = [&] {
+    int64_t row = -1;
+    const int box = tid / HV * a.box;  // this lane's box: its first row of a tile
+    auto whole = [&](int t) { return a.box && (w.t0 + t + 1) * TM <= w.count; };
+    auto bring = [&](int page, int y, int64_t row) {
       const int st = ring.stage(pos);
-      if (ok) ok = warp_wait(bar(s.empty[st]), (ring.turn(pos) + 1) & 1, s, a);
-      if (ok && w.draft(tile)) {
-        bring_draft<D, NPT>(a, w, s, ring.base + st * C::TILE, tile, kind, tid);
-      } else if (ok) {
-        copy_paged<D, NPT>(ring.base + st * C::TILE, a, kind ? V : K, row, tid);
+      const uint32_t full = bar(s.full[st]), dst = ring.base + st * C::TILE;
+      // With boxes the first warp alone follows the barriers: nothing would keep the others from
+      // falling two phases behind, where a parity says the opposite.  For a tile by chunks
+      // it calls them, and comes to them whether its wait gave up or not.
+      if (ok && (!a.box || tid < 32)) ok = warp_wait(bar(s.empty[st]), (ring.turn(pos) + 1) & 1, s, a);
+      if (whole(tile)) {
+        if (ok && tid < 32) {
+          if (tid == 0) mbar_arrive_expect_tx(full, C::TILE);
+          __syncwarp();
+          if (box < TM)
+            bring_box(dst + tid % HV * HALF + box * 128, kind ? &maps.v : &maps.k, tid % HV * 64, y, w.h, page, full);
+        }
+      } else {
+        if (a.box) named_sync(2, NPT);
+        if (ok && w.draft(tile)) bring_draft<D, NPT>(a, w, s, dst, tile, kind, tid);
+        else if (ok) copy_paged<D, NPT>(dst, kind ? V : K, row, tid);
+        if (!a.box) {
+          cp_async_arrive_noinc(full);
+        } else {
+          cp_async_wait_all();
+          fence_proxy_async();
+          named_sync(2, NPT);
+          if (ok && tid == 0) mbar_arrive(full);
+        }
       }
-      cp_async_arrive_noinc(bar(s.full[st]));
+      if (ok) last = pos;
     };
     in_order(w.T, A, [&](int t, bool v) {
-      const PagedRow next =
-          w.draft(t) ? PagedRow{-1, 0} : look_up<D, NPT>(a, w.b, (w.t0 + t) * TM, w.count, tid);
-      if (tile >= 0) bring();
+      int64_t next = -1;
+      int next_page = 0, next_y = 0;
+      if (w.draft(t)) {
+      } else if (!whole(t)) {
+        next = look_up<D, NPT>(a, w.b, (w.t0 + t) * TM, w.count, tid);
+      } else if (tid < 32 && box < TM) {
+        const PagedRow r = paged_row(a, w.b, (w.t0 + t) * TM + box);
+        next_page = r.page;
+        next_y = r.flat - r.page * (int)a.by_ps.d;
+      }
+      if (tile >= 0) bring(page, y, row);
       row = next;
+      page = next_page;
+      y = next_y;
       kind = v;
       tile = t;
       ++pos;
     });
-    if (tile >= 0) bring();
+    if (tile >= 0) bring(page, y, row);
     cp_async_wait_all();
+    // No copy is in flight when the range ends, nor when a wait gave up.
+    if (a.box && tid == 0)
+      for (int p = max(gone.pos, last - ring.n + 1); p <= last; ++p)
+        (void)mbar_wait_bounded(bar(s.full[ring.stage(p)]), ring.turn(p) & 1, kDefaultWaitLimit);
     return;
   }
   if (!C::CODES || w.own) {
@@ -402,27 +463,39 @@ __device__ void produce(const PrefixArgs& a, const Item& w, const Gone& gone, co
     const int x = gt % PX + PX * (gt / 8 % (CR / PX)), rr = gt / PX % (8 / PX) + 8 / PX * (gt / (8 * CR / PX));
     const uint32_t chunk = (uint32_t)(rr * CR + C::place(x, rr)) * 16;
     const uint32_t scale = TM * C::ROWB + rr * 4 + x * EL / kMxBlock;
-    const int lead = min(A, w.T), paired = 2 * w.T - lead;
-    int raw_at = PAGED ? gone.raw : 0;
+    // wf_tree_attn: drafted tiles come last, from ring position `drafted` of the range on
+    // mixed with the last cached values.
+    const int lead = min(A, w.T);
+    int drafted = 2 * w.T, codes = 0;
+    if (PAGED) {
+      const int t = max(0, w.cached - w.t0);
+      if (t < w.T) drafted = t < lead ? t : lead + 2 * (t - A) + 1;
+    }
 #pragma unroll 1
-    for (int p0 = PAGED ? 0 : group; p0 < 2 * w.T; p0 += PAGED ? 1 : 2) {
+    for (int p0 = group; p0 < 2 * w.T; p0 += 2) {
       const int p = (PAGED ? gone.pos : 0) + p0, st = ring.stage(p), n = ring.turn(p);
-      const int code_at = PAGED ? raw_at : p0, slot = code_at % C::DEPTH;
-      if (PAGED) {
-        const int o = p0 - lead;  // see in_order
-        const bool v = o >= 0 && (p0 >= paired || !(o & 1)), mine = (p0 & 1) == group;
-        const int t = o < 0 ? p0 : p0 >= paired ? p0 - w.T : o / 2 + ((o & 1) ? A : 0);
+      int code_at = (PAGED ? gone.raw : 0) + p0;
+      if (PAGED && p0 >= drafted) {
+        // Position p0's tile (see in_order), and the positions of codes up to it.
+        int t = 0;
+        bool v = false;
+        codes = 0;
+        for (int x = drafted; x <= p0; ++x) {
+          const int o = x - lead, paired = 2 * w.T - lead;
+          v = o >= 0 && (x >= paired || !(o & 1));
+          t = o < 0 ? x : x >= paired ? x - w.T : o / 2 + ((o & 1) ? A : 0);
+          codes += !w.draft(t);
+        }
         if (w.draft(t)) {
-          if (!mine) continue;
           if (!warp_wait(bar(s.empty[st]), (n + 1) & 1, s, a)) break;
           bring_draft<D, NG>(a, w, s, ring.base + st * C::TILE, t, v, gt);
           __syncwarp();
           if ((gt & 31) == 0) mbar_arrive(bar(s.full[st]));
           continue;
         }
-        ++raw_at;
-        if (!mine) continue;
+        code_at = gone.raw + drafted + codes - 1;
       }
+      const int slot = code_at % C::DEPTH;
       if (!warp_wait(bar(s.raw_full[slot]), code_at / C::DEPTH & 1, s, a)) break;
       // All of the thread's codes first, and the slot back to the loaders, so that a
       // copy's latency covers one tile's widening and not two (82 against 85 us for
@@ -894,8 +967,9 @@ __device__ void soften(const PrefixArgs& a, const Item& w, const Gone& gone, uin
   }
 }
 
-template <int D, int FMT, bool PAGED>
-__global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_constant__ PrefixArgs a) {
+template <int D, int FMT, bool PAGED, typename M>
+__global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1)
+    tc_kernel(const __grid_constant__ PrefixArgs a, const __grid_constant__ M maps) {
   typedef Cfg<D, FMT> C;
   extern __shared__ __align__(1024) uint8_t sm[];
   uint8_t* raw = sm + (2 + C::STAGES) * C::TILE;
@@ -915,7 +989,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   }
   // A barrier a thread: one after the other they took 0.4 us.
   if (tid < 2 * kMaxStages) {
-    const int arrivals = C::CODES && (PAGED || !w.own) ? C::NPT / 64 : C::NPT;
+    const int arrivals = C::CODES && (PAGED || !w.own) ? C::NPT / 64 : PAGED && a.box ? 1 : C::NPT;
     // A stage is free with a commit of every MMA warp that reads it.
     mbar_init(bar(tid < kMaxStages ? s.full[tid] : s.empty[tid - kMaxStages]), tid < kMaxStages ? arrivals : wide ? 2 : 1);
   } else if (tid >= 32 && tid < 40) {
@@ -959,7 +1033,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
     if (warp < 16) {
       soften<D, FMT, PAGED>(a, w, gone, sm, stages, s, tid);
     } else if (warp < MMA_WARP) {
-      produce<D, FMT, PAGED>(a, w, gone, ring, smem_u32(raw), s, tid - 512);
+      produce<D, FMT, PAGED>(a, maps, w, gone, ring, smem_u32(raw), s, tid - 512);
     } else {
       if (warp < MMA_WARP + 2) multiply<D, FMT, PAGED>(a, w, gone, smem_u32(sm), ring, s, warp - MMA_WARP);
       else if (PAGED || !w.own) load_codes<D, FMT, PAGED>(a, w, gone, smem_u32(raw), s, warp - MMA_WARP - 2, tid & 31);
@@ -971,6 +1045,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
 #pragma unroll 1
     while (s.more) {
       work(s.range, s.gone);
+      fence_proxy_async();  // the rows went out through stages that the copy engine writes next
       __syncthreads();  // the range is over: its stages, and what the roles share, are free
       if (tid == 0) {
         s.gone.by(s.range, ns);
@@ -988,14 +1063,44 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1) tc_kernel(const __grid_co
   }
 }
 
+#ifdef WF_TREE
+// The pages as the copy engine takes them, in boxes of 64 channels and `rows` rows, their
+// chunks permuted as swizzled() has them; false where it does not take these strides.
+bool map_pages(CUtensorMap* map, const PrefixArgs& a, const void* base, int rows) {
+  typedef decltype(&cuTensorMapEncodeTiled) Encode;
+  static const Encode encode = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+    return e == cudaSuccess && found == cudaDriverEntryPointSuccess ? reinterpret_cast<Encode>(f) : nullptr;
+  }();
+  if (!encode) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)a.d, a.by_ps.d, (cuuint64_t)a.H, (cuuint64_t)a.pool};
+  const cuuint64_t strides[3] = {(cuuint64_t)a.kss * 2, (cuuint64_t)a.ksh * 2, (cuuint64_t)a.ksb * 2};
+  const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1}, each[4] = {1, 1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, each,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+#else
+[[maybe_unused]] bool map_pages(CUtensorMap*, const PrefixArgs&, const void*, int) { return false; }
+#endif
+
 template <int D, int FMT, bool PAGED>
 cudaError_t launch(const PrefixArgs& a, cudaStream_t s) {
   typedef Cfg<D, FMT> C;
   const int64_t items = PAGED ? a.C : (int64_t)a.P * a.H * a.mt * a.S + (int64_t)a.B * a.H * a.mto * a.So;
   if (!items) return cudaSuccess;
-  const auto k = tc_kernel<D, FMT, PAGED>;
+  typedef typename std::conditional<PAGED && !C::CODES, TreeMaps, NoMaps>::type M;
+  M maps = {};
+  PrefixArgs b = a;
+  if constexpr (PAGED && !C::CODES) {
+    b.box = std::gcd((int)a.by_ps.d, TM);
+    if (b.box < 8 || !map_pages(&maps.k, a, a.K, b.box) || !map_pages(&maps.v, a, a.V, b.box)) b.box = 0;
+  }
+  const auto k = tc_kernel<D, FMT, PAGED, M>;
   const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(k), C::SMEM);
-  return e != cudaSuccess ? e : Launch(dim3((unsigned)items), C::NTH, C::SMEM, s)(k, a);
+  return e != cudaSuccess ? e : Launch(dim3((unsigned)items), C::NTH, C::SMEM, s)(k, b, maps);
 }
 template <bool PAGED>
 cudaError_t launch_cached(const PrefixPlan& p, cudaStream_t s) {
