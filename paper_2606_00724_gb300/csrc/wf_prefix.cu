@@ -513,6 +513,7 @@ PrefixPlan plan_tree(const wf_tensor& q, const wf_tensor& kv, int k, int n_t) {
   a.S = a.So = a.direct = a.whole = 0;
   p.few = a.Ro <= kFewRows;
   a.tk = p.few ? kFewKeys : kPrefixTcRows / 2;
+  a.pad = p.few ? kFewPad : kTreePad;
   a.mt = (a.Ro + kPrefixTcRows - 1) / kPrefixTcRows;
   // Row tiles of equal height, whole warps of them.
   a.tr = a.mt == 1 ? a.Ro : ((a.Ro + a.mt - 1) / a.mt + 31) / 32 * 32;

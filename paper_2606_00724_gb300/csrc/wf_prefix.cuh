@@ -58,7 +58,7 @@ struct PrefixArgs {
   // are spread over C CTAs evenly (see Spread), a unit's rows in mt tiles of tr.  A
   // part is a slot of tr rows; info says where an item's are and how many, flags
   // which of them left drafted values out that are not finite.
-  int C, tk, tr;
+  int C, tk, tr, pad;
   int box;               // rows of the pieces of pages that the copy engine brings; 0: not by it
   int2* info;
   int* flags;
@@ -104,6 +104,7 @@ cudaError_t launch_tree_few(const PrefixPlan& p, cudaStream_t s);
 cudaError_t launch_tree_join(const PrefixPlan& p, cudaStream_t s);
 // Query rows of a unit that the kernel for few of them takes, keys of its tiles, and
 // its CTAs.
+constexpr int kFewPad = 1, kTreePad = 4;  // see Spread
 constexpr int kFewRows = 16, kFewKeys = 64, kFewCtas = 3 * kPrefixSms;
 
 // Sequence, query head and block row of row r of the unit of prompt p (or of
@@ -150,14 +151,17 @@ __device__ __forceinline__ int64_t paged_scale(const PrefixArgs& a, const PagedR
 // row tile of tr rows of a unit, lie in one line, items in the order [sequence][key
 // head][row tile], an item's cached tiles before its drafted ones and one tile at
 // least; CTA c takes tiles [c per, (c + 1) per), which are ranges of one item or of
-// several that follow each other.  The lengths are known on the device alone, so
-// every warp finds its place in the line from them.  A range is a part, and its slot is
+// several that follow each other.  A range that begins inside a CTA's share costs it
+// `pad` tiles' time more (rows in, first products, rows out), so the line has as many
+// empty places before each item.  The lengths are known on the device alone, so every
+// warp finds its place in the line from them.  A range is a part, and its slot is
 // c + item: along the line either grows by one from range to range, so no two
 // ranges share a slot and those of an item follow each other.
 struct Spread {
   int64_t total, per;
+  // The places of an item of sequence b.
   __device__ __forceinline__ static int tiles_of(const PrefixArgs& a, int b) {
-    return b < a.B ? max(1, (prompt_count(a, b) + a.tk - 1) / a.tk + (own_count(a, b) + a.tk - 1) / a.tk) : 0;
+    return b < a.B ? a.pad + max(1, (prompt_count(a, b) + a.tk - 1) / a.tk + (own_count(a, b) + a.tk - 1) / a.tk) : 0;
   }
   // By a whole warp.
   __device__ __forceinline__ void measure(const PrefixArgs& a) {
@@ -168,7 +172,7 @@ struct Spread {
     total = t * a.H * a.mt;
     per = total < 0x7fffffff ? (int64_t)(((uint32_t)total + a.C - 1) / (uint32_t)a.C) : (total + a.C - 1) / a.C;
   }
-  // The sequence whose items hold tile x < total, and its first tile in the line; by a
+  // The sequence whose items hold place x < total, and its first tile in the line; by a
   // whole warp.
   __device__ __forceinline__ int find(const PrefixArgs& a, int64_t x, int64_t* first) const {
     const int lane = threadIdx.x & 31;
@@ -194,7 +198,7 @@ struct Spread {
 
 // The ranges of one CTA, one after the other.
 struct Walk {
-  int64_t x, end, first;      // next tile, end of the CTA's; first tile of sequence b
+  int64_t x, end, first;      // next place, end of the CTA's; first place of sequence b
   int64_t per;
   int b, count, drafts;       // sequence, its cached and drafted rows
   int cached, tiles;          // tiles of an item of b: cached ones, all
@@ -219,26 +223,29 @@ struct Walk {
   }
   // To the next range; false behind the last.
   __device__ __forceinline__ bool next(const PrefixArgs& a) {
-    if (x >= end) return false;
-    while (x >= first + (int64_t)tiles * a.H * a.mt) {
-      first += (int64_t)tiles * a.H * a.mt;
-      enter(a, b + 1);
+    for (;;) {
+      if (x >= end) return false;
+      const int places = a.pad + tiles;
+      const int64_t in = x - first, all = (int64_t)places * a.H * a.mt;
+      if (in >= all) {
+        first += all;
+        enter(a, b + 1);
+        continue;
+      }
+      item = in < 0x7fffffff ? (int)((uint32_t)in / (uint32_t)places) : (int)(in / places);
+      const int at = (int)(in - (int64_t)item * places), to = (int)min((int64_t)places, at + (end - x));
+      x += to - at;
+      t0 = max(0, at - a.pad);
+      t1 = to - a.pad;
+      if (t1 > t0) return true;  // else empty places alone
     }
-    const int64_t in = x - first;
-    item = in < 0x7fffffff ? (int)((uint32_t)in / (uint32_t)tiles) : (int)(in / tiles);
-    t0 = (int)(in - (int64_t)item * tiles);
-    t1 = (int)min((int64_t)tiles, t0 + (end - x));
-    x += t1 - t0;
-    return true;
   }
   __device__ __forceinline__ int64_t items(const PrefixArgs& a) const { return (int64_t)b * a.H * a.mt + item; }
   __device__ __forceinline__ int64_t slot(const PrefixArgs& a) const { return blockIdx.x + items(a); }
   // The whole item: there are no other parts.
   __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == tiles; }
   // The parts of the item whose first one this is.
-  __device__ __forceinline__ int parts() const {
-    return (int)((x - (t1 - t0) + tiles - 1) / per) - (int)blockIdx.x + 1;
-  }
+  __device__ __forceinline__ int parts() const { return (int)((x - t1 + tiles - 1) / per) - (int)blockIdx.x + 1; }
 };
 
 // Whether one of a pair of bf16 is an infinity or a NaN; the pair with 0 there.  Drafted

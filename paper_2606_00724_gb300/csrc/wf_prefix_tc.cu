@@ -463,40 +463,10 @@ __device__ void produce(const PrefixArgs& a, const M& maps, const Item& w, const
     const int x = gt % PX + PX * (gt / 8 % (CR / PX)), rr = gt / PX % (8 / PX) + 8 / PX * (gt / (8 * CR / PX));
     const uint32_t chunk = (uint32_t)(rr * CR + C::place(x, rr)) * 16;
     const uint32_t scale = TM * C::ROWB + rr * 4 + x * EL / kMxBlock;
-    // wf_tree_attn: drafted tiles come last, from ring position `drafted` of the range on
-    // mixed with the last cached values.
-    const int lead = min(A, w.T);
-    int drafted = 2 * w.T, codes = 0;
-    if (PAGED) {
-      const int t = max(0, w.cached - w.t0);
-      if (t < w.T) drafted = t < lead ? t : lead + 2 * (t - A) + 1;
-    }
-#pragma unroll 1
-    for (int p0 = group; p0 < 2 * w.T; p0 += 2) {
-      const int p = (PAGED ? gone.pos : 0) + p0, st = ring.stage(p), n = ring.turn(p);
-      int code_at = (PAGED ? gone.raw : 0) + p0;
-      if (PAGED && p0 >= drafted) {
-        // Position p0's tile (see in_order), and the positions of codes up to it.
-        int t = 0;
-        bool v = false;
-        codes = 0;
-        for (int x = drafted; x <= p0; ++x) {
-          const int o = x - lead, paired = 2 * w.T - lead;
-          v = o >= 0 && (x >= paired || !(o & 1));
-          t = o < 0 ? x : x >= paired ? x - w.T : o / 2 + ((o & 1) ? A : 0);
-          codes += !w.draft(t);
-        }
-        if (w.draft(t)) {
-          if (!warp_wait(bar(s.empty[st]), (n + 1) & 1, s, a)) break;
-          bring_draft<D, NG>(a, w, s, ring.base + st * C::TILE, t, v, gt);
-          __syncwarp();
-          if ((gt & 31) == 0) mbar_arrive(bar(s.full[st]));
-          continue;
-        }
-        code_at = gone.raw + drafted + codes - 1;
-      }
-      const int slot = code_at % C::DEPTH;
-      if (!warp_wait(bar(s.raw_full[slot]), code_at / C::DEPTH & 1, s, a)) break;
+    // Ring position p from codes' position at; false if a wait gave up.
+    auto widen = [&](int p, int at) {
+      const int slot = at % C::DEPTH, st = ring.stage(p), n = ring.turn(p);
+      if (!warp_wait(bar(s.raw_full[slot]), at / C::DEPTH & 1, s, a)) return false;
       // All of the thread's codes first, and the slot back to the loaders, so that a
       // copy's latency covers one tile's widening and not two (82 against 85 us for
       // a token from 8 bits, with four chunks at a time).
@@ -514,7 +484,7 @@ __device__ void produce(const PrefixArgs& a, const M& maps, const Item& w, const
       large = __any_sync(0xffffffffu, large);
       __syncwarp();  // every lane has read its chunks
       if ((gt & 31) == 0) mbar_arrive(bar(s.raw_empty[slot]));
-      if ((PAGED || n > 0) && !warp_wait(bar(s.empty[st]), (n + 1) & 1, s, a)) break;
+      if ((PAGED || n > 0) && !warp_wait(bar(s.empty[st]), (n + 1) & 1, s, a)) return false;
 #pragma unroll
       for (int i = 0; i < CPT; ++i) {
         const uint32_t cw[4] = {code[i].x, code[i].y, code[i].z, code[i].w};
@@ -536,6 +506,42 @@ __device__ void produce(const PrefixArgs& a, const M& maps, const Item& w, const
       fence_proxy_async();
       __syncwarp();
       if ((gt & 31) == 0) mbar_arrive(bar(s.full[st]));
+      return true;
+    };
+    if constexpr (!PAGED) {
+#pragma unroll 1
+      for (int p = group; p < 2 * w.T; p += 2)
+        if (!widen(p, p)) break;
+    } else {
+      // Drafted tiles come last, from position `drafted` of the range on mixed with the last
+      // cached values.
+      const int T = w.T, lead = min(A, T), cached = min(T, max(0, w.cached - w.t0));
+      const int drafted = cached == T ? 2 * T : cached < lead ? cached : lead + 2 * (cached - A) + 1;
+      const int pos = gone.pos, codes = gone.raw;
+      bool ok = true;
+      int p = group;
+#pragma unroll 1
+      for (; p < drafted && ok; p += 2) ok = widen(pos + p, codes + p);
+      int at = codes + drafted;  // of position x below
+#pragma unroll 1
+      for (int x = drafted; x < 2 * T && ok; ++x) {
+        const int o = x - lead;  // see in_order
+        const bool v = o >= 0 && (x >= 2 * T - lead || !(o & 1));
+        const int t = o < 0 ? x : x >= 2 * T - lead ? x - T : o / 2 + ((o & 1) ? A : 0);
+        if (t < cached) ++at;
+        if (x != p) continue;
+        p += 2;
+        if (t < cached) {
+          ok = widen(pos + x, at - 1);
+        } else {
+          const int st = ring.stage(pos + x);
+          ok = warp_wait(bar(s.empty[st]), (ring.turn(pos + x) + 1) & 1, s, a);
+          if (!ok) break;
+          bring_draft<D, NG>(a, w, s, ring.base + st * C::TILE, t, v, gt);
+          __syncwarp();
+          if ((gt & 31) == 0) mbar_arrive(bar(s.full[st]));
+        }
+      }
     }
   }
 }
@@ -648,16 +654,19 @@ template <int D, int FMT, bool PAGED>
 __device__ void multiply(const PrefixArgs& a, const Item& w, const Gone& gone, uint32_t sq, const Ring& ring, Bars& s,
                          int g) {
   typedef Cfg<D, FMT> C;
-  if (w.T == 0) return;
+  const int T = w.T;
+  const bool wide = w.wide;
+  if (T == 0) return;
   const uint32_t tm = __shfl_sync(0xffffffffu, s.tmem, 0);
   constexpr uint32_t qk = idesc_bf16(TM, TM, 0, 0), pv = idesc_bf16(TM, D, 0, 1);
   constexpr int T4 = C::TILE >> 4, H4 = HALF >> 4;  // in units of a descriptor's address
-  const uint64_t q = smem_desc_sw128(sq, 16, 1024) + (w.wide ? g : 0) * T4, k0 = smem_desc_sw128(ring.base, 16, 1024),
+  const uint64_t q = smem_desc_sw128(sq, 16, 1024) + (wide ? g : 0) * T4, k0 = smem_desc_sw128(ring.base, 16, 1024),
                  v0 = smem_desc_sw128(ring.base, HALF, 1024);
-  const int A = w.wide ? 1 : 2, first = w.wide ? 0 : g;
+  const int A = wide ? 1 : 2, first = wide ? 0 : g;
+  const int steps = PAGED ? gone.step(g) : 0, turns = PAGED ? gone.turn(g) : 0;
   bool ok = warp_wait(bar(a.stall ? s.stall : s.qfull), (PAGED ? gone.range : 0) & 1, s, a);
   // Ring position of key tile t and of value tile t: see in_order.
-  const int lead = min(A, w.T), base = PAGED ? gone.pos : 0;
+  const int lead = min(A, T), base = PAGED ? gone.pos : 0;
   auto arrived = [&](int pos) {
     if (ok) ok = warp_wait(bar(s.full[ring.stage(pos)]), ring.turn(pos) & 1, s, a);
     fence_proxy_async();
@@ -674,18 +683,18 @@ __device__ void multiply(const PrefixArgs& a, const Item& w, const Gone& gone, u
     }
     __syncwarp();
   };
-  if (first < w.T) {
+  if (first < T) {
     arrived(base + first);
     if (ok) scores(PAGED ? ring.stage(base + first) : first);
   }
 #pragma unroll 1
-  for (int j = first, i = 0; j < w.T && ok; j += A, ++i) {
-    const bool more = j + A < w.T;
-    const int pv_pos = base + (j < w.T - lead ? lead + 2 * j : w.T + j), pk_pos = pv_pos + 1;
+  for (int j = first, i = 0; j < T && ok; j += A, ++i) {
+    const bool more = j + A < T;
+    const int pv_pos = base + (j < T - lead ? lead + 2 * j : T + j), pk_pos = pv_pos + 1;
     arrived(pv_pos);
-    if (more && w.wide) arrived(pk_pos);
-    if (ok) ok = warp_wait(bar(s.pready[g]), ((PAGED ? gone.step(g) : 0) + i) & 1, s, a);
-    if (ok && (g || i > 0)) ok = warp_wait(bar(s.turn[g]), ((PAGED ? gone.turn(g) : 0) + (g ? i : i - 1)) & 1, s, a);
+    if (more && wide) arrived(pk_pos);
+    if (ok) ok = warp_wait(bar(s.pready[g]), (steps + i) & 1, s, a);
+    if (ok && (g || i > 0)) ok = warp_wait(bar(s.turn[g]), (turns + (g ? i : i - 1)) & 1, s, a);
     tc_fence_after();
     if (!ok) break;
     const int sv = ring.stage(pv_pos);
@@ -701,7 +710,7 @@ __device__ void multiply(const PrefixArgs& a, const Item& w, const Gone& gone, u
     // With one row tile the products are short and the rows' arrival is what
     // bounds the loop: the value tile's stage goes back before the wait for the
     // next key tile.
-    if (more && !w.wide) arrived(pk_pos);
+    if (more && !wide) arrived(pk_pos);
     if (more && ok) scores(ring.stage(pk_pos));
     if (elect()) mbar_arrive(bar(s.turn[g ^ 1]));
     __syncwarp();
@@ -854,37 +863,37 @@ __device__ void soften(const PrefixArgs& a, const Item& w, const Gone& gone, uin
   float m = -FLT_MAX, l = 0.f;  // finite, so that logits of -inf add 0 and not 2^(-inf + inf)
   bool ok = true;
   if (active) {
+    // Whole cached tiles, and steps before this range.
+    const int T = w.T, full = PAGED ? min(T, w.count / TM - w.t0) : (w.k1 - w.k0) / TM, steps = PAGED ? gone.step(g) : 0;
     int i = 0;
 #pragma unroll 1
-    for (int t = first; t < w.T; t += step, ++i) {
+    for (int t = first; t < T; t += step, ++i) {
       // One warp of a pair waits and tells the other: a wait that gives up must
       // not leave one of them at the barriers below.
       if (!half) {
-        ok = warp_wait(bar(s.sfull[g]), ((PAGED ? gone.step(g) : 0) + i) & 1, s, a);
+        ok = warp_wait(bar(s.sfull[g]), (steps + i) & 1, s, a);
         if (lane == 0) s.go[g][r >> 5] = ok;
       }
       named_sync(pair, 64);
       ok = s.go[g][r >> 5];
       if (!ok) break;
       tc_fence_after();
-      const bool draft = PAGED && w.draft(t);
-      const int nk = !PAGED  ? w.k1 - (w.k0 + t * TM)  // keys of the tile
-                     : draft ? w.drafts - (w.t0 + t - w.cached) * TM
-                             : w.count - (w.t0 + t) * TM;
-      if (nk >= TM && !(draft && a.mask)) {
+      if (t < full) {
         soften_tile<D, false, false>(a, s, sc, oc, i > 0, TM, nullptr, g, half, r, pair, m, l);
       } else if (PAGED) {
+        const bool draft = w.draft(t), mask = draft && a.mask;
         uint32_t bits[2];
-        const int left = nk - TM / 2 * half, row = row_at(a, w, min(rt + r, w.nr - 1)).i;
+        const int t0 = (w.t0 + t - (draft ? w.cached : 0)) * TM + TM / 2 * half, left = (draft ? w.drafts : w.count) - t0;
+        const int row = row_at(a, w, min(rt + r, w.nr - 1)).i;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const int in = left - 32 * x;  // keys of this word
           bits[x] = in >= 32 ? 0xffffffffu : in > 0 ? (1u << in) - 1 : 0u;
-          if (draft && a.mask && in > 0)
-            bits[x] &= __ldg(a.mask + ((int64_t)w.b * a.q + row) * a.mw + (w.t0 + t - w.cached) * (TM / 32) + 2 * half + x);
+          if (mask && in > 0) bits[x] &= __ldg(a.mask + ((int64_t)w.b * a.q + row) * a.mw + t0 / 32 + x);
         }
         soften_tile<D, true, true>(a, s, sc, oc, i > 0, 0, bits, g, half, r, pair, m, l);
       } else {
+        const int nk = w.k1 - (w.k0 + t * TM);  // keys of the tile
         soften_tile<D, true, false>(a, s, sc, oc, i > 0, nk - TM / 2 * half, nullptr, g, half, r, pair, m, l);
       }
       tmem_wait_st();

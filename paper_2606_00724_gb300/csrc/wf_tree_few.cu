@@ -276,7 +276,8 @@ __global__ void __launch_bounds__(NTH, kFewCtas / kPrefixSms) few_kernel(const _
           for (int i = 0; i < 2; ++i) {
             top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
             top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
-            const float mn = fmaxf(m[i], top[i]), f = ex2(m[i] - mn);
+            // Of rows that ask for it themselves: a row's bits do not depend on its neighbours.
+            const float mn = top[i] > m[i] + kLazy ? top[i] : m[i], f = ex2(m[i] - mn);
             m[i] = mn;
             l[i] *= f;
 #pragma unroll
