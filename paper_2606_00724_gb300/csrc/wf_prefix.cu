@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(kThreads<TR>, TR == 128 ? 1 : 2) simt_kernel(c
   const int64_t cached = PAGED ? h * a.ksh : b * a.ksb + h * a.ksh;
   auto row_of = [&](int j, int64_t* scales) {
     if (PAGED) {
-      const PagedRow w = paged_row(a, b, j);
+      const PagedRow w = paged_row(a, page_entry(a, b, j), j);
       *scales = paged_scale(a, w, h);
       return paged_offset(a, w);
     }

@@ -135,10 +135,14 @@ __device__ __forceinline__ int own_count(const PrefixArgs& a, int b) {
 struct PagedRow {
   int flat, page;
 };
-__device__ __forceinline__ PagedRow paged_row(const PrefixArgs& a, int b, int j) {
-  const int entry = fastdiv((uint32_t)j, a.by_ps);
-  const int page = min(max(__ldg(a.pages + (int64_t)b * a.table + entry), 0), a.pool - 1);
-  return {page * (int)a.by_ps.d + (j - entry * (int)a.by_ps.d), page};
+// In two steps, so that what is loaded is not used before it has to be: the table's
+// entry of row j, and the row itself.
+__device__ __forceinline__ int page_entry(const PrefixArgs& a, int b, int j) {
+  return __ldg(a.pages + (int64_t)b * a.table + fastdiv((uint32_t)j, a.by_ps));
+}
+__device__ __forceinline__ PagedRow paged_row(const PrefixArgs& a, int entry, int j) {
+  const int page = min(max(entry, 0), a.pool - 1), in = j - (int)(fastdiv((uint32_t)j, a.by_ps) * a.by_ps.d);
+  return {page * (int)a.by_ps.d + in, page};
 }
 __device__ __forceinline__ int64_t paged_offset(const PrefixArgs& a, const PagedRow& r) {
   return r.flat * a.kss + r.page * a.kx;

@@ -316,12 +316,13 @@ struct NoMaps {};
       "l"(map), "r"(x), "r"(y), "r"(h), "r"(page), "r"(mbar)
       : "memory");
 }
+// The row of a tile from t0 on that this lane looks up, or -1.
 template <int D, int NPT>
-__device__ __forceinline__ int64_t look_up(const PrefixArgs& a, int b, int t0, int k1, int tid) {
+__device__ __forceinline__ int looked_up(int t0, int k1, int tid) {
   constexpr int CH = D / 8, RS = NPT / CH, NI = TM / RS;
   static_assert(NI <= CH, "one row a lane");
   const int ch = tid % CH, j = t0 + tid / CH + RS * ch;
-  return ch < NI && j < k1 ? paged_offset(a, paged_row(a, b, j)) : -1;
+  return ch < NI && j < k1 ? j : -1;
 }
 template <int D, int NPT>
 __device__ __forceinline__ void copy_paged(uint32_t st, const bf16* base, int64_t at, int tid) {
@@ -372,12 +373,11 @@ __device__ void produce(const PrefixArgs& a, const M& maps, const Item& w, const
   if constexpr (PAGED && !C::CODES) {
     const bf16 *K = static_cast<const bf16*>(a.K) + h * a.ksh, *V = static_cast<const bf16*>(a.V) + h * a.ksh;
     constexpr int HV = D / 64;  // boxes side by side
-    int pos = gone.pos - 1, tile = -1, page = 0, y = 0, last = pos;
+    int pos = gone.pos - 1, tile = -1, entry = 0, row = -1, last = pos;  // row: what this lane looked up
     bool ok = true, kind = false;
-    int64_t row = -1;
     const int box = tid / HV * a.box;  // this lane's box: its first row of a tile
     auto whole = [&](int t) { return a.box && (w.t0 + t + 1) * TM <= w.count; };
-    auto bring = [&](int page, int y, int64_t row) {
+    auto bring = [&] {
       const int st = ring.stage(pos);
       const uint32_t full = bar(s.full[st]), dst = ring.base + st * C::TILE;
       // With boxes the first warp alone follows the barriers: nothing would keep the others from
@@ -388,13 +388,16 @@ __device__ void produce(const PrefixArgs& a, const M& maps, const Item& w, const
         if (ok && tid < 32) {
           if (tid == 0) mbar_arrive_expect_tx(full, C::TILE);
           __syncwarp();
-          if (box < TM)
-            bring_box(dst + tid % HV * HALF + box * 128, kind ? &maps.v : &maps.k, tid % HV * 64, y, w.h, page, full);
+          if (box < TM) {
+            const PagedRow r = paged_row(a, entry, row);
+            bring_box(dst + tid % HV * HALF + box * 128, kind ? &maps.v : &maps.k, tid % HV * 64,
+                      r.flat - r.page * (int)a.by_ps.d, w.h, r.page, full);
+          }
         }
       } else {
         if (a.box) named_sync(2, NPT);
         if (ok && w.draft(tile)) bring_draft<D, NPT>(a, w, s, dst, tile, kind, tid);
-        else if (ok) copy_paged<D, NPT>(dst, kind ? V : K, row, tid);
+        else if (ok) copy_paged<D, NPT>(dst, kind ? V : K, row < 0 ? -1 : paged_offset(a, paged_row(a, entry, row)), tid);
         if (!a.box) {
           cp_async_arrive_noinc(full);
         } else {
@@ -407,25 +410,20 @@ __device__ void produce(const PrefixArgs& a, const M& maps, const Item& w, const
       if (ok) last = pos;
     };
     in_order(w.T, A, [&](int t, bool v) {
-      int64_t next = -1;
-      int next_page = 0, next_y = 0;
-      if (w.draft(t)) {
-      } else if (!whole(t)) {
-        next = look_up<D, NPT>(a, w.b, (w.t0 + t) * TM, w.count, tid);
-      } else if (tid < 32 && box < TM) {
-        const PagedRow r = paged_row(a, w.b, (w.t0 + t) * TM + box);
-        next_page = r.page;
-        next_y = r.flat - r.page * (int)a.by_ps.d;
+      int next = -1, next_entry = 0;
+      if (!w.draft(t)) {
+        if (!whole(t)) next = looked_up<D, NPT>((w.t0 + t) * TM, w.count, tid);
+        else if (tid < 32 && box < TM) next = (w.t0 + t) * TM + box;
       }
-      if (tile >= 0) bring(page, y, row);
+      if (next >= 0) next_entry = page_entry(a, w.b, next);
+      if (tile >= 0) bring();
       row = next;
-      page = next_page;
-      y = next_y;
+      entry = next_entry;
       kind = v;
       tile = t;
       ++pos;
     });
-    if (tile >= 0) bring(page, y, row);
+    if (tile >= 0) bring();
     cp_async_wait_all();
     // No copy is in flight when the range ends, nor when a wait gave up.
     if (a.box && tid == 0)
@@ -552,42 +550,35 @@ __device__ void produce(const PrefixArgs& a, const M& maps, const Item& w, const
 // their scales, and the lanes pass the rows on for the chunks.  A row's scale
 // bytes have 4 bytes of a slot; where they are 2, they are stored by the thread,
 // since the smallest copy is 4 bytes on 4.
-template <int D, int FMT, bool PAGED>
-__device__ void load_codes(const PrefixArgs& a, const Item& w, const Gone& gone, uint32_t raw, Bars& s, int warp, int lane) {
+template <int D, int FMT>
+__device__ void load_codes(const PrefixArgs& a, const Item& w, uint32_t raw, Bars& s, int warp, int lane) {
   typedef Cfg<D, FMT> C;
   constexpr int CR = C::CR, RP = 32 / CR, NI = 64 / RP, SR = D / kMxBlock;  // rows a pass of the warp, passes
   const int64_t b = w.b, h = w.h;
   const int x = lane % CR;
-  const int32_t* idx = !PAGED && a.idx ? a.idx + (int64_t)w.u * a.k : nullptr;
-  const int64_t unit = (PAGED ? 0 : b * a.ksb) + h * a.ksh + x * 16;
-  const uint8_t* kbase = static_cast<const uint8_t*>(a.K) + unit;
-  const uint8_t* vbase = static_cast<const uint8_t*>(a.V) + unit;
-  const int64_t srow = PAGED ? 0 : (int64_t)w.u * a.n * SR;
+  const int32_t* idx = a.idx ? a.idx + (int64_t)w.u * a.k : nullptr;
+  const uint8_t* kbase = static_cast<const uint8_t*>(a.K) + b * a.ksb + h * a.ksh + x * 16;
+  const uint8_t* vbase = static_cast<const uint8_t*>(a.V) + b * a.ksb + h * a.ksh + x * 16;
+  const int64_t srow = (int64_t)w.u * a.n * SR;
   // Row q of the warp's half is row 64 warp + q of the tile; -1 past the last.
-  auto look_up = [&](int t, int* row, int* page) {
+  auto look_up = [&](int t, int* row) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const int j = (PAGED ? w.t0 * TM : w.k0) + t * TM + 64 * warp + lane + 32 * k;
-      if (PAGED) {
-        const PagedRow r = j >= w.count ? PagedRow{-1, 0} : paged_row(a, w.b, j);
-        row[k] = r.flat;
-        page[k] = r.page;
-      } else {
-        row[k] = j >= w.k1 ? -1 : idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j;
-      }
+      const int j = w.k0 + t * TM + 64 * warp + lane + 32 * k;
+      row[k] = j >= w.k1 ? -1 : idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j;
     }
   };
-  int slot = PAGED ? gone.raw % C::DEPTH : 0, n = PAGED ? gone.raw / C::DEPTH : 0;
+  int slot = 0, n = 0;
   bool ok = true;
   const uint32_t first = (uint32_t)((64 * warp + lane / CR) * CR) * 16;  // this lane's first row in a slot
-  auto bring = [&](int t, const int* row, const int* page, bool v) {
-    if (ok && (PAGED || n > 0)) ok = warp_wait(bar(s.raw_empty[slot]), (n + 1) & 1, s, a);
+  auto bring = [&](int t, const int* row, bool v) {
+    if (ok && n > 0) ok = warp_wait(bar(s.raw_empty[slot]), (n - 1) & 1, s, a);
     if (ok) {
       const uint32_t dst = raw + slot * C::SLOT;
       const uint8_t* base = v ? vbase : kbase;
       const uint8_t* sc = (v ? a.Vs : a.Ks) + srow;
       const bool full = w.k0 + (t + 1) * TM <= w.k1;
-      if (!PAGED && !idx && full) {
+      if (!idx && full) {
         const uint8_t* p = base + (w.k0 + t * TM + 64 * warp + lane / CR) * a.kss;
 #pragma unroll
         for (int i = 0; i < NI; ++i, p += RP * a.kss)
@@ -596,15 +587,14 @@ __device__ void load_codes(const PrefixArgs& a, const Item& w, const Gone& gone,
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
           const int at = __shfl_sync(0xffffffffu, row[RP * i / 32], (RP * i + lane / CR) % 32);
-          int64_t from = max(at, 0) * a.kss;
-          if (PAGED) from += __shfl_sync(0xffffffffu, page[RP * i / 32], (RP * i + lane / CR) % 32) * a.kx;
-          cp_async16_zfill(dst + first + RP * CR * 16 * i + C::place(x, lane / CR + RP * i) * 16, base + from, at >= 0);
+          cp_async16_zfill(dst + first + RP * CR * 16 * i + C::place(x, lane / CR + RP * i) * 16,
+                           base + max(at, 0) * a.kss, at >= 0);
         }
       }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const uint32_t at = dst + TM * C::ROWB + (uint32_t)(64 * warp + lane + 32 * k) * 4;
-        const uint8_t* p = sc + (PAGED ? paged_scale(a, {max(row[k], 0), page[k]}, w.h) : max(row[k], 0)) * SR;
+        const uint8_t* p = sc + (int64_t)max(row[k], 0) * SR;
         if (SR == 4) cp_async4(at, p, row[k] < 0 ? 0 : 4);  // rows past the last: scale 2^-127 of zeros
         else sts_u32(at, row[k] < 0 ? 0u : __ldg(reinterpret_cast<const uint16_t*>(p)));
       }
@@ -613,21 +603,98 @@ __device__ void load_codes(const PrefixArgs& a, const Item& w, const Gone& gone,
     cp_async_arrive_noinc(bar(s.raw_full[slot]));
     if (++slot == C::DEPTH) { slot = 0; ++n; }
   };
-  int row[2], ahead[2], page[2], page_ahead[2], tile = -1;
+  int row[2], ahead[2], tile = -1;
   bool kind = false;
   in_order(w.T, w.wide ? 1 : 2, [&](int t, bool v) {
-    if (PAGED && w.draft(t)) return;
-    look_up(t, ahead, page_ahead);
-    if (tile >= 0) bring(tile, row, page, kind);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      row[k] = ahead[k];
-      page[k] = page_ahead[k];
-    }
+    look_up(t, ahead);
+    if (tile >= 0) bring(tile, row, kind);
+    row[0] = ahead[0];
+    row[1] = ahead[1];
     kind = v;
     tile = t;
   });
-  if (tile >= 0) bring(tile, row, page, kind);
+  if (tile >= 0) bring(tile, row, kind);
+  cp_async_wait_all();
+}
+
+// The same of wf_tree_attn's cached tiles, and the same slots.  Where a warp's 64 rows lie
+// in one page they are found by adding strides; else a lane looks up two of them and the lanes
+// pass their offsets on.  (With a row's offset formed at every chunk the loaders were the
+// slowest of all: a tile of 8-bit codes took 2.2 us whatever else it was spared.)
+template <int D, int FMT>
+__device__ void load_paged_codes(const PrefixArgs& a, const Item& w, const Gone& gone, uint32_t raw, Bars& s, int warp,
+                                 int lane) {
+  typedef Cfg<D, FMT> C;
+  constexpr int CR = C::CR, RP = 32 / CR, NI = 64 / RP, SR = D / kMxBlock;
+  const int x = lane % CR, mine = lane / CR, b = w.b, count = w.count, T = min(w.T, w.cached - w.t0);
+  const int j0 = w.t0 * TM + 64 * warp;
+  const uint8_t* kbase = static_cast<const uint8_t*>(a.K) + w.h * a.ksh + x * 16;
+  const uint8_t* vbase = static_cast<const uint8_t*>(a.V) + w.h * a.ksh + x * 16;
+  const int64_t head = (int64_t)w.h * a.by_ps.d;  // rows of scales before the head's
+  const bool in_page = a.by_ps.d % 64 == 0;
+  const int64_t kss = a.kss;
+  int slot = gone.raw % C::DEPTH, n = gone.raw / C::DEPTH;
+  bool ok = true;
+  auto bring = [&](int t, const int* entry, bool v) {
+    if (ok) ok = warp_wait(bar(s.raw_empty[slot]), (n + 1) & 1, s, a);
+    if (ok) {
+      const uint32_t dst = raw + slot * C::SLOT, to = dst + (uint32_t)((64 * warp + mine) * CR) * 16;
+      const uint8_t* base = v ? vbase : kbase;
+      const int j = j0 + t * TM, left = count - j;  // rows of the warp that count
+      PagedRow row[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) row[k] = paged_row(a, entry[k], j + (lane + 32 * k < left ? lane + 32 * k : 0));
+      if (in_page && left >= 64) {
+        const int in = fastdiv((uint32_t)j, a.by_ps) * a.by_ps.d;
+        const uint8_t* p = base + row[0].page * a.ksb + (j - in + mine) * kss;
+#pragma unroll
+        for (int i = 0; i < NI; ++i, p += RP * kss) cp_async16(to + RP * CR * 16 * i + C::place(x, mine + RP * i) * 16, p);
+      } else {
+        int lo[2], hi[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int64_t o = lane + 32 * k < left ? paged_offset(a, row[k]) : 0;
+          lo[k] = (int)(uint32_t)o;
+          hi[k] = (int)(o >> 32);
+        }
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          const int from = (RP * i + mine) % 32, k = RP * i / 32;
+          const int64_t o =
+              (int64_t)__shfl_sync(0xffffffffu, hi[k], from) << 32 | (uint32_t)__shfl_sync(0xffffffffu, lo[k], from);
+          cp_async16_zfill(to + RP * CR * 16 * i + C::place(x, mine + RP * i) * 16, base + o, RP * i + mine < left);
+        }
+      }
+      const uint8_t* sc = v ? a.Vs : a.Ks;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t at = dst + TM * C::ROWB + (uint32_t)(64 * warp + lane + 32 * k) * 4;
+        const bool have = lane + 32 * k < left;
+        const uint8_t* p = sc + (have ? row[k].flat + (int64_t)row[k].page * (a.H - 1) * a.by_ps.d + head : 0) * SR;
+        if (SR == 4) cp_async4(at, p, have ? 4 : 0);  // rows past the last: scale 2^-127 of zeros
+        else sts_u32(at, have ? __ldg(reinterpret_cast<const uint16_t*>(p)) : 0u);
+      }
+    }
+    if (SR == 2) mbar_arrive(bar(s.raw_full[slot]));  // releases the plain stores
+    cp_async_arrive_noinc(bar(s.raw_full[slot]));
+    if (++slot == C::DEPTH) { slot = 0; ++n; }
+  };
+  int entry[2] = {0, 0}, ahead[2], tile = -1;
+  bool kind = false;
+  in_order(w.T, w.wide ? 1 : 2, [&](int t, bool v) {
+    if (t >= T) return;  // drafted
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int j = j0 + t * TM + lane + 32 * k;
+      ahead[k] = j < count ? page_entry(a, b, j) : 0;
+    }
+    if (tile >= 0) bring(tile, entry, kind);
+    entry[0] = ahead[0];
+    entry[1] = ahead[1];
+    kind = v;
+    tile = t;
+  });
+  if (tile >= 0) bring(tile, entry, kind);
   cp_async_wait_all();
 }
 
@@ -1045,7 +1112,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1)
       produce<D, FMT, PAGED>(a, maps, w, gone, ring, smem_u32(raw), s, tid - 512);
     } else {
       if (warp < MMA_WARP + 2) multiply<D, FMT, PAGED>(a, w, gone, smem_u32(sm), ring, s, warp - MMA_WARP);
-      else if (PAGED || !w.own) load_codes<D, FMT, PAGED>(a, w, gone, smem_u32(raw), s, warp - MMA_WARP - 2, tid & 31);
+      else if (PAGED) load_paged_codes<D, FMT>(a, w, gone, smem_u32(raw), s, warp - MMA_WARP - 2, tid & 31);
+      else if (!w.own) load_codes<D, FMT>(a, w, smem_u32(raw), s, warp - MMA_WARP - 2, tid & 31);
     }
   };
   if (!PAGED) {

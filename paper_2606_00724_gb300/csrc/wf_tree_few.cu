@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(NTH, kFewCtas / kPrefixSms) few_kernel(const _
   constexpr int EB = C::CODES ? 1 : 2;  // bytes of a stride's unit
   int t = 0, t_end = 0;
   bool more = true;
-  PagedRow at = {0, 0};
+  int entry = 0, row_in = 0;  // what this lane looked up
   const uint8_t *K = nullptr, *V = nullptr;
   const int64_t kss = a.kss * EB, kx = a.kx * EB;
   auto enter = [&] {
@@ -128,14 +128,15 @@ __global__ void __launch_bounds__(NTH, kFewCtas / kPrefixSms) few_kernel(const _
     V = static_cast<const uint8_t*>(a.V) + in.item * a.ksh * EB + lane % C::CPR * 16;
   };
   auto look_up = [&] {
-    const int j = t * kFewKeys + warp * SK + (in_page ? 0 : lane % SK);
-    at = more && j < in.count ? paged_row(a, in.b, j) : PagedRow{0, 0};
+    row_in = t * kFewKeys + warp * SK + (in_page ? 0 : lane % SK);
+    entry = more && row_in < in.count ? page_entry(a, in.b, row_in) : 0;
   };
   uint32_t odd = 0;  // D = 64: whether the scales that this lane copied are the second half of their word
   auto bring = [&](uint32_t slot) {
     if (more) {
       const int left = in.count - (t * kFewKeys + warp * SK);
       const bool full = left >= SK;
+      const PagedRow at = row_in < in.count ? paged_row(a, entry, row_in) : PagedRow{0, 0};
       const int64_t first = at.flat * kss + at.page * kx;  // bytes to the step's first row, where that finds them all
 #pragma unroll
       for (int n = 0; n < SK / C::RPI; ++n) {
