@@ -48,16 +48,6 @@ __device__ __forceinline__ At row_at(const MxArgs& a, uint32_t r) {
   return w;
 }
 
-// Bits of the largest magnitude of a thread's channels, as an fp32 number (a NaN
-// wins over every number).
-__device__ __forceinline__ uint32_t top_bits(const float*, const uint4& v) {
-  return max(max(v.x & 0x7fffffffu, v.y & 0x7fffffffu), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu));
-}
-__device__ __forceinline__ uint32_t top_bits(const bf16*, const uint4& v) {
-  const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
-  return max(m & 0xffff0000u, m << 16);
-}
-
 // A thread's values from its codes and their scale byte, stored: bf16 by exact
 // products of pairs, fp32 by way of half precision.
 template <bool FP4>

@@ -44,6 +44,16 @@ __device__ __forceinline__ uint32_t mx_encode2(float a, float b) {
   if (FP4) return __nv_cvt_float2_to_fp4x2(make_float2(a, b), __NV_E2M1, cudaRoundNearest);
   return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
+// Bits of the largest magnitude of a thread's channels, as an fp32 number (a NaN
+// wins over every number).
+__device__ __forceinline__ uint32_t top_bits(const float*, const uint4& v) {
+  return max(max(v.x & 0x7fffffffu, v.y & 0x7fffffffu), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu));
+}
+__device__ __forceinline__ uint32_t top_bits(const bf16*, const uint4& v) {
+  const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+  return max(m & 0xffff0000u, m << 16);
+}
+
 template <int BYTES> struct Word;
 template <> struct Word<8> { typedef uint2 type; };
 template <> struct Word<4> { typedef uint32_t type; };

@@ -12,6 +12,7 @@
 // row, not to a head, so a thread keeps its chunk's cosines and sines and takes
 // the same chunk of several heads, UN of them loaded before the first is used.
 #include <algorithm>
+#include <type_traits>
 
 #include "wf_mx.cuh"
 #include "wf_rows.cuh"
@@ -43,10 +44,27 @@ __device__ __forceinline__ void turned(unsigned long long t, float& c, float& s)
   if (q & 2) { c = -c; s = -s; }
 }
 
+// max(|a|, |b|, |c|), NaN if one of them is.
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+  float r;
+  asm("{\n\t.reg .f32 x, y, z;\n\t"
+      "abs.f32 x, %1;\n\tabs.f32 y, %2;\n\tabs.f32 z, %3;\n\t"
+      "max.NaN.f32 %0, x, y, z;\n\t}"
+      : "=f"(r)
+      : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// The first head of tensor 1 in the line of both tensors' heads g, g + groups, ..
+__device__ __forceinline__ int second_head(uint32_t g, const RowsArgs& a) {
+  const int in = a.heads[0] - (int)g;  // line places from g to tensor 1
+  return in <= 0 ? -in : (in + a.groups - 1) / a.groups * a.groups - in;
+}
+
 enum Kept { kRows, kFp8, kFp4 };
 
 template <typename T, int KEPT, int D, int UN>
-__global__ void __launch_bounds__(NTH) rows_kernel(const __grid_constant__ RowsArgs a) {
+__global__ void __launch_bounds__(NTH, 3) rows_kernel(const __grid_constant__ RowsArgs a) {
   constexpr int N = Vec<T>::N;       // channels a thread
   constexpr int TPR = D / N;         // threads a row
   constexpr int RPC = NTH / TPR;     // rows a CTA
@@ -54,10 +72,11 @@ __global__ void __launch_bounds__(NTH) rows_kernel(const __grid_constant__ RowsA
   typedef typename Word<FP4 ? N / 2 : N>::type W;
   const T* const type = nullptr;
   const int t = threadIdx.x % TPR;
-  const uint32_t item = blockIdx.x * RPC + threadIdx.x / TPR;
-  bool ok = item < a.total * a.groups;
-  const uint32_t at = ok ? item : 0;
-  const uint32_t r = fastdiv(at, a.by_groups), g = at - r * a.groups;
+  // The CTA's heads, the same for all of its rows, so that its warps stay together.
+  const uint32_t block = fastdiv(blockIdx.x, a.by_groups), g = blockIdx.x - block * a.groups;
+  const uint32_t mine = block * RPC + threadIdx.x / TPR;
+  bool ok = mine < a.total;
+  const uint32_t r = ok ? mine : 0;
   const uint32_t b = fastdiv(r, a.by_m), i = r - b * a.by_m.d;
   sm100::grid_dep_wait();
   const int row = a.rows_at ? min(max(__ldg(a.rows_at + r), 0), a.rows - 1) : (int)i;
@@ -96,61 +115,103 @@ __global__ void __launch_bounds__(NTH) rows_kernel(const __grid_constant__ RowsA
     }
   }
 
-  const int heads = a.heads[0] + a.heads[1];
+  if (!__any_sync(0xffffffffu, ok)) {  // rows past a count are not read either
+    sm100::grid_dep_launch();
+    return;
+  }
+  // The thread's heads, of both tensors in one line: g, g + groups, ..  Addresses go from one to
+  // the next by a stride; formed anew they were half of the instructions.
 #pragma unroll 1
-  for (int k = 0; k < a.each; k += UN) {
-    uint4 v[UN];
-#pragma unroll
-    for (int x = 0; x < UN; ++x) {
-      const int hh = min((int)g + a.groups * (k + x), heads - 1), w = hh >= a.heads[0], h = w ? hh - a.heads[0] : hh;
-      v[x] = *(reinterpret_cast<const uint4*>(static_cast<const T*>(a.src[w]) + b * a.ssb[w] + h * a.ssh[w] +
-                                              row * a.sss[w]) + t);
+  for (int w = 0; w < 2; ++w) {
+    const int heads = a.heads[w], h0 = w ? second_head(g, a) : (int)g;
+    if (h0 >= heads) continue;
+    const bool turn = a.plan && (!w || a.both);
+    const int64_t sstep = a.ssh[w] * a.groups, dstep = a.dsh[w] * a.groups;
+    const T* src = static_cast<const T*>(a.src[w]) + b * a.ssb[w] + h0 * a.ssh[w] + row * a.sss[w] + t * N;
+    typedef typename std::conditional<KEPT == kRows, T, char>::type Out;
+    Out* dst = static_cast<Out*>(a.dst[w]) + to * a.dsb[w] + h0 * a.dsh[w] + in * a.dss[w] + t * (KEPT == kRows ? N : (int)sizeof(W));
+    uint8_t* scale = nullptr;
+    int64_t zstep = 0;
+    if (KEPT != kRows) {
+      zstep = (int64_t)a.by_ps.d * (D / kMxBlock) * a.groups;
+      scale = a.scales[w] + ((to * heads + h0) * (int64_t)a.by_ps.d + in) * (D / kMxBlock) + t / (kMxBlock / N);
     }
+    // The next UN rows are on their way while UN are worked on.
+    uint4 v[UN], next[UN];
+    auto load = [&](int h) {
 #pragma unroll
-    for (int x = 0; x < UN; ++x) {
-      const int hh = (int)g + a.groups * (k + x), w = hh >= a.heads[0], h = w ? hh - a.heads[0] : hh;
-      const bool put = ok && hh < heads && k + x < a.each, turn = a.plan && (!w || a.both);
-      float y[N];
-      widen_vec(type, v[x], y);
-      if (!a.adjacent && __any_sync(0xffffffffu, turn)) {  // the rows of a warp may be of both tensors
-        uint4 u;
-        u.x = __shfl_sync(0xffffffffu, v[x].x, partner, TPR);
-        u.y = __shfl_sync(0xffffffffu, v[x].y, partner, TPR);
-        u.z = __shfl_sync(0xffffffffu, v[x].z, partner, TPR);
-        u.w = __shfl_sync(0xffffffffu, v[x].w, partner, TPR);
-        float z[N];
-        widen_vec(type, u, z);
-        if (turn && turns) {
-#pragma unroll
-          for (int e = 0; e < N; ++e) y[e] = fmaf(y[e], c[e], z[e] * s[e]);
-        }
-      } else if (turn && turns) {
-#pragma unroll
-        for (int e = 0; e < N / 2; ++e) {
-          const float p = y[2 * e], q = y[2 * e + 1];
-          y[2 * e] = fmaf(p, c[e], -q * s[e]);
-          y[2 * e + 1] = fmaf(q, c[e], p * s[e]);
-        }
+      for (int x = 0; x < UN; ++x) {
+        next[x] = make_uint4(0, 0, 0, 0);
+        if (h + x * a.groups < heads) next[x] = *reinterpret_cast<const uint4*>(src + x * sstep);
       }
-      if (KEPT == kRows) {
-        if (put) st_vec(static_cast<T*>(a.dst[w]) + to * a.dsb[w] + h * a.dsh[w] + in * a.dss[w] + t * N, y);
-      } else {
-        constexpr int TPB = kMxBlock / N;  // threads a block
-        uint32_t top = 0;
+      src += UN * sstep;
+    };
+    load(h0);
+#pragma unroll 1
+    for (int h = h0; h < heads; h += UN * a.groups) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) top = max(top, __float_as_uint(y[e]) & 0x7fffffffu);
+      for (int x = 0; x < UN; ++x) v[x] = next[x];
+      load(h + UN * a.groups);
 #pragma unroll
-        for (int d = 1; d < TPB; d *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-        const uint32_t byte = mx_scale_byte<FP4>(top);
-        const float inv = byte == 255 ? 0.f : mx_inv_scale(byte);
+      for (int x = 0; x < UN; ++x) {
+        const bool put = ok && h + x * a.groups < heads;
+        float y[N];
+        widen_vec(type, v[x], y);
+        if (!a.adjacent && turn) {
+          uint4 u;
+          u.x = __shfl_sync(0xffffffffu, v[x].x, partner, TPR);
+          u.y = __shfl_sync(0xffffffffu, v[x].y, partner, TPR);
+          u.z = __shfl_sync(0xffffffffu, v[x].z, partner, TPR);
+          u.w = __shfl_sync(0xffffffffu, v[x].w, partner, TPR);
+          float z[N];
+          widen_vec(type, u, z);
+          if (turns) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) y[e] = byte == 255 ? 0.f : y[e] * inv;
-        if (put) {
-          reinterpret_cast<W*>(static_cast<char*>(a.dst[w]) + to * a.dsb[w] + h * a.dsh[w] + in * a.dss[w])[t] =
-              pack_codes<FP4, N>(y);
-          if (t % TPB == 0)
-            a.scales[w][(((to * a.heads[w]) + h) * a.by_ps.d + in) * (D / kMxBlock) + t / TPB] = (uint8_t)byte;
+            for (int e = 0; e < N; ++e) y[e] = fmaf(y[e], c[e], z[e] * s[e]);
+          }
+        } else if (turn && turns) {
+#pragma unroll
+          for (int e = 0; e < N / 2; ++e) {
+            const float p = y[2 * e], q = y[2 * e + 1];
+            y[2 * e] = fmaf(p, c[e], -q * s[e]);
+            y[2 * e + 1] = fmaf(q, c[e], p * s[e]);
+          }
         }
+        if constexpr (KEPT == kRows) {
+          if (put) st_vec(dst, y);
+        } else {
+          constexpr int TPB = kMxBlock / N;  // threads a block
+          uint32_t top;
+          if (turn) {
+            float y0 = 0.f;
+#pragma unroll
+            for (int e = 0; e < N; e += 2) y0 = max_abs(y0, y[e], y[e + 1]);
+            top = __float_as_uint(y0) & 0x7fffffffu;
+          } else {
+            top = top_bits(type, v[x]);
+          }
+#pragma unroll
+          for (int d = 1; d < TPB; d *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+          const uint32_t byte = mx_scale_byte<FP4>(top);
+          const float inv = byte == 255 ? 0.f : mx_inv_scale(byte);
+          const sm100::f32x2 inv2 = sm100::pk2(inv, inv);
+#pragma unroll
+          for (int e = 0; e < N; e += 2) {
+            const float2 p = sm100::up2(sm100::mul2(sm100::pk2(y[e], y[e + 1]), inv2));
+            y[e] = p.x;
+            y[e + 1] = p.y;
+          }
+          if (byte == 255) {  // nothing finite to keep
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] = 0.f;
+          }
+          if (put) {
+            *reinterpret_cast<W*>(dst) = pack_codes<FP4, N>(y);
+            if (t % TPB == 0) *scale = (uint8_t)byte;
+          }
+          scale += zstep;
+        }
+        dst += dstep;
       }
     }
   }
@@ -167,7 +228,7 @@ cudaError_t launch_rows(RowsArgs& a, cudaStream_t s) {
   a.each = (int)((heads + groups - 1) / groups);
   a.groups = (heads + a.each - 1) / a.each;
   a.by_groups = make_fastdiv((uint32_t)a.groups);
-  const dim3 grid((unsigned)(((int64_t)a.total * a.groups + RPC - 1) / RPC));
+  const dim3 grid((unsigned)(((int64_t)a.total + RPC - 1) / RPC * a.groups));
   Launch l(grid, NTH, 0, s);
   return a.each >= 4 ? l(rows_kernel<T, KEPT, D, 4>, a) : l(rows_kernel<T, KEPT, D, 1>, a);
 }
