@@ -64,7 +64,7 @@ __device__ __forceinline__ int second_head(uint32_t g, const RowsArgs& a) {
 enum Kept { kRows, kFp8, kFp4 };
 
 template <typename T, int KEPT, int D, int UN>
-__global__ void __launch_bounds__(NTH, 3) rows_kernel(const __grid_constant__ RowsArgs a) {
+__global__ void __launch_bounds__(NTH, KEPT == kRows ? 3 : 4) rows_kernel(const __grid_constant__ RowsArgs a) {
   constexpr int N = Vec<T>::N;       // channels a thread
   constexpr int TPR = D / N;         // threads a row
   constexpr int RPC = NTH / TPR;     // rows a CTA
@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(NTH, 3) rows_kernel(const __grid_constant__ Ro
     int64_t zstep = 0;
     if (KEPT != kRows) {
       zstep = (int64_t)a.by_ps.d * (D / kMxBlock) * a.groups;
-      scale = a.scales[w] + ((to * heads + h0) * (int64_t)a.by_ps.d + in) * (D / kMxBlock) + t / (kMxBlock / N);
+      scale = a.scales[w] + ((to * heads + h0) * (int64_t)a.by_ps.d + in) * (D / kMxBlock);
     }
     // The next UN rows are on their way while UN are worked on.
     uint4 v[UN], next[UN];
@@ -205,9 +205,15 @@ __global__ void __launch_bounds__(NTH, 3) rows_kernel(const __grid_constant__ Ro
 #pragma unroll
             for (int e = 0; e < N; ++e) y[e] = 0.f;
           }
+          uint32_t bytes = byte << 8 * (t / TPB);
+#pragma unroll
+          for (int d = TPB; d < TPR; d *= 2) bytes |= __shfl_xor_sync(0xffffffffu, bytes, d);
           if (put) {
             *reinterpret_cast<W*>(dst) = pack_codes<FP4, N>(y);
-            if (t % TPB == 0) *scale = (uint8_t)byte;
+            if (t == 0) {  // the row's scales in one store
+              if (D == 128) *reinterpret_cast<uint32_t*>(scale) = bytes;
+              else *reinterpret_cast<uint16_t*>(scale) = (uint16_t)bytes;
+            }
           }
           scale += zstep;
         }
@@ -230,7 +236,10 @@ cudaError_t launch_rows(RowsArgs& a, cudaStream_t s) {
   a.by_groups = make_fastdiv((uint32_t)a.groups);
   const dim3 grid((unsigned)(((int64_t)a.total + RPC - 1) / RPC * a.groups));
   Launch l(grid, NTH, 0, s);
-  return a.each >= 4 ? l(rows_kernel<T, KEPT, D, 4>, a) : l(rows_kernel<T, KEPT, D, 1>, a);
+  // Codes are bound by instructions as well, and gain more from a fourth CTA an SM than from
+  // four rows in flight (two prompts of 8K, 32 heads: 88 against 92 us).
+  constexpr int UN = KEPT == kRows ? 4 : 2;
+  return a.each >= UN ? l(rows_kernel<T, KEPT, D, UN>, a) : l(rows_kernel<T, KEPT, D, 1>, a);
 }
 
 template <typename T, int D>
