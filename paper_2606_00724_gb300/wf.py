@@ -115,19 +115,38 @@ def _check(status: int, what: str):
         raise WfError(status, what)
 
 
-def desc(t: torch.Tensor) -> wf_tensor:
-    """wf_tensor for a [B, H, rows, d] tensor with a contiguous last axis."""
-    shape = t.shape
+# Descriptors by what they describe (never by an address): building one takes longer
+# than finding it.  No call writes to a descriptor.
+_DESCS: dict = {}
+
+
+def _desc(shape, stride, dtype, fmt=None) -> wf_tensor:
+    key = (shape, stride, dtype, fmt)
+    d = _DESCS.get(key)
+    if d is None:
+        d = _row_desc(shape, stride, dtype) if fmt is None else _code_desc(shape, stride, dtype.itemsize, fmt)
+        if len(_DESCS) >= 4096:
+            _DESCS.clear()
+        _DESCS[key] = d
+    return d
+
+
+def _row_desc(shape, stride, dtype) -> wf_tensor:
     if len(shape) != 4:
         raise ValueError("expected a [B, H, rows, d] tensor")
-    code = _DTYPES.get(t.dtype)
+    code = _DTYPES.get(dtype)
     if code is None:
-        raise ValueError(f"unsupported dtype {t.dtype}")
-    sb, sh, ss, sd = t.stride()
+        raise ValueError(f"unsupported dtype {dtype}")
+    sb, sh, ss, sd = stride
     B, H, S, D = shape
     if D > 1 and sd != 1:
         raise ValueError("head_dim axis must be contiguous")
     return wf_tensor(B, H, S, D, sb, sh, ss, code)
+
+
+def desc(t: torch.Tensor) -> wf_tensor:
+    """wf_tensor for a [B, H, rows, d] tensor with a contiguous last axis."""
+    return _row_desc(t.shape, t.stride(), t.dtype)
 
 
 def _code_desc(shape, stride, size: int, fmt: int) -> wf_tensor:
@@ -176,7 +195,7 @@ def _pair_desc(K, V, what: str, fmt=None) -> wf_tensor:
     shape, stride, dtype = K.shape, K.stride(), K.dtype
     if V is not None and (V.stride() != stride or V.shape != shape or V.dtype != dtype):
         raise ValueError(f"{what} must share dtype, shape and strides")
-    return desc(K) if fmt is None else _code_desc(shape, stride, dtype.itemsize, fmt)
+    return _desc(shape, stride, dtype, fmt)
 
 
 def _ptr(t):
@@ -187,7 +206,7 @@ def _ints(t):
     """Address of a contiguous int32 tensor, or None."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or not t.is_contiguous():
+    if t.dtype is not torch.int32 or not t.is_contiguous():
         raise ValueError("indices and lengths must be contiguous int32 tensors")
     return t.data_ptr()
 
@@ -447,31 +466,49 @@ def wf_rotary_plan(freq: torch.Tensor, axis: torch.Tensor | None = None) -> torc
 
 
 def _plan(plan):
-    """Pairs of a plan on the GPU (0 where there is none)."""
+    """Address and pairs of a plan on the GPU (None and 0 where there is none)."""
     if plan is None:
-        return 0
-    if plan.dtype != torch.int64 or plan.dim() != 2 or plan.shape[1] != 2 or not plan.is_contiguous():
+        return None, 0
+    shape = plan.shape
+    if len(shape) != 2 or shape[1] != 2 or plan.dtype != torch.int64 or not plan.is_contiguous():
         raise ValueError("expected a plan of wf_rotary_plan")
-    return plan.shape[0]
+    return plan.data_ptr(), shape[0]
+
+
+def _positions(pos, batch: int, rows: int):
+    """Address and axes of positions [axes, B, rows] (None and 0 where there are none)."""
+    if pos is None:
+        return None, 0
+    shape = pos.shape
+    if len(shape) != 3 or shape[1] != batch or shape[2] != rows:
+        raise ValueError("positions must be [axes, B, rows]")
+    return _ints(pos), shape[0]
 
 
 def wf_rotary_apply(Q, K, plan, pos, Qout, Kout, adjacent: bool = False, stream=None) -> None:
     """Q [B, Hq, rows, d] and K [B, Hk, rows, d] (None: Q alone) rotated by pos
     [axes, B, rows] into Qout and Kout, which may be Q and K (see the C header)."""
     _on_gpu(Q, K, plan, pos, Qout, Kout)
-    dq, do = desc(Q), desc(Qout)
-    dk, dl = (desc(K), desc(Kout)) if K is not None and Kout is not None else (None, None)
-    if pos.dim() != 3 or tuple(pos.shape[1:]) != (dq.batch, dq.seq):
-        raise ValueError("positions must be [axes, B, rows]")
-    _check(lib().wf_rotary_apply(_ptr(Q), dq, _ptr(K), dk, _ptr(plan), _plan(plan), int(adjacent), _ints(pos),
-                                 pos.shape[0], _ptr(Qout), do, _ptr(Kout), dl, _stream(stream)), "wf_rotary_apply")
+    shape, dtype = Q.shape, Q.dtype
+    dq, do = _desc(shape, Q.stride(), dtype), _desc(Qout.shape, Qout.stride(), Qout.dtype)
+    dk = dl = k = l = None
+    if K is not None and Kout is not None:
+        dk, dl = _desc(K.shape, K.stride(), K.dtype), _desc(Kout.shape, Kout.stride(), Kout.dtype)
+        k, l = K.data_ptr(), Kout.data_ptr()
+    elif K is not Kout:
+        raise ValueError("keys and their outputs are given together")
+    at, pairs = _plan(plan)
+    where, axes = _positions(pos, shape[0], shape[2])
+    _check(lib().wf_rotary_apply(Q.data_ptr(), dq, k, dk, at, pairs, adjacent, where, axes, Qout.data_ptr(), do, l, dl,
+                                 _stream(stream)), "wf_rotary_apply")
 
 
-def _table(pages, batch: int) -> int:
-    """Entries a sequence of a page table [B, entries]."""
-    if pages.dim() != 2 or pages.shape[0] != batch:
+def _table(pages, batch: int):
+    """Address and entries a sequence of a page table [B, entries]."""
+    shape = pages.shape
+    if len(shape) != 2 or shape[0] != batch:
         raise ValueError("a page table has a row a sequence")
-    return pages.shape[1]
+    return _ints(pages), shape[1]
 
 
 def wf_paged_append(Knew, Vnew, K, V, pages, start, Ks=None, Vs=None, fmt=None, rows=None, count=None, plan=None,
@@ -483,19 +520,21 @@ def wf_paged_append(Knew, Vnew, K, V, pages, start, Ks=None, Vs=None, fmt=None, 
     [axes, B, rows], or by their place."""
     _on_gpu(Knew, Vnew, K, V, pages, start, Ks, Vs, rows, count, plan, pos)
     dn, dk = _pair_desc(Knew, Vnew, "Knew and Vnew"), _pair_desc(K, V, "K and V", fmt)
-    B, m = dn.batch, dn.seq
+    B, n = dn.batch, dn.seq
+    m = n
     if rows is not None:
         if rows.dim() != 2 or rows.shape[0] != B:
             raise ValueError("rows must be [B, m]")
         m = rows.shape[1]
     if start.numel() != B or (count is not None and count.numel() != B):
         raise ValueError("start and count must have an entry a sequence")
-    if pos is not None and (pos.dim() != 3 or tuple(pos.shape[1:]) != (B, dn.seq)):
-        raise ValueError("positions must be [axes, B, rows]")
-    _check(lib().wf_paged_append(_ptr(Knew), _ptr(Vnew), dn, _ints(rows), m, _ints(start), _ints(count), _ptr(plan),
-                                 _plan(plan), int(adjacent), _ints(pos), 0 if pos is None else pos.shape[0], _ptr(K),
-                                 _ptr(V), _ptr(Ks), _ptr(Vs), dk, _scales(Ks, Vs), _ints(pages), _table(pages, B),
-                                 _stream(stream)), "wf_paged_append")
+    at, pairs = _plan(plan)
+    where, axes = _positions(pos, B, n)
+    table, entries = _table(pages, B)
+    _check(lib().wf_paged_append(Knew.data_ptr(), _ptr(Vnew), dn, _ints(rows), m, _ints(start), _ints(count), at, pairs,
+                                 adjacent, where, axes, K.data_ptr(), _ptr(V), _ptr(Ks), _ptr(Vs), dk,
+                                 0 if Ks is None else _scales(Ks, Vs), table, entries, _stream(stream)),
+           "wf_paged_append")
 
 
 def wf_tree_attn_workspace_bytes(Q: torch.Tensor, K: torch.Tensor, n: int, n_t: int, fmt=None) -> int:
@@ -510,22 +549,24 @@ def wf_tree_attn(Q, K, V, pages, n: int, Kt, Vt, O, ws, cache_len=None, tree_len
     tree_len [B] of them, that mask [B, q, words] lets each query row see (see the C
     header).  fmt: K and V are codes, with scales Ks and Vs."""
     _on_gpu(Q, K, V, pages, Kt, Vt, O, ws, cache_len, tree_len, mask, Ks, Vs)
-    dq = desc(Q)
-    do = dq if O.stride() == Q.stride() and O.shape == Q.shape and O.dtype == Q.dtype else desc(O)
+    dq, do = _desc(Q.shape, Q.stride(), Q.dtype), _desc(O.shape, O.stride(), O.dtype)
     dk = _pair_desc(K, V, "K and V", fmt)
-    dt = _pair_desc(Kt, Vt, "Kt and Vt") if Kt is not None else None
+    dt, n_t = None, 0
+    if Kt is not None:
+        dt = _pair_desc(Kt, Vt, "Kt and Vt")
+        n_t = dt.seq
+    B = dq.batch
     if fmt is not None:
         if Ks is None or Vs is None or _scales(Ks, Vs) < dk.batch * dk.heads * dk.seq * (dk.head_dim // 32):
             raise ValueError("a quantised cache needs the scales of its K and V")
-    for t in (cache_len, tree_len):
-        if t is not None and t.numel() != dq.batch:
-            raise ValueError("lengths must have an entry a sequence")
-    if mask is not None and tuple(mask.shape) != (dq.batch, dq.seq, ((dt.seq if dt else 0) + 31) // 32):
+    if (cache_len is not None and cache_len.numel() != B) or (tree_len is not None and tree_len.numel() != B):
+        raise ValueError("lengths must have an entry a sequence")
+    if mask is not None and tuple(mask.shape) != (B, dq.seq, (n_t + 31) // 32):
         raise ValueError("the mask must be [B, q, words of 32 drafted rows]")
-    _check(lib().wf_tree_attn(_ptr(Q), dq, _ptr(K), _ptr(V), dk, _ptr(Ks), _ptr(Vs), _ints(pages),
-                              _table(pages, dq.batch), n, _ints(cache_len), _ptr(Kt), _ptr(Vt), dt, _ints(tree_len),
-                              _ints(mask), _ptr(O), do, float(scale), _ptr(ws), ws.nbytes, _stream(stream)),
-           "wf_tree_attn")
+    table, entries = _table(pages, B)
+    _check(lib().wf_tree_attn(Q.data_ptr(), dq, K.data_ptr(), V.data_ptr(), dk, _ptr(Ks), _ptr(Vs), table, entries, n,
+                              _ints(cache_len), _ptr(Kt), _ptr(Vt), dt, _ints(tree_len), _ints(mask), O.data_ptr(), do,
+                              scale, ws.data_ptr(), ws.nbytes, _stream(stream)), "wf_tree_attn")
 
 
 def wf_workspace_status(ws: torch.Tensor, stream=None):
