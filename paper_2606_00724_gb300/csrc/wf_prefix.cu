@@ -512,14 +512,14 @@ PrefixPlan plan_tree(const wf_tensor& q, const wf_tensor& kv, int k, int n_t) {
   PrefixArgs& a = p.a;
   a.S = a.So = a.direct = a.whole = 0;
   p.few = a.Ro <= kFewRows;
-  a.tk = p.few ? kFewKeys : kPrefixTcRows / 2;
+  a.tk = p.few ? few_keys(p.fmt) : kPrefixTcRows / 2;
   a.pad = p.few ? kFewPad : kTreePad;
   a.mt = (a.Ro + kPrefixTcRows - 1) / kPrefixTcRows;
   // Row tiles of equal height, whole warps of them.
   a.tr = a.mt == 1 ? a.Ro : ((a.Ro + a.mt - 1) / a.mt + 31) / 32 * 32;
   const int64_t U = (int64_t)a.B * a.H, items = U * a.mt;
   const int64_t tiles = std::max<int64_t>(1, ((int64_t)k + a.tk - 1) / a.tk + ((int64_t)n_t + a.tk - 1) / a.tk);
-  a.C = (int)std::min<int64_t>(p.few ? kFewCtas : kPrefixSms, items * tiles);
+  a.C = (int)std::min<int64_t>(kPrefixSms * (p.few ? few_per_sm(a.d) : 1), items * tiles);
   p.join = tiles > 1;
   const size_t slots = (size_t)(a.C + items) * a.tr;
   p.off_info = 256;
@@ -528,9 +528,10 @@ PrefixPlan plan_tree(const wf_tensor& q, const wf_tensor& kv, int k, int n_t) {
   p.used = p.off_o + sizeof(float) * slots * a.d;
   // The size is the most that a call with as many rows and keys, or fewer of any, can take:
   // tr is R at most, or, with several row tiles, 256, and R + 32 mt in all.
-  const int64_t reserved = kFewCtas * (int64_t)std::min(a.Ro, kFewRows) +
+  const int64_t most = kPrefixSms * few_per_sm(a.d);
+  const int64_t reserved = most * std::min(a.Ro, kFewRows) +
                            kPrefixSms * (int64_t)std::min(a.Ro, kPrefixTcRows) + U * (a.Ro + (a.mt > 1 ? 32 * (int64_t)a.mt : 0));
-  const size_t heads = align_up(p.off_info + (size_t)items * (sizeof(int2) + sizeof(int)) + kFewCtas * sizeof(int), 256);
+  const size_t heads = align_up(p.off_info + (size_t)items * (sizeof(int2) + sizeof(int)) + (size_t)most * sizeof(int), 256);
   p.total = align_up(heads + sizeof(float2) * (size_t)reserved, 256) + sizeof(float) * (size_t)reserved * a.d;
   return p;
 }

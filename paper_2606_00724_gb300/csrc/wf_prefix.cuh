@@ -105,7 +105,13 @@ cudaError_t launch_tree_join(const PrefixPlan& p, cudaStream_t s);
 // Query rows of a unit that the kernel for few of them takes, keys of its tiles, and
 // its CTAs.
 constexpr int kFewPad = 1, kTreePad = 4;  // see Spread
-constexpr int kFewRows = 16, kFewKeys = 64, kFewCtas = 3 * kPrefixSms;
+constexpr int kFewRows = 16;
+// Keys of its tiles: four warps' steps, of 16 rows, or of 32 rows of codes, whose
+// bytes are fewer while a step's set-up is the same.
+constexpr int few_keys(int fmt) { return fmt == WF_BF16 ? 64 : 128; }
+// Its CTAs an SM: at head_dim 128 two, whose threads have the registers (three spilled: one token of 32
+// sequences of 8K 195 against 186 us), at 64 three (109 against 117).
+constexpr int few_per_sm(int d) { return d == 128 ? 2 : 3; }
 
 // Sequence, query head and block row of row r of the unit of prompt p (or of
 // sequence b) and key head h.

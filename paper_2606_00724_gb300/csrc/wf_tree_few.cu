@@ -26,9 +26,8 @@ namespace {
 using namespace sm100;
 
 constexpr int NTH = 128, NW = NTH / 32;
-constexpr int SK = kFewKeys / NW;  // keys a step
 constexpr float kLazy = 8.f;
-static_assert(SK == 16 && kFewRows == 16, "one m16n8k16 operand each");
+static_assert(kFewRows == 16, "one m16n8k16 operand");
 
 __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -66,7 +65,8 @@ struct Few {
   __device__ static int v_place(int r, int ch) {
     return r * ROWB + (CPR >= 8 ? ch ^ (r >> 1 & 3) * 2 : CPR == 4 ? ch ^ (r >> 1 & 3) : ch) * 16;
   }
-  static constexpr int STEP = 2 * SK * ROWB + (CODES ? 128 : 0);
+  static constexpr int TK = few_keys(FMT), SK = TK / NW;  // keys a tile, a step of a warp: one or two times 16
+  static constexpr int STEP = 2 * SK * ROWB + (CODES ? 8 * SK : 0);
   static constexpr int QD = 16896 / STEP > 8 ? 8 : 16896 / STEP;
   static constexpr int PO = D + 4;
   static constexpr size_t QUEUE = (size_t)NW * QD * STEP, SMEM = QUEUE + 16 * (PO + 2) * sizeof(float);
@@ -95,8 +95,9 @@ __device__ __forceinline__ void pairs_of(const uint32_t* w, uint32_t byte, uint3
 }
 
 template <int D, int FMT>
-__global__ void __launch_bounds__(NTH, kFewCtas / kPrefixSms) few_kernel(const __grid_constant__ PrefixArgs a) {
+__global__ void __launch_bounds__(NTH, few_per_sm(D)) few_kernel(const __grid_constant__ PrefixArgs a) {
   typedef Few<D, FMT> C;
+  constexpr int SK = C::SK, TK = C::TK;
   extern __shared__ __align__(128) uint8_t sm[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
   const uint32_t queue = smem_u32(sm) + warp * C::QD * C::STEP;
@@ -128,13 +129,13 @@ __global__ void __launch_bounds__(NTH, kFewCtas / kPrefixSms) few_kernel(const _
     V = static_cast<const uint8_t*>(a.V) + in.item * a.ksh * EB + lane % C::CPR * 16;
   };
   auto look_up = [&] {
-    row_in = t * kFewKeys + warp * SK + (in_page ? 0 : lane % SK);
+    row_in = t * TK + warp * SK + (in_page ? 0 : lane % SK);
     entry = more && row_in < in.count ? page_entry(a, in.b, row_in) : 0;
   };
   uint32_t odd = 0;  // D = 64: whether the scales that this lane copied are the second half of their word
   auto bring = [&](uint32_t slot) {
     if (more) {
-      const int left = in.count - (t * kFewKeys + warp * SK);
+      const int left = in.count - (t * TK + warp * SK);
       const bool full = left >= SK;
       const PagedRow at = row_in < in.count ? paged_row(a, entry, row_in) : PagedRow{0, 0};
       const int64_t first = at.flat * kss + at.page * kx;  // bytes to the step's first row, where that finds them all
@@ -152,23 +153,22 @@ __global__ void __launch_bounds__(NTH, kFewCtas / kPrefixSms) few_kernel(const _
         cp_async16_zfill(slot + C::k_place(r, lane % C::CPR), K + o, ok);
         cp_async16_zfill(slot + SK * C::ROWB + C::v_place(r, lane % C::CPR), V + o, ok);
       }
-      if constexpr (C::CODES) {  // lanes 0 to 15: scales of K's rows, 16 to 31: of V's
-        const int r = lane & 15;
+      if constexpr (C::CODES) {  // a lane copies the scales of row lane of K and of V
         PagedRow w = at;
-        if (in_page) w.flat += r;
-        else w = {__shfl_sync(0xffffffffu, at.flat, r), __shfl_sync(0xffffffffu, at.page, r)};
-        const int64_t s = r < left ? paged_scale(a, w, in.item) : 0;
-        const uint8_t* p = (lane < 16 ? a.Ks : a.Vs) + s * SR;
+        if (in_page) w.flat += lane;
+        const bool ok = lane < left;
+        const int64_t z = ok ? paged_scale(a, w, in.item) : 0;
         const uint32_t to = slot + 2 * SK * C::ROWB + lane * 4;
-        if (D == 128) {
-          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(p), "r"(r < left ? 4 : 0) : "memory");
-        } else {  // the smallest copy is 4 bytes on 4; the word's other half is another row's, or nobody's
-          const bool second = s & 1;
-          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(p - (second ? 2 : 0)),
-                       "r"(r < left ? (second ? 4 : 2) : 0)
-                       : "memory");
-          odd = odd << 1 | (uint32_t)second;
+        // The smallest copy is 4 bytes on 4; at D = 64 the word's other half is another row's, or
+        // nobody's.
+        const bool second = D == 64 && (z & 1);
+        const int size = !ok ? 0 : D == 128 || second ? 4 : 2;
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const uint8_t* p = (v ? a.Vs : a.Ks) + z * SR - (second ? 2 : 0);
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 128 * v), "l"(p), "r"(size) : "memory");
         }
+        if (D == 64) odd = odd << 1 | (uint32_t)second;
       }
       if (++t == t_end) enter();
       look_up();
@@ -211,25 +211,28 @@ __global__ void __launch_bounds__(NTH, kFewCtas / kPrefixSms) few_kernel(const _
     for (int tile = now.t0; tile < now.t1; ++tile) {
       const uint32_t slot = queue + stage * C::STEP;
       const bool draft = tile >= now.cached;
-      const int first = (draft ? tile - now.cached : tile) * kFewKeys + warp * SK;
-      const int left = (draft ? now.drafts : now.count) - first;
+      const int first0 = (draft ? tile - now.cached : tile) * TK + warp * SK;
       if (!draft) {
         cp_async_wait<C::QD - 1>();
         if constexpr (C::CODES) {
-          if (D == 64) {  // every lane puts the scales that it copied in the word's first half
+          if (D == 64 && (odd >> (C::QD - 1) & 1)) {  // every lane puts the scales that it copied in the word's first half
             const uint32_t w = slot + 2 * SK * C::ROWB + lane * 4;
-            if (odd >> (C::QD - 1) & 1) sts_u32(w, lds_u32(w) >> 16);
+            sts_u32(w, lds_u32(w) >> 16);
+            sts_u32(w + 128, lds_u32(w + 128) >> 16);
           }
         }
         __syncwarp();  // every lane's copies are there
       }
       const int64_t own = now.b * a.gsb + now.item * a.gsh;  // drafted rows come straight from memory
-      if (left > 0) {
+#pragma unroll 1
+      for (int part = 0; part < SK / 16; ++part) {  // 16 keys at a time
+        const int first = first0 + 16 * part, left = (draft ? now.drafts : now.count) - first;
+        if (left <= 0) break;
         float s[2][4];
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
           s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
-          const uint32_t scale = C::CODES && !draft ? lds_u32(slot + 2 * SK * C::ROWB + (8 * n + g) * 4) : 0;
+          const uint32_t scale = C::CODES && !draft ? lds_u32(slot + 2 * SK * C::ROWB + (16 * part + 8 * n + g) * 4) : 0;
           uint32_t k[D / 8];
           if (draft) {
             const bf16* p = static_cast<const bf16*>(a.Kg) + own + (int64_t)(first + min(8 * n + g, left - 1)) * a.gss;
@@ -244,14 +247,14 @@ __global__ void __launch_bounds__(NTH, kFewCtas / kPrefixSms) few_kernel(const _
           for (int j = 0; j < C::KN; ++j) {
             uint32_t w[C::KB / 4];
             const int at = (4 * j + c) * C::KB;
-            fetch<C::KB>(w, slot + C::k_place(8 * n + g, at / 16) + at % 16);
+            fetch<C::KB>(w, slot + 16 * part * C::ROWB + C::k_place(8 * n + g, at / 16) + at % 16);
             pairs_of<D, FMT, C::KB>(w, scale >> 8 * ((4 * j + c) * C::KE / kMxBlock) & 0xffu, k + j * C::KE / 2);
           }
           }
 #pragma unroll
           for (int i = 0; i < D / 16; ++i) mma16816(s[n], q[i], k[2 * i], k[2 * i + 1]);
         }
-        if (left < SK) {
+        if (left < 16) {
 #pragma unroll
           for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -322,9 +325,9 @@ __global__ void __launch_bounds__(NTH, kFewCtas / kPrefixSms) few_kernel(const _
             }
             uint32_t w[C::VB / 4], byte = 0;
             const int at = (8 * j + g) * C::VB;
-            fetch<C::VB>(w, slot + SK * C::ROWB + C::v_place(r, at / 16) + at % 16);
+            fetch<C::VB>(w, slot + (SK + 16 * part) * C::ROWB + C::v_place(r, at / 16) + at % 16);
             if (C::CODES)
-              byte = lds_u32(slot + 2 * SK * C::ROWB + (16 + r) * 4) >> 8 * ((8 * j + g) * C::VE / kMxBlock) & 0xffu;
+              byte = lds_u32(slot + 2 * SK * C::ROWB + (32 + 16 * part + r) * 4) >> 8 * ((8 * j + g) * C::VE / kMxBlock) & 0xffu;
             pairs_of<D, FMT, C::VB>(w, byte, v[n]);
           }
 #pragma unroll
