@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(NTH, few_per_sm(D)) few_kernel(const __grid_co
   Walk in;  // the range of the next step to be copied
   if (!in.start(a)) return;
   Walk now = in;  // the range at work
-  const bool in_page = a.by_ps.d % SK == 0;
+  const bool in_page = a.by_ps.d % 16 == 0;  // 16 rows of a step are in one page
   const int SR = D / kMxBlock;
 
   // The next step: its place is looked up a step before it is copied, since a table's
@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(NTH, few_per_sm(D)) few_kernel(const __grid_co
     V = static_cast<const uint8_t*>(a.V) + in.item * a.ksh * EB + lane % C::CPR * 16;
   };
   auto look_up = [&] {
-    row_in = t * TK + warp * SK + (in_page ? 0 : lane % SK);
+    row_in = t * TK + warp * SK + (in_page ? lane & (SK - 16) : lane % SK);
     entry = more && row_in < in.count ? page_entry(a, in.b, row_in) : 0;
   };
   uint32_t odd = 0;  // D = 64: whether the scales that this lane copied are the second half of their word
@@ -138,24 +138,40 @@ __global__ void __launch_bounds__(NTH, few_per_sm(D)) few_kernel(const __grid_co
       const int left = in.count - (t * TK + warp * SK);
       const bool full = left >= SK;
       const PagedRow at = row_in < in.count ? paged_row(a, entry, row_in) : PagedRow{0, 0};
-      const int64_t first = at.flat * kss + at.page * kx;  // bytes to the step's first row, where that finds them all
+      const int64_t first = at.flat * kss + at.page * kx;  // bytes to the first of its 16 rows, where that finds them all
+      auto half = [&](int n) { return SK == 16 ? first : __shfl_sync(0xffffffffu, first, 16 * n); };
+      if (in_page && full) {
 #pragma unroll
-      for (int n = 0; n < SK / C::RPI; ++n) {
-        const int r = C::RPI * n + lane / C::CPR;
-        const bool ok = full || r < left;
-        int64_t o;
-        if (in_page) {
-          o = ok ? first + r * kss : 0;
-        } else {
-          const PagedRow w = {__shfl_sync(0xffffffffu, at.flat, r), __shfl_sync(0xffffffffu, at.page, r)};
-          o = w.flat * kss + w.page * kx;
+        for (int n = 0; n < SK / 16; ++n) {
+          const int64_t o = half(n) + lane / C::CPR * kss;
+          const uint8_t *k = K + o, *v = V + o;
+#pragma unroll
+          for (int x = 0; x < 16 / C::RPI; ++x, k += C::RPI * kss, v += C::RPI * kss) {
+            const int r = 16 * n + C::RPI * x + lane / C::CPR;
+            cp_async16(slot + C::k_place(r, lane % C::CPR), k);
+            cp_async16(slot + SK * C::ROWB + C::v_place(r, lane % C::CPR), v);
+          }
         }
-        cp_async16_zfill(slot + C::k_place(r, lane % C::CPR), K + o, ok);
-        cp_async16_zfill(slot + SK * C::ROWB + C::v_place(r, lane % C::CPR), V + o, ok);
+      } else {
+#pragma unroll
+        for (int n = 0; n < SK / C::RPI; ++n) {
+          const int r = C::RPI * n + lane / C::CPR;
+          const bool ok = r < left;
+          int64_t o;
+          if (in_page) {
+            o = half(C::RPI * n / 16);
+            o = ok ? o + r % 16 * kss : 0;
+          } else {
+            const PagedRow w = {__shfl_sync(0xffffffffu, at.flat, r), __shfl_sync(0xffffffffu, at.page, r)};
+            o = w.flat * kss + w.page * kx;
+          }
+          cp_async16_zfill(slot + C::k_place(r, lane % C::CPR), K + o, ok);
+          cp_async16_zfill(slot + SK * C::ROWB + C::v_place(r, lane % C::CPR), V + o, ok);
+        }
       }
       if constexpr (C::CODES) {  // a lane copies the scales of row lane of K and of V
         PagedRow w = at;
-        if (in_page) w.flat += lane;
+        if (in_page) w.flat += lane % 16;
         const bool ok = lane < left;
         const int64_t z = ok ? paged_scale(a, w, in.item) : 0;
         const uint32_t to = slot + 2 * SK * C::ROWB + lane * 4;
