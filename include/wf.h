@@ -530,7 +530,8 @@ wf_status wf_prefix_attn(const void* Q, const wf_tensor* q, const void* K, const
  * drafted row does not touch the query rows that do not see it, whatever it
  * holds.
  *
- * Errors: as elsewhere; WF_ERR_INVALID_ARG for n outside [0, table ps].
+ * Errors: as elsewhere; WF_ERR_INVALID_ARG for n outside [0, table ps];
+ * WF_ERR_UNSUPPORTED for B H ceil(G q / 256) (n + n_t + 1024) of 2^37 and more.
  * ------------------------------------------------------------------------- */
 wf_status wf_rotary_plan(const double* freq, const int32_t* axis, int pairs, int64_t* plan);
 wf_status wf_rotary_apply(const void* Q, const wf_tensor* q, const void* K, const wf_tensor* k, const int64_t* plan,

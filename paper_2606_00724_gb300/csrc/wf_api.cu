@@ -706,6 +706,9 @@ wf_status check_tree(const wf_tensor* q, const wf_tensor* pool, int n, int n_t, 
   if (n < 0 || n_t < 0) return WF_ERR_INVALID_ARG;
   if (too_many_rows((int64_t)q->batch * q->heads, q->seq) || too_many_rows(1, n) || too_many_rows(1, n_t))
     return WF_ERR_UNSUPPORTED;
+  // All key tiles, and empty places between them, lie in one line of less than 2^31 (see wf::Walk).
+  const int64_t group = q->heads / pool->heads, tiles = (group * q->seq + 255) / 256;
+  if ((int64_t)q->batch * pool->heads * tiles * ((int64_t)n + n_t + 1024) >= (int64_t)1 << 37) return WF_ERR_UNSUPPORTED;
   *cache = *pool;
   cache->batch = q->batch;
   cache->seq = n;

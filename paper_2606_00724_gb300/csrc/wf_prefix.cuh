@@ -55,7 +55,7 @@ struct PrefixArgs {
   const uint32_t* mask;
   int mw;                // words a row
   // bf16 queries over pages: the key tiles (tk keys each) that the sequences really have
-  // are spread over C CTAs evenly (see Spread), a unit's rows in mt tiles of tr.  A
+  // are spread over C CTAs evenly (see Walk), a unit's rows in mt tiles of tr.  A
   // part is a slot of tr rows; info says where an item's are and how many, flags
   // which of them left drafted values out that are not finite.
   int C, tk, tr, pad;
@@ -104,7 +104,7 @@ cudaError_t launch_tree_few(const PrefixPlan& p, cudaStream_t s);
 cudaError_t launch_tree_join(const PrefixPlan& p, cudaStream_t s);
 // Query rows of a unit that the kernel for few of them takes, keys of its tiles, and
 // its CTAs.
-constexpr int kFewPad = 1, kTreePad = 4;  // see Spread
+constexpr int kFewPad = 1, kTreePad = 4;  // see Walk
 constexpr int kFewRows = 16;
 // Keys of its tiles: four warps' steps, of 16 rows, or of 32 rows of codes, whose
 // bytes are fewer while a step's set-up is the same.
@@ -167,49 +167,9 @@ __device__ __forceinline__ int64_t paged_scale(const PrefixArgs& a, const PagedR
 // warp finds its place in the line from them.  A range is a part, and its slot is
 // c + item: along the line either grows by one from range to range, so no two
 // ranges share a slot and those of an item follow each other.
-struct Spread {
-  int64_t total, per;
-  // The places of an item of sequence b.
-  __device__ __forceinline__ static int tiles_of(const PrefixArgs& a, int b) {
-    return b < a.B ? a.pad + max(1, (prompt_count(a, b) + a.tk - 1) / a.tk + (own_count(a, b) + a.tk - 1) / a.tk) : 0;
-  }
-  // By a whole warp.
-  __device__ __forceinline__ void measure(const PrefixArgs& a) {
-    int64_t t = 0;
-    for (int b = threadIdx.x & 31; b < a.B; b += 32) t += tiles_of(a, b);
-#pragma unroll
-    for (int w = 1; w < 32; w *= 2) t += __shfl_xor_sync(0xffffffffu, t, w);
-    total = t * a.H * a.mt;
-    per = total < 0x7fffffff ? (int64_t)(((uint32_t)total + a.C - 1) / (uint32_t)a.C) : (total + a.C - 1) / a.C;
-  }
-  // The sequence whose items hold place x < total, and its first tile in the line; by a
-  // whole warp.
-  __device__ __forceinline__ int find(const PrefixArgs& a, int64_t x, int64_t* first) const {
-    const int lane = threadIdx.x & 31;
-    int64_t before = 0;
-    for (int b0 = 0;; b0 += 32) {
-      const int64_t mine = (int64_t)tiles_of(a, b0 + lane) * a.H * a.mt;
-      int64_t sum = mine;
-#pragma unroll
-      for (int w = 1; w < 32; w *= 2) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, sum, w);
-        if (lane >= w) sum += y;
-      }
-      const uint32_t past = __ballot_sync(0xffffffffu, x < before + sum);
-      if (past || b0 + 32 >= a.B) {
-        const int at = past ? __ffs(past) - 1 : 31;
-        *first = before + __shfl_sync(0xffffffffu, sum - mine, at);
-        return min(b0 + at, a.B - 1);
-      }
-      before += __shfl_sync(0xffffffffu, sum, 31);
-    }
-  }
-};
-
-// The ranges of one CTA, one after the other.
 struct Walk {
-  int64_t x, end, first;      // next place, end of the CTA's; first place of sequence b
-  int64_t per;
+  uint32_t per;               // places a CTA; all of them are below 2^31
+  uint32_t x, end, first;     // next place, end of the CTA's; first place of sequence b
   int b, count, drafts;       // sequence, its cached and drafted rows
   int cached, tiles;          // tiles of an item of b: cached ones, all
   int item, t0, t1;           // the range: item of b, tiles [t0, t1)
@@ -220,30 +180,55 @@ struct Walk {
     cached = (count + a.tk - 1) / a.tk;
     tiles = max(1, cached + (drafts + a.tk - 1) / a.tk);
   }
+  // The places of the items of sequence b.
+  __device__ __forceinline__ static uint32_t places_of(const PrefixArgs& a, int b) {
+    if (b >= a.B) return 0;
+    return (a.pad + max(1, (prompt_count(a, b) + a.tk - 1) / a.tk + (own_count(a, b) + a.tk - 1) / a.tk)) * a.H * a.mt;
+  }
   // By a whole warp; false if the CTA has nothing to do.
   __device__ __forceinline__ bool start(const PrefixArgs& a) {
-    Spread s;
-    s.measure(a);
-    per = s.per;
+    const int lane = threadIdx.x & 31;
+    const uint32_t here = places_of(a, lane);  // of the first 32 sequences, often all
+    uint32_t mine = here;
+    for (int s = lane + 32; s < a.B; s += 32) mine += places_of(a, s);
+    const uint32_t total = __reduce_add_sync(0xffffffffu, mine);
+    per = (total + a.C - 1) / a.C;
     x = blockIdx.x * per;
-    end = min(x + per, s.total);
+    end = min(x + per, total);
     if (x >= end) return false;
-    enter(a, s.find(a, x, &first));
-    return true;
+    first = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+      const uint32_t p = b0 ? places_of(a, b0 + lane) : here;
+      uint32_t sum = p;
+#pragma unroll
+      for (int w = 1; w < 32; w *= 2) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, sum, w);
+        if (lane >= w) sum += y;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, x < first + sum);
+      if (past) {
+        const int at = __ffs(past) - 1;
+        first += __shfl_sync(0xffffffffu, sum - p, at);
+        enter(a, b0 + at);
+        return true;
+      }
+      first += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    return false;
   }
   // To the next range; false behind the last.
   __device__ __forceinline__ bool next(const PrefixArgs& a) {
     for (;;) {
       if (x >= end) return false;
-      const int places = a.pad + tiles;
-      const int64_t in = x - first, all = (int64_t)places * a.H * a.mt;
+      const uint32_t places = a.pad + tiles, in = x - first, all = places * a.H * a.mt;
       if (in >= all) {
+        if (b + 1 >= a.B) return false;
         first += all;
         enter(a, b + 1);
         continue;
       }
-      item = in < 0x7fffffff ? (int)((uint32_t)in / (uint32_t)places) : (int)(in / places);
-      const int at = (int)(in - (int64_t)item * places), to = (int)min((int64_t)places, at + (end - x));
+      item = (int)(in / places);
+      const int at = (int)(in - item * places), to = (int)min(places, at + (end - x));
       x += to - at;
       t0 = max(0, at - a.pad);
       t1 = to - a.pad;
@@ -255,7 +240,7 @@ struct Walk {
   // The whole item: there are no other parts.
   __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == tiles; }
   // The parts of the item whose first one this is.
-  __device__ __forceinline__ int parts() const { return (int)((x - t1 + tiles - 1) / per) - (int)blockIdx.x + 1; }
+  __device__ __forceinline__ int parts() const { return (int)((x - t1 + tiles - 1) / per - blockIdx.x) + 1; }
 };
 
 // Whether one of a pair of bf16 is an infinity or a NaN; the pair with 0 there.  Drafted

@@ -10,7 +10,7 @@
 // channels in any order, so a lane's operands of K are 16 consecutive bytes of a row;
 // V's pairs of keys are put together by byte permutes.
 //
-// The CTAs share all the sequences' keys evenly (Spread), a range's four warps
+// The CTAs share all the sequences' keys evenly (Walk), a range's four warps
 // taking every fourth 16 keys of it; the ranges are joined where the drafted rows
 // are attended (own_join_kernel).  m is raised lazily, by more than 2^8, as in the
 // kernels for more rows; P is one bf16 term, l is summed before the rounding.

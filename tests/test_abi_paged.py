@@ -151,6 +151,8 @@ def test_tree_attn_rejects(lib):
     assert call(pool=_desc(40, 2, 16, 128, FP8), size=10 ** 9) == INVALID
     assert call(Ks=P(0x90000), Vs=P(0xa0000)) == INVALID
     assert call(q=_desc(1 << 15, 1 << 10, 64, 128, sb=0, sh=0), pool=_desc(1, 1, 64, 128)) == UNSUPPORTED
+    assert call(q=_desc(1 << 9, 4, 64, 128, sb=0, sh=0), o=_desc(1 << 9, 4, 64, 128, sb=0, sh=0), t=None, Kt=None,
+                Vt=None, pool=_desc(1, 2, 1 << 28, 128, sb=0, sh=0), n=1 << 28) == UNSUPPORTED   # too many tiles
     assert lib.wf_tree_attn_workspace_bytes(q, pool, -1, 0) == 0
     assert lib.wf_tree_attn_workspace_bytes(q, pool, 0, 0) >= 256
 
