@@ -439,3 +439,92 @@ def test_as_they_are_used_together():
         count = torch.tensor([len(t) for t in took], dtype=torch.int32, device="cuda")
         wf.wf_paged_append(Kt, Vt, K, V, pages, length, rows=rows.cuda(), count=count)
         length += count
+
+
+@pytest.mark.parametrize("fmt", ["mxfp8", "mxfp4"])
+@pytest.mark.parametrize("dtype,q", [("bf16", 1), ("bf16", 20), ("f32", 1)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_every_code_and_scale_is_read_exactly(d, dtype, q, fmt):
+    # One cached row a sequence: the weight is 1, so O is the value row, to the bit.  Page h holds other codes; the
+    # scale bytes go through 0 (2^-127) to 254.  What bf16 rounds below its smallest normal number is left out.
+    B = 255
+    codes = np.concatenate([np.arange(127), [0], np.arange(128, 255), [0]]).astype(np.uint8)
+    V = np.zeros((B, 1, 1, d if fmt == "mxfp8" else d // 2), np.uint8)
+    for h in range(B):
+        V[h, 0, 0] = np.roll(codes, 37 * h)[:d] if fmt == "mxfp8" else (np.arange(d // 2) * 7 + h) % 256
+    S = np.repeat(np.arange(B, dtype=np.uint8)[:, None, None, None], d // 32, axis=3)
+    want = torch.from_numpy(mx.values(V, S, fmt))[:, 0, 0]
+    K, one = np.zeros_like(V), np.full_like(S, 127)
+    Q = torch.ones(B, 1, q, d, dtype=DT[dtype], device="cuda")
+    K, V, one, S = (torch.from_numpy(x).cuda() for x in (K, V, one, S))
+    pages = torch.arange(B, dtype=torch.int32, device="cuda").view(B, 1)
+    O = torch.empty_like(Q)
+    ws = torch.zeros(wf.wf_tree_attn_workspace_bytes(Q, K, 1, 0, fmt=FMT[fmt]), dtype=torch.uint8, device="cuda")
+    wf.wf_tree_attn(Q, K, V, pages, 1, None, None, O, ws, Ks=one, Vs=S, fmt=FMT[fmt])
+    wf.wf_workspace_status(ws)
+    normal = (want == 0) | ((want.abs() >= 2.0 ** -126) & (want.abs() <= torch.finfo(DT[dtype]).max))
+    for i in (0, q - 1):
+        assert torch.equal(O[:, 0, i].double().cpu()[normal], want[normal])
+    assert normal.double().mean() > 0.9
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,H,G,q,n,ps,n_t", [
+    (70, 1, 1, 20, 150, 16, 20),      # more sequences than a warp has lanes
+    (70, 1, 1, 2, 150, 8, 2),
+    (3, 2, 1, 40, 1500, 100, 40),     # pages without common parts of 8 rows
+    (3, 1, 4, 2, 1500, 100, 2),
+    (2, 1, 4, 2, 700, 48, 300),       # long drafts
+    (2, 1, 2, 400, 260, 16, 150),     # several row tiles, of which the last is short
+])
+def test_walks_and_tiles(B, H, G, q, n, ps, n_t, dtype):
+    r = np.random.default_rng(21)
+    clen = [int(x) for x in r.integers(0, n + 1, B)]
+    tlen = [int(x) for x in r.integers(0, n_t + 1, B)]
+    Case(B, H, G, q, 128, n, ps, n_t, dtype, clen=clen, tlen=tlen, seed=22).check()
+
+
+@pytest.mark.parametrize("q", [1, 40])
+def test_masked_values_in_any_part_of_a_long_draft(q):
+    # Drafted rows that nothing sees but the last query row hold NaN, in tiles that different ranges have.
+    c = Case(1, 1, 2, q + 1, 128, 600, 16, 280, seed=23)
+    hidden = [3, 70, 129, 200, 279]
+    c.sees[:, :, hidden] = False
+    before = c.run()
+    for j in hidden:
+        c.Vt[0, 0, j, j % 128] = float("nan")
+        c.Vt[0, 0, j, (j + 1) % 128] = -float("inf")
+    assert torch.equal(c.run(), before)
+    c.sees[:, -1, hidden] = True
+    after = c.run()
+    assert torch.equal(after[:, :, :-1], before[:, :, :-1])
+    for j in hidden:
+        assert torch.isnan(after[0, :, -1, j % 128]).all()
+
+
+@pytest.mark.parametrize("q", [1, 24])
+def test_heads_that_share_their_rows(q):
+    # A pool whose key heads have a stride of 0: all of them are the same rows.
+    c = Case(2, 1, 3, q, 128, 300, 16, q, "bf16", seed=24)
+    want, A = c.check(), c.want(True)
+    c.K, c.V = (t.expand(-1, 3, -1, -1) for t in (c.K, c.V))
+    c.Kt, c.Vt = (t.expand(-1, 3, -1, -1) for t in (c.Kt, c.Vt))
+    assert c.K.stride(1) == 0
+    got = c.run()     # three query heads on three key heads
+    # Each is within its tolerance of the definition.
+    assert (np.abs(f64(got) - f64(want)) <= 2 * (2.0 ** -8 * np.abs(f64(want)) + (2.0 ** -8 + 2.0 ** -10) * A)).all()
+
+
+def test_smaller_calls_leave_the_rest_alone():
+    # Outputs inside a wider tensor, and rows of the workspace of a larger call.
+    c = Case(3, 2, 2, 5, 128, 400, 16, 5, seed=25)
+    want = c.run()
+    wide = torch.full((3, 4, 9, 256), 7.0, dtype=torch.bfloat16, device="cuda")
+    O, args = wide[:, :, 2:7, :128], c.args()
+    ws = torch.full((wf.wf_tree_attn_workspace_bytes(c.Q, c.K, 100000, 300) + 512,), 0x7f, dtype=torch.uint8, device="cuda")
+    ws[:4] = 0
+    wf.wf_tree_attn(c.Q, c.K, c.V, c.pages.cuda(), c.n, c.Kt, c.Vt, O, ws, **args)
+    assert torch.equal(O, want)
+    O.fill_(7.0)
+    assert (wide == 7.0).all()
+    assert (ws[-512:] == 0x7f).all()
