@@ -104,7 +104,7 @@ cudaError_t launch_tree_few(const PrefixPlan& p, cudaStream_t s);
 cudaError_t launch_tree_join(const PrefixPlan& p, cudaStream_t s);
 // Query rows of a unit that the kernel for few of them takes, keys of its tiles, and
 // its CTAs.
-constexpr int kFewPad = 1, kTreePad = 4;  // see Walk
+constexpr int kFewPad = 1, kTreePad = 6;  // see Walk
 constexpr int kFewRows = 16;
 // Keys of its tiles: four warps' steps, of 16 rows, or of 32 rows of codes, whose
 // bytes are fewer while a step's set-up is the same.

@@ -1015,12 +1015,14 @@ __device__ void soften(const PrefixArgs& a, const Item& w, const Gone& gone, uin
   }
   named_sync(1, 512);
   constexpr int LPR = D / 4, RPW = 32 / LPR;  // lanes a row, rows a warp
-  const int cc = lane % LPR;
+  const int cc = lane % LPR, nr = cut ? 0 : w.nr;
+  const bool wide = w.wide;
+  float* const out = PAGED ? a.part_o + w.slot * a.tr * D + 4 * cc : nullptr;
 #pragma unroll 4
-  for (int q = tid / LPR; q < w.nr && !cut; q += 16 * RPW) {
+  for (int q = tid / LPR; q < nr; q += 16 * RPW) {
     const float* row = buf + q * D + ((cc ^ (q & 7)) << 2);
     float4 y = *reinterpret_cast<const float4*>(row);
-    if (!w.wide) {
+    if (!wide) {
       const float4 z = *reinterpret_cast<const float4*>(row + TM * D);
       y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
     }
@@ -1029,8 +1031,7 @@ __device__ void soften(const PrefixArgs& a, const Item& w, const Gone& gone, uin
       *reinterpret_cast<uint2*>(static_cast<bf16*>(a.O) + at.b * a.osb + at.hq * a.osh + at.i * a.oss + 4 * cc) =
           make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
     } else {
-      const int64_t to = PAGED ? w.slot * a.tr + q : (int64_t)w.part * a.rows + s.row[q];
-      *reinterpret_cast<float4*>(a.part_o + to * D + 4 * cc) = y;
+      *reinterpret_cast<float4*>(PAGED ? out + q * D : a.part_o + ((int64_t)w.part * a.rows + s.row[q]) * D + 4 * cc) = y;
     }
   }
   const int row = rt + r;
