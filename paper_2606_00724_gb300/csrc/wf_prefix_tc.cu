@@ -460,7 +460,8 @@ __device__ void produce(const PrefixArgs& a, const M& maps, const Item& w, const
     const int group = tid / NG, gt = tid % NG;
     const int x = gt % PX + PX * (gt / 8 % (CR / PX)), rr = gt / PX % (8 / PX) + 8 / PX * (gt / (8 * CR / PX));
     const uint32_t chunk = (uint32_t)(rr * CR + C::place(x, rr)) * 16;
-    const uint32_t scale = TM * C::ROWB + rr * 4 + x * EL / kMxBlock;
+    // Of wf_tree_attn, two bytes of scales lie where they lie in a word of the pool.
+    const uint32_t scale = TM * C::ROWB + rr * 4 + x * EL / kMxBlock + (PAGED && D == 64 ? 2 * (rr & 1) : 0);
     // Ring position p from codes' position at; false if a wait gave up.
     auto widen = [&](int p, int at) {
       const int slot = at % C::DEPTH, st = ring.stage(p), n = ring.turn(p);
@@ -631,7 +632,10 @@ __device__ void load_paged_codes(const PrefixArgs& a, const Item& w, const Gone&
   const uint8_t* kbase = static_cast<const uint8_t*>(a.K) + w.h * a.ksh + x * 16;
   const uint8_t* vbase = static_cast<const uint8_t*>(a.V) + w.h * a.ksh + x * 16;
   const int64_t head = (int64_t)w.h * a.by_ps.d;  // rows of scales before the head's
-  const bool in_page = a.by_ps.d % 64 == 0;
+  // With two bytes a row, the smallest copy, 4 on 4, takes a word of which the row is the first or
+  // second half as it is in its tile, where pages are even.  (Loaded and stored by the lane they took a memory
+  // latency a tile: 64 query rows of 16 heads on 128K, d = 64, 277 us.)
+  const bool in_page = a.by_ps.d % 64 == 0, even = a.by_ps.d % 2 == 0;
   const int64_t kss = a.kss;
   int slot = gone.raw % C::DEPTH, n = gone.raw / C::DEPTH;
   bool ok = true;
@@ -670,9 +674,11 @@ __device__ void load_paged_codes(const PrefixArgs& a, const Item& w, const Gone&
       for (int k = 0; k < 2; ++k) {
         const uint32_t at = dst + TM * C::ROWB + (uint32_t)(64 * warp + lane + 32 * k) * 4;
         const bool have = lane + 32 * k < left;
-        const uint8_t* p = sc + (have ? row[k].flat + (int64_t)row[k].page * (a.H - 1) * a.by_ps.d + head : 0) * SR;
+        const uint8_t* p = sc + (have ? row[k].flat + (int64_t)row[k].page * (a.H - 1) * a.by_ps.d + head : lane & 1) * SR;
+        const int second = lane & 1;  // of a word's two rows
         if (SR == 4) cp_async4(at, p, have ? 4 : 0);  // rows past the last: scale 2^-127 of zeros
-        else sts_u32(at, have ? __ldg(reinterpret_cast<const uint16_t*>(p)) : 0u);
+        else if (even) cp_async4(at, p - 2 * second, have ? 2 + 2 * second : 0);
+        else sts_u32(at, have ? (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p)) << 16 * second : 0u);
       }
     }
     if (SR == 2) mbar_arrive(bar(s.raw_full[slot]));  // releases the plain stores
