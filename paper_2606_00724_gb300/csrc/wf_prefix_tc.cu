@@ -936,8 +936,8 @@ __device__ void soften(const PrefixArgs& a, const Item& w, const Gone& gone, uin
   float m = -FLT_MAX, l = 0.f;  // finite, so that logits of -inf add 0 and not 2^(-inf + inf)
   bool ok = true;
   if (active) {
-    // Whole cached tiles, and steps before this range.
-    const int T = w.T, full = PAGED ? min(T, w.count / TM - w.t0) : (w.k1 - w.k0) / TM, steps = PAGED ? gone.step(g) : 0;
+    // Cached rows from the range's first tile on, and steps before it.
+    const int T = w.T, cached = PAGED ? w.count - w.t0 * TM : 0, steps = PAGED ? gone.step(g) : 0;
     int i = 0;
 #pragma unroll 1
     for (int t = first; t < T; t += step, ++i) {
@@ -951,7 +951,8 @@ __device__ void soften(const PrefixArgs& a, const Item& w, const Gone& gone, uin
       ok = s.go[g][r >> 5];
       if (!ok) break;
       tc_fence_after();
-      if (t < full) {
+      const int nk = PAGED ? cached - t * TM : w.k1 - (w.k0 + t * TM);  // (cached) keys of the tile
+      if (nk >= TM) {
         soften_tile<D, false, false>(a, s, sc, oc, i > 0, TM, nullptr, g, half, r, pair, m, l);
       } else if (PAGED) {
         const bool draft = w.draft(t), mask = draft && a.mask;
@@ -966,7 +967,6 @@ __device__ void soften(const PrefixArgs& a, const Item& w, const Gone& gone, uin
         }
         soften_tile<D, true, true>(a, s, sc, oc, i > 0, 0, bits, g, half, r, pair, m, l);
       } else {
-        const int nk = w.k1 - (w.k0 + t * TM);  // keys of the tile
         soften_tile<D, true, false>(a, s, sc, oc, i > 0, nk - TM / 2 * half, nullptr, g, half, r, pair, m, l);
       }
       tmem_wait_st();
