@@ -1,4 +1,5 @@
-// Attention over shared prompts (wf_prefix_attn): what its kernels share.
+// Attention over shared prompts (wf_prefix_attn) and over pages (wf_tree_attn): what
+// their kernels share.
 #pragma once
 
 #include "wf_div.cuh"
@@ -104,7 +105,9 @@ cudaError_t launch_tree_few(const PrefixPlan& p, cudaStream_t s);
 cudaError_t launch_tree_join(const PrefixPlan& p, cudaStream_t s);
 // Query rows of a unit that the kernel for few of them takes, keys of its tiles, and
 // its CTAs.
-constexpr int kFewPad = 1, kTreePad = 6;  // see Walk
+// Empty places before an item (see Walk), in tiles of either kernel.  256 rows of 32 units on 32K: none 132 us,
+// two 127, four 125, six 124, eight 125.
+constexpr int kFewPad = 1, kTreePad = 6;
 constexpr int kFewRows = 16;
 // Keys of its tiles: four warps' steps, of 16 rows, or of 32 rows of codes, whose
 // bytes are fewer while a step's set-up is the same.

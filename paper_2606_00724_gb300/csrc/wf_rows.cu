@@ -10,7 +10,11 @@
 // Both move bytes: 16 of them a thread, so that a row is 8 to 32 lanes and a
 // rotated channel's partner comes from another lane.  The angles belong to the
 // row, not to a head, so a thread keeps its chunk's cosines and sines and takes
-// the same chunk of several heads, UN of them loaded before the first is used.
+// the same chunk of several heads, whose addresses differ by a stride, UN of them on
+// their way while UN are worked on.  Bound by HBM: 4 prompts of up to 8K and 32 heads into
+// bf16 pages 136 us from cold caches (5.9 TB/s), 25K rows of 32 heads rotated 75 (a plain
+// copy of their bytes takes 67); into codes by instructions as well (2 prompts of 8K
+// 89 us, 61 at the memory's rate).
 #include <algorithm>
 #include <type_traits>
 
