@@ -406,7 +406,9 @@ __device__ void produce(const PrefixArgs& a, const M& maps, const Item& w, const
         if (ok && w.draft(tile)) bring_draft<D, NPT>(a, w, s, dst, tile, kind, tid);
         else if (ok) copy_paged<D, NPT>(dst, kind ? V : K, row < 0 ? -1 : paged_offset(a, paged_row(a, entry, row)), tid);
         if (!a.box) {
-          cp_async_arrive_noinc(full);
+          // The copies' arrival orders the copies alone: what bring_draft stored in their places takes a plain one.
+          if (w.draft(tile)) mbar_arrive(full);
+          else cp_async_arrive_noinc(full);
         } else {
           cp_async_wait_all();
           fence_proxy_async();
@@ -1050,11 +1052,7 @@ __device__ void soften(const PrefixArgs& a, const Item& w, const Gone& gone, uin
   const int row = rt + r;
   if ((PAGED || !whole) && !cut && row < w.nr && !half && (w.wide || g == 0))
     a.part_ml[PAGED ? w.slot * a.tr + row : (int64_t)w.part * a.rows + s.row[row]] = make_float2(m, l);
-  if (PAGED && !cut && tid == 0) {
-    if (w.t0 == 0) a.info[s.walk.items(a)] = make_int2((int)w.slot, s.walk.parts());
-    a.flags[w.slot] = s.flag;
-    s.flag = 0;
-  }
+  if (PAGED && !cut && tid == 0 && w.t0 == 0) a.info[s.walk.items(a)] = make_int2((int)w.slot, s.walk.parts());
 }
 
 template <int D, int FMT, bool PAGED, typename M>
@@ -1139,6 +1137,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1)
       fence_proxy_async();  // the rows went out through stages that the copy engine writes next
       __syncthreads();  // the range is over: its stages, and what the roles share, are free
       if (tid == 0) {
+        if (!s.abort) a.flags[s.range.slot] = s.flag;  // behind the barrier, since the producers set it
+        s.flag = 0;
         s.gone.by(s.range, ns);
         s.more = !s.abort && s.walk.next(a);
         if (s.more) s.range = range_of(a, s.walk);
