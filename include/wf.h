@@ -528,7 +528,9 @@ wf_status wf_prefix_attn(const void* Q, const wf_tensor* q, const void* K, const
  * wf_prefix_attn's arithmetic, scale, workspace rules, limits and status word.  A
  * row that sees nothing gets O = 0.  Rows past a length are never read, and a
  * drafted row does not touch the query rows that do not see it, whatever it
- * holds.
+ * holds.  A value of V that is not finite leaves none finite in its channel of the
+ * query rows that see its row, however small the row's weight is (of a row whose
+ * logit is -inf it may, or may not), with a mask and without one.
  *
  * Errors: as elsewhere; WF_ERR_INVALID_ARG for n outside [0, table ps];
  * WF_ERR_UNSUPPORTED for B H ceil(G q / 256) (n + n_t + 1024) of 2^37 and more.

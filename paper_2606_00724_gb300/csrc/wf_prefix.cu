@@ -227,7 +227,10 @@ __global__ void __launch_bounds__(kThreads<TR>, TR == 128 ? 1 : 2) simt_kernel(c
             h2 = fmaf(sq[at<D>(ty * RT + i, c / 4) + c % 4], sk[at<D>(tx + 16 * j, c / 4) + c % 4], h2);
         }
         s[i][j] = tx + 16 * j < nk ? h2 : -INFINITY;
-        if (PAGED && own && a.mask && tx + 16 * j < nk && !sees(a, b, block_row, t0 + tx + 16 * j)) s[i][j] = -INFINITY;
+        if (PAGED && own && a.mask && tx + 16 * j < nk && !sees(a, b, block_row, t0 + tx + 16 * j)) {
+          s[i][j] = -INFINITY;
+          low[i][j] = -1.f;  // hidden: its weight is -0
+        }
         top = fmaxf(top, s[i][j]);
       }
 #pragma unroll
@@ -237,7 +240,8 @@ __global__ void __launch_bounds__(kThreads<TR>, TR == 128 ? 1 : 2) simt_kernel(c
       float sum = 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float p = s[i][j] == -INFINITY ? 0.f : exp2f(fmaf(low[i][j], a.sl2, fmaf(s[i][j], a.sl2, -mn)));
+        const float none = PAGED && low[i][j] < 0.f ? -0.f : 0.f;
+        const float p = s[i][j] == -INFINITY ? none : exp2f(fmaf(low[i][j], a.sl2, fmaf(s[i][j], a.sl2, -mn)));
         sum += p;
         sp[(ty * RT + i) * PP + tx + 16 * j] = p;
       }
@@ -268,8 +272,9 @@ __global__ void __launch_bounds__(kThreads<TR>, TR == 128 ? 1 : 2) simt_kernel(c
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
           const float pi = k == 0 ? p[i].x : k == 1 ? p[i].y : k == 2 ? p[i].z : p[i].w;
-          // A masked row of V may hold anything: 0 times it is not 0.
-          if (PAGED && own && pi == 0.f) continue;
+          // A hidden row of V may hold anything, and 0 times it is not 0; a weight that is 0 for its
+          // smallness (+0) is a seen row's, which counts.
+          if (PAGED && own && __float_as_uint(pi) == 0x80000000u) continue;
           const f32x2 pp = pk2(pi, pi);
 #pragma unroll
           for (int c = 0; c < C; ++c) {
