@@ -77,30 +77,21 @@ __global__ void __launch_bounds__(kThreads<TR>, TR == 128 ? 1 : 2) simt_kernel(c
   const int k0 = min(count, sp_i * per * TK), k1 = min(count, (sp_i + 1) * per * TK);
   const bool coded = CACHE != kPlain && !own;
   const int32_t* idx = a.idx && !own ? a.idx + (int64_t)u * a.k : nullptr;
-  // Elements, or bytes of codes, from row 0 to row j of the prompt, and its row of scales.
-  const int64_t cached = PAGED ? h * a.ksh : b * a.ksb + h * a.ksh;
-  auto row_of = [&](int j, int64_t* scales) {
-    if (PAGED) {
-      const PagedRow w = paged_row(a, page_entry(a, b, j), j);
-      *scales = paged_scale(a, w, h);
-      return paged_offset(a, w);
-    }
-    const int64_t row = idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j;
-    *scales = (int64_t)u * a.n + row;
-    return row * a.kss;
-  };
+  // Row j of a contiguous prompt; pages are looked up with it.
+  auto row_of = [&](int j) { return idx ? min(max(__ldg(idx + j), 0), a.n - 1) : j; };
+  auto place = [&](int j) { return paged_row(a, page_entry(a, b, j), j); };
 
   // Rows t0 .. of K or V as they are, by cp.async.
   auto copy = [&](bool v, int t0) {
     const float* base = static_cast<const float*>(v ? (own ? a.Vg : a.V) : (own ? a.Kg : a.K)) +
-                        (own ? b * a.gsb + h * a.gsh : cached);
+                        (PAGED && !own ? 0 : b * (own ? a.gsb : a.ksb)) + h * (own ? a.gsh : a.ksh);
+    const int64_t ss = own ? a.gss : a.kss;
     const uint32_t dst = smem_u32(v ? sv : sk);
 #pragma unroll 4
     for (int e = tid; e < TK * (D / 4); e += NTH) {
       const int r = e / (D / 4), c = e % (D / 4);
       const bool ok = t0 + r < k1;
-      int64_t scales;
-      const int64_t o = !ok ? 0 : own ? (t0 + r) * a.gss : row_of(t0 + r, &scales);
+      const int64_t o = !ok ? 0 : PAGED && !own ? paged_offset(a, place(t0 + r)) : row_of(t0 + r) * ss;
       cp_async16_zfill(dst + 4 * at<D>(r, c), base + o + 4 * c, ok);
     }
     cp_async_commit();
@@ -115,8 +106,17 @@ __global__ void __launch_bounds__(kThreads<TR>, TR == 128 ? 1 : 2) simt_kernel(c
       code[i] = make_uint4(0, 0, 0, 0);
       byte[i] = 0;
       if (r < TK && t0 + r < k1) {
-        int64_t scales;
-        const uint8_t* p = static_cast<const uint8_t*>(v ? a.V : a.K) + cached + row_of(t0 + r, &scales);
+        int64_t offset, scales;
+        if (PAGED) {
+          const PagedRow w = place(t0 + r);
+          offset = h * a.ksh + paged_offset(a, w);
+          scales = paged_scale(a, w, h);
+        } else {
+          const int64_t row = row_of(t0 + r);
+          offset = b * a.ksb + h * a.ksh + row * a.kss;
+          scales = (int64_t)u * a.n + row;
+        }
+        const uint8_t* p = static_cast<const uint8_t*>(v ? a.V : a.K) + offset;
         if (FP4) {
           const uint2 w = __ldg(reinterpret_cast<const uint2*>(p) + c);
           code[i].x = w.x;
