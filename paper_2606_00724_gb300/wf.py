@@ -552,6 +552,8 @@ def wf_tree_attn(Q, K, V, pages, n: int, Kt, Vt, O, ws, cache_len=None, tree_len
     dq, do = _desc(Q.shape, Q.stride(), Q.dtype), _desc(O.shape, O.stride(), O.dtype)
     dk = _pair_desc(K, V, "K and V", fmt)
     dt, n_t = None, 0
+    if (Kt is None) != (Vt is None):
+        raise ValueError("drafted keys and values are given together")
     if Kt is not None:
         dt = _pair_desc(Kt, Vt, "Kt and Vt")
         n_t = dt.seq
