@@ -58,6 +58,8 @@ class PagedCache:
 
     def append(self, K, V, counts: list[int], rows=None, rotated: bool = False) -> None:
         """The first counts[b] new rows of each sequence, or of the rows [B, m] of them."""
+        if len(counts) != K.shape[0] or min(counts) < 0 or max(counts) > (K.shape[2] if rows is None else rows.shape[1]):
+            raise ValueError("counts of rows that are not there")
         self._reserve(counts)
         count = torch.tensor(counts, dtype=torch.int32, device="cuda")
         wf.wf_paged_append(K, V, self.K, self.V, self.table, self.length, Ks=self.Ks, Vs=self.Vs, fmt=self.fmt, rows=rows,
