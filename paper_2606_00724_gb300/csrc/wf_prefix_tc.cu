@@ -773,10 +773,17 @@ __device__ void multiply(const PrefixArgs& a, const Item& w, const Gone& gone, u
   for (int j = first, i = 0; j < T && ok; j += A, ++i) {
     const bool more = j + A < T;
     const int pv_pos = base + (j < T - lead ? lead + 2 * j : T + j), pk_pos = pv_pos + 1;
-    arrived(pv_pos);
+    // A stage whose last turn has not arrived yet looks as if this one had (a parity tells two turns
+    // apart), so a position may be waited for when the one a ring before it is known to be there.  With one
+    // row tile a warp waits for its own positions alone, and knows the other's when the turn is its own: in the
+    // first two steps it waits for V behind that (K_0 may be behind K_1, with 4 stages in V_1's
+    // place); later steps know enough from the turns before.
+    const bool late = !wide && i < 2;
+    if (!late) arrived(pv_pos);
     if (more && wide) arrived(pk_pos);
     if (ok) ok = warp_wait(bar(s.pready[g]), (steps + i) & 1, s, a);
     if (ok && (g || i > 0)) ok = warp_wait(bar(s.turn[g]), (turns + (g ? i : i - 1)) & 1, s, a);
+    if (late) arrived(pv_pos);
     tc_fence_after();
     if (!ok) break;
     const int sv = ring.stage(pv_pos);
