@@ -732,12 +732,15 @@ __device__ __forceinline__ bool elect() {
   return r != 0;
 }
 
-template <int D, int FMT, bool PAGED>
+// FORM 0: one row tile, 1: two, 2: as w says.  Pages have a copy of the loop for each (64 rows of two sequences of 128K
+// in 8 bits 196 against 215 us, 182 rows at 16K 61.7 against 63.6); contiguous prompts share one, since short calls wait
+// for instructions (18.9 against 19.2 us for 24 rows of 16 heads of 64 on 8K).
+template <int D, int FMT, bool PAGED, int FORM>
 __device__ void multiply(const PrefixArgs& a, const Item& w, const Gone& gone, uint32_t sq, const Ring& ring, Bars& s,
                          int g) {
   typedef Cfg<D, FMT> C;
   const int T = w.T;
-  const bool wide = w.wide;
+  const bool wide = FORM == 2 ? w.wide : FORM == 1;
   if (T == 0) return;
   const uint32_t tm = __shfl_sync(0xffffffffu, s.tmem, 0);
   constexpr uint32_t qk = idesc_bf16(TM, TM, 0, 0), pv = idesc_bf16(TM, D, 0, 1);
@@ -775,10 +778,11 @@ __device__ void multiply(const PrefixArgs& a, const Item& w, const Gone& gone, u
     const int pv_pos = base + (j < T - lead ? lead + 2 * j : T + j), pk_pos = pv_pos + 1;
     // A stage whose last turn has not arrived yet looks as if this one had (a parity tells two turns
     // apart), so a position may be waited for when the one a ring before it is known to be there.  With one
-    // row tile a warp waits for its own positions alone, and knows the other's when the turn is its own: in the
-    // first two steps it waits for V behind that (K_0 may be behind K_1, with 4 stages in V_1's
-    // place); later steps know enough from the turns before.
-    const bool late = !wide && i < 2;
+    // row tile a warp waits for its own positions alone and knows the other's when the turn is its own.
+    // Where positions may arrive out of order (codes, whose tiles two groups widen; pages, whose
+    // boxes the copy engine brings) V is therefore waited for behind the turn: K_0 may be behind K_1, in whose
+    // step V_1 takes its stage, the first of four.
+    const bool late = !wide && (PAGED || C::CODES);
     if (!late) arrived(pv_pos);
     if (more && wide) arrived(pk_pos);
     if (ok) ok = warp_wait(bar(s.pready[g]), (steps + i) & 1, s, a);
@@ -1130,9 +1134,12 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::NTH, 1)
     } else if (warp < MMA_WARP) {
       produce<D, FMT, PAGED>(a, maps, w, gone, ring, smem_u32(raw), s, tid - 512);
     } else {
-      if (warp < MMA_WARP + 2) multiply<D, FMT, PAGED>(a, w, gone, smem_u32(sm), ring, s, warp - MMA_WARP);
-      else if (PAGED) load_paged_codes<D, FMT>(a, w, gone, smem_u32(raw), s, warp - MMA_WARP - 2, tid & 31);
-      else if (!w.own) load_codes<D, FMT>(a, w, smem_u32(raw), s, warp - MMA_WARP - 2, tid & 31);
+      const int g = warp - MMA_WARP;
+      if (!PAGED && g < 2) multiply<D, FMT, PAGED, 2>(a, w, gone, smem_u32(sm), ring, s, g);
+      else if (g < 2 && w.wide) multiply<D, FMT, PAGED, 1>(a, w, gone, smem_u32(sm), ring, s, g);
+      else if (g < 2) multiply<D, FMT, PAGED, 0>(a, w, gone, smem_u32(sm), ring, s, g);
+      else if (PAGED) load_paged_codes<D, FMT>(a, w, gone, smem_u32(raw), s, g - 2, tid & 31);
+      else if (!w.own) load_codes<D, FMT>(a, w, smem_u32(raw), s, g - 2, tid & 31);
     }
   };
   if (!PAGED) {
