@@ -103,11 +103,11 @@ cudaError_t launch_prefix_tc(const PrefixPlan& p, cudaStream_t s);  // the parts
 cudaError_t launch_tree_tc(const PrefixPlan& p, cudaStream_t s);
 cudaError_t launch_tree_few(const PrefixPlan& p, cudaStream_t s);
 cudaError_t launch_tree_join(const PrefixPlan& p, cudaStream_t s);
-// Query rows of a unit that the kernel for few of them takes, keys of its tiles, and
-// its CTAs.
 // Empty places before an item (see Walk), in tiles of either kernel.  256 rows of 32 units on 32K: none 132 us,
-// two 127, four 125, six 124, eight 125.
+// two 127, four 125, six 124, eight 125.  Few rows: one token of 8 sequences of 2K none 21.0, one 20.7, two 19.5, four
+// 19.1; of one of 8K 17.2, 16.1, 14.6, 14.4; of 32 of 16K in 8 bits 363, 364, 366, 368.
 constexpr int kFewPad = 1, kTreePad = 6;
+// Query rows of a unit that the kernel for few of them takes.
 constexpr int kFewRows = 16;
 // Keys of its tiles: four warps' steps, of 16 rows, or of 32 rows of codes, whose
 // bytes are fewer while a step's set-up is the same.

@@ -21,14 +21,14 @@
 // Measured (d = 128): 512 rows of 32 heads on 32K keys 245 us, 1.1 PFLOP/s, a
 // tile of 256 rows 3100 cycles where its products take 2048 and its softmax 1050
 // to 1180 in turn; 128 rows of 48 heads on 32K 131 us, 6.2 TB/s; 32 rows of 8
-// heads on 128K in 8 bits 82 us, where widening fills half of the integer pipe.
+// heads on 128K in 8 bits 81 us, where widening fills half of the integer pipe.
 //
 // For caches in pages (wf_tree_attn, compiled by wf_tree_tc.cu) a CTA goes through several
 // ranges of key tiles (Walk), one thread moving them along in shared memory and the
 // barriers' phases carried on (Gone); drafted rows are an item's last tiles, their mask and
 // the ends of lengths bits that a thread holds for its row.  Measured: 256 rows of 8
 // heads and 4 sequences of 32K 124 us, 1.1 PFLOP/s, a tile 1.9 with 152 SMs busy (a contiguous
-// prompt's 1.7 with 128); 64 rows of 2 sequences of 128K in 8 bits 199 us.
+// prompt's 1.7 with 128); 64 rows of 2 sequences of 128K in 8 bits 196 us, in 4 bits 186.
 //
 // bf16 prompt rows are copied by cp.async into the 128-byte-swizzled stages,
 // gathered through idx where there is one.  Codes are copied as they are by two

@@ -11,10 +11,10 @@
 // rotated channel's partner comes from another lane.  The angles belong to the
 // row, not to a head, so a thread keeps its chunk's cosines and sines and takes
 // the same chunk of several heads, whose addresses differ by a stride, UN of them on
-// their way while UN are worked on.  Bound by HBM: 4 prompts of up to 8K and 32 heads into
-// bf16 pages 136 us from cold caches (5.9 TB/s), 25K rows of 32 heads rotated 75 (a plain
-// copy of their bytes takes 67); into codes by instructions as well (2 prompts of 8K
-// 89 us, 61 at the memory's rate).
+// their way while UN are worked on.  Bound by HBM: 2 prompts of 8K and 32 heads into
+// bf16 pages 89 us (6.0 TB/s), 25K rows of 32 heads rotated 73 (a plain copy of their bytes
+// takes 67); into codes by instructions as well (the same prompts 79 us in 8 bits, 61 at the
+// memory's rate, and 79 to 81 in 4 bits, 51).
 #include <algorithm>
 #include <type_traits>
 
@@ -31,9 +31,9 @@ constexpr int NTH = 256;
 // quarter turn, at most pi / 4 = x, by their series in x^2 (the first terms left
 // out are x^12 / 12! < 2^-33 and x^11 / 11! < 2^-29).  x and its square are held in two
 // numbers and what 1 - x^2 / 2 rounds off is added back, so that the last sum's rounding is
-// nearly all that is lost: 0.9 of 2^-24 at most, where a plain x left 1.6 and a third more codes
-// came out other than exact arithmetic's (95 to 117, now 60 to 92, of 67M; a row's heads share it, so
-// that 25K rows of 32 heads take 72.6 us for 72.1, 32 single rows 3.2 for 3.1).
+// nearly all that is lost: 0.9 of 2^-24 at most, where a plain x left 1.6, and of 67M codes of rotated keys
+// 60 to 92 are other than exact arithmetic's, where that left 87 to 117.  A row's heads share it: 25K rows of 32
+// heads 72.6 us for 72.1, 32 single rows 3.2 for 3.1.
 __device__ __forceinline__ void turned(unsigned long long t, float& c, float& s) {
   constexpr double kUnit = 3.14159265358979323846 / 2147483648.0;  // 2 pi / 2^32
   constexpr float kHigh = (float)kUnit, kLow = (float)(kUnit - (double)kHigh);

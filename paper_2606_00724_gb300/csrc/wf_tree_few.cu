@@ -14,12 +14,17 @@
 // fourth step of it; the ranges are joined by tree_join_kernel, and a range that is
 // its whole item goes out as it is.  Drafted rows are the last steps of an item, straight
 // from memory, since they are few.  m is raised lazily, by more than 2^8, as in the kernel
-// for more rows, each row for itself; P is one bf16 term, l is summed before the rounding.
+// for more rows, each row for itself.  P is one bf16 term, as in all of the library's attention on the
+// tensor cores but wf_sparse_attn's, and l is summed before the rounding: against 64 bits O is 1.8e-3 to 2.0e-3 off,
+// where its own rounding leaves 1.5e-3 to 1.7e-3.  What P's rounding drops, as a second operand, brings it to that
+// and costs 1 % from bf16 pages (136.2 against 134.5 us for 32 sequences of up to 8K) and 4 to 5 % from codes, whose own
+// rounding is 2^-4 and more (379 against 364 for 32 of 16K in 8 bits).
 //
 // Measured (d = 128, 4 query rows of 8 key heads): 32 sequences of 8K in bf16 177 to 185 us,
 // 6 TB/s, bound by the rows' way in (176 us without the arithmetic); 32 of 16K in 8 bits
-// 353 us, bound by instructions, 850 a 16 keys; against the kernel for more rows 145 and 205 us
-// for 32 sequences of up to 8K, 12 and 25 for 32 of 64 rows.
+// 353 to 364 us, bound by chains of the 850 instructions a 16 keys: 232 registers leave two warps a scheduler, which
+// issues in 45 % of its cycles (the integer pipe is 42 % busy, HBM at 2.9 TB/s); against the kernel for
+// more rows 145 and 205 us for 32 sequences of up to 8K, 12 and 25 for 32 of 64 rows.
 #include <float.h>
 
 #include "wf_mx.cuh"

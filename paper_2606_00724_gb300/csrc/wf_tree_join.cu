@@ -4,7 +4,11 @@
 // 2^(m - M) l; a part without weight (l = 0) adds nothing, and a row without any is 0.
 // A row that is one part was written by the kernel before, which is all that its warp
 // finds here.  D / 4 lanes hold a row; where a row may have many parts, GR groups
-// of them take every GR-th part and the first adds them up, in their order.
+// of them take every GR-th part and the first adds them up, in their order: from eight parts
+// on that a row has where all sequences are equally long.  One group against eight, the whole call: a token of one
+// sequence of 8K (38 parts) 20.7 and 16.1 us, of 128K 95 and 89; 182 rows of 8 sequences (4.75) 63 and 74; 64-wide
+// heads of 32 sequences (1.8) 96 and 135.  One long sequence among many short ones counts as equal lengths do: a
+// token of one of 128K and 63 of 64 rows, one key head, 74 and 29.
 //
 // Bound by two loads one after the other, the item's place and its parts: 2 to 5 us behind the
 // kernel before, where attending the drafted rows here as well had taken 12 to 16.
@@ -117,7 +121,7 @@ __global__ void __launch_bounds__(NTH) tree_join_kernel(const __grid_constant__ 
 
 template <int D>
 cudaError_t launch(const PrefixArgs& a, cudaStream_t s) {
-  // Parts of a row where all sequences are equally long; eight groups from nine parts on.
+  // Parts of a row where all sequences are equally long.
   const bool many = a.C / std::max<int64_t>(1, (int64_t)a.B * a.H * a.mt) >= 8;
   const int per = NTH / (D / 4) / (many ? 8 : 1);
   Launch l(dim3((unsigned)((a.rows + per - 1) / per)), NTH, 0, s);
