@@ -507,9 +507,10 @@ wf_status wf_prefix_attn(const void* Q, const wf_tensor* q, const void* K, const
  * row i, clamped to [0, rows), e.g. the accepted ones of a draft; without it
  * m = rows.  With a plan (NULL: none) keys are rotated on the way, by
  * pos[axis][b][new row] (int32 [axes][B][rows]) or, where pos is NULL, by their
- * place (start[b] + i, whichever new row that is), and rounded once.  A row whose place is outside the table or on a page
- * outside the pool is left out; nothing else in the pool is touched.  Two rows
- * for the same place of the same page: one of them is kept, which is not said.
+ * place (start[b] + i, whichever new row that is), and rounded once.  A row whose
+ * place is outside the table or on a page outside the pool is left out; nothing
+ * else in the pool is touched.  Two rows for the same place of the same page: one
+ * of them is kept, which is not said.
  * The new rows must not overlap the pool.
  *
  * wf_tree_attn: q query rows of each sequence, e.g. the nodes of a tree of

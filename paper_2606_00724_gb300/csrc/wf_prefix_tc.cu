@@ -780,8 +780,8 @@ __device__ void multiply(const PrefixArgs& a, const Item& w, const Gone& gone, u
     // apart), so a position may be waited for when the one a ring before it is known to be there.  With one
     // row tile a warp waits for its own positions alone and knows the other's when the turn is its own.
     // Where positions may arrive out of order (codes, whose tiles two groups widen; pages, whose
-    // boxes the copy engine brings) V is therefore waited for behind the turn: K_0 may be behind K_1, in whose
-    // step V_1 takes its stage, the first of four.
+    // boxes the copy engine brings) V is therefore waited for behind the turn: with four stages V_1
+    // takes K_0's, and K_1 may be there before K_0.
     const bool late = !wide && (PAGED || C::CODES);
     if (!late) arrived(pv_pos);
     if (more && wide) arrived(pk_pos);
